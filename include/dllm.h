@@ -408,6 +408,194 @@ int dllm_quantize_q4_0(const void* d_src, int32_t src_dtype, int32_t rows, int32
 int dllm_quantize_int8(const void* d_src, int32_t src_dtype, int32_t rows, int32_t K, int8_t* d_codes,
                        float* d_scales, dllm_stream stream);
 
+/* ------------------------------------------------------------------------------
+ * Batches: several sequences over a paged K/V cache
+ *
+ * The operators of one step over a batch of sequences that share a long prefix (one
+ * prompt, several candidate continuations or requests), apart from its matrix
+ * products: the plan of the step's rows, Q/K normalisation with rotation and the cache
+ * write, the attention, and the selection from the logits.  dllm_batch_step runs a
+ * whole step of a model with them; each can be called on its own.  None keeps state,
+ * allocates or synchronises; all can be captured into a HIP graph.
+ *
+ * Paged cache: a pool of n_pages pages of `page` positions (32, 64, 128 or 256).  One
+ * layer's K plane is [n_pages][n_kv_heads][page][head_dim], its V^T plane
+ * [n_pages][n_kv_heads][head_dim][page].  Position p of sequence b lies in the page
+ * table[b][p / page] (block table, row stride table_ld) at offset p % page; its slot is
+ * page id * page + offset.  Slots are 32-bit (n_pages * page < 2^31); offsets into the
+ * planes are 64-bit.
+ * ------------------------------------------------------------------------------ */
+#define DLLM_F16 4       /* IEEE half (batch operators: tensors of one type throughout, DLLM_F32, DLLM_BF16 or DLLM_F16) */
+#define DLLM_MAX_SEQS 4096  /* sequences of one batch call */
+
+/* Plan of a step: block tables, row positions and cache slots from the sequences'
+ * lengths, on the GPU.  Sequence b holds d_len[b] cached positions in d_owned[b] pages
+ * and gets d_new[b] rows (0: it waits).  Afterwards it owns
+ *     need_b = ceil((d_len[b] + d_new[b]) / page)
+ * pages: missing ones are taken from the stack of free pages, pages past need_b (a
+ * rewound or finished sequence) are given back, except the first shared_pages of a
+ * table, which belong to all sequences.  In order of the sequences (and of the
+ * pages in a sequence), all given back pages are pushed onto the stack d_free[0 ..
+ * *d_n_free), then all missing ones are popped off its top.  d_owned_out and
+ * d_n_free_out receive the new counts; they must be other memory than d_owned and
+ * d_n_free.  d_table entries past a sequence's pages, and d_free past the stack, are
+ * left as they were.  Row arrays, each of max_rows entries:
+ *     d_row0 [n_seqs + 1]  sequence b has rows [d_row0[b], d_row0[b + 1])
+ *     d_pos, d_slot        a row's position and cache slot
+ *     d_seq, d_lim         its sequence and its key limit d_len[b] + d_new[b] (a window
+ *                          sees all of itself, as in dllm_denoise_step)
+ * Rows behind the last get pos 0, slot -1, seq -1, lim 0; a row whose table entry is
+ * no page id gets slot -1.  d_status [3]: rows asked for, pages short, and 0 if the
+ * plan was granted.  It is refused (1) as a whole if pages are short, if there are more
+ * rows than max_rows, if a sequence needs more than table_ld pages, or if a length or
+ * count is out of range: then tables, stack and counts stay as they were and every row
+ * is one behind the last (d_row0 all 0).
+ * E_INVAL unless 1 <= n_seqs <= DLLM_MAX_SEQS, 1 <= max_rows <= 2^24, table_ld in
+ * [1, 2^18], shared_pages in [0, table_ld], table_ld * page and n_pages * page < 2^31. */
+int dllm_batch_plan(const int32_t* d_len, const int32_t* d_new, const int32_t* d_owned, int32_t* d_owned_out,
+                    int32_t n_seqs, int32_t* d_table, int32_t table_ld, int32_t* d_free, const int32_t* d_n_free,
+                    int32_t* d_n_free_out, int32_t n_pages, int32_t page, int32_t shared_pages, int32_t max_rows,
+                    int32_t* d_row0, int32_t* d_pos, int32_t* d_slot, int32_t* d_seq, int32_t* d_lim,
+                    int32_t* d_status, dllm_stream stream);
+
+/* Table of (cos, sin) of p * rope_base^(-2j / head_dim) for p < max_pos, j < head_dim /
+ * 2, evaluated in double: d_table float [max_pos][head_dim / 2][2].  It is the table
+ * dllm_model_create builds for a model. */
+int dllm_rope_table(float* d_table, int32_t max_pos, int32_t head_dim, float rope_base, dllm_stream stream);
+
+/* Norm of every query and key head, rotation and cache write in one pass, for n_rows
+ * rows.  Per row and head, in fp32: y = x * rsqrt(mean(x^2) + eps) * gain (skipped where
+ * the gain is NULL), then rotate-half with the table's entry of d_pos[row] (clamped to
+ * [0, max_pos)): out_j = y_j cos - y_{j + D/2} sin, out_{j + D/2} = y_{j + D/2} cos + y_j
+ * sin.  Q goes to d_q_out [n_rows][n_heads][head_dim], K and V (unchanged) to the slots
+ * d_slot[row] of the planes, each rounded to `dtype` once (fp16 saturates at +-65504).
+ * A row with a slot outside [0, n_pages * page) writes no K/V; two rows must not have
+ * the same slot.  ld_*: row strides in elements.  Head_dim is 32, 64 or 128.  E_INVAL
+ * unless all pointers and row strides are multiples of 16 bytes (integer arrays: 4). */
+typedef struct dllm_qk_args {
+    int32_t dtype;
+    int32_t n_rows;
+    int32_t n_heads;
+    int32_t n_kv_heads;
+    int32_t head_dim;
+    int32_t page;
+    int32_t n_pages;
+    int32_t max_pos;
+    float eps;
+    const void* d_q;       /* [n_rows][n_heads][head_dim], row stride ld_q */
+    const void* d_k;       /* [n_rows][n_kv_heads][head_dim], row stride ld_k */
+    const void* d_v;       /* the same, row stride ld_v */
+    int64_t ld_q, ld_k, ld_v;
+    const float* d_q_gain; /* [head_dim] or NULL */
+    const float* d_k_gain; /* [head_dim] or NULL */
+    const float* d_rope;   /* [max_pos][head_dim / 2][2] */
+    const int32_t* d_pos;
+    const int32_t* d_slot;
+    void* d_q_out;         /* contiguous; may be d_q if that is contiguous */
+    void* d_k_pages;
+    void* d_v_pages;
+} dllm_qk_args;
+int dllm_qk_norm_rope(const dllm_qk_args* args, dllm_stream stream);
+
+/* Attention of the rows of a batch over the paged cache.  Row r of sequence b (d_row0)
+ * attends to the positions [0, e) of its sequence, e = min(d_lim[r], d_len[b]) or
+ * d_len[b] where d_lim is NULL (a causal step: d_lim[r] = position + 1), with query head
+ * h reading K/V head h / (n_heads / n_kv_heads):
+ *     out_r = sum_j softmax_j(scale * q_r k_j) v_j,
+ * and zeros where e = 0.  The first shared_len positions (a multiple of page) must lie in
+ * the same pages for all sequences: they are read through the table of sequence 0, once
+ * for all rows.  Scores, softmax and sums are fp32; the probabilities are rounded to
+ * `dtype` for their product with V.  Keys past e, and pages whose table entry is no page
+ * id, are never used, whatever they hold.  Rows from d_row0[n_seqs] on are left as they
+ * were.  max_rows and max_len bound the rows and keys (d_len) of any sequence: they size
+ * the launch; a sequence beyond them gets wrong values, but no access is out of bounds.
+ * n_rows bounds d_row0[n_seqs].  The workspace of dllm_attention_paged_ws() bytes is the
+ * caller's; calls that may overlap, and captured graphs that may, need one each.  E_INVAL for
+ * NULL pointers, sizes out of range, pointers or row strides that are not multiples of
+ * 16 bytes (integer arrays: 4); E_DTYPE for another type or head_dim (32, 64, 128; 32 only
+ * DLLM_F32); E_CAPACITY for a workspace too small. */
+typedef struct dllm_attn_args {
+    int32_t dtype;
+    int32_t n_rows;
+    int32_t n_seqs;
+    int32_t n_heads;
+    int32_t n_kv_heads;
+    int32_t head_dim;
+    int32_t page;
+    int32_t n_pages;
+    int32_t table_ld;
+    int32_t shared_len;
+    int32_t max_rows;
+    int32_t max_len;
+    float scale;
+    const void* d_q;        /* [n_rows][n_heads][head_dim], row stride ld_q elements */
+    int64_t ld_q;
+    const void* d_k_pages;
+    const void* d_v_pages;
+    const int32_t* d_table;
+    const int32_t* d_row0;  /* [n_seqs + 1] */
+    const int32_t* d_len;   /* [n_seqs]: positions of each sequence, its new rows included */
+    const int32_t* d_lim;   /* [n_rows] or NULL */
+    void* d_out;            /* [n_rows][n_heads][head_dim], row stride ld_out elements */
+    int64_t ld_out;
+    void* d_ws;
+    size_t ws_bytes;
+} dllm_attn_args;
+int dllm_attention_paged_ws(const dllm_attn_args* args, size_t* bytes);
+int dllm_attention_paged(const dllm_attn_args* args, dllm_stream stream);
+
+/* Penalties, biases and masks on logits, then the id and its confidence: what
+ * dllm_denoise_step's LM head reports, for logits the caller controls.  For row r of
+ * sequence b (d_row0; NULL: one sequence has all rows) and id v, in fp32 and in this order:
+ *   - l = l > 0 ? l / repetition : l * repetition where v is in the sequence's history,
+ *   - l -= frequency * c and, where c > 0, l -= presence, c the times v occurs in the
+ *     history past its first d_n_prompt[b] entries,
+ *   - l += bias where v is in the sequence's bias list (listed twice: its last entry),
+ *   - NaN counts as -inf, values above the largest float as that,
+ *   - -inf where v is mask_id or its bit in the row's allow mask is 0.
+ * d_out_id[r] = the id of the largest l (ties: the lowest), d_out_conf[r] = its softmax
+ * probability; -1 and 0 where nothing is left.  d_out_logits (nullable; may be d_logits
+ * with the same stride) receives l in `dtype`.  Histories and bias lists: entries
+ * [d_x0[b], d_x0[b + 1]) of one array each; ids outside the vocabulary are ignored.  Each
+ * of the three parts is skipped where its arrays are NULL; NULL parameters are 1, 0 and 0.
+ * Masks: bit v % 32 of word v / 32 of row d_allow_row[r] of d_allow [n_allow][allow_ld],
+ * -1 for none; d_allow_row NULL: row r has mask r (n_allow >= n_rows); a row that is no
+ * mask counts as one that allows nothing.  Rows outside [d_row0[0], d_row0[n_seqs])
+ * are left as they were.  The workspace of dllm_select_ws() bytes is the caller's; calls
+ * that may overlap, and captured graphs that may, need one each.  E_INVAL for NULL pointers, pointers
+ * not aligned to their elements and sizes out of range; E_DTYPE for another type; E_CAPACITY for a workspace too small. */
+typedef struct dllm_select_args {
+    int32_t dtype;
+    int32_t n_rows;
+    int32_t vocab;
+    int32_t mask_id;            /* -1: none */
+    int32_t n_seqs;
+    const void* d_logits;       /* [n_rows][vocab], row stride ld elements */
+    int64_t ld;
+    const int32_t* d_row0;      /* [n_seqs + 1] or NULL (n_seqs = 1) */
+    const int32_t* d_hist;      /* ids, or NULL */
+    const int32_t* d_hist0;     /* [n_seqs + 1] */
+    const int32_t* d_n_prompt;  /* [n_seqs] or NULL (0) */
+    const float* d_repetition;  /* [n_seqs] or NULL */
+    const float* d_presence;
+    const float* d_frequency;
+    const int32_t* d_bias_id;   /* ids, or NULL */
+    const float* d_bias;
+    const int32_t* d_bias0;     /* [n_seqs + 1] */
+    const uint32_t* d_allow;    /* [n_allow][allow_ld] words, or NULL */
+    int32_t n_allow;
+    int32_t allow_ld;
+    const int32_t* d_allow_row; /* [n_rows] or NULL */
+    void* d_out_logits;         /* or NULL */
+    int64_t ld_out;
+    int32_t* d_out_id;
+    float* d_out_conf;
+    void* d_ws;
+    size_t ws_bytes;
+} dllm_select_args;
+int dllm_select_ws(const dllm_select_args* args, size_t* bytes);
+int dllm_select(const dllm_select_args* args, dllm_stream stream);
+
 /* Measurement helper: one launch of a plain streaming read over `bytes` bytes of
  * the device buffer d_buf (16-byte aligned; bytes a multiple of 16), the same
  * 16-byte-per-lane non-temporal loads the GEMMs stream weights with.  The caller

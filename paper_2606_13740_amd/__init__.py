@@ -16,6 +16,8 @@ LIB_PATH = os.path.join(_HERE, "libdllm.so")
 
 DLLM_OK, DLLM_E_INVAL, DLLM_E_CAPACITY, DLLM_E_DTYPE, DLLM_E_HIP, DLLM_E_UNIMPL, DLLM_E_NOMEM = 0, -1, -2, -3, -4, -5, -6
 DLLM_F32, DLLM_BF16, DLLM_W8, DLLM_Q4 = 0, 1, 2, 3
+DLLM_F16 = 4                      # element type of the batch operators
+DLLM_MAX_SEQS = 4096
 K_QKV, K_ATTN, K_OPROJ, K_GATEUP, K_DOWN, K_LMHEAD = range(6)
 KERNEL_CLASSES = {"qkv": K_QKV, "attn": K_ATTN, "oproj": K_OPROJ, "gateup": K_GATEUP, "down": K_DOWN,
                   "lmhead": K_LMHEAD}
@@ -47,6 +49,34 @@ class dllm_weights(ctypes.Structure):
 
 _lib = None
 _vp, _i32, _sz = ctypes.c_void_p, ctypes.c_int32, ctypes.c_size_t
+_i64, _f32 = ctypes.c_int64, ctypes.c_float
+
+
+def _fields(ctype, names):
+    return [(n, ctype) for n in names.split()]
+
+
+class dllm_qk_args(ctypes.Structure):
+    _fields_ = (_fields(_i32, "dtype n_rows n_heads n_kv_heads head_dim page n_pages max_pos") + [("eps", _f32)] +
+                _fields(_vp, "d_q d_k d_v") + _fields(_i64, "ld_q ld_k ld_v") +
+                _fields(_vp, "d_q_gain d_k_gain d_rope d_pos d_slot d_q_out d_k_pages d_v_pages"))
+
+
+class dllm_attn_args(ctypes.Structure):
+    _fields_ = (_fields(_i32, "dtype n_rows n_seqs n_heads n_kv_heads head_dim page n_pages table_ld shared_len "
+                              "max_rows max_len") +
+                [("scale", _f32), ("d_q", _vp), ("ld_q", _i64)] +
+                _fields(_vp, "d_k_pages d_v_pages d_table d_row0 d_len d_lim d_out") +
+                [("ld_out", _i64), ("d_ws", _vp), ("ws_bytes", _sz)])
+
+
+class dllm_select_args(ctypes.Structure):
+    _fields_ = (_fields(_i32, "dtype n_rows vocab mask_id n_seqs") + [("d_logits", _vp), ("ld", _i64)] +
+                _fields(_vp, "d_row0 d_hist d_hist0 d_n_prompt d_repetition d_presence d_frequency d_bias_id d_bias "
+                             "d_bias0 d_allow") +
+                _fields(_i32, "n_allow allow_ld") + _fields(_vp, "d_allow_row d_out_logits") + [("ld_out", _i64)] +
+                _fields(_vp, "d_out_id d_out_conf d_ws") + [("ws_bytes", _sz)])
+
 
 _SIGNATURES = {
     "dllm_last_error": ([], ctypes.c_char_p),
@@ -80,6 +110,13 @@ _SIGNATURES = {
     "dllm_read_bandwidth": ([_vp, ctypes.c_size_t, _vp, _vp], ctypes.c_int),
     "dllm_quantize_q4_0": ([_vp, _i32, _i32, _i32, _vp, _vp, _vp], ctypes.c_int),
     "dllm_quantize_int8": ([_vp, _i32, _i32, _i32, _vp, _vp, _vp], ctypes.c_int),
+    "dllm_batch_plan": ([_vp] * 4 + [_i32, _vp, _i32] + [_vp] * 3 + [_i32] * 4 + [_vp] * 7, ctypes.c_int),
+    "dllm_rope_table": ([_vp, _i32, _i32, _f32, _vp], ctypes.c_int),
+    "dllm_qk_norm_rope": ([ctypes.POINTER(dllm_qk_args), _vp], ctypes.c_int),
+    "dllm_attention_paged_ws": ([ctypes.POINTER(dllm_attn_args), ctypes.POINTER(_sz)], ctypes.c_int),
+    "dllm_attention_paged": ([ctypes.POINTER(dllm_attn_args), _vp], ctypes.c_int),
+    "dllm_select_ws": ([ctypes.POINTER(dllm_select_args), ctypes.POINTER(_sz)], ctypes.c_int),
+    "dllm_select": ([ctypes.POINTER(dllm_select_args), _vp], ctypes.c_int),
     "dllm_commit_staged": ([_vp, _vp, _vp, _vp, _vp, _i32, _i32, ctypes.c_float, ctypes.c_float, _vp, _vp, _vp],
                            ctypes.c_int),
 }
@@ -272,6 +309,186 @@ def dllm_quantize_int8(src, src_dtype: int, rows: int, K: int, codes, scales, st
 
 def dllm_read_bandwidth(buf, nbytes: int, sink, stream=None):
     _check(lib().dllm_read_bandwidth(_ptr(buf), nbytes, _ptr(sink), _stream(stream)), "dllm_read_bandwidth")
+
+
+# ----------------------------------------------------------------------------
+# Batch operators: sizes, types and row strides come from the tensors; workspaces,
+# where none is given, from torch's allocator on the current stream
+# ----------------------------------------------------------------------------
+
+_elem_types = {}
+
+
+def _elem(t) -> int:
+    if not _elem_types:
+        import torch
+        _elem_types.update({torch.float32: DLLM_F32, torch.bfloat16: DLLM_BF16, torch.float16: DLLM_F16})
+    return _elem_types.get(t.dtype, -1)
+
+
+def _refuse(func: str, msg: str):
+    raise DllmError(DLLM_E_INVAL, func, msg)
+
+
+def _like(func: str, ref, dtype, **tensors):
+    """Every tensor that is there: on ref's device (the current one), contiguous, of `dtype` (None: ref's)."""
+    import torch
+
+    if not ref.is_cuda or ref.device.index != torch.cuda.current_device():
+        _refuse(func, "tensors must be on the current GPU")
+    dt = ref.dtype if dtype is None else dtype
+    for name, t in tensors.items():
+        if t is None:
+            continue
+        if t.device != ref.device:
+            _refuse(func, f"{name} is on another device")
+        if t.dtype != dt:
+            _refuse(func, f"{name} must be {dt}")
+        if not t.is_contiguous():
+            _refuse(func, f"{name} must be contiguous")
+
+
+def _rows(func: str, name: str, t, ref, heads: int, dim: int) -> int:
+    """Row stride of a [rows][heads * dim] or [rows][heads][dim] tensor whose rows are whole; checks its shape."""
+    sh, st = t.shape, t.stride()
+    if t.dtype != ref.dtype or t.device != ref.device:
+        _refuse(func, f"{name} must have q's type and device")
+    if sh[0] != ref.shape[0] or st[-1] != 1 or not (
+            len(sh) == 2 and sh[1] == heads * dim or len(sh) == 3 and sh[1] == heads and sh[2] == dim and (heads == 1 or st[1] == dim)):
+        _refuse(func, f"{name} must be [rows][{heads}][{dim}] with whole rows")
+    return st[0] if sh[0] > 1 else heads * dim
+
+
+def _at_least(func: str, n: int, **tensors):
+    for name, t in tensors.items():
+        if t is not None and t.numel() < n:
+            _refuse(func, f"{name} must have at least {n} entries")
+
+
+def dllm_batch_plan(length, new, owned, owned_out, table, free, n_free, n_free_out, page: int, shared_pages: int, row0,
+                    pos, slot, seq, lim, status, stream=None):
+    """The row arrays' common length is the plan's max_rows; free has an entry per page of the pool."""
+    f, B, ld = "dllm_batch_plan", length.numel(), table.shape[-1]
+    import torch
+    _like(f, length, torch.int32, length=length, new=new, owned=owned, owned_out=owned_out, table=table, free=free,
+          n_free=n_free, n_free_out=n_free_out, row0=row0, pos=pos, slot=slot, seq=seq, lim=lim, status=status)
+    _at_least(f, B, new=new, owned=owned, owned_out=owned_out)
+    _at_least(f, B * ld, table=table)
+    _at_least(f, B + 1, row0=row0)
+    _at_least(f, pos.numel(), slot=slot, seq=seq, lim=lim)
+    _at_least(f, 3, status=status)
+    _at_least(f, 1, n_free=n_free, n_free_out=n_free_out)
+    _check(lib().dllm_batch_plan(length.data_ptr(), new.data_ptr(), owned.data_ptr(), owned_out.data_ptr(), B,
+                                 table.data_ptr(), ld, free.data_ptr(), n_free.data_ptr(), n_free_out.data_ptr(),
+                                 free.numel(), page, shared_pages, pos.numel(), row0.data_ptr(), pos.data_ptr(),
+                                 slot.data_ptr(), seq.data_ptr(), lim.data_ptr(), status.data_ptr(), _stream(stream)), f)
+
+
+def dllm_rope_table(table, head_dim: int, rope_base: float, stream=None):
+    """table: float32 [max_pos][head_dim / 2][2]."""
+    f = "dllm_rope_table"
+    import torch
+    _like(f, table, torch.float32, table=table)
+    if table.numel() % head_dim != 0:
+        _refuse(f, "table must be [max_pos][head_dim / 2][2]")
+    _check(lib().dllm_rope_table(table.data_ptr(), table.numel() // head_dim, head_dim, rope_base, _stream(stream)), f)
+
+
+def _pages(f: str, q, k_pages, v_pages):
+    """(n_pages, kv heads, page, head_dim) of a K plane [n_pages][kv][page][dim] and a V^T plane [n_pages][kv][dim][page]."""
+    _like(f, q, None, k_pages=k_pages, v_pages=v_pages)
+    n, kv, page, dim = k_pages.shape
+    if tuple(v_pages.shape) != (n, kv, dim, page):
+        _refuse(f, "v_pages must be [n_pages][kv_heads][head_dim][page]")
+    return n, kv, page, dim
+
+
+def dllm_qk_norm_rope(q, k, v, rope, pos, slot, q_out, k_pages, v_pages, q_gain=None, k_gain=None, eps: float = 1e-6,
+                      stream=None):
+    """q, k, v: [rows][heads][dim] or [rows][heads * dim], rows may be strided (slices of one projection's output)."""
+    f = "dllm_qk_norm_rope"
+    import torch
+    n_pages, kv, page, dim = _pages(f, q, k_pages, v_pages)
+    T = q.shape[0]
+    H = q_out.shape[1] if q_out.dim() == 3 else q_out.shape[1] // dim
+    ld_q, ld_k, ld_v = (_rows(f, n, t, q, h, dim) for n, t, h in (("q", q, H), ("k", k, kv), ("v", v, kv)))
+    _like(f, q, None, q_out=q_out)
+    _like(f, q, torch.float32, rope=rope, q_gain=q_gain, k_gain=k_gain)
+    _like(f, q, torch.int32, pos=pos, slot=slot)
+    _at_least(f, T, pos=pos, slot=slot)
+    _at_least(f, T * H * dim, q_out=q_out)
+    _at_least(f, dim, q_gain=q_gain, k_gain=k_gain)
+    a = dllm_qk_args(_elem(q), T, H, kv, dim, page, n_pages, rope.numel() // dim, eps, q.data_ptr(), k.data_ptr(),
+                     v.data_ptr(), ld_q, ld_k, ld_v, _ptr(q_gain), _ptr(k_gain), rope.data_ptr(), pos.data_ptr(),
+                     slot.data_ptr(), q_out.data_ptr(), k_pages.data_ptr(), v_pages.data_ptr())
+    _check(lib().dllm_qk_norm_rope(ctypes.byref(a), _stream(stream)), f)
+
+
+def _workspace(query, a, ws, device, f: str):
+    """Sets a's workspace: `ws`, or memory of the call's own (which the caller keeps until the call has been made)."""
+    n = _sz()
+    _check(query(ctypes.byref(a), ctypes.byref(n)), f + "_ws")
+    if ws is None and n.value:
+        import torch
+        ws = torch.empty(n.value, dtype=torch.uint8, device=device)
+    if ws is not None:
+        a.d_ws, a.ws_bytes = ws.data_ptr(), ws.numel() * ws.element_size()
+    return ws
+
+
+def dllm_attention_paged(q, k_pages, v_pages, table, row0, length, out, max_rows: int, max_len: int,
+                         shared_len: int = 0, lim=None, scale: Optional[float] = None, ws=None, stream=None):
+    """q, out: [rows][heads][dim] or [rows][heads * dim], rows may be strided; scale: 1 / sqrt(dim) if None."""
+    f = "dllm_attention_paged"
+    import torch
+    n_pages, kv, page, dim = _pages(f, q, k_pages, v_pages)
+    H = q.shape[1] if q.dim() == 3 else q.shape[1] // dim
+    ld_q, ld_out = _rows(f, "q", q, q, H, dim), _rows(f, "out", out, q, H, dim)
+    B, ld = length.numel(), table.shape[-1]
+    _like(f, q, torch.int32, table=table, row0=row0, length=length, lim=lim)
+    _at_least(f, B * ld, table=table)
+    _at_least(f, B + 1, row0=row0)
+    _at_least(f, q.shape[0], lim=lim)
+    if stream is not None and ws is None:
+        _refuse(f, "a call on a given stream needs a workspace")
+    a = dllm_attn_args(_elem(q), q.shape[0], B, H, kv, dim, page, n_pages, ld, shared_len, max_rows, max_len,
+                       dim ** -0.5 if scale is None else scale, q.data_ptr(), ld_q, k_pages.data_ptr(),
+                       v_pages.data_ptr(), table.data_ptr(), row0.data_ptr(), length.data_ptr(), _ptr(lim),
+                       out.data_ptr(), ld_out)
+    keep = _workspace(lib().dllm_attention_paged_ws, a, ws, q.device, f)
+    _check(lib().dllm_attention_paged(ctypes.byref(a), _stream(stream)), f)
+    del keep
+
+
+def dllm_select(logits, out_id, out_conf, mask_id: int = -1, row0=None, hist=None, hist0=None, n_prompt=None,
+                repetition=None, presence=None, frequency=None, bias_id=None, bias=None, bias0=None, allow=None,
+                allow_row=None, out_logits=None, ws=None, stream=None):
+    """logits, out_logits: [rows][vocab], rows may be strided; allow: int32 words [masks][words]."""
+    f = "dllm_select"
+    import torch
+    T, V = logits.shape
+    B = row0.numel() - 1 if row0 is not None else 1
+    _like(f, logits, torch.int32, out_id=out_id, row0=row0, hist=hist, hist0=hist0, n_prompt=n_prompt, bias_id=bias_id,
+          bias0=bias0, allow=allow, allow_row=allow_row)
+    _like(f, logits, torch.float32, out_conf=out_conf, repetition=repetition, presence=presence, frequency=frequency,
+          bias=bias)
+    _at_least(f, T, out_id=out_id, out_conf=out_conf, allow_row=allow_row)
+    _at_least(f, B, n_prompt=n_prompt, repetition=repetition, presence=presence, frequency=frequency)
+    _at_least(f, B + 1, hist0=hist0, bias0=bias0)
+    for name, t in (("logits", logits), ("out_logits", out_logits)):
+        if t is not None and (t.shape != logits.shape or t.dtype != logits.dtype or t.device != logits.device or (V > 1 and t.stride(1) != 1)):
+            _refuse(f, f"{name} must be [rows][vocab] of one type with whole rows")
+    if stream is not None and ws is None:
+        _refuse(f, "a call on a given stream needs a workspace")
+    a = dllm_select_args(_elem(logits), T, V, mask_id, B, logits.data_ptr(), logits.stride(0) if T > 1 else V, _ptr(row0),
+                         _ptr(hist), _ptr(hist0), _ptr(n_prompt), _ptr(repetition), _ptr(presence), _ptr(frequency),
+                         _ptr(bias_id), _ptr(bias), _ptr(bias0), _ptr(allow), 0 if allow is None else allow.shape[0],
+                         0 if allow is None else allow.shape[1], _ptr(allow_row), _ptr(out_logits),
+                         0 if out_logits is None else (out_logits.stride(0) if T > 1 else V), out_id.data_ptr(),
+                         out_conf.data_ptr())
+    keep = _workspace(lib().dllm_select_ws, a, ws, logits.device, f)
+    _check(lib().dllm_select(ctypes.byref(a), _stream(stream)), f)
+    del keep
 
 
 # ----------------------------------------------------------------------------

@@ -22,28 +22,23 @@
 #include "common.hpp"
 #include "gemm.hpp"
 #include "gemm_tiled.hpp"
+#include "host.hpp"
 #include "kernels.hpp"
 
 using namespace dllm;
 
-namespace {
+namespace dllm {
 
-thread_local std::string g_last_error;
+static thread_local std::string g_last_error;
 
 int fail(int code, const std::string& msg) {
     g_last_error = msg;
     return code;
 }
 
-#define HIP_TRY(expr)                                                                           \
-    do {                                                                                        \
-        hipError_t _e = (expr);                                                                 \
-        if (_e != hipSuccess)                                                                   \
-            return fail(DLLM_E_HIP, std::string(#expr) + ": " + hipGetErrorString(_e));        \
-    } while (0)
+}  // namespace dllm
 
-inline int ceil_div(long a, long b) { return (int)((a + b - 1) / b); }
-inline long round_up(long a, long b) { return (a + b - 1) / b * b; }
+namespace {
 
 // One packed GEMM operand.
 struct PackedW {
@@ -1502,6 +1497,19 @@ int dllm_quantize_int8(const void* d_src, int32_t src_dtype, int32_t rows, int32
     else
         hipLaunchKernelGGL((quantize_i8_kernel<uint16_t>), dim3(rows), dim3(256), 0, (hipStream_t)stream,
                            (const uint16_t*)d_src, K, d_codes, d_scales);
+    HIP_TRY(hipGetLastError());
+    return DLLM_OK;
+}
+
+int dllm_rope_table(float* d_table, int32_t max_pos, int32_t head_dim, float rope_base, dllm_stream stream) {
+    if (!d_table) return fail(DLLM_E_INVAL, "table is NULL");
+    if (((uintptr_t)d_table & 15) != 0) return fail(DLLM_E_INVAL, "table must be 16-byte aligned");
+    if (max_pos < 1 || head_dim < 2 || head_dim % 2 != 0 || (long)max_pos * (head_dim / 2) >= (1l << 31))
+        return fail(DLLM_E_INVAL, "max_pos must be >= 1, head_dim even, and the table hold fewer than 2^31 entries");
+    if (!(rope_base > 1.f) || !std::isfinite(rope_base)) return fail(DLLM_E_INVAL, "rope_base must be finite and > 1");
+    const int half = head_dim / 2;
+    hipLaunchKernelGGL(rope_table_kernel, dim3(ceil_div((long)max_pos * half, 256)), dim3(256), 0, (hipStream_t)stream,
+                       (float2*)d_table, max_pos, half, (double)rope_base);
     HIP_TRY(hipGetLastError());
     return DLLM_OK;
 }

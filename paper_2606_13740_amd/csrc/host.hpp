@@ -1,0 +1,25 @@
+// What the library's translation units share on the host: errors and small arithmetic.
+#pragma once
+
+#include <hip/hip_runtime.h>
+
+#include <string>
+
+#include "../../include/dllm.h"
+
+namespace dllm {
+
+// Records msg as the thread's dllm_last_error() and returns code (dllm.hip).
+int fail(int code, const std::string& msg);
+
+#define HIP_TRY(expr)                                                                           \
+    do {                                                                                        \
+        hipError_t _e = (expr);                                                                 \
+        if (_e != hipSuccess)                                                                   \
+            return fail(DLLM_E_HIP, std::string(#expr) + ": " + hipGetErrorString(_e));        \
+    } while (0)
+
+inline int ceil_div(long a, long b) { return (int)((a + b - 1) / b); }
+inline long round_up(long a, long b) { return (a + b - 1) / b * b; }
+
+}  // namespace dllm
