@@ -1,4 +1,24 @@
 // Attention of a batch of sequences that share a prefix, over a paged cache.
+//
+// For a row and head, o = sum_j p_j v_j / sum_j p_j with p_j = 2^(s_j - m), s_j the score in
+// log2 units and m any reference near the row's maximum: one pass over the keys keeps (m, sum,
+// o) and rescales when m moves.  (m, sum, o) of disjoint key sets merge the same way, so the
+// keys are cut into parts that run side by side and a second kernel merges:
+//   - the shared prefix, once for the rows of ALL sequences: its K/V tiles meet as many rows as
+//     there are, and it is read from HBM once (rows of one sequence alone would leave a
+//     32-row window at 16 flops a byte);
+//   - each sequence's own keys, for its own rows.
+// Both may be split further along the keys where the tiles alone do not fill the chip.
+//
+// Rows of the query heads of one K/V head are packed together: "virtual row" f = row * G + g
+// of a K/V head (G query heads each), so that grouped heads share K/V tiles too.
+//
+// Products, transposed so that no operand is shuffled (16 x 16 MFMA tiles):
+//   S^T (16 keys x 16 rows) = K tile (A) * Q^T (B),   O^T (16 dims x 16 rows) += V^T tile (A) * P^T (B).
+//   16-bit types, 32 keys a step: key tile t takes keys 8 (r / 4) + 4 t + r % 4, so that lane group g ends
+//   up with the probabilities of keys 8g .. 8g+7, which is the B operand of a 32-key product.
+//   fp32 (4 keys a product): key tile t takes keys 16 t + r; lane group g has keys 16 t + 4g + i and
+//   product i takes exactly key i of every group.  Dims of a 16-dim step go 4g + i the same way.
 #pragma once
 
 #include "common.hpp"
@@ -15,8 +35,15 @@ struct PagedArgs {
     const int *row0, *len, *lim;
     void* out;
     long ld_out;
-    int T, B, H, Hk, page_shift, n_pages, shared, max_rows, max_len;
-    float scale;
+    int T, B, H, Hk, G, page_shift, n_pages, shared, max_rows, max_len;
+    float sl2;                    // |scale| * log2(e)
+    float qmul;                   // sign of the scale (0: all scores are 0)
+    int ns_s, ns_o;               // key splits of the shared part and of a sequence's own
+    int nt_s, nt_o;               // row tiles of the shared part and of a sequence
+    int n_s;                      // workgroups of the shared part (the first ones)
+    int direct;                   // one part in all: the output is written here, not merged
+    float* opart;                 // [ns_s + ns_o][T][H][Dh] unnormalised partial outputs
+    float* mlpart;                // [ns_s + ns_o][T][H][2]  (reference in log2 units, sum)
 };
 
 // Largest b with row0[b] <= r, or -1 where r is no row of a sequence.
@@ -31,78 +58,410 @@ __device__ __forceinline__ int row_seq(const int* row0, int B, int r) {
     return lo;
 }
 
-// One workgroup of 4 waves per (row, head): wave w takes the 64-key chunks w, w + 4, ...,
-// scores with one key per lane, outputs with one dim (DH 128: two) per lane; the waves'
-// (max, sum, output) are merged in wave order.
-template <typename T, int DH>
-__global__ void __launch_bounds__(256) attn_paged_row_kernel(PagedArgs a) {
-    constexpr int NW = 4, ND = (DH + 63) / 64;
-    __shared__ float q_s[DH], p_s[NW][64], o_s[NW][DH], m_s[NW], l_s[NW];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int row = blockIdx.x, h = blockIdx.y, hk = h / (a.H / a.Hk);
-    const int b = row_seq(a.row0, a.B, row);
-    if (b < 0) return;
-    int n = min(min(a.len[b], a.max_len), a.table_ld << a.page_shift);
-    if (a.lim != nullptr) n = min(n, a.lim[row]);
-    if (threadIdx.x < DH) q_s[threadIdx.x] = elem_to_f32<T>(((const T*)a.q)[row * a.ld_q + h * DH + threadIdx.x]);
-    __syncthreads();
-    float m = -INFINITY, l = 0.f, o[ND];
+// Element type: one product step, and the rounding of the probabilities.
+template <typename T> struct PagedElem;
+template <> struct PagedElem<_Float16> {
+    using x2 = _Float16 __attribute__((ext_vector_type(2)));
+    static __device__ __forceinline__ f32x4_t mfma(const u32x4_t& a, const u32x4_t& b, f32x4_t c) { return mfma_f16(a, b, c); }
+};
+template <> struct PagedElem<__bf16> {
+    using x2 = __bf16 __attribute__((ext_vector_type(2)));
+    static __device__ __forceinline__ f32x4_t mfma(const u32x4_t& a, const u32x4_t& b, f32x4_t c) { return mfma_bf16(a, b, c); }
+};
+template <> struct PagedElem<float> {
+    using x2 = float __attribute__((ext_vector_type(2)));
+    static __device__ __forceinline__ f32x4_t mfma(const u32x4_t& a, const u32x4_t& b, f32x4_t c) {
 #pragma unroll
-    for (int d = 0; d < ND; ++d) o[d] = 0.f;
-    const int mask = (1 << a.page_shift) - 1;
-    for (int k0 = 64 * wave; k0 < n; k0 += 64 * NW) {
-        const int key = k0 + lane;
-        int pg = -1;
-        if (key < n) pg = a.table[(size_t)(key < a.shared ? 0 : b) * a.table_ld + (key >> a.page_shift)];
-        if (pg >= a.n_pages) pg = -1;
-        float s = -INFINITY;
-        if (pg >= 0) {
-            const T* kr = (const T*)a.kp + ((((size_t)pg * a.Hk + hk) << a.page_shift) + (key & mask)) * DH;
-            s = 0.f;
-            for (int d = 0; d < DH; ++d) s = fmaf(q_s[d], elem_to_f32<T>(kr[d]), s);
-            s *= a.scale;
-        }
-        const float mn = fmaxf(m, warp_max(s));
-        if (mn == -INFINITY) continue;
-        const float alpha = expf(m - mn), p = pg >= 0 ? expf(s - mn) : 0.f;
-        l = l * alpha + warp_sum(p);
-        m = mn;
-        p_s[wave][lane] = p;
-        __builtin_amdgcn_wave_barrier();
+        for (int i = 0; i < 4; ++i) c = mfma_f32(__uint_as_float(a[i]), __uint_as_float(b[i]), c);
+        return c;
+    }
+};
+
+__device__ __forceinline__ int swz_paged(int key) { return (key & 3) | (((key >> 3) & 3) << 2); }
+
+// log2-domain slack of the lazily moved reference: probabilities <= 2^8 (fits fp16)
+constexpr float PAGED_SLACK = 8.f;
+
+// Workgroup = (part, K/V head, key split, tile of QG x QT x 16 virtual rows), QG waves of QT
+// 16-row tiles.  The split's 32-key blocks are staged in LDS with direct global->LDS loads
+// in a ring of NB buffers and read from there by all waves.  LDS rows are swizzled in 16-byte
+// columns so that the 16 rows of a fragment read lie in different banks.  Lane i holds the
+// page of block 64 n + i, so a block's page is one lane read.
+template <typename T, int DH, int QG, int QT, int NB>
+__global__ void __launch_bounds__(QG * 64)
+__attribute__((amdgpu_waves_per_eu(QG * (160 * 1024 / (NB * 64 * DH * (int)sizeof(T))) >= 8 ? 2 : 1)))
+attn_paged_kernel(PagedArgs a) {
+    using E = PagedElem<T>;
+    constexpr bool F32 = sizeof(T) == 4;
+    constexpr int ES = sizeof(T);
+    constexpr int CD = F32 ? 16 : 32;         // dims of one 16-byte K fragment step (4 lane groups)
+    constexpr int NC = DH / CD;
+    constexpr int ND = DH / 16;               // 16-dim output tiles
+    constexpr int NV = F32 ? 2 : 1;           // V^T fragments of a block per output tile
+    constexpr int KC = DH * ES / 16;          // 16-byte columns of a key's row
+    constexpr int VC = 32 * ES / 16;          // and of a dim's row of V^T
+    constexpr int KPLANE = 32 * DH * ES, BUF = 2 * KPLANE;
+    constexpr int KI = KPLANE / 1024;         // 1 KiB wave loads per plane
+    constexpr int LPW = 2 * (KI / QG);        // loads each wave issues per staged block, at least
+    constexpr int TM = 16 * QG * QT;          // virtual rows of a workgroup
+    static_assert(KI * 1024 == KPLANE, "planes must be whole wave loads");
+    static_assert(TM <= 256, "at most four virtual rows per lane");
+    __shared__ __attribute__((aligned(1024))) char lds[NB * BUF];
+
+    const int lane = threadIdx.x & 63, qw = QG == 1 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int r = lane & 15, g = lane >> 4;
+
+    // Which item.  The dispatcher deals consecutive workgroups to the 8 XCDs in turn; XCD x
+    // takes the x-th of 8 shares, so that tiles that read the same K/V share one L2.
+    const bool own = (int)blockIdx.x >= a.n_s;
+    const int n_items = own ? (int)gridDim.x - a.n_s : a.n_s;
+    const int L = (int)blockIdx.x - (own ? a.n_s : 0), xcd = L & 7;
+    const int item = xcd * (n_items >> 3) + min(xcd, n_items & 7) + (L >> 3);
+    int tile, split, hk, b, ks, ke, R0, R1, bps, part;
+    if (own) {
+        tile = item % a.nt_o;
+        const int i1 = item / a.nt_o, i2 = i1 / a.ns_o;
+        split = i1 % a.ns_o;
+        hk = i2 % a.Hk;
+        b = i2 / a.Hk;
+        R0 = a.row0[b];
+        R1 = min(a.row0[b + 1], R0 + a.max_rows);
+        ks = a.shared;
+        ke = min(a.len[b], a.max_len);
+        // blocks per split from the sequence's own length: a short one is still spread
+        const int nblk = max(0, ke - ks + 31) >> 5;
+        bps = max((nblk + a.ns_o - 1) / a.ns_o, 2);
+        part = a.ns_s + split;
+    } else {
+        tile = item % a.nt_s;
+        const int i1 = item / a.nt_s;
+        split = i1 % a.ns_s;
+        hk = i1 / a.ns_s;
+        b = 0;
+        R0 = a.row0[0];
+        R1 = a.row0[a.B];
+        ks = 0;
+        ke = min(a.shared, a.max_len);
+        bps = (((ke + 31) >> 5) + a.ns_s - 1) / a.ns_s;
+        part = split;
+    }
+    R0 = max(R0, 0);
+    R1 = min(R1, a.T);
+    const int nv = (R1 - R0) * a.G;           // virtual rows of the part
+    const int f0 = tile * TM;
+    if (f0 >= nv) return;
+
+    // Key limit of virtual row f.  The rows of the shared part need their sequence's length only if some
+    // sequence ends inside it.
+    int short_len = 0x7FFFFFFF;
+    if (!own) {
+        for (int i = lane; i < a.B; i += 64) short_len = min(short_len, a.len[i]);
 #pragma unroll
-        for (int d = 0; d < ND; ++d) {
-            const int dim = min(lane + 64 * d, DH - 1);       // every lane stays: the pages come from all of them
-            float acc = o[d] * alpha;
-            for (int j = 0; j < 64; ++j) {
-                const int pj = __shfl(pg, j);
-                if (pj < 0) continue;
-                const T v = ((const T*)a.vp)[((((size_t)pj * a.Hk + hk) * DH + dim) << a.page_shift) + ((k0 + j) & mask)];
-                acc = fmaf(p_s[wave][j], elem_to_f32<T>(v), acc);
+        for (int o = 32; o > 0; o >>= 1) short_len = min(short_len, __shfl_xor(short_len, o));
+    }
+    auto row_limit = [&](int f) {
+        const int row = R0 + f / a.G;
+        const int n = own || short_len >= ke ? ke : min(ke, a.len[row_seq(a.row0, a.B, row)]);
+        return a.lim != nullptr ? min(n, a.lim[row]) : n;
+    };
+    // The largest limit of the tile's rows ends its keys: what lies behind may be anything.
+    int ktop = ks;
+#pragma unroll
+    for (int i = 0; i < (TM + 63) / 64; ++i)
+        if (lane + 64 * i < TM) ktop = max(ktop, row_limit(min(f0 + lane + 64 * i, nv - 1)));
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) ktop = max(ktop, __shfl_xor(ktop, o));
+    ktop = __builtin_amdgcn_readfirstlane(ktop);
+    const int kb0 = split * bps, nblk = (ktop - ks + 31) >> 5;
+    const int rounds = max(0, min(nblk, kb0 + bps) - kb0);
+
+    u32x4_t qf[QT][NC];
+    int lim[QT];
+#pragma unroll
+    for (int q = 0; q < QT; ++q) {
+        // rows past the last repeat it (the rescale below is decided over a tile's 16 rows)
+        const int f = min(f0 + 16 * (QT * qw + q) + r, nv - 1);
+        const int row = R0 + f / a.G, h = hk * a.G + f % a.G;
+        const T* src = (const T*)a.q + row * a.ld_q + h * DH + (16 / ES) * g;
+#pragma unroll
+        for (int c = 0; c < NC; ++c) {
+            qf[q][c] = ldg16(src + CD * c);
+            if (a.qmul != 1.f) {
+                constexpr uint32_t sign = F32 ? 0x80000000u : 0x80008000u;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) qf[q][c][e] = a.qmul == 0.f ? 0u : qf[q][c][e] ^ sign;
             }
-            o[d] = acc;
         }
-        __builtin_amdgcn_wave_barrier();
+        lim[q] = row_limit(f);
     }
+
+    // Pages of the 64 blocks of a chunk: lane i has block 64 n + i's (-1: no page).  Blocks are staged
+    // up to NB - 1 ahead of their use, so the chunk before keeps a bit a block: whether it has a page.
+    const int* trow = a.table + (size_t)b * a.table_ld;
+    auto chunk_pages = [&](int n) {
+        const int t = 64 * n + lane, k = ks + 32 * (kb0 + t);
+        int pg = -1;
+        if (t < rounds) pg = trow[k >> a.page_shift];
+        return pg < a.n_pages ? pg : -1;
+    };
+    int pgv = chunk_pages(0);
+    uint64_t have = __builtin_amdgcn_ballot_w64(pgv >= 0), have_before = 0;
+    const long page_elems = (long)DH << a.page_shift;
+
+    // Stage block t: wave load i of a plane is its bytes [1024 i, 1024 i + 1024), taken by wave
+    // i % QG.  A block without a page is staged from page 0 (and not used).
+    auto stage = [&](int t, int buf) {
+        const int pg = max(0, __builtin_amdgcn_readlane(pgv, t & 63));
+        const int off = (ks + 32 * (kb0 + t)) & ((1 << a.page_shift) - 1);
+        const long head = ((long)pg * a.Hk + hk) * page_elems;
+        const T* Kp = (const T*)a.kp + head;
+        const T* Vp = (const T*)a.vp + head;
+        char* base = lds + buf * BUF;
 #pragma unroll
-    for (int d = 0; d < ND; ++d)
-        if (lane + 64 * d < DH) o_s[wave][lane + 64 * d] = o[d];
-    if (lane == 0) {
-        m_s[wave] = m;
-        l_s[wave] = l;
+        for (int j = 0; j < (KI + QG - 1) / QG; ++j) {
+            const int i = qw + j * QG;
+            if (KI % QG != 0 && i >= KI) break;
+            const int key = (i * 64 + lane) / KC, pc = lane % KC;
+            const int sw = F32 ? key & 15 : swz_paged(key);
+            buffer_to_lds16(Kp, key * (DH * ES) + ((pc ^ (sw & (KC - 1))) << 4), off * (DH * ES), base + i * 1024);
+        }
+#pragma unroll
+        for (int j = 0; j < (KI + QG - 1) / QG; ++j) {
+            const int i = qw + j * QG;
+            if (KI % QG != 0 && i >= KI) break;
+            const int dim = (i * 64 + lane) / VC, pc = lane % VC;
+            const int sw = F32 ? dim & 7 : (dim >> 2) & 3;
+            buffer_to_lds16(Vp, ((dim << a.page_shift) * ES) + ((pc ^ sw) << 4), off * ES, base + KPLANE + i * 1024);
+        }
+    };
+    // zero the V^T values of keys >= end in the slots this wave staged
+    auto zero_tail = [&](int k0, int end, int buf) {
+        char* base = lds + buf * BUF + KPLANE;
+#pragma unroll
+        for (int j = 0; j < (KI + QG - 1) / QG; ++j) {
+            const int i = qw + j * QG;
+            if (KI % QG != 0 && i >= KI) break;
+            const int dim = (i * 64 + lane) / VC, pc = lane % VC;
+            const int sw = F32 ? dim & 7 : (dim >> 2) & 3;
+            const int key = k0 + (16 / ES) * (pc ^ sw);             // the slot's first key
+            if (key + 16 / ES <= end) continue;
+            u32x4_t* slot = (u32x4_t*)(base + i * 1024 + lane * 16);
+            u32x4_t v = *slot;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                if (F32) v[e] = key + e >= end ? 0u : v[e];
+                else v[e] &= (key + 2 * e >= end ? 0u : 0x0000FFFFu) | (key + 2 * e + 1 >= end ? 0u : 0xFFFF0000u);
+            }
+            *slot = v;
+        }
+    };
+
+#pragma unroll
+    for (int j = 0; j < NB - 1; ++j)
+        if (j < rounds) stage(j, j);
+
+    // smallest limit of the wave's rows: blocks below it need no per-key mask
+    int lim_w = ktop;
+#pragma unroll
+    for (int q = 0; q < QT; ++q)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) lim_w = min(lim_w, __builtin_amdgcn_readlane(lim[q], i));
+
+    float mrun[QT], lrun[QT];
+    f32x4_t oacc[QT][ND];
+#pragma unroll
+    for (int q = 0; q < QT; ++q) {
+        mrun[q] = -INFINITY;
+        lrun[q] = 0.f;
+#pragma unroll
+        for (int dt = 0; dt < ND; ++dt) oacc[q][dt] = f32x4_t{0.f, 0.f, 0.f, 0.f};
     }
-    __syncthreads();
-    if (threadIdx.x >= DH) return;
-    float mx = m_s[0];
+    const int krow0 = F32 ? r : 8 * (r >> 2) + (r & 3);     // the key this lane reads for tile 0
+    constexpr int KT = F32 ? 16 : 4;                        // and the step to tile 1
+
+    // no scalar load outstanding past here: the compiler does not see the waits in the loop's
+    // asm and would otherwise wait for all LDS reads at each use
+    __builtin_amdgcn_s_waitcnt(0xC07F);
+    for (int t = 0; t < rounds; ++t) {
+        const int cur = t % NB;
+        const int k0 = ks + 32 * (kb0 + t);
+        // (the chunk moves on with the block staged in the round before)
+        const bool before = (t >> 6) != ((min(t + NB - 2, rounds - 1)) >> 6);
+        const bool there = ((before ? have_before : have) >> (t & 63)) & 1;
+        // This wave's loads of block t have landed once at most LPW of the block staged after it are
+        // outstanding (loads complete in issue order; a page refill waits for all); the barrier makes
+        // every wave's visible and frees the buffer that round t - 1 read.
+        const int end = there ? ktop : 0;
+        if (k0 + 32 > end) {
+            asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+            zero_tail(k0, end, cur);
+        }
+        if (NB > 2 && t + 1 < rounds) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(LPW) : "memory");
+        else asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+        if (t + NB - 1 < rounds) {
+            if (((t + NB - 1) & 63) == 0) {
+                pgv = chunk_pages((t + NB - 1) >> 6);
+                have_before = have;
+                have = __builtin_amdgcn_ballot_w64(pgv >= 0);
+            }
+            stage(t + NB - 1, (t + NB - 1) % NB);
+        }
+        const char* Kb = lds + cur * BUF;
+        const char* Vb = Kb + KPLANE;
+
+        // all of the block's K fragments are read before the first product, its V^T fragments between
+        // the scores and the softmax, which covers their latency
+        u32x4_t kf[NC][2], vf[ND][NV];
 #pragma unroll
-    for (int w = 1; w < NW; ++w) mx = fmaxf(mx, m_s[w]);
-    float L = 0.f, ov = 0.f;
+        for (int c = 0; c < NC; ++c)
 #pragma unroll
-    for (int w = 0; w < NW; ++w) {
-        const float e = m_s[w] == -INFINITY ? 0.f : expf(m_s[w] - mx);
-        L += l_s[w] * e;
-        ov += o_s[w][threadIdx.x] * e;
+            for (int u = 0; u < 2; ++u) {
+                const int key = krow0 + KT * u;
+                const int sw = F32 ? key & 15 : swz_paged(key);
+                kf[c][u] = *(const u32x4_t*)(Kb + key * (DH * ES) + (((4 * c + g) ^ (sw & (KC - 1))) << 4));
+            }
+        __builtin_amdgcn_sched_barrier(0);
+        f32x4_t s[QT][2];
+#pragma unroll
+        for (int q = 0; q < QT; ++q) s[q][0] = s[q][1] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int c = 0; c < NC; ++c)
+#pragma unroll
+            for (int q = 0; q < QT; ++q)
+#pragma unroll
+                for (int u = 0; u < 2; ++u) s[q][u] = E::mfma(kf[c][u], qf[q][c], s[q][u]);
+#pragma unroll
+        for (int dt = 0; dt < ND; ++dt)
+#pragma unroll
+            for (int u = 0; u < NV; ++u) {
+                const int dim = 16 * dt + r;
+                const int sw = F32 ? dim & 7 : (dim >> 2) & 3;
+                vf[dt][u] = *(const u32x4_t*)(Vb + dim * (32 * ES) + (((4 * u + g) ^ sw) << 4));
+            }
+        __builtin_amdgcn_sched_barrier(0);
+
+        u32x4_t pf[QT][NV];
+#pragma unroll
+        for (int q = 0; q < QT; ++q) {
+            // sv[4u + i]: the score of key k0 + (16-bit) 8g + 4u + i, (fp32) 16u + 4g + i
+            float sv[8];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                sv[i] = s[q][0][i];
+                sv[4 + i] = s[q][1][i];
+            }
+            if (k0 + 32 > lim_w || !there) {
+                const int e = there ? lim[q] : 0;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const int key0 = k0 + (F32 ? 4 : 8) * g + i;
+                    if (key0 >= e) sv[i] = -INFINITY;
+                    if (key0 + KT >= e) sv[4 + i] = -INFINITY;
+                }
+            }
+            // the row's block maximum over its four lane groups (max is symmetric: a swap hands a
+            // lane its partner's value)
+            float bm = fmaxf(fmaxf(fmaxf(sv[0], sv[1]), fmaxf(sv[2], sv[3])),
+                             fmaxf(fmaxf(sv[4], sv[5]), fmaxf(sv[6], sv[7])));
+            const auto w32 = __builtin_amdgcn_permlane32_swap(__float_as_uint(bm), __float_as_uint(bm), false, false);
+            bm = fmaxf(__uint_as_float(w32[0]), __uint_as_float(w32[1]));
+            const auto w16 = __builtin_amdgcn_permlane16_swap(__float_as_uint(bm), __float_as_uint(bm), false, false);
+            bm = fmaxf(__uint_as_float(w16[0]), __uint_as_float(w16[1]));
+            const float bms = bm * a.sl2;
+            // the reference moves only when some row of the tile exceeds it by PAGED_SLACK: O, sum and
+            // merge are exact for any reference, and most blocks skip the rescale
+            if (__builtin_expect(__builtin_amdgcn_ballot_w64(bms > mrun[q] + PAGED_SLACK) != 0, 0)) {
+                const float mnew = fmaxf(mrun[q], bms);
+                const float alpha = (mnew == -INFINITY) ? 1.f : __builtin_amdgcn_exp2f(mrun[q] - mnew);
+                lrun[q] *= alpha;
+#pragma unroll
+                for (int dt = 0; dt < ND; ++dt)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) oacc[q][dt][i] *= alpha;
+                mrun[q] = mnew;
+            }
+            const float mref = (mrun[q] == -INFINITY) ? 0.f : mrun[q];
+            float p[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) p[e] = __builtin_amdgcn_exp2f(fmaf(sv[e], a.sl2, -mref));
+            lrun[q] += ((p[0] + p[1]) + (p[2] + p[3])) + ((p[4] + p[5]) + (p[6] + p[7]));
+            if constexpr (F32) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) pf[q][e >> 2][e & 3] = __float_as_uint(p[e]);
+            } else {
+                // rounded to nearest for the product with V (half a step of T a probability: as much as the
+                // output's own rounding); the sum keeps fp32
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    pf[q][0][e] = __builtin_bit_cast(uint32_t, (typename E::x2){(T)p[2 * e], (T)p[2 * e + 1]});
+            }
+        }
+#pragma unroll
+        for (int dt = 0; dt < ND; ++dt)
+#pragma unroll
+            for (int q = 0; q < QT; ++q)
+#pragma unroll
+                for (int u = 0; u < NV; ++u) oacc[q][dt] = E::mfma(vf[dt][u], pf[q][u], oacc[q][dt]);
     }
-    ((T*)a.out)[row * a.ld_out + h * DH + threadIdx.x] = elem_from_f32<T>(L > 0.f ? ov / L : 0.f);
+
+#pragma unroll
+    for (int q = 0; q < QT; ++q) {
+        float l = lrun[q] + __shfl_xor(lrun[q], 16);
+        l += __shfl_xor(l, 32);
+        const int f = f0 + 16 * (QT * qw + q) + r;
+        if (f >= nv) continue;
+        const int row = R0 + f / a.G, h = hk * a.G + f % a.G;
+        if (a.direct) {
+            const float inv = l > 0.f ? 1.f / l : 0.f;
+            T* op = (T*)a.out + row * a.ld_out + h * DH;
+#pragma unroll
+            for (int dt = 0; dt < ND; ++dt) {
+                T e[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) e[i] = elem_from_f32<T>(oacc[q][dt][i] * inv);
+                __builtin_memcpy(__builtin_assume_aligned(op + 16 * dt + 4 * g, 4 * ES), e, sizeof(e));
+            }
+        } else {
+            const size_t rec = ((size_t)part * a.T + row) * a.H + h;
+            if (rounds > 0) {
+                float* op = a.opart + rec * DH;
+#pragma unroll
+                for (int dt = 0; dt < ND; ++dt)
+                    *(float4*)(op + 16 * dt + 4 * g) =
+                        make_float4(oacc[q][dt][0], oacc[q][dt][1], oacc[q][dt][2], oacc[q][dt][3]);
+            }
+            if (g == 0) *(float2*)(a.mlpart + rec * 2) = make_float2(mrun[q], l);
+        }
+    }
+}
+
+// Merge of the parts: o = sum_s o_s 2^(m_s - M) / sum_s l_s 2^(m_s - M).  DH / 4 lanes per
+// (row, head), four dims each; parts with an empty sum wrote no output and are skipped.
+template <typename T, int DH>
+__global__ void __launch_bounds__(256) attn_paged_merge_kernel(PagedArgs a) {
+    constexpr int LPP = DH / 4;
+    const int pair = blockIdx.x * (256 / LPP) + threadIdx.x / LPP, l4 = (threadIdx.x % LPP) * 4;
+    const int R0 = max(a.row0[0], 0), R1 = min(a.row0[a.B], a.T);
+    const int row = R0 + pair / a.H, h = pair % a.H;
+    if (row >= R1) return;
+    const size_t rec = (size_t)row * a.H + h, step = (size_t)a.T * a.H;
+    const int np = a.ns_s + a.ns_o;
+    float M = -INFINITY;
+    for (int s = 0; s < np; ++s) M = fmaxf(M, a.mlpart[(s * step + rec) * 2]);
+    float L = 0.f;
+    float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int s = 0; s < np; ++s) {
+        const float2 ml = *(const float2*)(a.mlpart + (s * step + rec) * 2);
+        if (!(ml.y > 0.f)) continue;
+        const float w = exp2f(ml.x - M);
+        const float4 v = *(const float4*)(a.opart + (s * step + rec) * DH + l4);
+        L += ml.y * w;
+        o.x += v.x * w; o.y += v.y * w; o.z += v.z * w; o.w += v.w * w;
+    }
+    const float inv = L > 0.f ? 1.f / L : 0.f;
+    T e[4] = {elem_from_f32<T>(o.x * inv), elem_from_f32<T>(o.y * inv), elem_from_f32<T>(o.z * inv),
+              elem_from_f32<T>(o.w * inv)};
+    __builtin_memcpy(__builtin_assume_aligned((T*)a.out + row * a.ld_out + h * DH + l4, 4 * sizeof(T)), e, sizeof(e));
 }
 
 }  // namespace dllm
