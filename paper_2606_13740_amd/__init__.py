@@ -150,10 +150,20 @@ def _ptr(t) -> Optional[int]:
     return t.data_ptr()
 
 
+_raw_stream = None
+
+
 def _stream(stream):
+    """The stream's handle; None: the current stream of the current device."""
+    global _raw_stream
     if stream is None:
-        import torch
-        return torch.cuda.current_stream().cuda_stream
+        if _raw_stream is None:
+            import torch
+            # the handle without the Stream object around it (2.7 us a call), where torch has it
+            raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+            device = torch.cuda.current_device
+            _raw_stream = (lambda: raw(device())) if raw else (lambda: torch.cuda.current_stream().cuda_stream)
+        return _raw_stream()
     return stream if isinstance(stream, int) else stream.cuda_stream
 
 
@@ -316,89 +326,93 @@ def dllm_read_bandwidth(buf, nbytes: int, sink, stream=None):
 # where none is given, from torch's allocator on the current stream
 # ----------------------------------------------------------------------------
 
-_elem_types = {}
+class _Types:
+    """torch and its element types, looked up at the first batch call (torch is not imported with this module)."""
 
+    torch = None
 
-def _elem(t) -> int:
-    if not _elem_types:
+    @classmethod
+    def load(cls):
         import torch
-        _elem_types.update({torch.float32: DLLM_F32, torch.bfloat16: DLLM_BF16, torch.float16: DLLM_F16})
-    return _elem_types.get(t.dtype, -1)
+        cls.i32, cls.f32 = torch.int32, torch.float32
+        cls.elem = {torch.float32: DLLM_F32, torch.bfloat16: DLLM_BF16, torch.float16: DLLM_F16}
+        cls.device = torch.cuda.current_device
+        cls.torch = torch
 
 
 def _refuse(func: str, msg: str):
     raise DllmError(DLLM_E_INVAL, func, msg)
 
 
-def _like(func: str, ref, dtype, **tensors):
-    """Every tensor that is there: on ref's device (the current one), contiguous, of `dtype` (None: ref's)."""
-    import torch
-
-    if not ref.is_cuda or ref.device.index != torch.cuda.current_device():
+def _gpu(func: str, ref) -> int:
+    """The current GPU's index, which ref must be on."""
+    if _Types.torch is None:
+        _Types.load()
+    if not ref.is_cuda or ref.get_device() != _Types.device():
         _refuse(func, "tensors must be on the current GPU")
-    dt = ref.dtype if dtype is None else dtype
-    for name, t in tensors.items():
-        if t is None:
-            continue
-        if t.device != ref.device:
-            _refuse(func, f"{name} is on another device")
-        if t.dtype != dt:
-            _refuse(func, f"{name} must be {dt}")
-        if not t.is_contiguous():
-            _refuse(func, f"{name} must be contiguous")
+    return ref.get_device()
 
 
-def _rows(func: str, name: str, t, ref, heads: int, dim: int) -> int:
+def _plain(func: str, dev: int, dtype, tensors, names: str):
+    """Every tensor that is there: on that GPU, of that type, contiguous."""
+    for t in tensors:
+        if t is not None and (t.dtype is not dtype or t.get_device() != dev or not t.is_contiguous()):
+            bad = names.split()[[u is t for u in tensors].index(True)]
+            _refuse(func, f"{bad} must be a contiguous {dtype} tensor on the same GPU")
+
+
+def _at_least(func: str, n: int, tensors, names: str):
+    for t in tensors:
+        if t is not None and t.numel() < n:
+            bad = names.split()[[u is t for u in tensors].index(True)]
+            _refuse(func, f"{bad} must have at least {n} entries")
+
+
+def _row_stride(func: str, name: str, t, ref, dev: int, heads: int, dim: int) -> int:
     """Row stride of a [rows][heads * dim] or [rows][heads][dim] tensor whose rows are whole; checks its shape."""
     sh, st = t.shape, t.stride()
-    if t.dtype != ref.dtype or t.device != ref.device:
+    if t.dtype is not ref.dtype or t.get_device() != dev:
         _refuse(func, f"{name} must have q's type and device")
-    if sh[0] != ref.shape[0] or st[-1] != 1 or not (
-            len(sh) == 2 and sh[1] == heads * dim or len(sh) == 3 and sh[1] == heads and sh[2] == dim and (heads == 1 or st[1] == dim)):
+    if len(sh) == 2:
+        ok = sh[1] == heads * dim and st[1] == 1
+    else:
+        ok = len(sh) == 3 and sh[1] == heads and sh[2] == dim and st[2] == 1 and (heads == 1 or st[1] == dim)
+    if not ok or sh[0] != ref.shape[0]:
         _refuse(func, f"{name} must be [rows][{heads}][{dim}] with whole rows")
     return st[0] if sh[0] > 1 else heads * dim
-
-
-def _at_least(func: str, n: int, **tensors):
-    for name, t in tensors.items():
-        if t is not None and t.numel() < n:
-            _refuse(func, f"{name} must have at least {n} entries")
 
 
 def dllm_batch_plan(length, new, owned, owned_out, table, free, n_free, n_free_out, page: int, shared_pages: int, row0,
                     pos, slot, seq, lim, status, stream=None):
     """The row arrays' common length is the plan's max_rows; free has an entry per page of the pool."""
-    f, B, ld = "dllm_batch_plan", length.numel(), table.shape[-1]
-    import torch
-    _like(f, length, torch.int32, length=length, new=new, owned=owned, owned_out=owned_out, table=table, free=free,
-          n_free=n_free, n_free_out=n_free_out, row0=row0, pos=pos, slot=slot, seq=seq, lim=lim, status=status)
-    _at_least(f, B, new=new, owned=owned, owned_out=owned_out)
-    _at_least(f, B * ld, table=table)
-    _at_least(f, B + 1, row0=row0)
-    _at_least(f, pos.numel(), slot=slot, seq=seq, lim=lim)
-    _at_least(f, 3, status=status)
-    _at_least(f, 1, n_free=n_free, n_free_out=n_free_out)
+    f, B, ld, R = "dllm_batch_plan", length.numel(), table.shape[-1], pos.numel()
+    _plain(f, _gpu(f, length), _Types.i32, (length, new, owned, owned_out, table, free, n_free, n_free_out, row0, pos, slot,
+                                            seq, lim, status),
+           "length new owned owned_out table free n_free n_free_out row0 pos slot seq lim status")
+    _at_least(f, B, (new, owned, owned_out), "new owned owned_out")
+    _at_least(f, R, (slot, seq, lim), "slot seq lim")
+    if table.numel() < B * ld or row0.numel() < B + 1 or status.numel() < 3 or not n_free.numel() or not n_free_out.numel():
+        _refuse(f, "table must have a row and row0 an entry per sequence (row0: one more), status 3 entries, n_free 1")
     _check(lib().dllm_batch_plan(length.data_ptr(), new.data_ptr(), owned.data_ptr(), owned_out.data_ptr(), B,
                                  table.data_ptr(), ld, free.data_ptr(), n_free.data_ptr(), n_free_out.data_ptr(),
-                                 free.numel(), page, shared_pages, pos.numel(), row0.data_ptr(), pos.data_ptr(),
-                                 slot.data_ptr(), seq.data_ptr(), lim.data_ptr(), status.data_ptr(), _stream(stream)), f)
+                                 free.numel(), page, shared_pages, R, row0.data_ptr(), pos.data_ptr(), slot.data_ptr(),
+                                 seq.data_ptr(), lim.data_ptr(), status.data_ptr(), _stream(stream)), f)
 
 
 def dllm_rope_table(table, head_dim: int, rope_base: float, stream=None):
     """table: float32 [max_pos][head_dim / 2][2]."""
     f = "dllm_rope_table"
-    import torch
-    _like(f, table, torch.float32, table=table)
+    _plain(f, _gpu(f, table), _Types.f32, (table,), "table")
     if table.numel() % head_dim != 0:
         _refuse(f, "table must be [max_pos][head_dim / 2][2]")
     _check(lib().dllm_rope_table(table.data_ptr(), table.numel() // head_dim, head_dim, rope_base, _stream(stream)), f)
 
 
-def _pages(f: str, q, k_pages, v_pages):
+def _pages(f: str, q, dev: int, k_pages, v_pages):
     """(n_pages, kv heads, page, head_dim) of a K plane [n_pages][kv][page][dim] and a V^T plane [n_pages][kv][dim][page]."""
-    _like(f, q, None, k_pages=k_pages, v_pages=v_pages)
+    _plain(f, dev, q.dtype, (k_pages, v_pages), "k_pages v_pages")
     n, kv, page, dim = k_pages.shape
-    if tuple(v_pages.shape) != (n, kv, dim, page):
+    if v_pages.shape != (n, kv, dim, page):
         _refuse(f, "v_pages must be [n_pages][kv_heads][head_dim][page]")
     return n, kv, page, dim
 
@@ -407,31 +421,39 @@ def dllm_qk_norm_rope(q, k, v, rope, pos, slot, q_out, k_pages, v_pages, q_gain=
                       stream=None):
     """q, k, v: [rows][heads][dim] or [rows][heads * dim], rows may be strided (slices of one projection's output)."""
     f = "dllm_qk_norm_rope"
-    import torch
-    n_pages, kv, page, dim = _pages(f, q, k_pages, v_pages)
-    T = q.shape[0]
-    H = q_out.shape[1] if q_out.dim() == 3 else q_out.shape[1] // dim
-    ld_q, ld_k, ld_v = (_rows(f, n, t, q, h, dim) for n, t, h in (("q", q, H), ("k", k, kv), ("v", v, kv)))
-    _like(f, q, None, q_out=q_out)
-    _like(f, q, torch.float32, rope=rope, q_gain=q_gain, k_gain=k_gain)
-    _like(f, q, torch.int32, pos=pos, slot=slot)
-    _at_least(f, T, pos=pos, slot=slot)
-    _at_least(f, T * H * dim, q_out=q_out)
-    _at_least(f, dim, q_gain=q_gain, k_gain=k_gain)
-    a = dllm_qk_args(_elem(q), T, H, kv, dim, page, n_pages, rope.numel() // dim, eps, q.data_ptr(), k.data_ptr(),
-                     v.data_ptr(), ld_q, ld_k, ld_v, _ptr(q_gain), _ptr(k_gain), rope.data_ptr(), pos.data_ptr(),
-                     slot.data_ptr(), q_out.data_ptr(), k_pages.data_ptr(), v_pages.data_ptr())
+    dev = _gpu(f, q)
+    n_pages, kv, page, dim = _pages(f, q, dev, k_pages, v_pages)
+    T, qs = q.shape[0], q_out.shape
+    H = qs[1] if len(qs) == 3 else qs[1] // dim
+    ld_q, ld_k = _row_stride(f, "q", q, q, dev, H, dim), _row_stride(f, "k", k, q, dev, kv, dim)
+    ld_v = _row_stride(f, "v", v, q, dev, kv, dim)
+    _plain(f, dev, q.dtype, (q_out,), "q_out")
+    _plain(f, dev, _Types.f32, (rope, q_gain, k_gain), "rope q_gain k_gain")
+    _plain(f, dev, _Types.i32, (pos, slot), "pos slot")
+    _at_least(f, T, (pos, slot), "pos slot")
+    _at_least(f, dim, (q_gain, k_gain), "q_gain k_gain")
+    if qs[0] < T or q_out.numel() != qs[0] * H * dim:
+        _refuse(f, "q_out must be [rows][heads][dim]")
+    a = dllm_qk_args(_Types.elem.get(q.dtype, -1), T, H, kv, dim, page, n_pages, rope.numel() // dim, eps, q.data_ptr(),
+                     k.data_ptr(), v.data_ptr(), ld_q, ld_k, ld_v, _ptr(q_gain), _ptr(k_gain), rope.data_ptr(),
+                     pos.data_ptr(), slot.data_ptr(), q_out.data_ptr(), k_pages.data_ptr(), v_pages.data_ptr())
     _check(lib().dllm_qk_norm_rope(ctypes.byref(a), _stream(stream)), f)
 
 
-def _workspace(query, a, ws, device, f: str):
-    """Sets a's workspace: `ws`, or memory of the call's own (which the caller keeps until the call has been made)."""
-    n = _sz()
-    _check(query(ctypes.byref(a), ctypes.byref(n)), f + "_ws")
-    if ws is None and n.value:
-        import torch
-        ws = torch.empty(n.value, dtype=torch.uint8, device=device)
-    if ws is not None:
+def _workspace(query, a, ws, stream, dev: int, f: str):
+    """Sets a's workspace: `ws`, or memory of the call's own (on the current stream; freed once the call has been made)."""
+    if ws is None:
+        n = _sz()
+        _check(query(ctypes.byref(a), ctypes.byref(n)), f + "_ws")
+        if not n.value:
+            return None
+        if stream is not None:
+            _refuse(f, "a call on a given stream needs a workspace of the caller's")
+        ws = _Types.torch.empty(n.value, dtype=_Types.torch.uint8, device=dev)
+        a.d_ws, a.ws_bytes = ws.data_ptr(), n.value
+    else:
+        if ws.get_device() != dev or not ws.is_contiguous():
+            _refuse(f, "ws must be a contiguous tensor on the same GPU")
         a.d_ws, a.ws_bytes = ws.data_ptr(), ws.numel() * ws.element_size()
     return ws
 
@@ -440,22 +462,20 @@ def dllm_attention_paged(q, k_pages, v_pages, table, row0, length, out, max_rows
                          shared_len: int = 0, lim=None, scale: Optional[float] = None, ws=None, stream=None):
     """q, out: [rows][heads][dim] or [rows][heads * dim], rows may be strided; scale: 1 / sqrt(dim) if None."""
     f = "dllm_attention_paged"
-    import torch
-    n_pages, kv, page, dim = _pages(f, q, k_pages, v_pages)
-    H = q.shape[1] if q.dim() == 3 else q.shape[1] // dim
-    ld_q, ld_out = _rows(f, "q", q, q, H, dim), _rows(f, "out", out, q, H, dim)
+    dev = _gpu(f, q)
+    n_pages, kv, page, dim = _pages(f, q, dev, k_pages, v_pages)
+    sh = q.shape
+    H = sh[1] if len(sh) == 3 else sh[1] // dim
+    ld_q, ld_out = _row_stride(f, "q", q, q, dev, H, dim), _row_stride(f, "out", out, q, dev, H, dim)
     B, ld = length.numel(), table.shape[-1]
-    _like(f, q, torch.int32, table=table, row0=row0, length=length, lim=lim)
-    _at_least(f, B * ld, table=table)
-    _at_least(f, B + 1, row0=row0)
-    _at_least(f, q.shape[0], lim=lim)
-    if stream is not None and ws is None:
-        _refuse(f, "a call on a given stream needs a workspace")
-    a = dllm_attn_args(_elem(q), q.shape[0], B, H, kv, dim, page, n_pages, ld, shared_len, max_rows, max_len,
+    _plain(f, dev, _Types.i32, (table, row0, length, lim), "table row0 length lim")
+    if table.numel() < B * ld or row0.numel() < B + 1 or (lim is not None and lim.numel() < sh[0]):
+        _refuse(f, "table must have a row and row0 an entry per sequence (row0: one more), lim an entry per row")
+    a = dllm_attn_args(_Types.elem.get(q.dtype, -1), sh[0], B, H, kv, dim, page, n_pages, ld, shared_len, max_rows, max_len,
                        dim ** -0.5 if scale is None else scale, q.data_ptr(), ld_q, k_pages.data_ptr(),
                        v_pages.data_ptr(), table.data_ptr(), row0.data_ptr(), length.data_ptr(), _ptr(lim),
                        out.data_ptr(), ld_out)
-    keep = _workspace(lib().dllm_attention_paged_ws, a, ws, q.device, f)
+    keep = _workspace(lib().dllm_attention_paged_ws, a, ws, stream, dev, f)
     _check(lib().dllm_attention_paged(ctypes.byref(a), _stream(stream)), f)
     del keep
 
@@ -465,28 +485,29 @@ def dllm_select(logits, out_id, out_conf, mask_id: int = -1, row0=None, hist=Non
                 allow_row=None, out_logits=None, ws=None, stream=None):
     """logits, out_logits: [rows][vocab], rows may be strided; allow: int32 words [masks][words]."""
     f = "dllm_select"
-    import torch
+    dev = _gpu(f, logits)
     T, V = logits.shape
     B = row0.numel() - 1 if row0 is not None else 1
-    _like(f, logits, torch.int32, out_id=out_id, row0=row0, hist=hist, hist0=hist0, n_prompt=n_prompt, bias_id=bias_id,
-          bias0=bias0, allow=allow, allow_row=allow_row)
-    _like(f, logits, torch.float32, out_conf=out_conf, repetition=repetition, presence=presence, frequency=frequency,
-          bias=bias)
-    _at_least(f, T, out_id=out_id, out_conf=out_conf, allow_row=allow_row)
-    _at_least(f, B, n_prompt=n_prompt, repetition=repetition, presence=presence, frequency=frequency)
-    _at_least(f, B + 1, hist0=hist0, bias0=bias0)
-    for name, t in (("logits", logits), ("out_logits", out_logits)):
-        if t is not None and (t.shape != logits.shape or t.dtype != logits.dtype or t.device != logits.device or (V > 1 and t.stride(1) != 1)):
-            _refuse(f, f"{name} must be [rows][vocab] of one type with whole rows")
-    if stream is not None and ws is None:
-        _refuse(f, "a call on a given stream needs a workspace")
-    a = dllm_select_args(_elem(logits), T, V, mask_id, B, logits.data_ptr(), logits.stride(0) if T > 1 else V, _ptr(row0),
-                         _ptr(hist), _ptr(hist0), _ptr(n_prompt), _ptr(repetition), _ptr(presence), _ptr(frequency),
-                         _ptr(bias_id), _ptr(bias), _ptr(bias0), _ptr(allow), 0 if allow is None else allow.shape[0],
-                         0 if allow is None else allow.shape[1], _ptr(allow_row), _ptr(out_logits),
-                         0 if out_logits is None else (out_logits.stride(0) if T > 1 else V), out_id.data_ptr(),
-                         out_conf.data_ptr())
-    keep = _workspace(lib().dllm_select_ws, a, ws, logits.device, f)
+    _plain(f, dev, _Types.i32, (out_id, row0, hist, hist0, n_prompt, bias_id, bias0, allow, allow_row),
+           "out_id row0 hist hist0 n_prompt bias_id bias0 allow allow_row")
+    _plain(f, dev, _Types.f32, (out_conf, repetition, presence, frequency, bias), "out_conf repetition presence frequency bias")
+    _at_least(f, T, (out_id, out_conf, allow_row), "out_id out_conf allow_row")
+    _at_least(f, B, (n_prompt, repetition, presence, frequency), "n_prompt repetition presence frequency")
+    _at_least(f, B + 1, (hist0, bias0), "hist0 bias0")
+    st, ld_out = logits.stride(), 0
+    if out_logits is not None:
+        so = out_logits.stride()
+        if out_logits.shape != logits.shape or out_logits.dtype is not logits.dtype or out_logits.get_device() != dev or (V > 1 and so[1] != 1):
+            _refuse(f, "out_logits must be of the logits' shape and type, with whole rows")
+        ld_out = so[0] if T > 1 else V
+    if V > 1 and st[1] != 1:
+        _refuse(f, "logits must have whole rows")
+    n_allow, allow_ld = allow.shape if allow is not None else (0, 0)
+    a = dllm_select_args(_Types.elem.get(logits.dtype, -1), T, V, mask_id, B, logits.data_ptr(), st[0] if T > 1 else V,
+                         _ptr(row0), _ptr(hist), _ptr(hist0), _ptr(n_prompt), _ptr(repetition), _ptr(presence),
+                         _ptr(frequency), _ptr(bias_id), _ptr(bias), _ptr(bias0), _ptr(allow), n_allow, allow_ld,
+                         _ptr(allow_row), _ptr(out_logits), ld_out, out_id.data_ptr(), out_conf.data_ptr())
+    keep = _workspace(lib().dllm_select_ws, a, ws, stream, dev, f)
     _check(lib().dllm_select(ctypes.byref(a), _stream(stream)), f)
     del keep
 

@@ -200,6 +200,25 @@ int check_attn(const dllm_attn_args* g, int& shift) {
     return DLLM_OK;
 }
 
+// Ranges of SEL_IDS ids, and rows of a workgroup: enough workgroups to fill the chip a few times over, and
+// otherwise as many rows as keep a sequence's tables.
+int select_ranges(int vocab) { return ceil_div(vocab, SEL_IDS); }
+int select_rows_per(int T, int n_ranges) {
+    const long per = (long)T * n_ranges / 1024;
+    return (int)std::min<long>(SEL_MAX_ROWS, std::max<long>(SEL_RB, per / SEL_RB * SEL_RB));
+}
+size_t select_ws_bytes(const dllm_select_args* g) {
+    const int n = select_ranges(g->vocab);
+    return n == 1 ? 0 : (size_t)g->n_rows * n * sizeof(SelectPart);
+}
+
+template <typename T>
+void launch_select(const SelectArgs& a, SelectPart* part, hipStream_t s) {
+    const int n = select_ranges(a.V), per = select_rows_per(a.T, n);
+    hipLaunchKernelGGL(select_kernel<T>, dim3((unsigned)n * ceil_div(a.T, per)), dim3(SEL_NT), 0, s, a, part, n, per);
+    if (n > 1) hipLaunchKernelGGL(select_merge_kernel, dim3(ceil_div(a.T, 4)), dim3(256), 0, s, a, (const SelectPart*)part, n);
+}
+
 int check_select(const dllm_select_args* g) {
     if (!g) return fail(DLLM_E_INVAL, "args is NULL");
     if (int rc = check_dtype(g->dtype)) return rc;
@@ -295,7 +314,7 @@ int dllm_attention_paged(const dllm_attn_args* g, dllm_stream stream) {
 int dllm_select_ws(const dllm_select_args* g, size_t* bytes) {
     if (!bytes) return fail(DLLM_E_INVAL, "bytes is NULL");
     if (int rc = check_select(g)) return rc;
-    *bytes = 0;
+    *bytes = select_ws_bytes(g);
     return DLLM_OK;
 }
 
@@ -328,14 +347,21 @@ int dllm_select(const dllm_select_args* g, dllm_stream stream) {
     for (const void* p : ints)
         if (!aligned(p, 4)) return fail(DLLM_E_INVAL, "arrays of 32-bit values must be 4-byte aligned");
     if (g->n_rows == 0) return DLLM_OK;
+    const size_t need = select_ws_bytes(g);
+    if ((long)select_ranges(g->vocab) * ceil_div(g->n_rows, SEL_RB) > 0x7FFFFFFF)
+        return fail(DLLM_E_INVAL, "n_rows and vocab need too many workgroups");
+    if (need > 0 && (!g->d_ws || !aligned(g->d_ws, 16))) return fail(DLLM_E_INVAL, "workspace: NULL or not 16-byte aligned");
+    if (need > g->ws_bytes)
+        return fail(DLLM_E_CAPACITY, "the call needs " + std::to_string(need) + " bytes of workspace");
     SelectArgs a{g->d_logits, g->ld, g->n_rows, g->vocab, g->mask_id, g->n_seqs, g->d_row0, g->d_hist, g->d_hist0,
                  g->d_n_prompt, g->d_repetition, g->d_presence, g->d_frequency, g->d_bias_id, g->d_bias, g->d_bias0,
                  g->d_allow, g->n_allow, g->allow_ld, g->d_allow_row, g->d_out_logits, g->ld_out, g->d_out_id,
                  g->d_out_conf};
     hipStream_t s = (hipStream_t)stream;
-    if (g->dtype == DLLM_F32) hipLaunchKernelGGL(select_row_kernel<float>, dim3(a.T), dim3(256), 0, s, a);
-    else if (g->dtype == DLLM_F16) hipLaunchKernelGGL(select_row_kernel<_Float16>, dim3(a.T), dim3(256), 0, s, a);
-    else hipLaunchKernelGGL(select_row_kernel<__bf16>, dim3(a.T), dim3(256), 0, s, a);
+    SelectPart* part = (SelectPart*)g->d_ws;
+    if (g->dtype == DLLM_F32) launch_select<float>(a, part, s);
+    else if (g->dtype == DLLM_F16) launch_select<_Float16>(a, part, s);
+    else launch_select<__bf16>(a, part, s);
     HIP_TRY(hipGetLastError());
     return DLLM_OK;
 }

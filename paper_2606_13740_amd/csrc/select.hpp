@@ -3,6 +3,7 @@
 
 #include <float.h>
 
+#include "attn_paged.hpp"
 #include "common.hpp"
 #include "qk_rope.hpp"
 
@@ -53,53 +54,227 @@ __device__ __forceinline__ float adjust_logit(float l, bool seen, int made, floa
     return l != l ? -INFINITY : fminf(l, FLT_MAX);
 }
 
-// Simple form: a workgroup per row; every id scans its sequence's history and bias list.
+// The six butterfly steps of a wave-wide reduction without LDS: lane permutes inside 16 lanes (a
+// mirror stands for the exchange of groups whose lanes agree already), then the two swaps.
+template <class F> __device__ __forceinline__ uint32_t wave_fold(uint32_t v, F f) {
+    v = f(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0xB1, 0xF, 0xF, true));      // lane ^ 1
+    v = f(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x4E, 0xF, 0xF, true));      // lane ^ 2
+    v = f(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x141, 0xF, 0xF, true));     // mirror in 8
+    v = f(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x140, 0xF, 0xF, true));     // mirror in 16
+    const auto a = __builtin_amdgcn_permlane16_swap(v, v, false, false);
+    v = f(a[0], a[1]);
+    const auto b = __builtin_amdgcn_permlane32_swap(v, v, false, false);
+    return f(b[0], b[1]);
+}
+__device__ __forceinline__ float wave_max_f(float v) {
+    return __uint_as_float(wave_fold(__float_as_uint(v), [](uint32_t a, uint32_t b) {
+        return __float_as_uint(fmaxf(__uint_as_float(a), __uint_as_float(b))); }));
+}
+__device__ __forceinline__ float wave_sum_f(float v) {
+    return __uint_as_float(wave_fold(__float_as_uint(v), [](uint32_t a, uint32_t b) {
+        return __float_as_uint(__uint_as_float(a) + __uint_as_float(b)); }));
+}
+__device__ __forceinline__ uint32_t wave_min_u(uint32_t v) {
+    return wave_fold(v, [](uint32_t a, uint32_t b) { return min(a, b); });
+}
+// Best of a wave's lanes, in every lane.
+__device__ __forceinline__ Best wave_best(const Best& b) {
+    const float mx = wave_max_f(b.id < 0 ? -INFINITY : b.mx);
+    const uint32_t id = wave_min_u(b.id >= 0 && b.mx == mx ? (uint32_t)b.id : 0xFFFFFFFFu);
+    const float s = wave_sum_f(b.id < 0 ? 0.f : b.s * __expf(b.mx - mx));
+    return Best{mx, (int)id, s};
+}
+
+// A workgroup takes SEL_IDS consecutive ids of `rows_per` consecutive rows.  A thread holds eight ids
+// for all of them, so a sequence's history and bias list are scanned once per workgroup, into
+// LDS tables of its ids, and each thread keeps its eight entries in registers; most threads have
+// none and skip the adjustment.  Four rows are loaded at a time.  The best of the workgroup's
+// ids goes to part[row][range]; with one range (small vocabularies) it is the result.
+//
+// What bounds it: reading the logits (16 bytes a lane, also from rows that start at odd
+// elements: the hardware takes unaligned addresses).
+constexpr int SEL_NT = 256, SEL_PT = 8, SEL_IDS = SEL_NT * SEL_PT, SEL_RB = 4, SEL_MAX_ROWS = 16;
+constexpr uint32_t SEL_SEEN = 0x80000000u, SEL_BIAS = 0x40000000u;
+
+struct alignas(16) SelectPart {
+    float mx;
+    int id;
+    float s;
+    int pad;
+};
+
 template <typename T>
-__global__ void __launch_bounds__(256) select_row_kernel(SelectArgs a) {
-    __shared__ Best red[4];
-    const int row = blockIdx.x;
-    int b = 0;
-    if (a.row0 != nullptr) {
-        if (row < a.row0[0] || row >= a.row0[a.B]) return;
-        while (b + 1 < a.B && a.row0[b + 1] <= row) ++b;
-    }
-    const T* src = (const T*)a.logits + row * a.ld;
-    T* dst = a.out ? (T*)a.out + row * a.ld_out : nullptr;
-    const float rep = a.rep ? a.rep[b] : 1.f, pres = a.pres ? a.pres[b] : 0.f, freq = a.freq ? a.freq[b] : 0.f;
-    const int h0 = a.hist ? a.hist0[b] : 0, h1 = a.hist ? a.hist0[b + 1] : 0;
-    const int hp = a.hist && a.n_prompt ? h0 + a.n_prompt[b] : h0;
-    const int i0 = a.bias ? a.bias0[b] : 0, i1 = a.bias ? a.bias0[b + 1] : 0;
-    const int ar = a.allow ? (a.allow_row ? a.allow_row[row] : row) : -1;
-    Best best{-INFINITY, -1, 0.f};
-    for (int v = threadIdx.x; v < a.V; v += 256) {
-        int made = 0;
-        bool seen = false, has = false;
-        float bias = 0.f;
-        for (int i = h0; i < h1; ++i)
-            if (a.hist[i] == v) {
-                seen = true;
-                made += i >= hp;
-            }
-        for (int i = i0; i < i1; ++i)
-            if (a.bias_id[i] == v) {
-                has = true;
-                bias = a.bias[i];
-            }
-        float l = adjust_logit(elem_to_f32<T>(src[v]), seen, made, bias, has, rep, pres, freq);
-        bool drop = v == a.mask_id;
-        if (a.allow && ar != -1)
-            drop |= ar < 0 || ar >= a.n_allow || (v >> 5) >= a.allow_ld || !(a.allow[(size_t)ar * a.allow_ld + (v >> 5)] >> (v & 31) & 1);
-        if (drop) l = -INFINITY;
-        if (dst) dst[v] = (T)l;
-        if (l > -INFINITY) best = best_merge(best, Best{l, v, 1.f});
-    }
+__global__ void __launch_bounds__(SEL_NT) select_kernel(SelectArgs a, SelectPart* part, int n_ranges, int rows_per) {
+    constexpr int NL = 16 / (int)sizeof(T), U = SEL_PT / NL;   // ids per 16-byte load, loads per row
+    __shared__ uint32_t adj_s[SEL_IDS], last_s[SEL_IDS];
+    __shared__ float bias_s[SEL_IDS];
+    __shared__ Best red[SEL_MAX_ROWS][SEL_NT / 64];
+    const int tid = threadIdx.x;
+    const int range = (int)(blockIdx.x % n_ranges), group = (int)(blockIdx.x / n_ranges);
+    const int v0 = range * SEL_IDS;
+    const int first = a.row0 ? max(0, a.row0[0]) : 0, behind = a.row0 ? min(a.T, a.row0[a.B]) : a.T;
+    const int r0 = max(first, group * rows_per), r1 = min(behind, (group + 1) * rows_per);
+    if (r0 >= r1) return;
+    // load u's first id of this thread
+    auto id_of = [&](int u) { return v0 + u * SEL_NT * NL + tid * NL; };
+
+    uint32_t adj[SEL_PT];
+    float bias[SEL_PT], rep = 1.f, pres = 0.f, freq = 0.f;
+    bool touched = false;
 #pragma unroll
-    for (int o = 1; o < 64; o <<= 1)
-        best = best_merge(best, Best{__shfl_xor(best.mx, o), __shfl_xor(best.id, o), __shfl_xor(best.s, o)});
-    if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = best;
+    for (int j = 0; j < SEL_PT; ++j) { adj[j] = 0; bias[j] = 0.f; }
+
+    // the tables of sequence b's history and biases at this workgroup's ids
+    auto enter = [&](int b) {
+        rep = a.rep ? a.rep[b] : 1.f;
+        pres = a.pres ? a.pres[b] : 0.f;
+        freq = a.freq ? a.freq[b] : 0.f;
+        const int h0 = a.hist ? a.hist0[b] : 0, h1 = a.hist ? a.hist0[b + 1] : 0;
+        const int i0 = a.bias ? a.bias0[b] : 0, i1 = a.bias ? a.bias0[b + 1] : 0;
+        touched = false;
+        if (h0 >= h1 && i0 >= i1) return;
+        const int hp = a.n_prompt ? h0 + a.n_prompt[b] : h0;
+        __syncthreads();                                       // the tables of the sequence before are read
+        for (int i = tid; i < SEL_IDS; i += SEL_NT) { adj_s[i] = 0; last_s[i] = 0; }
+        __syncthreads();
+        for (int i = h0 + tid; i < h1; i += SEL_NT) {
+            const int v = a.hist[i], k = v - v0;
+            if ((unsigned)k < (unsigned)SEL_IDS && v < a.V) {
+                atomicOr(&adj_s[k], SEL_SEEN);
+                if (i >= hp) atomicAdd(&adj_s[k], 1u);         // whole numbers: any order gives the same sum
+            }
+        }
+        for (int i = i0 + tid; i < i1; i += SEL_NT) {
+            const int v = a.bias_id[i], k = v - v0;
+            if ((unsigned)k < (unsigned)SEL_IDS && v < a.V) atomicMax(&last_s[k], (uint32_t)(i - i0) + 1u);
+        }
+        __syncthreads();
+        for (int i = i0 + tid; i < i1; i += SEL_NT) {
+            const int v = a.bias_id[i], k = v - v0;
+            if ((unsigned)k < (unsigned)SEL_IDS && v < a.V && last_s[k] == (uint32_t)(i - i0) + 1u) {
+                bias_s[k] = a.bias[i];                         // the last entry of an id: one thread
+                atomicOr(&adj_s[k], SEL_BIAS);
+            }
+        }
+        __syncthreads();
+#pragma unroll
+        for (int j = 0; j < SEL_PT; ++j) {
+            const int k = id_of(j / NL) - v0 + j % NL;
+            adj[j] = adj_s[k];
+            bias[j] = (adj[j] & SEL_BIAS) ? bias_s[k] : 0.f;
+            touched |= adj[j] != 0;
+        }
+    };
+
+    int b = -1, b_end = r0;                                    // rows below b_end belong to b
+    for (int rb = r0; rb < r1; rb += SEL_RB) {
+        T x[SEL_RB][SEL_PT];
+#pragma unroll
+        for (int i = 0; i < SEL_RB; ++i) {
+            const T* src = (const T*)a.logits + (long)min(rb + i, r1 - 1) * a.ld;
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const int v = id_of(u);
+                if (v + NL <= a.V) {
+                    __builtin_memcpy(&x[i][u * NL], src + v, 16);
+                } else {
+#pragma unroll
+                    for (int j = 0; j < NL; ++j) x[i][u * NL + j] = v + j < a.V ? src[v + j] : (T)0.f;
+                }
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < SEL_RB; ++i) {
+            const int row = rb + i;
+            if (row >= r1) break;
+            if (row >= b_end) {
+                int nb = 0;
+                b_end = a.T;
+                if (a.row0 != nullptr) {
+                    nb = row_seq(a.row0, a.B, row);
+                    b_end = a.row0[nb + 1];
+                }
+                if (nb != b) enter(b = nb);
+            }
+            const int ar = a.allow ? (a.allow_row ? a.allow_row[row] : row) : -1;
+            const bool none = a.allow && ar != -1 && (ar < 0 || ar >= a.n_allow);
+            float l[SEL_PT];
+            Best best{-INFINITY, -1, 0.f};
+#pragma unroll
+            for (int j = 0; j < SEL_PT; ++j) {
+                l[j] = elem_to_f32<T>(x[i][j]);
+                l[j] = l[j] != l[j] ? -INFINITY : fminf(l[j], FLT_MAX);
+            }
+            if (touched) {
+#pragma unroll
+                for (int j = 0; j < SEL_PT; ++j)
+                    if (adj[j] != 0)
+                        l[j] = adjust_logit(elem_to_f32<T>(x[i][j]), (adj[j] & SEL_SEEN) != 0, (int)(adj[j] & 0x3FFFFFFFu),
+                                            bias[j], (adj[j] & SEL_BIAS) != 0, rep, pres, freq);
+            }
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const int v = id_of(u);
+                uint32_t bits = 0xFFFFFFFFu;
+                if (none) bits = 0;
+                else if (a.allow && ar != -1 && v < a.V) bits = a.allow[(size_t)ar * a.allow_ld + (v >> 5)] >> (v & 31);
+#pragma unroll
+                for (int j = 0; j < NL; ++j)
+                    if (!(bits >> j & 1) || v + j == a.mask_id || v + j >= a.V) l[u * NL + j] = -INFINITY;
+            }
+            if (a.out != nullptr) {
+                T* dst = (T*)a.out + (long)row * a.ld_out;
+                T y[SEL_PT];
+#pragma unroll
+                for (int j = 0; j < SEL_PT; ++j) y[j] = (T)l[j];
+#pragma unroll
+                for (int u = 0; u < U; ++u) {
+                    const int v = id_of(u);
+                    if (v + NL <= a.V) {
+                        __builtin_memcpy(dst + v, &y[u * NL], 16);
+                    } else {
+#pragma unroll
+                        for (int j = 0; j < NL; ++j)
+                            if (v + j < a.V) dst[v + j] = y[u * NL + j];
+                    }
+                }
+            }
+#pragma unroll
+            for (int j = SEL_PT - 1; j >= 0; --j)              // downwards: the lowest id of the largest stays
+                if (l[j] >= best.mx && l[j] > -INFINITY) { best.mx = l[j]; best.id = id_of(j / NL) + j % NL; }
+            if (best.id >= 0)
+#pragma unroll
+                for (int j = 0; j < SEL_PT; ++j) best.s += __expf(l[j] - best.mx);
+            best = wave_best(best);
+            if ((tid & 63) == 0) red[row - r0][tid >> 6] = best;
+        }
+    }
     __syncthreads();
-    if (threadIdx.x == 0) {
-        for (int w = 1; w < 4; ++w) best = best_merge(best, red[w]);
+    if (tid < r1 - r0) {
+        Best best = red[tid][0];
+#pragma unroll
+        for (int w = 1; w < SEL_NT / 64; ++w) best = best_merge(best, red[tid][w]);
+        const int row = r0 + tid;
+        if (n_ranges == 1) {
+            a.out_id[row] = best.id;
+            a.out_conf[row] = best.id >= 0 ? 1.f / best.s : 0.f;
+        } else {
+            part[(size_t)row * n_ranges + range] = SelectPart{best.mx, best.id, best.s, 0};
+        }
+    }
+}
+
+// Merge of the ranges: one wave per row.
+__global__ void __launch_bounds__(256) select_merge_kernel(SelectArgs a, const SelectPart* part, int n_ranges) {
+    const int row = blockIdx.x * 4 + (threadIdx.x >> 6), lane = threadIdx.x & 63;
+    if (row >= a.T || (a.row0 != nullptr && (row < a.row0[0] || row >= a.row0[a.B]))) return;
+    Best best{-INFINITY, -1, 0.f};
+    for (int i = lane; i < n_ranges; i += 64) {
+        const SelectPart p = part[(size_t)row * n_ranges + i];
+        best = best_merge(best, Best{p.mx, p.id, p.s});
+    }
+    best = wave_best(best);
+    if (lane == 0) {
         a.out_id[row] = best.id;
         a.out_conf[row] = best.id >= 0 ? 1.f / best.s : 0.f;
     }
