@@ -79,6 +79,8 @@ template <> struct PagedElem<float> {
 
 __device__ __forceinline__ int swz_paged(int key) { return (key & 3) | (((key >> 3) & 3) << 2); }
 
+constexpr int MAX_ATTN_SPLITS = 64;           // key splits of a part
+
 // log2-domain slack of the lazily moved reference: probabilities <= 2^8 (fits fp16)
 constexpr float PAGED_SLACK = 8.f;
 
@@ -87,9 +89,9 @@ constexpr float PAGED_SLACK = 8.f;
 // in a ring of NB buffers and read from there by all waves.  LDS rows are swizzled in 16-byte
 // columns so that the 16 rows of a fragment read lie in different banks.  Lane i holds the
 // page of block 64 n + i, so a block's page is one lane read.
-template <typename T, int DH, int QG, int QT, int NB>
+template <typename T, int DH, int QG, int QT, int NB, int SUB>
 __global__ void __launch_bounds__(QG * 64)
-__attribute__((amdgpu_waves_per_eu(QG * (160 * 1024 / (NB * 64 * DH * (int)sizeof(T))) >= 8 ? 2 : 1)))
+__attribute__((amdgpu_waves_per_eu(QG * (160 * 1024 / (NB * SUB * 64 * DH * (int)sizeof(T))) >= 8 ? 2 : 1)))
 attn_paged_kernel(PagedArgs a) {
     using E = PagedElem<T>;
     constexpr bool F32 = sizeof(T) == 4;
@@ -100,9 +102,10 @@ attn_paged_kernel(PagedArgs a) {
     constexpr int NV = F32 ? 2 : 1;           // V^T fragments of a block per output tile
     constexpr int KC = DH * ES / 16;          // 16-byte columns of a key's row
     constexpr int VC = 32 * ES / 16;          // and of a dim's row of V^T
-    constexpr int KPLANE = 32 * DH * ES, BUF = 2 * KPLANE;
+    constexpr int KPLANE = 32 * DH * ES, SBUF = 2 * KPLANE, BUF = SUB * SBUF;
     constexpr int KI = KPLANE / 1024;         // 1 KiB wave loads per plane
-    constexpr int LPW = 2 * (KI / QG);        // loads each wave issues per staged block, at least
+    constexpr int LPW = SUB * 2 * (KI / QG);  // loads each wave issues per staged step, at least
+    static_assert(64 % SUB == 0, "a step's pages lie in one chunk");
     constexpr int TM = 16 * QG * QT;          // virtual rows of a workgroup
     static_assert(KI * 1024 == KPLANE, "planes must be whole wave loads");
     static_assert(TM <= 256, "at most four virtual rows per lane");
@@ -128,9 +131,9 @@ attn_paged_kernel(PagedArgs a) {
         R1 = min(a.row0[b + 1], R0 + a.max_rows);
         ks = a.shared;
         ke = min(a.len[b], a.max_len);
-        // blocks per split from the sequence's own length: a short one is still spread
-        const int nblk = max(0, ke - ks + 31) >> 5;
-        bps = max((nblk + a.ns_o - 1) / a.ns_o, 2);
+        // steps per split from the sequence's own length: a short one is still spread
+        const int nst = (max(0, ke - ks) + 32 * SUB - 1) / (32 * SUB);
+        bps = (nst + a.ns_o - 1) / a.ns_o;
         part = a.ns_s + split;
     } else {
         tile = item % a.nt_s;
@@ -142,7 +145,7 @@ attn_paged_kernel(PagedArgs a) {
         R1 = a.row0[a.B];
         ks = 0;
         ke = min(a.shared, a.max_len);
-        bps = (((ke + 31) >> 5) + a.ns_s - 1) / a.ns_s;
+        bps = ((ke + 32 * SUB - 1) / (32 * SUB) + a.ns_s - 1) / a.ns_s;
         part = split;
     }
     R0 = max(R0, 0);
@@ -172,8 +175,9 @@ attn_paged_kernel(PagedArgs a) {
 #pragma unroll
     for (int o = 32; o > 0; o >>= 1) ktop = max(ktop, __shfl_xor(ktop, o));
     ktop = __builtin_amdgcn_readfirstlane(ktop);
-    const int kb0 = split * bps, nblk = (ktop - ks + 31) >> 5;
-    const int rounds = max(0, min(nblk, kb0 + bps) - kb0);
+    const int kb0 = SUB * split * bps;        // the split's first 32-key block
+    const int blocks = max(0, min((ktop - ks + 31) >> 5, kb0 + SUB * bps) - kb0);
+    const int rounds = (blocks + SUB - 1) / SUB;
 
     u32x4_t qf[QT][NC];
     int lim[QT];
@@ -201,42 +205,46 @@ attn_paged_kernel(PagedArgs a) {
     auto chunk_pages = [&](int n) {
         const int t = 64 * n + lane, k = ks + 32 * (kb0 + t);
         int pg = -1;
-        if (t < rounds) pg = trow[k >> a.page_shift];
+        if (t < blocks) pg = trow[k >> a.page_shift];
         return pg < a.n_pages ? pg : -1;
     };
     int pgv = chunk_pages(0);
     uint64_t have = __builtin_amdgcn_ballot_w64(pgv >= 0), have_before = 0;
     const long page_elems = (long)DH << a.page_shift;
 
-    // Stage block t: wave load i of a plane is its bytes [1024 i, 1024 i + 1024), taken by wave
+    // Stage step t: wave load i of a plane is its bytes [1024 i, 1024 i + 1024), taken by wave
     // i % QG.  A block without a page is staged from page 0 (and not used).
     auto stage = [&](int t, int buf) {
-        const int pg = max(0, __builtin_amdgcn_readlane(pgv, t & 63));
-        const int off = (ks + 32 * (kb0 + t)) & ((1 << a.page_shift) - 1);
-        const long head = ((long)pg * a.Hk + hk) * page_elems;
-        const T* Kp = (const T*)a.kp + head;
-        const T* Vp = (const T*)a.vp + head;
-        char* base = lds + buf * BUF;
 #pragma unroll
-        for (int j = 0; j < (KI + QG - 1) / QG; ++j) {
-            const int i = qw + j * QG;
-            if (KI % QG != 0 && i >= KI) break;
-            const int key = (i * 64 + lane) / KC, pc = lane % KC;
-            const int sw = F32 ? key & 15 : swz_paged(key);
-            buffer_to_lds16(Kp, key * (DH * ES) + ((pc ^ (sw & (KC - 1))) << 4), off * (DH * ES), base + i * 1024);
-        }
+        for (int u = 0; u < SUB; ++u) {
+            const int blk = SUB * t + u;
+            const int pg = max(0, __builtin_amdgcn_readlane(pgv, blk & 63));
+            const int off = (ks + 32 * (kb0 + blk)) & ((1 << a.page_shift) - 1);
+            const long head = ((long)pg * a.Hk + hk) * page_elems;
+            const T* Kp = (const T*)a.kp + head;
+            const T* Vp = (const T*)a.vp + head;
+            char* base = lds + buf * BUF + u * SBUF;
 #pragma unroll
-        for (int j = 0; j < (KI + QG - 1) / QG; ++j) {
-            const int i = qw + j * QG;
-            if (KI % QG != 0 && i >= KI) break;
-            const int dim = (i * 64 + lane) / VC, pc = lane % VC;
-            const int sw = F32 ? dim & 7 : (dim >> 2) & 3;
-            buffer_to_lds16(Vp, ((dim << a.page_shift) * ES) + ((pc ^ sw) << 4), off * ES, base + KPLANE + i * 1024);
+            for (int j = 0; j < (KI + QG - 1) / QG; ++j) {
+                const int i = qw + j * QG;
+                if (KI % QG != 0 && i >= KI) break;
+                const int key = (i * 64 + lane) / KC, pc = lane % KC;
+                const int sw = F32 ? key & 15 : swz_paged(key);
+                buffer_to_lds16(Kp, key * (DH * ES) + ((pc ^ (sw & (KC - 1))) << 4), off * (DH * ES), base + i * 1024);
+            }
+#pragma unroll
+            for (int j = 0; j < (KI + QG - 1) / QG; ++j) {
+                const int i = qw + j * QG;
+                if (KI % QG != 0 && i >= KI) break;
+                const int dim = (i * 64 + lane) / VC, pc = lane % VC;
+                const int sw = F32 ? dim & 7 : (dim >> 2) & 3;
+                buffer_to_lds16(Vp, ((dim << a.page_shift) * ES) + ((pc ^ sw) << 4), off * ES, base + KPLANE + i * 1024);
+            }
         }
     };
-    // zero the V^T values of keys >= end in the slots this wave staged
-    auto zero_tail = [&](int k0, int end, int buf) {
-        char* base = lds + buf * BUF + KPLANE;
+    // zero the V^T values of keys >= end in the slots of a block that this wave staged
+    auto zero_tail = [&](int k0, int end, char* sub) {
+        char* base = sub + KPLANE;
 #pragma unroll
         for (int j = 0; j < (KI + QG - 1) / QG; ++j) {
             const int i = qw + j * QG;
@@ -282,94 +290,112 @@ attn_paged_kernel(PagedArgs a) {
     // no scalar load outstanding past here: the compiler does not see the waits in the loop's
     // asm and would otherwise wait for all LDS reads at each use
     __builtin_amdgcn_s_waitcnt(0xC07F);
+    // a wave without rows of its own only stages
+    const bool busy = f0 + 16 * QT * qw < nv;
     for (int t = 0; t < rounds; ++t) {
         const int cur = t % NB;
-        const int k0 = ks + 32 * (kb0 + t);
-        // (the chunk moves on with the block staged in the round before)
-        const bool before = (t >> 6) != ((min(t + NB - 2, rounds - 1)) >> 6);
-        const bool there = ((before ? have_before : have) >> (t & 63)) & 1;
-        // This wave's loads of block t have landed once at most LPW of the block staged after it are
-        // outstanding (loads complete in issue order; a page refill waits for all); the barrier makes
+        const int k0 = ks + 32 * (kb0 + SUB * t);
+        // which blocks have a page (the chunk moves on with the step staged in the round before)
+        const bool before = ((SUB * t) >> 6) != ((SUB * min(t + NB - 2, rounds - 1)) >> 6);
+        const uint32_t there = (uint32_t)((before ? have_before : have) >> ((SUB * t) & 63)) & ((1u << SUB) - 1);
+        const bool whole = there == (1u << SUB) - 1;
+        // This wave's loads of step t have landed once at most LPW of the step staged after it are
+        // outstanding (loads complete in issue order; a chunk's pages wait for all); the barrier makes
         // every wave's visible and frees the buffer that round t - 1 read.
-        const int end = there ? ktop : 0;
-        if (k0 + 32 > end) {
+        if (!whole || k0 + 32 * SUB > ktop) {
             asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-            zero_tail(k0, end, cur);
+#pragma unroll
+            for (int u = 0; u < SUB; ++u)
+                zero_tail(k0 + 32 * u, (there >> u) & 1 ? ktop : 0, lds + cur * BUF + u * SBUF);
         }
         if (NB > 2 && t + 1 < rounds) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(LPW) : "memory");
         else asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
         if (t + NB - 1 < rounds) {
-            if (((t + NB - 1) & 63) == 0) {
-                pgv = chunk_pages((t + NB - 1) >> 6);
+            if (((SUB * (t + NB - 1)) & 63) == 0) {
+                pgv = chunk_pages((SUB * (t + NB - 1)) >> 6);
                 have_before = have;
                 have = __builtin_amdgcn_ballot_w64(pgv >= 0);
             }
             stage(t + NB - 1, (t + NB - 1) % NB);
         }
-        const char* Kb = lds + cur * BUF;
-        const char* Vb = Kb + KPLANE;
+        if (!busy) continue;
 
-        // all of the block's K fragments are read before the first product, its V^T fragments between
+        // all of the step's K fragments are read before the first product, its V^T fragments between
         // the scores and the softmax, which covers their latency
-        u32x4_t kf[NC][2], vf[ND][NV];
+        const char* buf = lds + cur * BUF;
+        u32x4_t kf[SUB][NC][2], vf[SUB][ND][NV];
 #pragma unroll
-        for (int c = 0; c < NC; ++c)
+        for (int w = 0; w < SUB; ++w)
 #pragma unroll
-            for (int u = 0; u < 2; ++u) {
-                const int key = krow0 + KT * u;
-                const int sw = F32 ? key & 15 : swz_paged(key);
-                kf[c][u] = *(const u32x4_t*)(Kb + key * (DH * ES) + (((4 * c + g) ^ (sw & (KC - 1))) << 4));
-            }
+            for (int c = 0; c < NC; ++c)
+#pragma unroll
+                for (int u = 0; u < 2; ++u) {
+                    const int key = krow0 + KT * u;
+                    const int sw = F32 ? key & 15 : swz_paged(key);
+                    kf[w][c][u] = *(const u32x4_t*)(buf + w * SBUF + key * (DH * ES) + (((4 * c + g) ^ (sw & (KC - 1))) << 4));
+                }
         __builtin_amdgcn_sched_barrier(0);
-        f32x4_t s[QT][2];
+        f32x4_t s[QT][SUB][2];
 #pragma unroll
-        for (int q = 0; q < QT; ++q) s[q][0] = s[q][1] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+        for (int q = 0; q < QT; ++q)
 #pragma unroll
-        for (int c = 0; c < NC; ++c)
+            for (int w = 0; w < SUB; ++w) s[q][w][0] = s[q][w][1] = f32x4_t{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-            for (int q = 0; q < QT; ++q)
+        for (int w = 0; w < SUB; ++w)
 #pragma unroll
-                for (int u = 0; u < 2; ++u) s[q][u] = E::mfma(kf[c][u], qf[q][c], s[q][u]);
+            for (int c = 0; c < NC; ++c)
 #pragma unroll
-        for (int dt = 0; dt < ND; ++dt)
+                for (int q = 0; q < QT; ++q)
 #pragma unroll
-            for (int u = 0; u < NV; ++u) {
-                const int dim = 16 * dt + r;
-                const int sw = F32 ? dim & 7 : (dim >> 2) & 3;
-                vf[dt][u] = *(const u32x4_t*)(Vb + dim * (32 * ES) + (((4 * u + g) ^ sw) << 4));
-            }
+                    for (int u = 0; u < 2; ++u) s[q][w][u] = E::mfma(kf[w][c][u], qf[q][c], s[q][w][u]);
+#pragma unroll
+        for (int w = 0; w < SUB; ++w)
+#pragma unroll
+            for (int dt = 0; dt < ND; ++dt)
+#pragma unroll
+                for (int u = 0; u < NV; ++u) {
+                    const int dim = 16 * dt + r;
+                    const int sw = F32 ? dim & 7 : (dim >> 2) & 3;
+                    vf[w][dt][u] = *(const u32x4_t*)(buf + w * SBUF + KPLANE + dim * (32 * ES) + (((4 * u + g) ^ sw) << 4));
+                }
         __builtin_amdgcn_sched_barrier(0);
 
-        u32x4_t pf[QT][NV];
+        u32x4_t pf[QT][SUB][NV];
 #pragma unroll
         for (int q = 0; q < QT; ++q) {
-            // sv[4u + i]: the score of key k0 + (16-bit) 8g + 4u + i, (fp32) 16u + 4g + i
-            float sv[8];
+            // sv[8w + 4u + i]: the score of key k0 + 32w + (16-bit) 8g + 4u + i, (fp32) 16u + 4g + i
+            float sv[8 * SUB];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                sv[i] = s[q][0][i];
-                sv[4 + i] = s[q][1][i];
-            }
-            if (k0 + 32 > lim_w || !there) {
-                const int e = there ? lim[q] : 0;
+            for (int w = 0; w < SUB; ++w)
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    const int key0 = k0 + (F32 ? 4 : 8) * g + i;
-                    if (key0 >= e) sv[i] = -INFINITY;
-                    if (key0 + KT >= e) sv[4 + i] = -INFINITY;
+                    sv[8 * w + i] = s[q][w][0][i];
+                    sv[8 * w + 4 + i] = s[q][w][1][i];
+                }
+            if (k0 + 32 * SUB > lim_w || !whole) {
+#pragma unroll
+                for (int w = 0; w < SUB; ++w) {
+                    const int e = (there >> w) & 1 ? lim[q] : 0;
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const int key0 = k0 + 32 * w + (F32 ? 4 : 8) * g + i;
+                        if (key0 >= e) sv[8 * w + i] = -INFINITY;
+                        if (key0 + KT >= e) sv[8 * w + 4 + i] = -INFINITY;
+                    }
                 }
             }
-            // the row's block maximum over its four lane groups (max is symmetric: a swap hands a
-            // lane its partner's value)
-            float bm = fmaxf(fmaxf(fmaxf(sv[0], sv[1]), fmaxf(sv[2], sv[3])),
-                             fmaxf(fmaxf(sv[4], sv[5]), fmaxf(sv[6], sv[7])));
+            // the row's maximum over the step and its four lane groups (max is symmetric: a swap hands
+            // a lane its partner's value)
+            float bm = sv[0];
+#pragma unroll
+            for (int e = 1; e < 8 * SUB; ++e) bm = fmaxf(bm, sv[e]);
             const auto w32 = __builtin_amdgcn_permlane32_swap(__float_as_uint(bm), __float_as_uint(bm), false, false);
             bm = fmaxf(__uint_as_float(w32[0]), __uint_as_float(w32[1]));
             const auto w16 = __builtin_amdgcn_permlane16_swap(__float_as_uint(bm), __float_as_uint(bm), false, false);
             bm = fmaxf(__uint_as_float(w16[0]), __uint_as_float(w16[1]));
             const float bms = bm * a.sl2;
             // the reference moves only when some row of the tile exceeds it by PAGED_SLACK: O, sum and
-            // merge are exact for any reference, and most blocks skip the rescale
+            // merge are exact for any reference, and most steps skip the rescale
             if (__builtin_expect(__builtin_amdgcn_ballot_w64(bms > mrun[q] + PAGED_SLACK) != 0, 0)) {
                 const float mnew = fmaxf(mrun[q], bms);
                 const float alpha = (mnew == -INFINITY) ? 1.f : __builtin_amdgcn_exp2f(mrun[q] - mnew);
@@ -381,27 +407,34 @@ attn_paged_kernel(PagedArgs a) {
                 mrun[q] = mnew;
             }
             const float mref = (mrun[q] == -INFINITY) ? 0.f : mrun[q];
-            float p[8];
+            float p[8 * SUB], sum = 0.f;
 #pragma unroll
-            for (int e = 0; e < 8; ++e) p[e] = __builtin_amdgcn_exp2f(fmaf(sv[e], a.sl2, -mref));
-            lrun[q] += ((p[0] + p[1]) + (p[2] + p[3])) + ((p[4] + p[5]) + (p[6] + p[7]));
-            if constexpr (F32) {
+            for (int e = 0; e < 8 * SUB; ++e) p[e] = __builtin_amdgcn_exp2f(fmaf(sv[e], a.sl2, -mref));
 #pragma unroll
-                for (int e = 0; e < 8; ++e) pf[q][e >> 2][e & 3] = __float_as_uint(p[e]);
-            } else {
-                // rounded to nearest for the product with V (half a step of T a probability: as much as the
-                // output's own rounding); the sum keeps fp32
+            for (int e = 0; e < 8 * SUB; e += 4) sum += (p[e] + p[e + 1]) + (p[e + 2] + p[e + 3]);
+            lrun[q] += sum;
 #pragma unroll
-                for (int e = 0; e < 4; ++e)
-                    pf[q][0][e] = __builtin_bit_cast(uint32_t, (typename E::x2){(T)p[2 * e], (T)p[2 * e + 1]});
+            for (int w = 0; w < SUB; ++w) {
+                if constexpr (F32) {
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) pf[q][w][e >> 2][e & 3] = __float_as_uint(p[8 * w + e]);
+                } else {
+                    // rounded to nearest for the product with V (half a step of T a probability: as much as
+                    // the output's own rounding); the sum keeps fp32
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        pf[q][w][0][e] = __builtin_bit_cast(uint32_t, (typename E::x2){(T)p[8 * w + 2 * e], (T)p[8 * w + 2 * e + 1]});
+                }
             }
         }
 #pragma unroll
-        for (int dt = 0; dt < ND; ++dt)
+        for (int w = 0; w < SUB; ++w)
 #pragma unroll
-            for (int q = 0; q < QT; ++q)
+            for (int dt = 0; dt < ND; ++dt)
 #pragma unroll
-                for (int u = 0; u < NV; ++u) oacc[q][dt] = E::mfma(vf[dt][u], pf[q][u], oacc[q][dt]);
+                for (int q = 0; q < QT; ++q)
+#pragma unroll
+                    for (int u = 0; u < NV; ++u) oacc[q][dt] = E::mfma(vf[w][dt][u], pf[q][w][u], oacc[q][dt]);
     }
 
 #pragma unroll
@@ -436,32 +469,58 @@ attn_paged_kernel(PagedArgs a) {
 }
 
 // Merge of the parts: o = sum_s o_s 2^(m_s - M) / sum_s l_s 2^(m_s - M).  DH / 4 lanes per
-// (row, head), four dims each; parts with an empty sum wrote no output and are skipped.
+// (row, head), four dims each.  The lanes first take a part's (m, l) each, so that all weights
+// cost one round trip, then the outputs are read eight parts at a time.  A part with an empty
+// sum wrote no output: what stands there is read and not used.
 template <typename T, int DH>
 __global__ void __launch_bounds__(256) attn_paged_merge_kernel(PagedArgs a) {
-    constexpr int LPP = DH / 4;
-    const int pair = blockIdx.x * (256 / LPP) + threadIdx.x / LPP, l4 = (threadIdx.x % LPP) * 4;
+    constexpr int LPP = DH / 4, MAXW = 2 * MAX_ATTN_SPLITS / LPP;      // weights per lane
+    const int pair = blockIdx.x * (256 / LPP) + threadIdx.x / LPP, li = threadIdx.x % LPP;
     const int R0 = max(a.row0[0], 0), R1 = min(a.row0[a.B], a.T);
-    const int row = R0 + pair / a.H, h = pair % a.H;
-    if (row >= R1) return;
+    const int row = min(R0 + pair / a.H, a.T - 1), h = pair % a.H;
     const size_t rec = (size_t)row * a.H + h, step = (size_t)a.T * a.H;
     const int np = a.ns_s + a.ns_o;
-    float M = -INFINITY;
-    for (int s = 0; s < np; ++s) M = fmaxf(M, a.mlpart[(s * step + rec) * 2]);
-    float L = 0.f;
-    float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-    for (int s = 0; s < np; ++s) {
-        const float2 ml = *(const float2*)(a.mlpart + (s * step + rec) * 2);
-        if (!(ml.y > 0.f)) continue;
-        const float w = exp2f(ml.x - M);
-        const float4 v = *(const float4*)(a.opart + (s * step + rec) * DH + l4);
-        L += ml.y * w;
-        o.x += v.x * w; o.y += v.y * w; o.z += v.z * w; o.w += v.w * w;
+    float m[MAXW], l[MAXW], M = -INFINITY, L = 0.f;
+#pragma unroll
+    for (int i = 0; i < MAXW; ++i) {
+        m[i] = -INFINITY;
+        l[i] = 0.f;
+        if (li + LPP * i < np) {
+            const float2 ml = *(const float2*)(a.mlpart + ((li + LPP * i) * step + rec) * 2);
+            m[i] = ml.x;
+            l[i] = ml.y;
+        }
+        M = fmaxf(M, m[i]);
     }
+#pragma unroll
+    for (int o = 1; o < LPP; o <<= 1) M = fmaxf(M, __shfl_xor(M, o));
+#pragma unroll
+    for (int i = 0; i < MAXW; ++i) {
+        m[i] = l[i] > 0.f ? exp2f(m[i] - M) : 0.f;                     // the part's weight
+        L += l[i] * m[i];
+    }
+#pragma unroll
+    for (int o = 1; o < LPP; o <<= 1) L += __shfl_xor(L, o);
+    float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+    const float* src = a.opart + rec * DH + 4 * li;
+#pragma unroll
+    for (int i = 0; i < MAXW; ++i) {
+        for (int s0 = LPP * i; s0 < min(np, LPP * (i + 1)); s0 += 8) {
+            float4 v[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[j] = *(const float4*)(src + (size_t)min(s0 + j, np - 1) * step * DH);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const float w = __shfl(m[i], (s0 + j) % LPP, LPP);
+                if (s0 + j < np && w > 0.f) { o.x += v[j].x * w; o.y += v[j].y * w; o.z += v[j].z * w; o.w += v[j].w * w; }
+            }
+        }
+    }
+    if (R0 + pair / a.H >= R1) return;
     const float inv = L > 0.f ? 1.f / L : 0.f;
     T e[4] = {elem_from_f32<T>(o.x * inv), elem_from_f32<T>(o.y * inv), elem_from_f32<T>(o.z * inv),
               elem_from_f32<T>(o.w * inv)};
-    __builtin_memcpy(__builtin_assume_aligned((T*)a.out + row * a.ld_out + h * DH + l4, 4 * sizeof(T)), e, sizeof(e));
+    __builtin_memcpy(__builtin_assume_aligned((T*)a.out + row * a.ld_out + h * DH + 4 * li, 4 * sizeof(T)), e, sizeof(e));
 }
 
 }  // namespace dllm

@@ -100,74 +100,63 @@ void launch_qk(const QkArgs& a, int Dh, hipStream_t s) {
     else hipLaunchKernelGGL((qk_norm_rope_kernel<T, 32>), grid, dim3(256), 0, s, a, qk_wgs);
 }
 
-// Launch of an attention call.  A part is the shared prefix (all rows) or the sequences' own
-// keys; each has its tile shape (QG waves of QT 16-row tiles) and key splits.
-struct AttnPart {
-    int qg = 0, qt = 0;   // 0: no such part
-    int nt = 0, ns = 0;   // row tiles (per K/V head, and per sequence), key splits
-    long wgs = 0;
-};
+// Launch of an attention call.  Both parts (the shared prefix for all rows, and the sequences' own
+// keys) run in one launch of one tile shape, QG waves of QT 16-row tiles, by the part with the most
+// rows; waves without rows only help staging.
 struct AttnPlan {
-    AttnPart sh, own;
-    bool direct() const { return sh.ns == 0 && own.ns == 1; }
+    int qg, qt;
+    int shared;           // positions taken as the shared part
+    int nt_s, ns_s;       // its row tiles and key splits per K/V head (0: no such part)
+    int nt_o, ns_o;       // and of a sequence's own keys
+    long wgs_s, wgs_o;
+    bool direct() const { return ns_s == 0 && ns_o == 1; }
 };
 
 constexpr int N_CU = 256;
-constexpr int MAX_ATTN_SPLITS = 64;
-
-AttnPart attn_part(long rows, long units, int keys) {
-    AttnPart p;
-    p.qg = rows <= 16 ? 1 : (rows <= 32 ? 2 : 4);
-    p.qt = rows <= 64 ? 1 : 2;
-    p.nt = std::max(1, ceil_div(rows, 16 * p.qg * p.qt));
-    const long wgs = units * p.nt;
-    const int blocks = std::max(1, ceil_div(keys, 32));
-    const long want = std::max(1l, 2 * N_CU / std::max(1l, wgs));
-    p.ns = (int)std::min<long>(std::min<long>(want, MAX_ATTN_SPLITS), std::max(1, blocks / 4));
-    p.ns = ceil_div(blocks, ceil_div(blocks, p.ns));      // splits of whole blocks, none empty
-    p.wgs = wgs * p.ns;
-    return p;
-}
 
 AttnPlan attn_plan(const dllm_attn_args* g) {
-    const int G = g->n_heads / g->n_kv_heads;
-    const int sh = std::min(g->shared_len, g->max_len);
-    AttnPlan p;
-    if (sh > 0) p.sh = attn_part((long)g->n_rows * G, g->n_kv_heads, sh);
-    p.own = attn_part((long)std::min(g->max_rows, g->n_rows) * G, (long)g->n_seqs * g->n_kv_heads, g->max_len - sh);
+    const int G = g->n_heads / g->n_kv_heads, es = esize(g->dtype), step = es == 4 ? 32 : 64;
+    AttnPlan p{};
+    p.shared = std::min(g->shared_len, g->max_len);
+    const long rows_o = (long)std::min(g->max_rows, g->n_rows) * G, rows_s = (long)g->n_rows * G;
+    // A shared part costs its merge: below 8 MB of K/V that the sequences would read again, they do
+    // (from L2), and with one sequence it is that sequence's own.
+    if ((long)(g->n_seqs - 1) * p.shared * g->n_kv_heads * g->head_dim * 2 * es < (8l << 20)) p.shared = 0;
+    const long rows = p.shared > 0 ? std::max(rows_s, rows_o) : rows_o;
+    p.qg = rows <= 16 ? 1 : (rows <= 32 ? 2 : 4);
+    p.qt = rows <= 64 ? 1 : 2;
+    const int tm = 16 * p.qg * p.qt;
+    p.nt_s = ceil_div(rows_s, tm);
+    p.nt_o = std::max(1, ceil_div(rows_o, tm));
+    // splits: two workgroups for every CU, of whole steps
+    auto splits = [&](double wgs, int keys) {
+        const int steps = std::max(1, ceil_div(keys, step));
+        const int want = std::max(1, (int)(2 * N_CU / std::max(1.0, wgs) + 0.5));
+        const int ns = std::min(std::min(want, MAX_ATTN_SPLITS), std::max(1, steps / 2));
+        return ceil_div(steps, ceil_div(steps, ns));
+    };
+    if (p.shared > 0) p.ns_s = splits((double)g->n_kv_heads * rows_s / tm, p.shared);
+    p.ns_o = splits((double)g->n_seqs * g->n_kv_heads * p.nt_o, g->max_len - p.shared);
+    p.wgs_s = p.shared > 0 ? (long)g->n_kv_heads * p.nt_s * p.ns_s : 0;
+    p.wgs_o = (long)g->n_seqs * g->n_kv_heads * p.nt_o * p.ns_o;
     return p;
 }
 
 size_t attn_ws_bytes(const dllm_attn_args* g, const AttnPlan& p) {
     if (p.direct()) return 0;
-    return (size_t)(p.sh.ns + p.own.ns) * g->n_rows * g->n_heads * (g->head_dim + 2) * 4;
-}
-
-template <typename T, int DH>
-void launch_attn_part(const PagedArgs& a, int qg, int qt, long wgs, hipStream_t s) {
-#define ATTN(QG_, QT_) hipLaunchKernelGGL((attn_paged_kernel<T, DH, QG_, QT_, 2>), dim3(wgs), dim3(QG_ * 64), 0, s, a)
-    if (qt == 2) ATTN(4, 2);
-    else if (qg == 4) ATTN(4, 1);
-    else if (qg == 2) ATTN(2, 1);
-    else ATTN(1, 1);
-#undef ATTN
+    return (size_t)(p.ns_s + p.ns_o) * g->n_rows * g->n_heads * (g->head_dim + 2) * 4;
 }
 
 template <typename T, int DH>
 void launch_attn_dh(PagedArgs a, const AttnPlan& p, hipStream_t s) {
-    a.ns_s = p.sh.ns; a.nt_s = p.sh.nt; a.ns_o = p.own.ns; a.nt_o = p.own.nt;
-    a.direct = p.direct();
-    if (p.sh.qg == p.own.qg && p.sh.qt == p.own.qt) {     // both parts in one launch, the shared one first
-        a.n_s = (int)p.sh.wgs;
-        launch_attn_part<T, DH>(a, p.own.qg, p.own.qt, p.sh.wgs + p.own.wgs, s);
-    } else {
-        if (p.sh.ns > 0) {
-            a.n_s = (int)p.sh.wgs;
-            launch_attn_part<T, DH>(a, p.sh.qg, p.sh.qt, p.sh.wgs, s);
-        }
-        a.n_s = 0;
-        launch_attn_part<T, DH>(a, p.own.qg, p.own.qt, p.own.wgs, s);
-    }
+    constexpr int SUB = sizeof(T) == 4 ? 1 : 2;
+    const dim3 grid((unsigned)(p.wgs_s + p.wgs_o));
+#define ATTN(QG_, QT_) hipLaunchKernelGGL((attn_paged_kernel<T, DH, QG_, QT_, 2, SUB>), grid, dim3(QG_ * 64), 0, s, a)
+    if (p.qt == 2) ATTN(4, 2);
+    else if (p.qg == 4) ATTN(4, 1);
+    else if (p.qg == 2) ATTN(2, 1);
+    else ATTN(1, 1);
+#undef ATTN
     if (!a.direct)
         hipLaunchKernelGGL((attn_paged_merge_kernel<T, DH>), dim3(ceil_div((long)a.T * a.H, 256 / (DH / 4))), dim3(256), 0,
                            s, a);
@@ -290,7 +279,7 @@ int dllm_attention_paged(const dllm_attn_args* g, dllm_stream stream) {
     if (g->n_rows == 0) return DLLM_OK;
     const AttnPlan p = attn_plan(g);
     const size_t need = attn_ws_bytes(g, p);
-    if (p.sh.wgs + p.own.wgs > 0x7FFFFFFF) return fail(DLLM_E_INVAL, "n_seqs, max_rows and n_rows need too many workgroups");
+    if (p.wgs_s + p.wgs_o > 0x7FFFFFFF) return fail(DLLM_E_INVAL, "n_seqs, max_rows and n_rows need too many workgroups");
     if (need > 0 && (!g->d_ws || !aligned(g->d_ws, 16))) return fail(DLLM_E_INVAL, "workspace: NULL or not 16-byte aligned");
     if (need > g->ws_bytes)
         return fail(DLLM_E_CAPACITY, "the call needs " + std::to_string(need) + " bytes of workspace");
@@ -298,11 +287,13 @@ int dllm_attention_paged(const dllm_attn_args* g, dllm_stream stream) {
     a.q = g->d_q; a.ld_q = g->ld_q; a.kp = g->d_k_pages; a.vp = g->d_v_pages; a.table = g->d_table; a.table_ld = g->table_ld;
     a.row0 = g->d_row0; a.len = g->d_len; a.lim = g->d_lim; a.out = g->d_out; a.ld_out = g->ld_out;
     a.T = g->n_rows; a.B = g->n_seqs; a.H = g->n_heads; a.Hk = g->n_kv_heads; a.G = a.H / a.Hk; a.page_shift = shift;
-    a.n_pages = g->n_pages; a.shared = std::min(g->shared_len, g->max_len); a.max_rows = g->max_rows; a.max_len = g->max_len;
+    a.n_pages = g->n_pages; a.shared = p.shared; a.max_rows = g->max_rows; a.max_len = g->max_len;
     a.sl2 = g->scale == 0.f ? 1.f : std::fabs(g->scale) * 1.4426950408889634f;
     a.qmul = g->scale == 0.f ? 0.f : (g->scale < 0.f ? -1.f : 1.f);
     a.opart = (float*)g->d_ws;
-    a.mlpart = a.opart + (size_t)(p.sh.ns + p.own.ns) * a.T * a.H * g->head_dim;
+    a.mlpart = a.opart + (size_t)(p.ns_s + p.ns_o) * a.T * a.H * g->head_dim;
+    a.ns_s = p.ns_s; a.nt_s = p.nt_s; a.ns_o = p.ns_o; a.nt_o = p.nt_o; a.n_s = (int)p.wgs_s;
+    a.direct = p.direct();
     hipStream_t s = (hipStream_t)stream;
     if (g->dtype == DLLM_F32) launch_attn<float>(a, p, g->head_dim, s);
     else if (g->dtype == DLLM_F16) launch_attn<_Float16>(a, p, g->head_dim, s);
