@@ -148,69 +148,24 @@ attn_paged_kernel(PagedArgs a) {
         bps = ((ke + 32 * SUB - 1) / (32 * SUB) + a.ns_s - 1) / a.ns_s;
         part = split;
     }
+    const int kb0 = SUB * split * bps;        // the split's first 32-key block
+
+    // Pages of the 64 blocks of a chunk: lane i has block 64 n + i's (-1: no page).  Blocks are staged
+    // up to NB - 1 steps ahead of their use, so the chunk before keeps a bit a block: whether it
+    // has a page.  The first chunk, and with it the first step's K/V, is asked for before the
+    // rows and their limits are known (a table row has table_ld entries whatever the length).
+    const int* trow = a.table + (size_t)b * a.table_ld;
+    auto chunk_pages = [&](int n) {
+        const int pg = trow[min((ks + 32 * (kb0 + 64 * n + lane)) >> a.page_shift, a.table_ld - 1)];
+        return pg < a.n_pages ? pg : -1;
+    };
+    int pgv = chunk_pages(0);
+    const long page_elems = (long)DH << a.page_shift;
     R0 = max(R0, 0);
     R1 = min(R1, a.T);
     const int nv = (R1 - R0) * a.G;           // virtual rows of the part
     const int f0 = tile * TM;
     if (f0 >= nv) return;
-
-    // Key limit of virtual row f.  The rows of the shared part need their sequence's length only if some
-    // sequence ends inside it.
-    int short_len = 0x7FFFFFFF;
-    if (!own) {
-        for (int i = lane; i < a.B; i += 64) short_len = min(short_len, a.len[i]);
-#pragma unroll
-        for (int o = 32; o > 0; o >>= 1) short_len = min(short_len, __shfl_xor(short_len, o));
-    }
-    auto row_limit = [&](int f) {
-        const int row = R0 + f / a.G;
-        const int n = own || short_len >= ke ? ke : min(ke, a.len[row_seq(a.row0, a.B, row)]);
-        return a.lim != nullptr ? min(n, a.lim[row]) : n;
-    };
-    // The largest limit of the tile's rows ends its keys: what lies behind may be anything.
-    int ktop = ks;
-#pragma unroll
-    for (int i = 0; i < (TM + 63) / 64; ++i)
-        if (lane + 64 * i < TM) ktop = max(ktop, row_limit(min(f0 + lane + 64 * i, nv - 1)));
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) ktop = max(ktop, __shfl_xor(ktop, o));
-    ktop = __builtin_amdgcn_readfirstlane(ktop);
-    const int kb0 = SUB * split * bps;        // the split's first 32-key block
-    const int blocks = max(0, min((ktop - ks + 31) >> 5, kb0 + SUB * bps) - kb0);
-    const int rounds = (blocks + SUB - 1) / SUB;
-
-    u32x4_t qf[QT][NC];
-    int lim[QT];
-#pragma unroll
-    for (int q = 0; q < QT; ++q) {
-        // rows past the last repeat it (the rescale below is decided over a tile's 16 rows)
-        const int f = min(f0 + 16 * (QT * qw + q) + r, nv - 1);
-        const int row = R0 + f / a.G, h = hk * a.G + f % a.G;
-        const T* src = (const T*)a.q + row * a.ld_q + h * DH + (16 / ES) * g;
-#pragma unroll
-        for (int c = 0; c < NC; ++c) {
-            qf[q][c] = ldg16(src + CD * c);
-            if (a.qmul != 1.f) {
-                constexpr uint32_t sign = F32 ? 0x80000000u : 0x80008000u;
-#pragma unroll
-                for (int e = 0; e < 4; ++e) qf[q][c][e] = a.qmul == 0.f ? 0u : qf[q][c][e] ^ sign;
-            }
-        }
-        lim[q] = row_limit(f);
-    }
-
-    // Pages of the 64 blocks of a chunk: lane i has block 64 n + i's (-1: no page).  Blocks are staged
-    // up to NB - 1 ahead of their use, so the chunk before keeps a bit a block: whether it has a page.
-    const int* trow = a.table + (size_t)b * a.table_ld;
-    auto chunk_pages = [&](int n) {
-        const int t = 64 * n + lane, k = ks + 32 * (kb0 + t);
-        int pg = -1;
-        if (t < blocks) pg = trow[k >> a.page_shift];
-        return pg < a.n_pages ? pg : -1;
-    };
-    int pgv = chunk_pages(0);
-    uint64_t have = __builtin_amdgcn_ballot_w64(pgv >= 0), have_before = 0;
-    const long page_elems = (long)DH << a.page_shift;
 
     // Stage step t: wave load i of a plane is its bytes [1024 i, 1024 i + 1024), taken by wave
     // i % QG.  A block without a page is staged from page 0 (and not used).
@@ -264,8 +219,60 @@ attn_paged_kernel(PagedArgs a) {
         }
     };
 
+    const int most = min(SUB * bps, ((ke - ks + 31) >> 5) - kb0);      // blocks of the split, at most
+    if (most > 0) stage(0, 0);
+
+    // Key limit of virtual row f.  The rows of the shared part need their sequence's length only if some
+    // sequence ends inside it.
+    int short_len = 0x7FFFFFFF;
+    if (!own) {
+        for (int i = lane; i < a.B; i += 64) short_len = min(short_len, a.len[i]);
 #pragma unroll
-    for (int j = 0; j < NB - 1; ++j)
+        for (int o = 32; o > 0; o >>= 1) short_len = min(short_len, __shfl_xor(short_len, o));
+    }
+    auto row_limit = [&](int f) {
+        const int row = R0 + f / a.G;
+        const int n = own || short_len >= ke ? ke : min(ke, a.len[row_seq(a.row0, a.B, row)]);
+        return a.lim != nullptr ? min(n, a.lim[row]) : n;
+    };
+    u32x4_t qf[QT][NC];
+    int lim[QT];
+#pragma unroll
+    for (int q = 0; q < QT; ++q) {
+        // rows past the last repeat it (the rescale below is decided over a tile's 16 rows)
+        const int f = min(f0 + 16 * (QT * qw + q) + r, nv - 1);
+        const int row = R0 + f / a.G, h = hk * a.G + f % a.G;
+        const T* src = (const T*)a.q + row * a.ld_q + h * DH + (16 / ES) * g;
+#pragma unroll
+        for (int c = 0; c < NC; ++c) {
+            qf[q][c] = ldg16(src + CD * c);
+            if (a.qmul != 1.f) {
+                constexpr uint32_t sign = F32 ? 0x80000000u : 0x80008000u;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) qf[q][c][e] = a.qmul == 0.f ? 0u : qf[q][c][e] ^ sign;
+            }
+        }
+        lim[q] = row_limit(f);
+    }
+    // The largest limit of the tile's rows ends its keys: what lies behind may be anything.
+    int ktop = ks;
+    if (a.lim == nullptr && (own || short_len >= ke)) {
+        ktop = max(ks, ke);
+    } else {
+#pragma unroll
+        for (int i = 0; i < (TM + 63) / 64; ++i)
+            if (lane + 64 * i < TM) ktop = max(ktop, row_limit(min(f0 + lane + 64 * i, nv - 1)));
+#pragma unroll
+        for (int o = 32; o > 0; o >>= 1) ktop = max(ktop, __shfl_xor(ktop, o));
+        ktop = __builtin_amdgcn_readfirstlane(ktop);
+    }
+    const int blocks = max(0, min((ktop - ks + 31) >> 5, kb0 + SUB * bps) - kb0);
+    const int rounds = (blocks + SUB - 1) / SUB;
+    auto chunk_have = [&](int n) { return __builtin_amdgcn_ballot_w64(pgv >= 0 && 64 * n + lane < blocks); };
+    uint64_t have = chunk_have(0), have_before = 0;
+
+#pragma unroll
+    for (int j = 1; j < NB - 1; ++j)
         if (j < rounds) stage(j, j);
 
     // smallest limit of the wave's rows: blocks below it need no per-key mask
@@ -314,7 +321,7 @@ attn_paged_kernel(PagedArgs a) {
             if (((SUB * (t + NB - 1)) & 63) == 0) {
                 pgv = chunk_pages((SUB * (t + NB - 1)) >> 6);
                 have_before = have;
-                have = __builtin_amdgcn_ballot_w64(pgv >= 0);
+                have = chunk_have((SUB * (t + NB - 1)) >> 6);
             }
             stage(t + NB - 1, (t + NB - 1) % NB);
         }

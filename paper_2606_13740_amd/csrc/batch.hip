@@ -89,20 +89,22 @@ int dllm_batch_plan(const int32_t* d_len, const int32_t* d_new, const int32_t* d
 
 namespace {
 
+// Heads a lane group takes one after another: as many as leave 16384 groups (eight waves for every CU's
+// worth of 8-lane groups), at most eight.
 template <typename T>
 void launch_qk(const QkArgs& a, int Dh, hipStream_t s) {
-    const int per = 256 / (Dh / 16);
-    const int qk_wgs = ceil_div((long)a.T * (a.H + a.Hk), per);
-    const int v_wgs = ceil_div((long)a.T * a.Hk * Dh, 256);
-    const dim3 grid(qk_wgs + v_wgs);
-    if (Dh == 128) hipLaunchKernelGGL((qk_norm_rope_kernel<T, 128>), grid, dim3(256), 0, s, a, qk_wgs);
-    else if (Dh == 64) hipLaunchKernelGGL((qk_norm_rope_kernel<T, 64>), grid, dim3(256), 0, s, a, qk_wgs);
-    else hipLaunchKernelGGL((qk_norm_rope_kernel<T, 32>), grid, dim3(256), 0, s, a, qk_wgs);
+    const int hp = (int)std::min<long>(8, std::max<long>(1, (long)a.T * (a.H + a.Hk) / 16384));
+    const long groups = (long)a.T * (ceil_div(a.H, hp) + ceil_div(a.Hk, hp));
+    const int qk_wgs = ceil_div(groups, 256 / (Dh / 16));
+    const dim3 grid((unsigned)(qk_wgs + (long)ceil_div(a.T, QK_VROWS) * a.Hk));
+    if (Dh == 128) hipLaunchKernelGGL((qk_norm_rope_kernel<T, 128>), grid, dim3(256), 0, s, a, qk_wgs, hp);
+    else if (Dh == 64) hipLaunchKernelGGL((qk_norm_rope_kernel<T, 64>), grid, dim3(256), 0, s, a, qk_wgs, hp);
+    else hipLaunchKernelGGL((qk_norm_rope_kernel<T, 32>), grid, dim3(256), 0, s, a, qk_wgs, hp);
 }
 
 // Launch of an attention call.  Both parts (the shared prefix for all rows, and the sequences' own
-// keys) run in one launch of one tile shape, QG waves of QT 16-row tiles, by the part with the most
-// rows; waves without rows only help staging.
+// keys) run in one launch of one tile shape, QG waves of QT 16-row tiles; waves without rows only
+// help staging.
 struct AttnPlan {
     int qg, qt;
     int shared;           // positions taken as the shared part
@@ -112,33 +114,49 @@ struct AttnPlan {
     bool direct() const { return ns_s == 0 && ns_o == 1; }
 };
 
-constexpr int N_CU = 256;
+// Workgroups resident at once: two for every CU (their LDS, at head_dim 128).
+constexpr int ATTN_SLOTS = 512;
 
+// us with its merge, measured (bf16 / fp16, 28 heads over 4 or 32 over 32, head_dim 128, but where said):
+//  - shared part or not: 16 x 1 rows behind 8192 keys 49 and 255; 16 x 3 behind 9984 26 and 38; 4 x 8 behind 2048
+//    (13 MB that the sequences would read again) 16.7 and 17.8; 16 x 48 rows, 4 heads of 64, behind 512 (8 MB) equal;
+//    8 x 1 behind 64 15.0 and 14.8.  With one sequence it is that sequence's own.
+//  - tile: 64 rows against 128: 12 x 40 rows behind 1024 36 and 41, 16 x 3 behind 9984 26.2 and 28.2, 6 x 20 rows
+//    of 16 heads of 64 behind 2976 13.7 and 15.5; from 12 steps of 128 rows a slot on 128 rows, which halve the LDS
+//    reads per product: 16 x 64 behind 16384 (56 steps) 150 and 186.  fp32 is bound by its products, where idle
+//    waves cost: by the rows of one sequence (6 x 24 rows of 32 heads behind 1024: 32 rows 62, 64 rows 66).
+//  - steps of a workgroup: all the call's steps (and two for each workgroup's start) over the slots, so that one
+//    round takes them, rounded towards fewer workgroups: 16 x 64 behind 16384 in 4 splits (448 workgroups) 150, 3 174,
+//    5 190; 8 x 32 of 32 heads behind 4096 in 3 splits 50, 2 62, 4 54; and at least four (two for tiles of 16 rows
+//    and in fp32), since a split is written and merged: 4 x 8 behind 2048 in 8 splits of 4 steps 16.7, in 16 of 2 19.0.
 AttnPlan attn_plan(const dllm_attn_args* g) {
     const int G = g->n_heads / g->n_kv_heads, es = esize(g->dtype), step = es == 4 ? 32 : 64;
     AttnPlan p{};
     p.shared = std::min(g->shared_len, g->max_len);
     const long rows_o = (long)std::min(g->max_rows, g->n_rows) * G, rows_s = (long)g->n_rows * G;
-    // A shared part costs its merge: below 8 MB of K/V that the sequences would read again, they do
-    // (from L2), and with one sequence it is that sequence's own.
     if ((long)(g->n_seqs - 1) * p.shared * g->n_kv_heads * g->head_dim * 2 * es < (8l << 20)) p.shared = 0;
-    const long rows = p.shared > 0 ? std::max(rows_s, rows_o) : rows_o;
+    const int steps_s = ceil_div(p.shared, step), steps_o = std::max(1, ceil_div(g->max_len - p.shared, step));
+    const long units_o = (long)g->n_seqs * g->n_kv_heads;
+    const long rows = es == 4 || p.shared == 0 ? rows_o : std::max(rows_s, rows_o);
     p.qg = rows <= 16 ? 1 : (rows <= 32 ? 2 : 4);
-    p.qt = rows <= 64 ? 1 : 2;
+    p.qt = 1;
+    if (es == 2 && rows > 64 &&
+        g->n_kv_heads * (rows_s / 128) * steps_s + units_o * (rows_o / 128) * steps_o >= 12 * ATTN_SLOTS)
+        p.qt = 2;
     const int tm = 16 * p.qg * p.qt;
     p.nt_s = ceil_div(rows_s, tm);
     p.nt_o = std::max(1, ceil_div(rows_o, tm));
-    // splits: two workgroups for every CU, of whole steps
-    auto splits = [&](double wgs, int keys) {
-        const int steps = std::max(1, ceil_div(keys, step));
-        const int want = std::max(1, (int)(2 * N_CU / std::max(1.0, wgs) + 0.5));
-        const int ns = std::min(std::min(want, MAX_ATTN_SPLITS), std::max(1, steps / 2));
-        return ceil_div(steps, ceil_div(steps, ns));
+    // (rows behind the last sequence make no work: rows_s / tm, not rounded up)
+    const double wgs_s = p.shared > 0 ? g->n_kv_heads * std::max(1.0, (double)rows_s / tm) : 0, wgs_o = (double)units_o * p.nt_o;
+    const double per = std::max((wgs_s * (steps_s + 2) + wgs_o * (steps_o + 2)) / ATTN_SLOTS, tm <= 16 || es == 4 ? 2.0 : 4.0);
+    auto splits = [&](int steps) {
+        const int ns = std::min(MAX_ATTN_SPLITS, std::max(1, (int)(steps / per + 0.25)));
+        return ceil_div(steps, ceil_div(steps, ns));           // none empty
     };
-    if (p.shared > 0) p.ns_s = splits((double)g->n_kv_heads * rows_s / tm, p.shared);
-    p.ns_o = splits((double)g->n_seqs * g->n_kv_heads * p.nt_o, g->max_len - p.shared);
+    if (p.shared > 0) p.ns_s = splits(steps_s);
+    p.ns_o = splits(steps_o);
     p.wgs_s = p.shared > 0 ? (long)g->n_kv_heads * p.nt_s * p.ns_s : 0;
-    p.wgs_o = (long)g->n_seqs * g->n_kv_heads * p.nt_o * p.ns_o;
+    p.wgs_o = units_o * p.nt_o * p.ns_o;
     return p;
 }
 
@@ -152,8 +170,11 @@ void launch_attn_dh(PagedArgs a, const AttnPlan& p, hipStream_t s) {
     constexpr int SUB = sizeof(T) == 4 ? 1 : 2;
     const dim3 grid((unsigned)(p.wgs_s + p.wgs_o));
 #define ATTN(QG_, QT_) hipLaunchKernelGGL((attn_paged_kernel<T, DH, QG_, QT_, 2, SUB>), grid, dim3(QG_ * 64), 0, s, a)
-    if (p.qt == 2) ATTN(4, 2);
-    else if (p.qg == 4) ATTN(4, 1);
+    if constexpr (sizeof(T) == 2) {
+        if (p.qt == 2) ATTN(4, 2);
+    }
+    if (p.qt == 2) {
+    } else if (p.qg == 4) ATTN(4, 1);
     else if (p.qg == 2) ATTN(2, 1);
     else ATTN(1, 1);
 #undef ATTN
