@@ -41,17 +41,28 @@ __device__ __forceinline__ Best best_merge(const Best& a, const Best& b) {
     return Best{mx, id, a.s * expf(a.mx - mx) + b.s * expf(b.mx - mx)};
 }
 
+// l / rep, rounded once, where rcp is 1 / rep rounded once: one step of the remainder is exact for
+// quotients away from the ends of the range, which take the division itself.
+__device__ __forceinline__ float div_by(float l, float rep, float rcp) {
+    const float q = l * rcp, d = fmaf(fmaf(-q, rep, l), rcp, q);
+    const float m = fabsf(l), n = fabsf(rep);
+    const bool plain = m > 0x1p-90f && m < 0x1p90f && n > 0x1p-30f && n < 0x1p30f;
+    return plain ? d : __fdiv_rn(l, rep);
+}
+
 // A logit after its sequence's penalties and bias.  Separate roundings (no fused
 // multiply-add), so that equal logits with equal adjustments stay equal.
 __device__ __forceinline__ float adjust_logit(float l, bool seen, int made, float bias, bool has_bias, float rep,
-                                              float pres, float freq) {
+                                              float rcp, float pres, float freq) {
 #pragma clang fp contract(off)
-    if (seen) l = l > 0.f ? __fdiv_rn(l, rep) : l * rep;
+    const float up = l * rep, down = div_by(l, rep, rcp);
+    l = seen ? (l > 0.f ? down : up) : l;
     const float f = freq * (float)made;
     l = l - f;
-    if (made > 0) l = l - pres;
-    if (has_bias) l = l + bias;
-    return l != l ? -INFINITY : fminf(l, FLT_MAX);
+    const float m = l - pres;
+    l = made > 0 ? m : l;
+    const float w = l + bias;
+    return has_bias ? w : l;
 }
 
 // The six butterfly steps of a wave-wide reduction without LDS: lane permutes inside 16 lanes (a
@@ -87,12 +98,15 @@ __device__ __forceinline__ Best wave_best(const Best& b) {
 
 // A workgroup takes SEL_IDS consecutive ids of `rows_per` consecutive rows.  A thread holds eight ids
 // for all of them, so a sequence's history and bias list are scanned once per workgroup, into
-// LDS tables of its ids, and each thread keeps its eight entries in registers; most threads have
-// none and skip the adjustment.  Four rows are loaded at a time.  The best of the workgroup's
-// ids goes to part[row][range]; with one range (small vocabularies) it is the result.
+// LDS tables of its ids, and each thread keeps its eight entries in registers; an adjustment
+// runs for the thread's j-th ids only where some lane of the wave has an entry there.  What may not be
+// picked is a bit of a word (allow mask, vocabulary end, MASK id).  Per row and wave: the largest
+// value, the lowest id of it from eight comparisons (lane masks, scalar), the sum of
+// exp(l - largest); the waves and then the ranges are merged.  With one range (small
+// vocabularies) the workgroup writes the result.
 //
 // What bounds it: reading the logits (16 bytes a lane, also from rows that start at odd
-// elements: the hardware takes unaligned addresses).
+// elements: the hardware takes unaligned addresses) and about 13 VALU instructions an id.
 constexpr int SEL_NT = 256, SEL_PT = 8, SEL_IDS = SEL_NT * SEL_PT, SEL_RB = 4, SEL_MAX_ROWS = 16;
 constexpr uint32_t SEL_SEEN = 0x80000000u, SEL_BIAS = 0x40000000u;
 
@@ -106,6 +120,7 @@ struct alignas(16) SelectPart {
 template <typename T>
 __global__ void __launch_bounds__(SEL_NT) select_kernel(SelectArgs a, SelectPart* part, int n_ranges, int rows_per) {
     constexpr int NL = 16 / (int)sizeof(T), U = SEL_PT / NL;   // ids per 16-byte load, loads per row
+    constexpr int HB = 4;                                      // history entries a thread loads at once
     __shared__ uint32_t adj_s[SEL_IDS], last_s[SEL_IDS];
     __shared__ float bias_s[SEL_IDS];
     __shared__ Best red[SEL_MAX_ROWS][SEL_NT / 64];
@@ -118,43 +133,68 @@ __global__ void __launch_bounds__(SEL_NT) select_kernel(SelectArgs a, SelectPart
     // load u's first id of this thread
     auto id_of = [&](int u) { return v0 + u * SEL_NT * NL + tid * NL; };
 
-    uint32_t adj[SEL_PT];
-    float bias[SEL_PT], rep = 1.f, pres = 0.f, freq = 0.f;
-    bool touched = false;
+    uint32_t adj[SEL_PT], valid = 0, jmask = 0;                // jmask: the j whose adj is set in some lane
+    float bias[SEL_PT], rep = 1.f, rcp = 1.f, pres = 0.f, freq = 0.f;
 #pragma unroll
-    for (int j = 0; j < SEL_PT; ++j) { adj[j] = 0; bias[j] = 0.f; }
+    for (int j = 0; j < SEL_PT; ++j) {
+        const int v = id_of(j / NL) + j % NL;
+        adj[j] = 0;
+        bias[j] = 0.f;
+        valid |= (uint32_t)(v < a.V && v != a.mask_id) << j;
+    }
 
     // the tables of sequence b's history and biases at this workgroup's ids
     auto enter = [&](int b) {
+        const int h0 = a.hist ? a.hist0[b] : 0, h1 = a.hist ? a.hist0[b + 1] : 0;
+        const int i0 = a.bias ? a.bias0[b] : 0, i1 = a.bias ? a.bias0[b + 1] : 0;
+        const int hp = a.n_prompt ? h0 + a.n_prompt[b] : h0;
         rep = a.rep ? a.rep[b] : 1.f;
         pres = a.pres ? a.pres[b] : 0.f;
         freq = a.freq ? a.freq[b] : 0.f;
-        const int h0 = a.hist ? a.hist0[b] : 0, h1 = a.hist ? a.hist0[b + 1] : 0;
-        const int i0 = a.bias ? a.bias0[b] : 0, i1 = a.bias ? a.bias0[b + 1] : 0;
-        touched = false;
+        rcp = __fdiv_rn(1.f, rep);
+        jmask = 0;
         if (h0 >= h1 && i0 >= i1) return;
-        const int hp = a.n_prompt ? h0 + a.n_prompt[b] : h0;
+        auto slot = [&](int v) { return (unsigned)(v - v0) < (unsigned)SEL_IDS && v < a.V ? v - v0 : -1; };
+        // the first entries of both lists are asked for before the tables are cleared
+        int hv[HB], bv = -1;
+        float bw = 0.f;
+        auto load_hist = [&](int at) {
+#pragma unroll
+            for (int k = 0; k < HB; ++k) {
+                const int i = at + k * SEL_NT;
+                hv[k] = i < h1 ? slot(a.hist[i]) : -1;
+            }
+        };
+        load_hist(h0 + tid);
+        if (i0 + tid < i1) { bv = slot(a.bias_id[i0 + tid]); bw = a.bias[i0 + tid]; }
         __syncthreads();                                       // the tables of the sequence before are read
-        for (int i = tid; i < SEL_IDS; i += SEL_NT) { adj_s[i] = 0; last_s[i] = 0; }
+#pragma unroll
+        for (int i = 0; i < SEL_IDS / SEL_NT; ++i) { adj_s[tid + i * SEL_NT] = 0; last_s[tid + i * SEL_NT] = 0; }
         __syncthreads();
-        for (int i = h0 + tid; i < h1; i += SEL_NT) {
-            const int v = a.hist[i], k = v - v0;
-            if ((unsigned)k < (unsigned)SEL_IDS && v < a.V) {
-                atomicOr(&adj_s[k], SEL_SEEN);
-                if (i >= hp) atomicAdd(&adj_s[k], 1u);         // whole numbers: any order gives the same sum
+        for (int at = h0 + tid; at < h1; at += HB * SEL_NT) {
+            if (at != h0 + tid) load_hist(at);
+#pragma unroll
+            for (int k = 0; k < HB; ++k) {
+                if (hv[k] < 0) continue;
+                // (whole numbers: any order gives the same sum)
+                atomicOr(&adj_s[hv[k]], SEL_SEEN);
+                if (at + k * SEL_NT >= hp) atomicAdd(&adj_s[hv[k]], 1u);
             }
         }
-        for (int i = i0 + tid; i < i1; i += SEL_NT) {
-            const int v = a.bias_id[i], k = v - v0;
-            if ((unsigned)k < (unsigned)SEL_IDS && v < a.V) atomicMax(&last_s[k], (uint32_t)(i - i0) + 1u);
-        }
-        __syncthreads();
-        for (int i = i0 + tid; i < i1; i += SEL_NT) {
-            const int v = a.bias_id[i], k = v - v0;
-            if ((unsigned)k < (unsigned)SEL_IDS && v < a.V && last_s[k] == (uint32_t)(i - i0) + 1u) {
-                bias_s[k] = a.bias[i];                         // the last entry of an id: one thread
+        if (i0 < i1) {
+            if (bv >= 0) atomicMax(&last_s[bv], (uint32_t)tid + 1u);
+            for (int i = i0 + tid + SEL_NT; i < i1; i += SEL_NT) {
+                const int k = slot(a.bias_id[i]);
+                if (k >= 0) atomicMax(&last_s[k], (uint32_t)(i - i0) + 1u);
+            }
+            __syncthreads();
+            auto win = [&](int k, int i, float w) {            // the last entry of an id: one thread
+                if (k < 0 || last_s[k] != (uint32_t)i + 1u) return;
+                bias_s[k] = w;
                 atomicOr(&adj_s[k], SEL_BIAS);
-            }
+            };
+            win(bv, tid, bw);
+            for (int i = i0 + tid + SEL_NT; i < i1; i += SEL_NT) win(slot(a.bias_id[i]), i - i0, a.bias[i]);
         }
         __syncthreads();
 #pragma unroll
@@ -162,7 +202,7 @@ __global__ void __launch_bounds__(SEL_NT) select_kernel(SelectArgs a, SelectPart
             const int k = id_of(j / NL) - v0 + j % NL;
             adj[j] = adj_s[k];
             bias[j] = (adj[j] & SEL_BIAS) ? bias_s[k] : 0.f;
-            touched |= adj[j] != 0;
+            jmask |= (uint32_t)(__builtin_amdgcn_ballot_w64(adj[j] != 0) != 0) << j;
         }
     };
 
@@ -196,31 +236,47 @@ __global__ void __launch_bounds__(SEL_NT) select_kernel(SelectArgs a, SelectPart
                 }
                 if (nb != b) enter(b = nb);
             }
-            const int ar = a.allow ? (a.allow_row ? a.allow_row[row] : row) : -1;
-            const bool none = a.allow && ar != -1 && (ar < 0 || ar >= a.n_allow);
-            float l[SEL_PT];
-            Best best{-INFINITY, -1, 0.f};
+            // bit j: this thread's j-th id may be picked
+            uint32_t bits = valid;
+            if (a.allow != nullptr) {
+                const int ar = a.allow_row ? a.allow_row[row] : row;
+                if (ar != -1) {
+                    uint32_t ok = 0;
+                    if (ar >= 0 && ar < a.n_allow) {
 #pragma unroll
-            for (int j = 0; j < SEL_PT; ++j) {
-                l[j] = elem_to_f32<T>(x[i][j]);
-                l[j] = l[j] != l[j] ? -INFINITY : fminf(l[j], FLT_MAX);
+                        for (int u = 0; u < U; ++u) {
+                            const int v = id_of(u);
+                            const uint32_t w = v < a.V ? a.allow[(size_t)ar * a.allow_ld + (v >> 5)] >> (v & 31) : 0u;
+                            ok |= (w & ((1u << NL) - 1)) << (u * NL);
+                        }
+                    }
+                    bits &= ok;
+                }
             }
-            if (touched) {
+            float l[SEL_PT];
+#pragma unroll
+            for (int j = 0; j < SEL_PT; ++j) l[j] = elem_to_f32<T>(x[i][j]);
+            if (jmask != 0) {
 #pragma unroll
                 for (int j = 0; j < SEL_PT; ++j)
-                    if (adj[j] != 0)
-                        l[j] = adjust_logit(elem_to_f32<T>(x[i][j]), (adj[j] & SEL_SEEN) != 0, (int)(adj[j] & 0x3FFFFFFFu),
-                                            bias[j], (adj[j] & SEL_BIAS) != 0, rep, pres, freq);
+                    if (jmask >> j & 1) {
+                        const float y = adjust_logit(l[j], (adj[j] & SEL_SEEN) != 0, (int)(adj[j] & 0x3FFFFFFFu), bias[j],
+                                                     (adj[j] & SEL_BIAS) != 0, rep, rcp, pres, freq);
+                        l[j] = adj[j] != 0 ? y : l[j];
+                    }
             }
+            // NaN counts as -inf: the median instruction returns the least of the others if one is a NaN (the
+            // bound is hidden from the compiler, which would drop it)
+            float least = -INFINITY;
+            asm("" : "+v"(least));
 #pragma unroll
-            for (int u = 0; u < U; ++u) {
-                const int v = id_of(u);
-                uint32_t bits = 0xFFFFFFFFu;
-                if (none) bits = 0;
-                else if (a.allow && ar != -1 && v < a.V) bits = a.allow[(size_t)ar * a.allow_ld + (v >> 5)] >> (v & 31);
+            for (int j = 0; j < SEL_PT; ++j) l[j] = __builtin_amdgcn_fmed3f(l[j], least, FLT_MAX);
+            if (__builtin_amdgcn_ballot_w64(bits != (1u << SEL_PT) - 1) != 0) {
 #pragma unroll
-                for (int j = 0; j < NL; ++j)
-                    if (!(bits >> j & 1) || v + j == a.mask_id || v + j >= a.V) l[u * NL + j] = -INFINITY;
+                for (int j = 0; j < SEL_PT; ++j) {
+                    const uint32_t m = (uint32_t)__builtin_amdgcn_sbfe((int)bits, j, 1);
+                    l[j] = __uint_as_float((__float_as_uint(l[j]) & m) | (0xFF800000u & ~m));
+                }
             }
             if (a.out != nullptr) {
                 T* dst = (T*)a.out + (long)row * a.ld_out;
@@ -239,13 +295,32 @@ __global__ void __launch_bounds__(SEL_NT) select_kernel(SelectArgs a, SelectPart
                     }
                 }
             }
+            float mx = l[0];
 #pragma unroll
-            for (int j = SEL_PT - 1; j >= 0; --j)              // downwards: the lowest id of the largest stays
-                if (l[j] >= best.mx && l[j] > -INFINITY) { best.mx = l[j]; best.id = id_of(j / NL) + j % NL; }
-            if (best.id >= 0)
+            for (int j = 1; j < SEL_PT; ++j) mx = fmaxf(mx, l[j]);
+            mx = wave_max_f(mx);
+            Best best{mx, -1, 0.f};
+            if (mx > -INFINITY) {                              // the same in every lane
+                // the first lane with the largest value and its first id, load by load
 #pragma unroll
-                for (int j = 0; j < SEL_PT; ++j) best.s += __expf(l[j] - best.mx);
-            best = wave_best(best);
+                for (int u = U - 1; u >= 0; --u) {
+                    uint64_t eq[NL], any = 0;
+#pragma unroll
+                    for (int j = 0; j < NL; ++j) any |= eq[j] = __builtin_amdgcn_ballot_w64(l[u * NL + j] == mx);
+                    if (any != 0) {
+                        const int ln = __builtin_ctzll(any);
+                        int j = NL - 1;
+#pragma unroll
+                        for (int k = NL - 2; k >= 0; --k)
+                            if (eq[k] >> ln & 1) j = k;
+                        best.id = v0 + u * SEL_NT * NL + ((tid & ~63) + ln) * NL + j;
+                    }
+                }
+                float s = 0.f;
+#pragma unroll
+                for (int j = 0; j < SEL_PT; ++j) s += __builtin_amdgcn_exp2f((l[j] - mx) * 1.4426950408889634f);
+                best.s = wave_sum_f(s);
+            }
             if ((tid & 63) == 0) red[row - r0][tid >> 6] = best;
         }
     }
