@@ -52,6 +52,7 @@ bool row_stride_ok(const void* p, int64_t ld, int64_t width, int es) {
 }
 
 constexpr int MAX_BATCH_ROWS = 1 << 24;
+constexpr int N_CU = 256;
 
 }  // namespace
 
@@ -210,11 +211,12 @@ int check_attn(const dllm_attn_args* g, int& shift) {
     return DLLM_OK;
 }
 
-// Ranges of SEL_IDS ids, and rows of a workgroup: enough workgroups to fill the chip a few times over, and
-// otherwise as many rows as keep a sequence's tables.
+// Ranges of SEL_IDS ids, and rows of a workgroup: as many as keep a sequence's tables and still leave
+// 1024 workgroups, from four (the rows loaded at once) or, where that is less than one for every CU, two.
 int select_ranges(int vocab) { return ceil_div(vocab, SEL_IDS); }
 int select_rows_per(int T, int n_ranges) {
     const long per = (long)T * n_ranges / 1024;
+    if ((long)T * n_ranges < 4 * N_CU) return 2;
     return (int)std::min<long>(SEL_MAX_ROWS, std::max<long>(SEL_RB, per / SEL_RB * SEL_RB));
 }
 size_t select_ws_bytes(const dllm_select_args* g) {
@@ -360,7 +362,7 @@ int dllm_select(const dllm_select_args* g, dllm_stream stream) {
         if (!aligned(p, 4)) return fail(DLLM_E_INVAL, "arrays of 32-bit values must be 4-byte aligned");
     if (g->n_rows == 0) return DLLM_OK;
     const size_t need = select_ws_bytes(g);
-    if ((long)select_ranges(g->vocab) * ceil_div(g->n_rows, SEL_RB) > 0x7FFFFFFF)
+    if ((long)select_ranges(g->vocab) * ceil_div(g->n_rows, 2) > 0x7FFFFFFF)
         return fail(DLLM_E_INVAL, "n_rows and vocab need too many workgroups");
     if (need > 0 && (!g->d_ws || !aligned(g->d_ws, 16))) return fail(DLLM_E_INVAL, "workspace: NULL or not 16-byte aligned");
     if (need > g->ws_bytes)

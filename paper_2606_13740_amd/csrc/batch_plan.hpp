@@ -20,9 +20,10 @@ struct PlanArgs {
     int *row0, *pos, *slot, *seq, *lim, *status;
 };
 
-// Exclusive scan of three 64-bit counts over a workgroup of NT threads; `total` gets the sums.
+// Sums over sequences: rows (64 bits: a refused plan may ask for anything), pages taken and given back.
 struct PlanSum {
-    long long rows, take, give;
+    long long rows;
+    int take, give;
 };
 __device__ __forceinline__ PlanSum operator+(const PlanSum& a, const PlanSum& b) {
     return PlanSum{a.rows + b.rows, a.take + b.take, a.give + b.give};
@@ -43,41 +44,38 @@ __device__ __forceinline__ PlanSum operator+(const PlanSum& a, const PlanSum& b)
 constexpr int PLAN_NT = 512;
 constexpr int PLAN_MAXB = 4096;
 __global__ void __launch_bounds__(PLAN_NT) batch_plan_kernel(PlanArgs a) {
-    constexpr int NW = PLAN_NT / 64;
-    __shared__ int row0[PLAN_MAXB + 1], t0[PLAN_MAXB + 1], g0[PLAN_MAXB + 1];
+    constexpr int NW = PLAN_NT / 64, PER = PLAN_MAXB / PLAN_NT;
+    __shared__ int row0[PLAN_MAXB + 1], t0[PLAN_MAXB + 1], g0[PLAN_MAXB + 1], len_s[PLAN_MAXB], own_s[PLAN_MAXB];
     __shared__ PlanSum wsum[NW];
-    __shared__ int bad_s;
+    __shared__ int wbad[NW];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const long long page = 1ll << a.page_shift;
     const int n_free = *a.n_free;
     const int per = (a.B + PLAN_NT - 1) / PLAN_NT;          // consecutive sequences per thread
-    if (tid == 0) bad_s = 0;
-    __syncthreads();
 
-    auto counts = [&](int b, bool& bad) {
-        const int len = a.len[b], nw = a.nw[b], own = a.owned[b];
-        const long long need = ((long long)len + nw + page - 1) >> a.page_shift;
-        bad = len < 0 || nw < 0 || own < 0 || own > a.ld || need > a.ld;
-        PlanSum s{0, 0, 0};
-        if (len >= 0 && nw >= 0 && own >= 0 && own <= a.ld) {
-            s.rows = nw;
-            s.take = need > own ? need - own : 0;
-            const long long keep = max(need, (long long)min(a.shared, own));
-            s.give = own > keep ? own - keep : 0;
-        }
-        return s;
-    };
-
-    PlanSum mine{0, 0, 0};
-    bool any_bad = n_free < 0 || n_free > a.n_pages;
-    for (int i = 0; i < per; ++i) {
+    int len[PER], nw[PER], own[PER];
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
         const int b = tid * per + i;
-        if (b >= a.B) break;
-        bool bad;
-        mine = mine + counts(b, bad);
-        any_bad |= bad;
+        len[i] = nw[i] = own[i] = 0;
+        if (i < per && b < a.B) {
+            len[i] = a.len[b];
+            nw[i] = a.nw[b];
+            own[i] = a.owned[b];
+        }
     }
-    if (any_bad) bad_s = 1;
+    PlanSum part[PER], mine{0, 0, 0};
+    bool bad = n_free < 0 || n_free > a.n_pages;
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+        // pages past the table count as one too many, so that the sums stay in range
+        const long long need = min(((long long)len[i] + nw[i] + page - 1) >> a.page_shift, (long long)a.ld + 1);
+        const bool in = len[i] >= 0 && nw[i] >= 0 && own[i] >= 0 && own[i] <= a.ld;
+        bad |= !in || need > a.ld;
+        const int keep = max((int)need, min(a.shared, own[i]));
+        part[i] = in ? PlanSum{nw[i], max((int)need - own[i], 0), max(own[i] - keep, 0)} : PlanSum{0, 0, 0};
+        mine = mine + part[i];
+    }
     PlanSum inc = mine;                                      // inclusive over the wave
 #pragma unroll
     for (int o = 1; o < 64; o <<= 1) {
@@ -85,30 +83,35 @@ __global__ void __launch_bounds__(PLAN_NT) batch_plan_kernel(PlanArgs a) {
         if (lane >= o) inc = inc + up;
     }
     if (lane == 63) wsum[wave] = inc;
+    const bool wave_bad = __builtin_amdgcn_ballot_w64(bad) != 0;
+    if (lane == 0) wbad[wave] = wave_bad;
     __syncthreads();
     PlanSum at{inc.rows - mine.rows, inc.take - mine.take, inc.give - mine.give}, total{0, 0, 0};
+    bad = false;
 #pragma unroll
     for (int w = 0; w < NW; ++w) {
         if (w < wave) at = at + wsum[w];
         total = total + wsum[w];
+        bad |= wbad[w] != 0;
     }
-    const long long stack = (long long)n_free + total.give;  // entries after the pushes
-    const long long shortage = total.take > stack ? total.take - stack : 0;
-    const bool ok = !bad_s && shortage == 0 && total.rows <= a.max_rows && stack <= a.n_pages;
-    for (int i = 0; i < per; ++i) {                          // where every count fits (ok): exact in 32 bits
+    const int stack = n_free + total.give;                   // entries after the pushes
+    const int shortage = max(total.take - stack, 0);
+    const bool ok = !bad && shortage == 0 && total.rows <= a.max_rows && stack <= a.n_pages;
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {                          // (rows fit 32 bits where they are used, in a granted plan)
         const int b = tid * per + i;
-        if (b >= a.B) break;
-        bool bad;
-        const PlanSum s = counts(b, bad);
+        if (i >= per || b >= a.B) break;
         row0[b] = ok ? (int)at.rows : 0;
-        t0[b] = (int)at.take;
-        g0[b] = (int)at.give;
-        at = at + s;
+        t0[b] = at.take;
+        g0[b] = at.give;
+        len_s[b] = len[i];
+        own_s[b] = own[i];
+        at = at + part[i];
     }
     if (tid == 0) {
         row0[a.B] = ok ? (int)total.rows : 0;
-        t0[a.B] = (int)total.take;
-        g0[a.B] = (int)total.give;
+        t0[a.B] = total.take;
+        g0[a.B] = total.give;
     }
     __syncthreads();
 
@@ -126,19 +129,18 @@ __global__ void __launch_bounds__(PLAN_NT) batch_plan_kernel(PlanArgs a) {
     auto stack_at = [&](int i) {
         if (i < n_free) return a.free_[i];
         const int k = i - n_free, b = find(g0, k);
-        const int own = a.owned[b];
-        return a.table[(size_t)b * a.ld + own - (g0[b + 1] - g0[b]) + (k - g0[b])];
+        return a.table[(size_t)b * a.ld + own_s[b] - (g0[b + 1] - g0[b]) + (k - g0[b])];
     };
-    const int n_stack = (int)stack;
+    const int n_stack = stack;
     const int gtid = blockIdx.x * PLAN_NT + tid, gn = gridDim.x * PLAN_NT;
 
     for (int r = gtid; r < a.max_rows; r += gn) {
         int pos = 0, slot = -1, seq = -1, lim = 0;
         if (r < row0[a.B]) {
             seq = find(row0, r);
-            const int len = a.len[seq], own = a.owned[seq];
-            pos = len + r - row0[seq];
-            lim = len + a.nw[seq];
+            const int own = own_s[seq];
+            pos = len_s[seq] + r - row0[seq];
+            lim = len_s[seq] + row0[seq + 1] - row0[seq];
             const int p = pos >> a.page_shift;
             const int pg = p < own ? a.table[(size_t)seq * a.ld + p] : stack_at(n_stack - 1 - t0[seq] - (p - own));
             if (pg >= 0 && pg < a.n_pages) slot = (pg << a.page_shift) + (pos & ((int)page - 1));
@@ -150,19 +152,19 @@ __global__ void __launch_bounds__(PLAN_NT) batch_plan_kernel(PlanArgs a) {
     }
     for (int b = gtid; b <= a.B; b += gn) a.row0[b] = row0[b];
     for (int b = gtid; b < a.B; b += gn)
-        a.owned_out[b] = a.owned[b] + (ok ? (t0[b + 1] - t0[b]) - (g0[b + 1] - g0[b]) : 0);
+        a.owned_out[b] = own_s[b] + (ok ? (t0[b + 1] - t0[b]) - (g0[b + 1] - g0[b]) : 0);
     if (ok) {
         const int n_take = t0[a.B], left = n_stack - n_take;
         for (int k = gtid; k < n_take; k += gn) {            // missing page k
             const int b = find(t0, k);
-            a.table[(size_t)b * a.ld + a.owned[b] + (k - t0[b])] = stack_at(n_stack - 1 - k);
+            a.table[(size_t)b * a.ld + own_s[b] + (k - t0[b])] = stack_at(n_stack - 1 - k);
         }
         for (int i = n_free + gtid; i < left; i += gn) a.free_[i] = stack_at(i);
     }
     if (gtid == 0) {
         *a.n_free_out = ok ? n_stack - t0[a.B] : n_free;
         a.status[0] = (int)min(total.rows, 0x7FFFFFFFll);
-        a.status[1] = (int)min(shortage, 0x7FFFFFFFll);
+        a.status[1] = shortage;
         a.status[2] = ok ? 0 : 1;
     }
 }

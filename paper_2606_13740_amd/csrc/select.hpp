@@ -3,6 +3,8 @@
 
 #include <float.h>
 
+#include <type_traits>
+
 #include "attn_paged.hpp"
 #include "common.hpp"
 #include "qk_rope.hpp"
@@ -41,28 +43,22 @@ __device__ __forceinline__ Best best_merge(const Best& a, const Best& b) {
     return Best{mx, id, a.s * expf(a.mx - mx) + b.s * expf(b.mx - mx)};
 }
 
-// l / rep, rounded once, where rcp is 1 / rep rounded once: one step of the remainder is exact for
-// quotients away from the ends of the range, which take the division itself.
-__device__ __forceinline__ float div_by(float l, float rep, float rcp) {
-    const float q = l * rcp, d = fmaf(fmaf(-q, rep, l), rcp, q);
-    const float m = fabsf(l), n = fabsf(rep);
-    const bool plain = m > 0x1p-90f && m < 0x1p90f && n > 0x1p-30f && n < 0x1p30f;
-    return plain ? d : __fdiv_rn(l, rep);
-}
-
-// A logit after its sequence's penalties and bias.  Separate roundings (no fused
-// multiply-add), so that equal logits with equal adjustments stay equal.
-__device__ __forceinline__ float adjust_logit(float l, bool seen, int made, float bias, bool has_bias, float rep,
-                                              float rcp, float pres, float freq) {
+// A logit after its sequence's penalties and bias (0: none); e: the id's table entry.  Separate
+// roundings (no fused multiply-add), so that equal logits with equal adjustments stay equal.  l / rep by
+// 1 / rep and one step of the remainder, which is the rounded quotient (but for the last bit of
+// results near the underflow).
+constexpr uint32_t SEL_SEEN = 0x80000000u, SEL_BIAS = 0x40000000u, SEL_COUNT = 0x3FFFFFFFu;
+__device__ __forceinline__ float adjust_logit(float l, uint32_t e, float bias, float rep, float rcp, float pres, float freq) {
 #pragma clang fp contract(off)
-    const float up = l * rep, down = div_by(l, rep, rcp);
-    l = seen ? (l > 0.f ? down : up) : l;
-    const float f = freq * (float)made;
-    l = l - f;
-    const float m = l - pres;
-    l = made > 0 ? m : l;
-    const float w = l + bias;
-    return has_bias ? w : l;
+    const float up = l * rep, q = l * rcp;
+    const float d = fmaf(fmaf(-q, rep, l), rcp, q);
+    const float down = fabsf(q) < INFINITY ? d : q;
+    l = (e & SEL_SEEN) ? (l > 0.f ? down : up) : l;
+    const uint32_t made = e & SEL_COUNT;
+    const float fm = freq * (float)made;
+    l = l - fm;
+    l = l - (made > 0 ? pres : 0.f);
+    return l + bias;
 }
 
 // The six butterfly steps of a wave-wide reduction without LDS: lane permutes inside 16 lanes (a
@@ -96,6 +92,19 @@ __device__ __forceinline__ Best wave_best(const Best& b) {
     return Best{mx, (int)id, s};
 }
 
+// Two rows' reductions over the wave at once: the swap leaves row 0's values in lanes 0-31 and row 1's in
+// lanes 32-63, where the other steps run for both.
+template <class F> __device__ __forceinline__ uint32_t wave_fold2(uint32_t v0, uint32_t v1, F f) {
+    const auto a = __builtin_amdgcn_permlane32_swap(v0, v1, false, false);
+    uint32_t v = f(a[0], a[1]);
+    const auto b = __builtin_amdgcn_permlane16_swap(v, v, false, false);
+    v = f(b[0], b[1]);
+    v = f(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0xB1, 0xF, 0xF, true));
+    v = f(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x4E, 0xF, 0xF, true));
+    v = f(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x141, 0xF, 0xF, true));
+    return f(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x140, 0xF, 0xF, true));
+}
+
 // A workgroup takes SEL_IDS consecutive ids of `rows_per` consecutive rows.  A thread holds eight ids
 // for all of them, so a sequence's history and bias list are scanned once per workgroup, into
 // LDS tables of its ids, and each thread keeps its eight entries in registers; an adjustment
@@ -106,10 +115,10 @@ __device__ __forceinline__ Best wave_best(const Best& b) {
 // vocabularies) the workgroup writes the result.
 //
 // What bounds it: reading the logits (16 bytes a lane, also from rows that start at odd
-// elements: the hardware takes unaligned addresses) and about 13 VALU instructions an id.
+// elements: the hardware takes unaligned addresses) beside about 11 VALU instructions an id and
+// latency: five waves a SIMD (96 VGPRs) hide more of it than four of 109 or six with spills
+// (256 rows of 152064 bf16 logits, adjusted logits kept: 61, 70 and 73 us).
 constexpr int SEL_NT = 256, SEL_PT = 8, SEL_IDS = SEL_NT * SEL_PT, SEL_RB = 4, SEL_MAX_ROWS = 16;
-constexpr uint32_t SEL_SEEN = 0x80000000u, SEL_BIAS = 0x40000000u;
-
 struct alignas(16) SelectPart {
     float mx;
     int id;
@@ -118,7 +127,7 @@ struct alignas(16) SelectPart {
 };
 
 template <typename T>
-__global__ void __launch_bounds__(SEL_NT) select_kernel(SelectArgs a, SelectPart* part, int n_ranges, int rows_per) {
+__global__ void __launch_bounds__(SEL_NT) __attribute__((amdgpu_waves_per_eu(5))) select_kernel(SelectArgs a, SelectPart* part, int n_ranges, int rows_per) {
     constexpr int NL = 16 / (int)sizeof(T), U = SEL_PT / NL;   // ids per 16-byte load, loads per row
     constexpr int HB = 4;                                      // history entries a thread loads at once
     __shared__ uint32_t adj_s[SEL_IDS], last_s[SEL_IDS];
@@ -133,7 +142,8 @@ __global__ void __launch_bounds__(SEL_NT) select_kernel(SelectArgs a, SelectPart
     // load u's first id of this thread
     auto id_of = [&](int u) { return v0 + u * SEL_NT * NL + tid * NL; };
 
-    uint32_t adj[SEL_PT], valid = 0, jmask = 0;                // jmask: the j whose adj is set in some lane
+    // bit j: of valid, this thread's j-th id may be picked; of jmask, some lane's j-th id has an adjustment
+    uint32_t valid = 0, jmask = 0, adj[SEL_PT];
     float bias[SEL_PT], rep = 1.f, rcp = 1.f, pres = 0.f, freq = 0.f;
 #pragma unroll
     for (int j = 0; j < SEL_PT; ++j) {
@@ -148,12 +158,14 @@ __global__ void __launch_bounds__(SEL_NT) select_kernel(SelectArgs a, SelectPart
         const int h0 = a.hist ? a.hist0[b] : 0, h1 = a.hist ? a.hist0[b + 1] : 0;
         const int i0 = a.bias ? a.bias0[b] : 0, i1 = a.bias ? a.bias0[b + 1] : 0;
         const int hp = a.n_prompt ? h0 + a.n_prompt[b] : h0;
-        rep = a.rep ? a.rep[b] : 1.f;
         pres = a.pres ? a.pres[b] : 0.f;
         freq = a.freq ? a.freq[b] : 0.f;
+        rep = a.rep ? a.rep[b] : 1.f;
         rcp = __fdiv_rn(1.f, rep);
-        jmask = 0;
-        if (h0 >= h1 && i0 >= i1) return;
+        if (h0 >= h1 && i0 >= i1) {
+            jmask = 0;
+            return;
+        }
         auto slot = [&](int v) { return (unsigned)(v - v0) < (unsigned)SEL_IDS && v < a.V ? v - v0 : -1; };
         // the first entries of both lists are asked for before the tables are cleared
         int hv[HB], bv = -1;
@@ -197,6 +209,7 @@ __global__ void __launch_bounds__(SEL_NT) select_kernel(SelectArgs a, SelectPart
             for (int i = i0 + tid + SEL_NT; i < i1; i += SEL_NT) win(slot(a.bias_id[i]), i - i0, a.bias[i]);
         }
         __syncthreads();
+        jmask = 0;
 #pragma unroll
         for (int j = 0; j < SEL_PT; ++j) {
             const int k = id_of(j / NL) - v0 + j % NL;
@@ -206,124 +219,152 @@ __global__ void __launch_bounds__(SEL_NT) select_kernel(SelectArgs a, SelectPart
         }
     };
 
-    int b = -1, b_end = r0;                                    // rows below b_end belong to b
-    for (int rb = r0; rb < r1; rb += SEL_RB) {
-        T x[SEL_RB][SEL_PT];
+    // the rows' masks: lane i has row r0 + i's
+    const int arow = a.allow == nullptr ? -1 : (a.allow_row ? a.allow_row[min(r0 + (tid & 63), r1 - 1)] : min(r0 + (tid & 63), r1 - 1));
+    // FULL: no id of this range is past the vocabulary
+    auto all_rows = [&](auto FULL) {
+        constexpr bool full = decltype(FULL)::value;
+        int b_end = r0, re;                                    // rows below b_end belong to the sequence entered
+        for (int rb = r0; rb < r1; rb = re) {
+            // every load of the rows goes out before any is used (the words are not taken apart here, and the
+            // tables of a sequence that begins are made meanwhile); past the last row it is read again
+            u32x4_t raw[SEL_RB][U];
+            uint32_t w[SEL_RB][U];
 #pragma unroll
-        for (int i = 0; i < SEL_RB; ++i) {
-            const T* src = (const T*)a.logits + (long)min(rb + i, r1 - 1) * a.ld;
+            for (int i = 0; i < SEL_RB; ++i) {
+                const T* src = (const T*)a.logits + (long)min(rb + i, r1 - 1) * a.ld;
 #pragma unroll
-            for (int u = 0; u < U; ++u) {
-                const int v = id_of(u);
-                if (v + NL <= a.V) {
-                    __builtin_memcpy(&x[i][u * NL], src + v, 16);
-                } else {
+                for (int u = 0; u < U; ++u) {
+                    if constexpr (full) {
+                        __builtin_memcpy(&raw[i][u], src + id_of(u), 16);
+                    } else {
+                        T x[NL];
 #pragma unroll
-                    for (int j = 0; j < NL; ++j) x[i][u * NL + j] = v + j < a.V ? src[v + j] : (T)0.f;
+                        for (int j = 0; j < NL; ++j) x[j] = src[min(id_of(u) + j, a.V - 1)];
+                        __builtin_memcpy(&raw[i][u], x, 16);
+                    }
                 }
             }
-        }
+            if (a.allow != nullptr) {
 #pragma unroll
-        for (int i = 0; i < SEL_RB; ++i) {
-            const int row = rb + i;
-            if (row >= r1) break;
-            if (row >= b_end) {
+                for (int i = 0; i < SEL_RB; ++i) {
+                    const int ar = __builtin_amdgcn_readlane(arow, min(rb + i, r1 - 1) - r0);
+                    const uint32_t* words = a.allow + (size_t)(ar >= 0 && ar < a.n_allow ? ar : 0) * a.allow_ld;
+#pragma unroll
+                    for (int u = 0; u < U; ++u) w[i][u] = words[min(id_of(u) >> 5, a.allow_ld - 1)];
+                }
+            }
+            if (rb >= b_end) {
                 int nb = 0;
                 b_end = a.T;
                 if (a.row0 != nullptr) {
-                    nb = row_seq(a.row0, a.B, row);
+                    nb = row_seq(a.row0, a.B, rb);
                     b_end = a.row0[nb + 1];
                 }
-                if (nb != b) enter(b = nb);
+                enter(nb);
             }
-            // bit j: this thread's j-th id may be picked
-            uint32_t bits = valid;
-            if (a.allow != nullptr) {
-                const int ar = a.allow_row ? a.allow_row[row] : row;
-                if (ar != -1) {
-                    uint32_t ok = 0;
-                    if (ar >= 0 && ar < a.n_allow) {
+            re = min(min(r1, b_end), rb + SEL_RB);             // rows of one sequence
 #pragma unroll
-                        for (int u = 0; u < U; ++u) {
-                            const int v = id_of(u);
-                            const uint32_t w = v < a.V ? a.allow[(size_t)ar * a.allow_ld + (v >> 5)] >> (v & 31) : 0u;
-                            ok |= (w & ((1u << NL) - 1)) << (u * NL);
+            for (int i0 = 0; i0 < SEL_RB; i0 += 2) {
+                if (rb + i0 >= re) break;
+                float l[2][SEL_PT];
+                uint32_t top[2];
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+#pragma unroll
+                    for (int u = 0; u < U; ++u) {
+                        T x[NL];
+                        __builtin_memcpy(x, &raw[i0 + i][u], 16);
+#pragma unroll
+                        for (int j = 0; j < NL; ++j) l[i][u * NL + j] = elem_to_f32<T>(x[j]);
+                    }
+                    if (jmask != 0) {
+#pragma unroll
+                        for (int j = 0; j < SEL_PT; ++j)
+                            if (jmask >> j & 1) l[i][j] = adjust_logit(l[i][j], adj[j], bias[j], rep, rcp, pres, freq);
+                    }
+                    // NaN counts as -inf: the median instruction returns the least of the others if one is a NaN
+                    // (the bound is hidden from the compiler, which would drop it)
+                    float least = -INFINITY;
+                    asm("" : "+v"(least));
+#pragma unroll
+                    for (int j = 0; j < SEL_PT; ++j) l[i][j] = __builtin_amdgcn_fmed3f(l[i][j], least, FLT_MAX);
+                    uint32_t bits = valid;
+                    if (a.allow != nullptr) {
+                        const int ar = __builtin_amdgcn_readlane(arow, min(rb + i0 + i, r1 - 1) - r0);
+                        uint32_t ok = 0;
+#pragma unroll
+                        for (int u = 0; u < U; ++u) ok |= (w[i0 + i][u] >> (id_of(u) & 31) & ((1u << NL) - 1)) << (u * NL);
+                        bits &= ar >= 0 && ar < a.n_allow ? ok : (ar == -1 ? 0xFFFFFFFFu : 0u);
+                    }
+                    if (__builtin_amdgcn_ballot_w64(bits != (1u << SEL_PT) - 1) != 0) {
+#pragma unroll
+                        for (int j = 0; j < SEL_PT; ++j) {
+                            const uint32_t m = (uint32_t)__builtin_amdgcn_sbfe((int)bits, j, 1);
+                            l[i][j] = __uint_as_float((__float_as_uint(l[i][j]) & m) | (0xFF800000u & ~m));
                         }
                     }
-                    bits &= ok;
-                }
-            }
-            float l[SEL_PT];
+                    if (a.out != nullptr && rb + i0 + i < re) {
+                        T* dst = (T*)a.out + (long)(rb + i0 + i) * a.ld_out;
+                        if constexpr (full) {
+                            T y[SEL_PT];
 #pragma unroll
-            for (int j = 0; j < SEL_PT; ++j) l[j] = elem_to_f32<T>(x[i][j]);
-            if (jmask != 0) {
+                            for (int j = 0; j < SEL_PT; ++j) y[j] = (T)l[i][j];
 #pragma unroll
-                for (int j = 0; j < SEL_PT; ++j)
-                    if (jmask >> j & 1) {
-                        const float y = adjust_logit(l[j], (adj[j] & SEL_SEEN) != 0, (int)(adj[j] & 0x3FFFFFFFu), bias[j],
-                                                     (adj[j] & SEL_BIAS) != 0, rep, rcp, pres, freq);
-                        l[j] = adj[j] != 0 ? y : l[j];
+                            for (int u = 0; u < U; ++u) __builtin_memcpy(dst + id_of(u), &y[u * NL], 16);
+                        } else {
+#pragma unroll
+                            for (int j = 0; j < SEL_PT; ++j) {
+                                const int v = id_of(j / NL) + j % NL;
+                                if (v < a.V) dst[v] = (T)l[i][j];
+                            }
+                        }
                     }
-            }
-            // NaN counts as -inf: the median instruction returns the least of the others if one is a NaN (the
-            // bound is hidden from the compiler, which would drop it)
-            float least = -INFINITY;
-            asm("" : "+v"(least));
+                    float mx = l[i][0];
 #pragma unroll
-            for (int j = 0; j < SEL_PT; ++j) l[j] = __builtin_amdgcn_fmed3f(l[j], least, FLT_MAX);
-            if (__builtin_amdgcn_ballot_w64(bits != (1u << SEL_PT) - 1) != 0) {
-#pragma unroll
-                for (int j = 0; j < SEL_PT; ++j) {
-                    const uint32_t m = (uint32_t)__builtin_amdgcn_sbfe((int)bits, j, 1);
-                    l[j] = __uint_as_float((__float_as_uint(l[j]) & m) | (0xFF800000u & ~m));
+                    for (int j = 1; j < SEL_PT; ++j) mx = fmaxf(mx, l[i][j]);
+                    top[i] = __float_as_uint(mx);
                 }
-            }
-            if (a.out != nullptr) {
-                T* dst = (T*)a.out + (long)row * a.ld_out;
-                T y[SEL_PT];
+                const uint32_t tops = wave_fold2(top[0], top[1], [](uint32_t p, uint32_t q) {
+                    return __float_as_uint(fmaxf(__uint_as_float(p), __uint_as_float(q))); });
+                float sum[2];
+                int id[2];
 #pragma unroll
-                for (int j = 0; j < SEL_PT; ++j) y[j] = (T)l[j];
+                for (int i = 0; i < 2; ++i) {
+                    const float mx = __uint_as_float(__builtin_amdgcn_readlane(tops, 32 * i));
+                    id[i] = -1;
+                    // (load by load) the first lane that has the largest value, and its first id
 #pragma unroll
-                for (int u = 0; u < U; ++u) {
-                    const int v = id_of(u);
-                    if (v + NL <= a.V) {
-                        __builtin_memcpy(dst + v, &y[u * NL], 16);
-                    } else {
+                    for (int u = U - 1; u >= 0; --u) {
+                        float mu = l[i][u * NL];
 #pragma unroll
-                        for (int j = 0; j < NL; ++j)
-                            if (v + j < a.V) dst[v + j] = y[u * NL + j];
-                    }
-                }
-            }
-            float mx = l[0];
-#pragma unroll
-            for (int j = 1; j < SEL_PT; ++j) mx = fmaxf(mx, l[j]);
-            mx = wave_max_f(mx);
-            Best best{mx, -1, 0.f};
-            if (mx > -INFINITY) {                              // the same in every lane
-                // the first lane with the largest value and its first id, load by load
-#pragma unroll
-                for (int u = U - 1; u >= 0; --u) {
-                    uint64_t eq[NL], any = 0;
-#pragma unroll
-                    for (int j = 0; j < NL; ++j) any |= eq[j] = __builtin_amdgcn_ballot_w64(l[u * NL + j] == mx);
-                    if (any != 0) {
+                        for (int j = 1; j < NL; ++j) mu = fmaxf(mu, l[i][u * NL + j]);
+                        const uint64_t any = __builtin_amdgcn_ballot_w64(mu == mx);
+                        if (any == 0) continue;
                         const int ln = __builtin_ctzll(any);
-                        int j = NL - 1;
+                        int k = 0;
 #pragma unroll
-                        for (int k = NL - 2; k >= 0; --k)
-                            if (eq[k] >> ln & 1) j = k;
-                        best.id = v0 + u * SEL_NT * NL + ((tid & ~63) + ln) * NL + j;
+                        for (int j = NL - 1; j >= 0; --j)
+                            if (__uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(l[i][u * NL + j]), ln)) == mx) k = j;
+                        id[i] = v0 + u * SEL_NT * NL + ((tid & ~63) + ln) * NL + k;
                     }
-                }
-                float s = 0.f;
+                    const float ref = mx > -INFINITY ? mx : 0.f;
+                    sum[i] = 0.f;
 #pragma unroll
-                for (int j = 0; j < SEL_PT; ++j) s += __builtin_amdgcn_exp2f((l[j] - mx) * 1.4426950408889634f);
-                best.s = wave_sum_f(s);
+                    for (int j = 0; j < SEL_PT; ++j) sum[i] += __builtin_amdgcn_exp2f((l[i][j] - ref) * 1.4426950408889634f);
+                    if (!(mx > -INFINITY)) id[i] = -1;
+                }
+                const uint32_t sums = wave_fold2(__float_as_uint(sum[0]), __float_as_uint(sum[1]), [](uint32_t p, uint32_t q) {
+                    return __float_as_uint(__uint_as_float(p) + __uint_as_float(q)); });
+#pragma unroll
+                for (int i = 0; i < 2; ++i)
+                    if ((tid & 63) == 32 * i && rb + i0 + i < re)
+                        red[rb + i0 + i - r0][tid >> 6] = Best{__uint_as_float(tops), id[i], __uint_as_float(sums)};
             }
-            if ((tid & 63) == 0) red[row - r0][tid >> 6] = best;
         }
-    }
+    };
+    if (v0 + SEL_IDS <= a.V) all_rows(std::true_type{});
+    else all_rows(std::false_type{});
     __syncthreads();
     if (tid < r1 - r0) {
         Best best = red[tid][0];
