@@ -596,6 +596,58 @@ typedef struct dllm_select_args {
 int dllm_select_ws(const dllm_select_args* args, size_t* bytes);
 int dllm_select(const dllm_select_args* args, dllm_stream stream);
 
+/* Norm of every query and key head before the rotation, for models that have one: per
+ * head, fp32, q * rsqrt(mean(q^2) + eps) * gain with cfg.eps and a gain of head_dim
+ * floats per layer (device pointers in HOST arrays of n_layers entries, copied during
+ * the call, which synchronises `stream`).  Every later call that uses the model's Q/K/V
+ * (prompts, steps, appends, refreshes, batch steps) applies it; cached K from before
+ * does not have it, so set it before the first.  E_INVAL for NULL pointers. */
+int dllm_model_set_qk_norm(dllm_model* m, const float* const* d_q_gain, const float* const* d_k_gain,
+                           dllm_stream stream);
+
+/* Bytes of a paged K/V cache of n_pages pages for all layers of a model: 2 planes per
+ * layer (K, V^T), layer l's at (2l + 0) and (2l + 1) times the plane's elements, in the
+ * types of dllm_kv_bytes (fp32 for DLLM_F32 models, else fp16).  E_INVAL for a page size
+ * or count out of range. */
+int dllm_batch_bytes(const dllm_model* m, int32_t n_pages, int32_t page, size_t* bytes);
+
+/* Rows of a batch step: a plan's arrays (dllm_batch_plan), device pointers. */
+typedef struct dllm_batch_rows {
+    int32_t n_rows;         /* rows of the call; those behind d_row0[n_seqs] are computed and mean nothing */
+    int32_t n_seqs;
+    int32_t page;
+    int32_t n_pages;
+    int32_t table_ld;
+    int32_t shared_len;     /* as in dllm_attn_args */
+    int32_t max_rows;
+    int32_t max_len;
+    const int32_t* d_table;
+    const int32_t* d_row0;  /* [n_seqs + 1] */
+    const int32_t* d_pos;   /* [n_rows] */
+    const int32_t* d_slot;  /* [n_rows] */
+    const int32_t* d_len;   /* [n_seqs]: d_len + d_new of the plan */
+    const int32_t* d_lim;   /* [n_rows], or NULL: d_len of the row's sequence */
+} dllm_batch_rows;
+
+/* A step of the model over the rows of several sequences (System Design, "Multi-Block
+ * Speculative Decoding": the window is the execution unit; here every sequence of the batch
+ * has one), streaming the weights once for all of them and the shared prefix's K/V once
+ * per layer.  Row r feeds the MASK id where d_mask[r] != 0 (d_mask nullable), else
+ * d_tok[r]; its K/V are written to its slot before the layer's attention.  A sequence's
+ * rows are, value for value up to rounding, dllm_denoise_step's over a cache of its own
+ * (Q is one fp16 value here, not a pair).  With outputs (both set): every row's argmax
+ * id and confidence, at most cfg.max_window rows.  Without: only the K/V, any number
+ * of rows (prompts, finished blocks).  `sel` (nullable): the logits are written to
+ * sel->d_logits (contiguous fp32 [n_rows][vocab], the caller's; MASK column -inf) and
+ * dllm_select with its penalties, biases and masks gives the outputs instead (its d_out_id,
+ * d_out_conf are this call's).  Workspaces grow at the first call of a size (the call then
+ * synchronises the device); later ones can be captured.  E_INVAL, E_CAPACITY and E_DTYPE as
+ * the operators' and dllm_denoise_step's; E_CAPACITY if max_len exceeds cfg.max_pos or
+ * the pages are fewer than dllm_batch_bytes(). */
+int dllm_batch_step(dllm_model* m, void* d_pages, size_t bytes, const dllm_batch_rows* rows, const int32_t* d_tok,
+                    const uint8_t* d_mask, const dllm_select_args* sel, int32_t* d_out_id, float* d_out_conf,
+                    dllm_stream stream);
+
 /* Measurement helper: one launch of a plain streaming read over `bytes` bytes of
  * the device buffer d_buf (16-byte aligned; bytes a multiple of 16), the same
  * 16-byte-per-lane non-temporal loads the GEMMs stream weights with.  The caller

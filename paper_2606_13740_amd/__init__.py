@@ -70,6 +70,11 @@ class dllm_attn_args(ctypes.Structure):
                 [("ld_out", _i64), ("d_ws", _vp), ("ws_bytes", _sz)])
 
 
+class dllm_batch_rows(ctypes.Structure):
+    _fields_ = (_fields(_i32, "n_rows n_seqs page n_pages table_ld shared_len max_rows max_len") +
+                _fields(_vp, "d_table d_row0 d_pos d_slot d_len d_lim"))
+
+
 class dllm_select_args(ctypes.Structure):
     _fields_ = (_fields(_i32, "dtype n_rows vocab mask_id n_seqs") + [("d_logits", _vp), ("ld", _i64)] +
                 _fields(_vp, "d_row0 d_hist d_hist0 d_n_prompt d_repetition d_presence d_frequency d_bias_id d_bias "
@@ -117,6 +122,10 @@ _SIGNATURES = {
     "dllm_attention_paged": ([ctypes.POINTER(dllm_attn_args), _vp], ctypes.c_int),
     "dllm_select_ws": ([ctypes.POINTER(dllm_select_args), ctypes.POINTER(_sz)], ctypes.c_int),
     "dllm_select": ([ctypes.POINTER(dllm_select_args), _vp], ctypes.c_int),
+    "dllm_model_set_qk_norm": ([_vp, ctypes.POINTER(_vp), ctypes.POINTER(_vp), _vp], ctypes.c_int),
+    "dllm_batch_bytes": ([_vp, _i32, _i32, ctypes.POINTER(_sz)], ctypes.c_int),
+    "dllm_batch_step": ([_vp, _vp, _sz, ctypes.POINTER(dllm_batch_rows), _vp, _vp, ctypes.POINTER(dllm_select_args), _vp, _vp,
+                         _vp], ctypes.c_int),
     "dllm_commit_staged": ([_vp, _vp, _vp, _vp, _vp, _i32, _i32, ctypes.c_float, ctypes.c_float, _vp, _vp, _vp],
                            ctypes.c_int),
 }
@@ -480,11 +489,10 @@ def dllm_attention_paged(q, k_pages, v_pages, table, row0, length, out, max_rows
     del keep
 
 
-def dllm_select(logits, out_id, out_conf, mask_id: int = -1, row0=None, hist=None, hist0=None, n_prompt=None,
-                repetition=None, presence=None, frequency=None, bias_id=None, bias=None, bias0=None, allow=None,
-                allow_row=None, out_logits=None, ws=None, stream=None):
-    """logits, out_logits: [rows][vocab], rows may be strided; allow: int32 words [masks][words]."""
-    f = "dllm_select"
+def _select_args(f, logits, out_id, out_conf, mask_id: int = -1, row0=None, hist=None, hist0=None, n_prompt=None,
+                 repetition=None, presence=None, frequency=None, bias_id=None, bias=None, bias0=None, allow=None,
+                 allow_row=None, out_logits=None, ws=None, stream=None):
+    """(struct, what keeps its workspace alive) of a selection."""
     dev = _gpu(f, logits)
     T, V = logits.shape
     B = row0.numel() - 1 if row0 is not None else 1
@@ -507,8 +515,53 @@ def dllm_select(logits, out_id, out_conf, mask_id: int = -1, row0=None, hist=Non
                          _ptr(row0), _ptr(hist), _ptr(hist0), _ptr(n_prompt), _ptr(repetition), _ptr(presence),
                          _ptr(frequency), _ptr(bias_id), _ptr(bias), _ptr(bias0), _ptr(allow), n_allow, allow_ld,
                          _ptr(allow_row), _ptr(out_logits), ld_out, out_id.data_ptr(), out_conf.data_ptr())
-    keep = _workspace(lib().dllm_select_ws, a, ws, stream, dev, f)
+    return a, _workspace(lib().dllm_select_ws, a, ws, stream, dev, f)
+
+
+def dllm_select(logits, out_id, out_conf, stream=None, **control):
+    """logits (and out_logits): [rows][vocab], rows may be strided.  control: mask_id, row0, hist, hist0, n_prompt,
+    repetition, presence, frequency, bias_id, bias, bias0, allow (int32 words [masks][words]), allow_row, out_logits, ws."""
+    f = "dllm_select"
+    a, keep = _select_args(f, logits, out_id, out_conf, stream=stream, **control)
     _check(lib().dllm_select(ctypes.byref(a), _stream(stream)), f)
+    del keep
+
+
+def dllm_model_set_qk_norm(model: int, q_gains, k_gains, stream=None):
+    """q_gains, k_gains: one float32 [head_dim] tensor per layer."""
+    f = "dllm_model_set_qk_norm"
+    _plain(f, _gpu(f, q_gains[0]), _Types.f32, tuple(q_gains) + tuple(k_gains), "gain " * (len(q_gains) + len(k_gains)))
+    q, k = ((_vp * len(g))(*[t.data_ptr() for t in g]) for g in (q_gains, k_gains))
+    _check(lib().dllm_model_set_qk_norm(model, q, k, _stream(stream)), f)
+
+
+def dllm_batch_bytes(model: int, n_pages: int, page: int) -> int:
+    n = _sz()
+    _check(lib().dllm_batch_bytes(model, n_pages, page, ctypes.byref(n)), "dllm_batch_bytes")
+    return n.value
+
+
+def dllm_batch_step(model: int, pages, n_pages: int, page: int, tok, mask, table, row0, pos, slot, length, max_rows: int,
+                    max_len: int, out_id=None, out_conf=None, shared_len: int = 0, lim=None, logits=None, control=None,
+                    stream=None):
+    """tok's length is the number of rows.  logits (float32 [rows][vocab]) with control, a dict of dllm_select's options:
+    the outputs come from the controlled logits."""
+    f = "dllm_batch_step"
+    dev, R, B, ld = _gpu(f, tok), tok.numel(), length.numel(), table.shape[-1]
+    _plain(f, dev, _Types.i32, (tok, table, row0, pos, slot, length, lim, out_id), "tok table row0 pos slot length lim out_id")
+    _plain(f, dev, _Types.torch.uint8, (mask,), "mask")
+    _plain(f, dev, _Types.f32, (out_conf, logits), "out_conf logits")
+    _at_least(f, R, (pos, slot, lim, mask, out_id, out_conf), "pos slot lim mask out_id out_conf")
+    if table.numel() < B * ld or row0.numel() < B + 1 or pages.get_device() != dev or not pages.is_contiguous():
+        _refuse(f, "table must have a row and row0 an entry per sequence (row0: one more), pages be on the same GPU")
+    rows = dllm_batch_rows(R, B, page, n_pages, ld, shared_len, max_rows, max_len, table.data_ptr(), row0.data_ptr(),
+                           pos.data_ptr(), slot.data_ptr(), length.data_ptr(), _ptr(lim))
+    sel = keep = None
+    if logits is not None:
+        a, keep = _select_args(f, logits, out_id, out_conf, stream=stream, **(control or {}))
+        sel = ctypes.byref(a)
+    _check(lib().dllm_batch_step(model, pages.data_ptr(), pages.numel() * pages.element_size(), ctypes.byref(rows),
+                                 tok.data_ptr(), _ptr(mask), sel, _ptr(out_id), _ptr(out_conf), _stream(stream)), f)
     del keep
 
 

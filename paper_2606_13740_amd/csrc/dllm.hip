@@ -19,6 +19,7 @@
 
 #include "../../include/dllm.h"
 #include "attention.hpp"
+#include "batch_step.hpp"
 #include "common.hpp"
 #include "gemm.hpp"
 #include "gemm_tiled.hpp"
@@ -85,6 +86,7 @@ struct Workspace {
     int* oid = nullptr;      // [rows] argmax ids of a merged pass
     float* oconf = nullptr;  // [rows] confidences of a merged pass
     uint8_t* need = nullptr; // [rows] LM-head row flags of a merged pass
+    float* qkv = nullptr;    // [rows][packed Q/K/V rows] where Q/K/V are finished outside the GEMM (else nullptr)
 };
 
 constexpr int MAX_SPLIT = 16;
@@ -110,6 +112,10 @@ struct dllm_model {
     uint16_t* qpool = nullptr;  // Q4_0 scales
     float* gpool = nullptr;  // norm gains
     float* bpool = nullptr;  // Q/K/V biases
+    float* hgpool = nullptr; // gains of the heads' norm [layer][2][head_dim], or nullptr (dllm_model_set_qk_norm)
+    bool rows_qkv = false;   // the workspace holds Q/K/V rows (heads' norm, batch steps)
+    void* attn_ws = nullptr; // workspace of the paged attention (batch steps)
+    size_t attn_ws_bytes = 0;
     Workspace ws;
     int n_lm_wg = 1;
     // probe
@@ -387,7 +393,7 @@ int launch_gemm(const Decomp& dc, int M, int MT, const GemmArgs& g0, const Epi& 
     if constexpr (WT != WT_F32 && KIND != G_LM) {
         if (dc.tiled()) {
             const int m_tiles = ceil_div(M, 16);
-            if constexpr (KIND == G_QKV) {
+            if constexpr (KIND == G_QKV && !std::is_same<Epi, EpiPartial>::value) {
                 if (dc.ks > 1) {
                     // K slices into partial sums, then split_epilogue_kernel sums them and
                     // runs the QKV epilogue (the bias goes in once, after the sum)
@@ -488,9 +494,11 @@ size_t part_floats_for(const dllm_model* m, int rows, int wrows) {
 int ensure_ws(dllm_model* m, int rows_needed) {
     const dllm_config& c = m->cfg;
     const int rows = (int)round_up(std::max(rows_needed, 1), 64);
-    if (m->ws.rows >= rows && m->ws.block) return DLLM_OK;
+    if (m->ws.rows >= rows && m->ws.block && (m->ws.qkv || !m->rows_qkv)) return DLLM_OK;
     HIP_TRY(hipDeviceSynchronize());
+    const int had = m->ws.rows;
     free_ws(m->ws);
+    if (had > rows) return ensure_ws(m, had);     // grown for the Q/K/V rows only: never smaller than before
     const int wrows = (int)round_up(c.max_window, 64);
     const size_t part_floats = part_floats_for(m, rows, wrows);
     const size_t bytes = ws_carve(m, rows, wrows, part_floats, nullptr, nullptr);
@@ -543,6 +551,7 @@ size_t ws_carve(const dllm_model* m, int rows, int wrows, size_t part_floats, ch
     take(v.oid, (size_t)rows * 4);
     take(v.oconf, (size_t)rows * 4);
     take(v.need, (size_t)rows);
+    if (m->rows_qkv) take(v.qkv, (size_t)rows * m->layers[0].qkv.n_tiles * 16 * 4);
     return off;
 }
 
@@ -628,6 +637,8 @@ struct FwdArgs {
     int replay = -1;          // >= 0: only launch this kernel class, n_replay times (timing)
     int n_replay = 0;
     Workspace* ws = nullptr;  // a caller-provided workspace (no growth), else the model's
+    const dllm_batch_rows* batch = nullptr;   // rows of several sequences over a paged cache
+    void* pages = nullptr;                    // that cache
 };
 
 // O / down projection: split-K GEMM into partials, then the reduction that adds
@@ -688,6 +699,56 @@ void fold_norm(GemmArgs& g, const dllm_model* m, const Workspace& w, int nssq) {
     g.eps = m->cfg.eps;
 }
 
+// QKV projection into rows, finished by a kernel of its own: the norm of every head (models that have
+// one) and the paged cache of a batch step, which the GEMM's epilogue has neither of.  g: the GEMM's
+// operands, with the folded RMSNorm if any.
+template <int WT, bool XF32>
+int qkv_rows(dllm_model* m, Workspace& w, int l, GemmArgs g, const Decomp& dc, int M, int MT, int gy, QkvRows r,
+             hipStream_t s) {
+    const dllm_config& c = m->cfg;
+    const PackedW& W = m->layers[l].qkv;
+    const int N = W.n_tiles * 16, m_tiles = ceil_div(M, 16);
+    if (w.qkv == nullptr) return fail(DLLM_E_INVAL, "internal: no Q/K/V rows in the workspace");
+    r.P = w.qkv; r.ks = 1; r.slice = 0; r.ldn = N; r.bias = nullptr;
+    if constexpr (WT != WT_F32) {
+        if (dc.tiled() && dc.ks > 1) {            // K slices: summed (and the bias added) by the finishing kernel
+            const int rows = m_tiles * 16;
+            if ((size_t)dc.ks * rows * N > w.part_floats) return fail(DLLM_E_INVAL, "internal: split-K buffer too small");
+            g.tpg = dc.tpg;
+            r.P = w.part; r.ks = dc.ks; r.slice = (size_t)rows * N; r.bias = g.bias;
+            g.bias = nullptr;
+            if (int rc = launch_tiled<WT>(dc, g, EpiPartial{w.part, N, rows}, m_tiles, s)) return rc;
+        }
+    }
+    if (r.ks == 1)
+        if (int rc = launch_gemm<WT, G_QKV>(dc, M, MT, g, EpiPartial{w.qkv, N, w.rows}, gy, s)) return rc;
+    r.M = M; r.H = c.n_heads; r.Hk = m->Hkv; r.eps = c.eps; r.rope = m->rope; r.max_pos = c.max_pos;
+    if (m->hgpool) {
+        r.gq = m->hgpool + (size_t)(2 * l) * c.head_dim;
+        r.gk = r.gq + c.head_dim;
+    }
+    const int qk_wgs = ceil_div((long)M * (r.H + r.Hk), 256 / (c.head_dim / 16));
+    const dim3 grid(qk_wgs + ceil_div((long)M * r.Hk * c.head_dim, 256));
+    if (c.head_dim == 128) hipLaunchKernelGGL((qkv_rows_kernel<XF32, 128>), grid, dim3(256), 0, s, r, qk_wgs);
+    else if (c.head_dim == 64) hipLaunchKernelGGL((qkv_rows_kernel<XF32, 64>), grid, dim3(256), 0, s, r, qk_wgs);
+    else hipLaunchKernelGGL((qkv_rows_kernel<XF32, 32>), grid, dim3(256), 0, s, r, qk_wgs);
+    return DLLM_OK;
+}
+
+// Arguments of a batch step's attention; q and out are the caller's to set.
+dllm_attn_args batch_attn_args(const dllm_model* m, const dllm_batch_rows* b) {
+    dllm_attn_args g{};
+    g.dtype = m->xf32 ? DLLM_F32 : DLLM_F16;
+    g.n_rows = b->n_rows; g.n_seqs = b->n_seqs; g.n_heads = m->cfg.n_heads; g.n_kv_heads = m->Hkv;
+    g.head_dim = m->cfg.head_dim; g.page = b->page; g.n_pages = b->n_pages; g.table_ld = b->table_ld;
+    g.shared_len = b->shared_len; g.max_rows = b->max_rows; g.max_len = b->max_len;
+    g.scale = 1.0f / sqrtf((float)m->cfg.head_dim);
+    g.ld_q = g.ld_out = m->cfg.d_model;
+    g.d_table = b->d_table; g.d_row0 = b->d_row0; g.d_len = b->d_len; g.d_lim = b->d_lim;
+    g.d_ws = m->attn_ws; g.ws_bytes = m->attn_ws_bytes;
+    return g;
+}
+
 template <int WT, typename AT>   // AT: element type of the embedding and the cache planes
 int forward_t(dllm_model* m, dllm_kv* kv, const FwdArgs& a, hipStream_t s) {
     constexpr bool XF32 = (WT == WT_F32);
@@ -739,14 +800,14 @@ int forward_t(dllm_model* m, dllm_kv* kv, const FwdArgs& a, hipStream_t s) {
                            a.n_sel);
 
     // Cache per layer: [K][V^T], fp32 or fp16; Hkv heads.  Q: fp32, or fp16 hi / lo planes.
-    const size_t plane = (size_t)m->Hkv * kv->Cs * Dh;
+    const size_t plane = a.batch ? (size_t)a.batch->n_pages * a.batch->page * m->Hkv * Dh : (size_t)m->Hkv * kv->Cs * Dh;
     const size_t layer_elems = 2 * plane;
     const size_t q_plane = XF32 ? 0 : (size_t)w.rows * d;
     const int n_iter = a.replay < 0 ? a.n_layers : (a.replay == DLLM_K_LMHEAD ? 0 : a.n_replay);
     for (int it = 0; it < n_iter; ++it) {
         const int l = it % c.n_layers;
         LayerW& L = m->layers[l];
-        AT* Kc = (AT*)kv->buf + (size_t)l * layer_elems;
+        AT* Kc = (AT*)(a.batch ? a.pages : kv->buf) + (size_t)l * layer_elems;
         AT* Vt = Kc + plane;
 
         // RMSNorm + QKV + RoPE -> Q buffer and K/V cache rows
@@ -754,14 +815,36 @@ int forward_t(dllm_model* m, dllm_kv* kv, const FwdArgs& a, hipStream_t s) {
             GemmArgs g{L.qkv.w, L.qkv.scale, w.xg, L.qkv.KCw, L.qkv.KCw * WTraits<WT>::XPER, L.qkv.n_tiles, L.bqkv};
             g.qs = L.qkv.qs;
             if (fused && (l == 0 || fuse_down)) fold_norm(g, m, w, nssq_qkv(l));
-            EpiQKV<XF32> e{d, m->dkv, Dh, a.M, a.pos_base, a.pos, m->rope, (AT*)w.q, q_plane, Kc, Vt, kv->Cs};
+            const Decomp dc = decomp(G_QKV, WT, L.qkv, a.M, MT, gy, d);
             ProbeScope ps(m, DLLM_K_QKV, s);
-            if ((rc = launch_gemm<WT, G_QKV>(decomp(G_QKV, WT, L.qkv, a.M, MT, gy, d), a.M, MT, g, e, gy, s,
-                                             w.part, w.part_floats)))
-                return rc;
+            if (a.batch || m->hgpool) {
+                QkvRows r{};
+                r.pos_base = a.pos_base; r.pos = a.pos; r.q = w.q; r.K = Kc; r.V = Vt;
+                if (a.batch) {
+                    r.slot = a.batch->d_slot;
+                    r.page_len = a.batch->page; r.page_shift = __builtin_ctz(a.batch->page); r.n_pages = a.batch->n_pages;
+                } else {
+                    r.page_len = kv->Cs;
+                    r.q_plane = q_plane;
+                }
+                if ((rc = qkv_rows<WT, XF32>(m, w, l, g, dc, a.M, MT, gy, r, s))) return rc;
+            } else {
+                EpiQKV<XF32> e{d, m->dkv, Dh, a.M, a.pos_base, a.pos, m->rope, (AT*)w.q, q_plane, Kc, Vt, kv->Cs};
+                if ((rc = launch_gemm<WT, G_QKV>(dc, a.M, MT, g, e, gy, s, w.part, w.part_floats))) return rc;
+            }
+        }
+        // attention of a batch's rows over their sequences' pages, into the O projection's operand
+        if (a.batch) {
+            dllm_attn_args g = batch_attn_args(m, a.batch);
+            g.d_q = w.q; g.d_k_pages = Kc; g.d_v_pages = Vt;
+            g.d_out = w.qkv;                       // the Q/K/V rows are spent
+            ProbeScope ps(m, DLLM_K_ATTN, s);
+            if ((rc = dllm_attention_paged(&g, (dllm_stream)s))) return rc;
+            hipLaunchKernelGGL(attn_operand_kernel<XF32>, dim3(Mc), dim3(256), 0, s, (const void*)w.qkv, a.M, d, w.of,
+                               m->KCx_d);
         }
         // attention over [0, T) (+ split merge)
-        if (run(DLLM_K_ATTN)) {
+        if (!a.batch && run(DLLM_K_ATTN)) {
             AttnArgs at{};
             at.q = w.q; at.q_plane = q_plane; at.K = Kc; at.Vt = Vt; at.Cs = kv->Cs; at.H = H;
             at.G = H / m->Hkv; at.T = a.T; at.lim = a.lim; at.M = a.M; at.rows = Mc;
@@ -1070,13 +1153,103 @@ int dllm_model_create(const dllm_config* cfg, const dllm_weights* w, dllm_stream
 int dllm_model_destroy(dllm_model* m) {
     if (!m) return DLLM_OK;
     free_ws(m->ws);
-    void* ptrs[] = {m->wpool, m->spool, m->qpool, m->gpool, m->bpool, m->embed, m->rope};
+    void* ptrs[] = {m->wpool, m->spool, m->qpool, m->gpool, m->bpool, m->embed, m->rope, m->hgpool, m->attn_ws};
     for (void* p : ptrs)
         if (p) (void)hipFree(p);
     for (auto e : m->ev_b) (void)hipEventDestroy(e);
     for (auto e : m->ev_e) (void)hipEventDestroy(e);
     delete m;
     return DLLM_OK;
+}
+
+int dllm_model_set_qk_norm(dllm_model* m, const float* const* d_q_gain, const float* const* d_k_gain, dllm_stream stream) {
+    if (!m || !d_q_gain || !d_k_gain) return fail(DLLM_E_INVAL, "NULL argument");
+    const int L = m->cfg.n_layers, D = m->cfg.head_dim;
+    for (int l = 0; l < L; ++l)
+        if (!d_q_gain[l] || !d_k_gain[l]) return fail(DLLM_E_INVAL, "NULL gain pointer in layer " + std::to_string(l));
+    float* pool = m->hgpool;
+    if (!pool) {
+        if (int rc = alloc_zero((void**)&pool, (size_t)2 * L * D * 4)) return rc;
+    }
+    hipStream_t s = (hipStream_t)stream;
+    hipError_t e = hipSuccess;
+    for (int l = 0; l < L && e == hipSuccess; ++l) {
+        e = hipMemcpyAsync(pool + (size_t)(2 * l) * D, d_q_gain[l], D * 4, hipMemcpyDeviceToDevice, s);
+        if (e == hipSuccess) e = hipMemcpyAsync(pool + (size_t)(2 * l + 1) * D, d_k_gain[l], D * 4, hipMemcpyDeviceToDevice, s);
+    }
+    if (e == hipSuccess) e = hipStreamSynchronize(s);
+    if (e != hipSuccess) {
+        if (pool != m->hgpool) (void)hipFree(pool);
+        return fail(DLLM_E_HIP, std::string("copying the heads' gains failed: ") + hipGetErrorString(e));
+    }
+    m->hgpool = pool;
+    m->rows_qkv = true;
+    return ensure_ws(m, m->ws.rows);
+}
+
+int dllm_batch_bytes(const dllm_model* m, int32_t n_pages, int32_t page, size_t* bytes) {
+    if (!m || !bytes) return fail(DLLM_E_INVAL, "NULL argument");
+    if (page != 32 && page != 64 && page != 128 && page != 256) return fail(DLLM_E_INVAL, "page must be 32, 64, 128 or 256");
+    if (n_pages < 1 || (long)n_pages * page >= (1l << 31)) return fail(DLLM_E_INVAL, "n_pages must be >= 1 and n_pages * page < 2^31");
+    *bytes = (size_t)m->cfg.n_layers * 2 * n_pages * page * m->Hkv * m->cfg.head_dim * m->kv_elem;
+    return DLLM_OK;
+}
+
+int dllm_batch_step(dllm_model* m, void* d_pages, size_t bytes, const dllm_batch_rows* b, const int32_t* d_tok,
+                    const uint8_t* d_mask, const dllm_select_args* sel, int32_t* d_out_id, float* d_out_conf,
+                    dllm_stream stream) {
+    if (!m || !d_pages || !b || !d_tok) return fail(DLLM_E_INVAL, "NULL argument");
+    size_t need = 0;
+    int rc = dllm_batch_bytes(m, b->n_pages, b->page, &need);
+    if (rc) return rc;
+    if (bytes < need) return fail(DLLM_E_CAPACITY, "pages smaller than dllm_batch_bytes()");
+    if (((uintptr_t)d_pages & 15) != 0) return fail(DLLM_E_INVAL, "pages must be 16-byte aligned");
+    if (!b->d_table || !b->d_row0 || !b->d_pos || !b->d_slot || !b->d_len) return fail(DLLM_E_INVAL, "rows: NULL array");
+    if (b->n_rows < 1) return fail(DLLM_E_INVAL, "n_rows must be >= 1");
+    if (b->max_len > m->cfg.max_pos) return fail(DLLM_E_CAPACITY, "max_len exceeds the model's max_pos");
+    if ((d_out_id == nullptr) != (d_out_conf == nullptr))
+        return fail(DLLM_E_INVAL, "out_id and out_conf must both be set or both be NULL");
+    if (d_out_id && b->n_rows > m->cfg.max_window)
+        return fail(DLLM_E_INVAL, "n_rows must be <= max_window for a step with outputs");
+    dllm_select_args sa{};
+    if (sel) {
+        if (!d_out_id) return fail(DLLM_E_INVAL, "a selection needs out_id and out_conf");
+        sa = *sel;
+        if (sa.dtype != DLLM_F32 || sa.n_rows != b->n_rows || sa.vocab != m->cfg.vocab || sa.ld != sa.vocab)
+            return fail(DLLM_E_INVAL, "selection: logits must be contiguous fp32 [n_rows][vocab]");
+        if (sa.mask_id != m->cfg.mask_id) return fail(DLLM_E_INVAL, "selection: mask_id must be the model's");
+        sa.d_out_id = d_out_id;
+        sa.d_out_conf = d_out_conf;
+        // (checked before any launch: a call without rows validates and queues nothing)
+        dllm_select_args probe = sa;
+        size_t ws = 0;
+        if ((rc = dllm_select_ws(&sa, &ws))) return rc;
+        if (sa.ws_bytes < ws) return fail(DLLM_E_CAPACITY, "selection: workspace smaller than dllm_select_ws()");
+        if (ws > 0 && !sa.d_ws) return fail(DLLM_E_INVAL, "selection: NULL workspace");
+        if (sa.d_allow && !sa.d_allow_row && sa.n_allow < sa.n_rows) return fail(DLLM_E_INVAL, "selection: a mask per row needs n_allow >= n_rows");
+        probe.n_rows = 0;
+        if ((rc = dllm_select(&probe, stream))) return rc;
+    }
+    dllm_attn_args ga = batch_attn_args(m, b);
+    size_t aws = 0;
+    if ((rc = dllm_attention_paged_ws(&ga, &aws))) return rc;
+    m->rows_qkv = true;
+    if ((rc = ensure_ws(m, b->n_rows))) return rc;
+    if (aws > m->attn_ws_bytes) {
+        HIP_TRY(hipDeviceSynchronize());
+        if (m->attn_ws) (void)hipFree(m->attn_ws);
+        m->attn_ws = nullptr;
+        m->attn_ws_bytes = 0;
+        if (hipMalloc(&m->attn_ws, aws) != hipSuccess)
+            return fail(DLLM_E_NOMEM, "device allocation of " + std::to_string(aws) + " bytes failed");
+        m->attn_ws_bytes = aws;
+    }
+    FwdArgs a{};
+    a.M = b->n_rows; a.tok = d_tok; a.mask = d_mask; a.pos = b->d_pos; a.n_layers = m->cfg.n_layers;
+    a.lm = d_out_id != nullptr; a.out_id = d_out_id; a.out_conf = d_out_conf; a.batch = b; a.pages = d_pages;
+    if (sel) a.logits = (float*)sa.d_logits;
+    if ((rc = forward(m, nullptr, a, (hipStream_t)stream))) return rc;
+    return sel ? dllm_select(&sa, stream) : DLLM_OK;
 }
 
 static int cs_of(int capacity) { return (int)round_up(capacity, 32); }

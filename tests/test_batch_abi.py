@@ -126,7 +126,7 @@ def test_argument_structs_have_the_headers_layout(dl, tmp_path):
         pytest.skip("no C compiler")
     root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
     lines, want = [], []
-    for name in ("dllm_qk_args", "dllm_attn_args", "dllm_select_args"):
+    for name in ("dllm_qk_args", "dllm_attn_args", "dllm_select_args", "dllm_batch_rows"):
         cls = getattr(dl, name)
         lines.append(f'printf("%zu\\n", sizeof({name}));')
         want.append(ctypes.sizeof(cls))
@@ -137,3 +137,13 @@ def test_argument_structs_have_the_headers_layout(dl, tmp_path):
     src.write_text('#include <stddef.h>\n#include <stdio.h>\n#include "dllm.h"\nint main(void) {\n' + "\n".join(lines) + "\nreturn 0;\n}\n")
     subprocess.check_call([cc, "-I", os.path.join(root, "include"), str(src), "-o", str(tmp_path / "layout")])
     assert [int(x) for x in subprocess.check_output([str(tmp_path / "layout")]).split()] == want
+
+
+def test_batch_step_refuses_null(dl):
+    L = dl.lib()
+    n = ctypes.c_size_t()
+    rows = dl.dllm_batch_rows()
+    ptrs = (ctypes.c_void_p * 1)(P)
+    assert L.dllm_batch_bytes(None, 8, 32, ctypes.byref(n)) == dl.DLLM_E_INVAL
+    assert L.dllm_batch_step(None, P, 1 << 40, ctypes.byref(rows), P, None, None, None, None, None) == dl.DLLM_E_INVAL
+    assert L.dllm_model_set_qk_norm(None, ptrs, ptrs, None) == dl.DLLM_E_INVAL
