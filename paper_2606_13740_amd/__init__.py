@@ -357,9 +357,13 @@ def _gpu(func: str, ref) -> int:
     """The current GPU's index, which ref must be on."""
     if _Types.torch is None:
         _Types.load()
-    if not ref.is_cuda or ref.get_device() != _Types.device():
+    dev = ref.get_device()
+    if dev < 0 or dev != _Types.device():
         _refuse(func, "tensors must be on the current GPU")
-    return ref.get_device()
+    return dev
+
+
+# The checks below run for every call, beside launches of 3 us: they test first and look for names only to refuse.
 
 
 def _plain(func: str, dev: int, dtype, tensors, names: str):
@@ -377,35 +381,36 @@ def _at_least(func: str, n: int, tensors, names: str):
             _refuse(func, f"{bad} must have at least {n} entries")
 
 
-def _row_stride(func: str, name: str, t, ref, dev: int, heads: int, dim: int) -> int:
+def _row_stride(func: str, name: str, t, dtype, dev: int, rows: int, heads: int, dim: int) -> int:
     """Row stride of a [rows][heads * dim] or [rows][heads][dim] tensor whose rows are whole; checks its shape."""
     sh, st = t.shape, t.stride()
-    if t.dtype is not ref.dtype or t.get_device() != dev:
-        _refuse(func, f"{name} must have q's type and device")
     if len(sh) == 2:
         ok = sh[1] == heads * dim and st[1] == 1
     else:
         ok = len(sh) == 3 and sh[1] == heads and sh[2] == dim and st[2] == 1 and (heads == 1 or st[1] == dim)
-    if not ok or sh[0] != ref.shape[0]:
-        _refuse(func, f"{name} must be [rows][{heads}][{dim}] with whole rows")
-    return st[0] if sh[0] > 1 else heads * dim
+    if not ok or sh[0] != rows or t.dtype is not dtype or t.get_device() != dev:
+        _refuse(func, f"{name} must be [rows][{heads}][{dim}] with whole rows, of q's type and device")
+    return st[0] if rows > 1 else heads * dim
 
 
 def dllm_batch_plan(length, new, owned, owned_out, table, free, n_free, n_free_out, page: int, shared_pages: int, row0,
                     pos, slot, seq, lim, status, stream=None):
     """The row arrays' common length is the plan's max_rows; free has an entry per page of the pool."""
-    f, B, ld, R = "dllm_batch_plan", length.numel(), table.shape[-1], pos.numel()
+    f, B, ld, R, N = "dllm_batch_plan", length.numel(), table.shape[-1], pos.numel(), free.numel()
     _plain(f, _gpu(f, length), _Types.i32, (length, new, owned, owned_out, table, free, n_free, n_free_out, row0, pos, slot,
                                             seq, lim, status),
            "length new owned owned_out table free n_free n_free_out row0 pos slot seq lim status")
-    _at_least(f, B, (new, owned, owned_out), "new owned owned_out")
-    _at_least(f, R, (slot, seq, lim), "slot seq lim")
-    if table.numel() < B * ld or row0.numel() < B + 1 or status.numel() < 3 or not n_free.numel() or not n_free_out.numel():
-        _refuse(f, "table must have a row and row0 an entry per sequence (row0: one more), status 3 entries, n_free 1")
-    _check(lib().dllm_batch_plan(length.data_ptr(), new.data_ptr(), owned.data_ptr(), owned_out.data_ptr(), B,
-                                 table.data_ptr(), ld, free.data_ptr(), n_free.data_ptr(), n_free_out.data_ptr(),
-                                 free.numel(), page, shared_pages, R, row0.data_ptr(), pos.data_ptr(), slot.data_ptr(),
-                                 seq.data_ptr(), lim.data_ptr(), status.data_ptr(), _stream(stream)), f)
+    if (new.numel() < B or owned.numel() < B or owned_out.numel() < B or slot.numel() < R or seq.numel() < R or
+            lim.numel() < R or table.numel() < B * ld or row0.numel() <= B or status.numel() < 3 or not n_free.numel() or
+            not n_free_out.numel()):
+        _refuse(f, "new, owned and owned_out must have an entry and table a row per sequence (row0: one entry more), slot, seq "
+                   "and lim as many as pos, status 3, n_free 1")
+    rc = lib().dllm_batch_plan(length.data_ptr(), new.data_ptr(), owned.data_ptr(), owned_out.data_ptr(), B,
+                               table.data_ptr(), ld, free.data_ptr(), n_free.data_ptr(), n_free_out.data_ptr(), N, page,
+                               shared_pages, R, row0.data_ptr(), pos.data_ptr(), slot.data_ptr(), seq.data_ptr(),
+                               lim.data_ptr(), status.data_ptr(), _stream(stream))
+    if rc:
+        _check(rc, f)
 
 
 def dllm_rope_table(table, head_dim: int, rope_base: float, stream=None):
@@ -417,43 +422,40 @@ def dllm_rope_table(table, head_dim: int, rope_base: float, stream=None):
     _check(lib().dllm_rope_table(table.data_ptr(), table.numel() // head_dim, head_dim, rope_base, _stream(stream)), f)
 
 
-def _pages(f: str, q, dev: int, k_pages, v_pages):
-    """(n_pages, kv heads, page, head_dim) of a K plane [n_pages][kv][page][dim] and a V^T plane [n_pages][kv][dim][page]."""
-    _plain(f, dev, q.dtype, (k_pages, v_pages), "k_pages v_pages")
-    n, kv, page, dim = k_pages.shape
-    if v_pages.shape != (n, kv, dim, page):
-        _refuse(f, "v_pages must be [n_pages][kv_heads][head_dim][page]")
-    return n, kv, page, dim
-
-
 def dllm_qk_norm_rope(q, k, v, rope, pos, slot, q_out, k_pages, v_pages, q_gain=None, k_gain=None, eps: float = 1e-6,
                       stream=None):
-    """q, k, v: [rows][heads][dim] or [rows][heads * dim], rows may be strided (slices of one projection's output)."""
-    f = "dllm_qk_norm_rope"
-    dev = _gpu(f, q)
-    n_pages, kv, page, dim = _pages(f, q, dev, k_pages, v_pages)
-    T, qs = q.shape[0], q_out.shape
+    """q, k, v: [rows][heads][dim] or [rows][heads * dim], rows may be strided (slices of one projection's output);
+    k_pages [n_pages][kv_heads][page][dim], v_pages [n_pages][kv_heads][dim][page]."""
+    f, dt = "dllm_qk_norm_rope", q.dtype
+    dev, T, qs = _gpu(f, q), q.shape[0], q_out.shape
+    n_pages, kv, page, dim = k_pages.shape
     H = qs[1] if len(qs) == 3 else qs[1] // dim
-    ld_q, ld_k = _row_stride(f, "q", q, q, dev, H, dim), _row_stride(f, "k", k, q, dev, kv, dim)
-    ld_v = _row_stride(f, "v", v, q, dev, kv, dim)
-    _plain(f, dev, q.dtype, (q_out,), "q_out")
+    ld_q, ld_k = _row_stride(f, "q", q, dt, dev, T, H, dim), _row_stride(f, "k", k, dt, dev, T, kv, dim)
+    ld_v = _row_stride(f, "v", v, dt, dev, T, kv, dim)
+    _plain(f, dev, dt, (k_pages, v_pages, q_out), "k_pages v_pages q_out")
     _plain(f, dev, _Types.f32, (rope, q_gain, k_gain), "rope q_gain k_gain")
     _plain(f, dev, _Types.i32, (pos, slot), "pos slot")
-    _at_least(f, T, (pos, slot), "pos slot")
-    _at_least(f, dim, (q_gain, k_gain), "q_gain k_gain")
-    if qs[0] < T or q_out.numel() != qs[0] * H * dim:
-        _refuse(f, "q_out must be [rows][heads][dim]")
-    a = dllm_qk_args(_Types.elem.get(q.dtype, -1), T, H, kv, dim, page, n_pages, rope.numel() // dim, eps, q.data_ptr(),
-                     k.data_ptr(), v.data_ptr(), ld_q, ld_k, ld_v, _ptr(q_gain), _ptr(k_gain), rope.data_ptr(),
-                     pos.data_ptr(), slot.data_ptr(), q_out.data_ptr(), k_pages.data_ptr(), v_pages.data_ptr())
-    _check(lib().dllm_qk_norm_rope(ctypes.byref(a), _stream(stream)), f)
+    if (v_pages.shape != (n_pages, kv, dim, page) or pos.numel() < T or slot.numel() < T or qs[0] < T or
+            q_out.numel() != qs[0] * H * dim or (q_gain is not None and q_gain.numel() < dim) or
+            (k_gain is not None and k_gain.numel() < dim)):
+        _refuse(f, "v_pages must be [n_pages][kv_heads][head_dim][page], q_out [rows][heads][dim], pos and slot have an entry "
+                   "per row, gains head_dim")
+    a = dllm_qk_args(_Types.elem.get(dt, -1), T, H, kv, dim, page, n_pages, rope.numel() // dim, eps, q.data_ptr(),
+                     k.data_ptr(), v.data_ptr(), ld_q, ld_k, ld_v, None if q_gain is None else q_gain.data_ptr(),
+                     None if k_gain is None else k_gain.data_ptr(), rope.data_ptr(), pos.data_ptr(), slot.data_ptr(),
+                     q_out.data_ptr(), k_pages.data_ptr(), v_pages.data_ptr())
+    rc = lib().dllm_qk_norm_rope(ctypes.byref(a), _stream(stream))
+    if rc:
+        _check(rc, f)
 
 
 def _workspace(query, a, ws, stream, dev: int, f: str):
     """Sets a's workspace: `ws`, or memory of the call's own (on the current stream; freed once the call has been made)."""
     if ws is None:
         n = _sz()
-        _check(query(ctypes.byref(a), ctypes.byref(n)), f + "_ws")
+        rc = query(ctypes.byref(a), ctypes.byref(n))
+        if rc:
+            _check(rc, f + "_ws")
         if not n.value:
             return None
         if stream is not None:
@@ -469,52 +471,85 @@ def _workspace(query, a, ws, stream, dev: int, f: str):
 
 def dllm_attention_paged(q, k_pages, v_pages, table, row0, length, out, max_rows: int, max_len: int,
                          shared_len: int = 0, lim=None, scale: Optional[float] = None, ws=None, stream=None):
-    """q, out: [rows][heads][dim] or [rows][heads * dim], rows may be strided; scale: 1 / sqrt(dim) if None."""
-    f = "dllm_attention_paged"
-    dev = _gpu(f, q)
-    n_pages, kv, page, dim = _pages(f, q, dev, k_pages, v_pages)
-    sh = q.shape
+    """q, out: [rows][heads][dim] or [rows][heads * dim], rows may be strided; scale: 1 / sqrt(dim) if None;
+    k_pages [n_pages][kv_heads][page][dim], v_pages [n_pages][kv_heads][dim][page]."""
+    f, dt, sh = "dllm_attention_paged", q.dtype, q.shape
+    dev, T, B, ld = _gpu(f, q), sh[0], length.numel(), table.shape[-1]
+    n_pages, kv, page, dim = k_pages.shape
     H = sh[1] if len(sh) == 3 else sh[1] // dim
-    ld_q, ld_out = _row_stride(f, "q", q, q, dev, H, dim), _row_stride(f, "out", out, q, dev, H, dim)
-    B, ld = length.numel(), table.shape[-1]
+    ld_q, ld_out = _row_stride(f, "q", q, dt, dev, T, H, dim), _row_stride(f, "out", out, dt, dev, T, H, dim)
+    _plain(f, dev, dt, (k_pages, v_pages), "k_pages v_pages")
     _plain(f, dev, _Types.i32, (table, row0, length, lim), "table row0 length lim")
-    if table.numel() < B * ld or row0.numel() < B + 1 or (lim is not None and lim.numel() < sh[0]):
-        _refuse(f, "table must have a row and row0 an entry per sequence (row0: one more), lim an entry per row")
-    a = dllm_attn_args(_Types.elem.get(q.dtype, -1), sh[0], B, H, kv, dim, page, n_pages, ld, shared_len, max_rows, max_len,
+    if (v_pages.shape != (n_pages, kv, dim, page) or table.numel() < B * ld or row0.numel() <= B or
+            (lim is not None and lim.numel() < T)):
+        _refuse(f, "v_pages must be [n_pages][kv_heads][head_dim][page], table must have a row and row0 an entry per sequence "
+                   "(row0: one more), lim an entry per row")
+    a = dllm_attn_args(_Types.elem.get(dt, -1), T, B, H, kv, dim, page, n_pages, ld, shared_len, max_rows, max_len,
                        dim ** -0.5 if scale is None else scale, q.data_ptr(), ld_q, k_pages.data_ptr(),
-                       v_pages.data_ptr(), table.data_ptr(), row0.data_ptr(), length.data_ptr(), _ptr(lim),
-                       out.data_ptr(), ld_out)
-    keep = _workspace(lib().dllm_attention_paged_ws, a, ws, stream, dev, f)
-    _check(lib().dllm_attention_paged(ctypes.byref(a), _stream(stream)), f)
+                       v_pages.data_ptr(), table.data_ptr(), row0.data_ptr(), length.data_ptr(),
+                       None if lim is None else lim.data_ptr(), out.data_ptr(), ld_out)
+    L = lib()
+    keep = _workspace(L.dllm_attention_paged_ws, a, ws, stream, dev, f)
+    rc = L.dllm_attention_paged(ctypes.byref(a), _stream(stream))
+    if rc:
+        _check(rc, f)
     del keep
 
 
-def _select_args(f, logits, out_id, out_conf, mask_id: int = -1, row0=None, hist=None, hist0=None, n_prompt=None,
-                 repetition=None, presence=None, frequency=None, bias_id=None, bias=None, bias0=None, allow=None,
-                 allow_row=None, out_logits=None, ws=None, stream=None):
+def _select_args(f, logits, out_id, out_conf, mask_id=-1, row0=None, hist=None, hist0=None, n_prompt=None, repetition=None,
+                 presence=None, frequency=None, bias_id=None, bias=None, bias0=None, allow=None, allow_row=None,
+                 out_logits=None, ws=None, stream=None):
     """(struct, what keeps its workspace alive) of a selection."""
-    dev = _gpu(f, logits)
-    T, V = logits.shape
+    dev, (T, V), dt = _gpu(f, logits), logits.shape, logits.dtype
     B = row0.numel() - 1 if row0 is not None else 1
-    _plain(f, dev, _Types.i32, (out_id, row0, hist, hist0, n_prompt, bias_id, bias0, allow, allow_row),
-           "out_id row0 hist hist0 n_prompt bias_id bias0 allow allow_row")
-    _plain(f, dev, _Types.f32, (out_conf, repetition, presence, frequency, bias), "out_conf repetition presence frequency bias")
-    _at_least(f, T, (out_id, out_conf, allow_row), "out_id out_conf allow_row")
-    _at_least(f, B, (n_prompt, repetition, presence, frequency), "n_prompt repetition presence frequency")
-    _at_least(f, B + 1, (hist0, bias0), "hist0 bias0")
-    st, ld_out = logits.stride(), 0
+    a = dllm_select_args(_Types.elem.get(dt, -1), T, V, mask_id, B, logits.data_ptr(), logits.stride(0) if T > 1 else V)
+    i32, f32 = [out_id], [out_conf]
+    ok = out_id.numel() >= T and out_conf.numel() >= T and (V == 1 or logits.stride(1) == 1)
+    if row0 is not None:
+        i32.append(row0)
+        a.d_row0 = row0.data_ptr()
+    if hist is not None:
+        i32 += [hist, hist0]
+        ok = ok and hist0.numel() > B
+        a.d_hist, a.d_hist0 = hist.data_ptr(), hist0.data_ptr()
+    if n_prompt is not None:
+        i32.append(n_prompt)
+        ok = ok and n_prompt.numel() >= B
+        a.d_n_prompt = n_prompt.data_ptr()
+    if repetition is not None:
+        f32.append(repetition)
+        a.d_repetition = repetition.data_ptr()
+    if presence is not None:
+        f32.append(presence)
+        a.d_presence = presence.data_ptr()
+    if frequency is not None:
+        f32.append(frequency)
+        a.d_frequency = frequency.data_ptr()
+    for t in f32[1:]:
+        ok = ok and t.numel() >= B
+    if bias is not None:
+        i32 += [bias_id, bias0]
+        f32.append(bias)
+        ok = ok and bias0.numel() > B and bias.numel() >= bias_id.numel()
+        a.d_bias_id, a.d_bias, a.d_bias0 = bias_id.data_ptr(), bias.data_ptr(), bias0.data_ptr()
+    if allow is not None:
+        i32.append(allow)
+        a.d_allow = allow.data_ptr()
+        a.n_allow, a.allow_ld = allow.shape
+    if allow_row is not None:
+        i32.append(allow_row)
+        ok = ok and allow_row.numel() >= T
+        a.d_allow_row = allow_row.data_ptr()
     if out_logits is not None:
-        so = out_logits.stride()
-        if out_logits.shape != logits.shape or out_logits.dtype is not logits.dtype or out_logits.get_device() != dev or (V > 1 and so[1] != 1):
-            _refuse(f, "out_logits must be of the logits' shape and type, with whole rows")
-        ld_out = so[0] if T > 1 else V
-    if V > 1 and st[1] != 1:
-        _refuse(f, "logits must have whole rows")
-    n_allow, allow_ld = allow.shape if allow is not None else (0, 0)
-    a = dllm_select_args(_Types.elem.get(logits.dtype, -1), T, V, mask_id, B, logits.data_ptr(), st[0] if T > 1 else V,
-                         _ptr(row0), _ptr(hist), _ptr(hist0), _ptr(n_prompt), _ptr(repetition), _ptr(presence),
-                         _ptr(frequency), _ptr(bias_id), _ptr(bias), _ptr(bias0), _ptr(allow), n_allow, allow_ld,
-                         _ptr(allow_row), _ptr(out_logits), ld_out, out_id.data_ptr(), out_conf.data_ptr())
+        ok = ok and (out_logits.shape == logits.shape and out_logits.dtype is dt and out_logits.get_device() == dev and
+                     (V == 1 or out_logits.stride(1) == 1))
+        a.d_out_logits, a.ld_out = out_logits.data_ptr(), out_logits.stride(0) if T > 1 else V
+    _plain(f, dev, _Types.i32, i32, "array " * len(i32))
+    _plain(f, dev, _Types.f32, f32, "array " * len(f32))
+    if not ok:
+        _refuse(f, "out_id, out_conf and allow_row must have an entry per row, n_prompt and the penalties one per sequence "
+                   "(hist0, bias0: one more), out_logits be of the logits' shape and type, rows be whole")
+    a.d_out_id, a.d_out_conf = out_id.data_ptr(), out_conf.data_ptr()
     return a, _workspace(lib().dllm_select_ws, a, ws, stream, dev, f)
 
 
@@ -523,7 +558,9 @@ def dllm_select(logits, out_id, out_conf, stream=None, **control):
     repetition, presence, frequency, bias_id, bias, bias0, allow (int32 words [masks][words]), allow_row, out_logits, ws."""
     f = "dllm_select"
     a, keep = _select_args(f, logits, out_id, out_conf, stream=stream, **control)
-    _check(lib().dllm_select(ctypes.byref(a), _stream(stream)), f)
+    rc = lib().dllm_select(ctypes.byref(a), _stream(stream))
+    if rc:
+        _check(rc, f)
     del keep
 
 

@@ -476,9 +476,10 @@ attn_paged_kernel(PagedArgs a) {
 }
 
 // Merge of the parts: o = sum_s o_s 2^(m_s - M) / sum_s l_s 2^(m_s - M).  DH / 4 lanes per
-// (row, head), four dims each.  The lanes first take a part's (m, l) each, so that all weights
-// cost one round trip, then the outputs are read eight parts at a time.  A part with an empty
-// sum wrote no output: what stands there is read and not used.
+// (row, head), four dims each.  The first eight parts' outputs are asked for beside the parts'
+// (m, l), of which the lanes take one each: one round trip for up to eight parts, one more for
+// each eight behind them.  A part with an empty sum wrote no output: what stands there is read
+// and not used.
 template <typename T, int DH>
 __global__ void __launch_bounds__(256) attn_paged_merge_kernel(PagedArgs a) {
     constexpr int LPP = DH / 4, MAXW = 2 * MAX_ATTN_SPLITS / LPP;      // weights per lane
@@ -487,12 +488,19 @@ __global__ void __launch_bounds__(256) attn_paged_merge_kernel(PagedArgs a) {
     const int row = min(R0 + pair / a.H, a.T - 1), h = pair % a.H;
     const size_t rec = (size_t)row * a.H + h, step = (size_t)a.T * a.H;
     const int np = a.ns_s + a.ns_o;
+    const float* src = a.opart + rec * DH + 4 * li;
+    float4 v[8];
+    auto load8 = [&](int s0) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] = *(const float4*)(src + (size_t)min(s0 + j, np - 1) * step * DH);
+    };
+    load8(0);
     float m[MAXW], l[MAXW], M = -INFINITY, L = 0.f;
 #pragma unroll
     for (int i = 0; i < MAXW; ++i) {
         m[i] = -INFINITY;
         l[i] = 0.f;
-        if (li + LPP * i < np) {
+        if (LPP * i < np && li + LPP * i < np) {
             const float2 ml = *(const float2*)(a.mlpart + ((li + LPP * i) * step + rec) * 2);
             m[i] = ml.x;
             l[i] = ml.y;
@@ -509,13 +517,10 @@ __global__ void __launch_bounds__(256) attn_paged_merge_kernel(PagedArgs a) {
 #pragma unroll
     for (int o = 1; o < LPP; o <<= 1) L += __shfl_xor(L, o);
     float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-    const float* src = a.opart + rec * DH + 4 * li;
 #pragma unroll
     for (int i = 0; i < MAXW; ++i) {
         for (int s0 = LPP * i; s0 < min(np, LPP * (i + 1)); s0 += 8) {
-            float4 v[8];
-#pragma unroll
-            for (int j = 0; j < 8; ++j) v[j] = *(const float4*)(src + (size_t)min(s0 + j, np - 1) * step * DH);
+            if (s0 > 0) load8(s0);
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
                 const float w = __shfl(m[i], (s0 + j) % LPP, LPP);
