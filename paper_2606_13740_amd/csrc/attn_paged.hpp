@@ -192,7 +192,7 @@ attn_paged_kernel(PagedArgs a) {
                 const int i = qw + j * QG;
                 if (KI % QG != 0 && i >= KI) break;
                 const int dim = (i * 64 + lane) / VC, pc = lane % VC;
-                const int sw = F32 ? dim & 7 : (dim >> 2) & 3;
+                const int sw = F32 ? dim & 7 : (dim >> 1) & 3;
                 buffer_to_lds16(Vp, ((dim << a.page_shift) * ES) + ((pc ^ sw) << 4), off * ES, base + KPLANE + i * 1024);
             }
         }
@@ -205,7 +205,7 @@ attn_paged_kernel(PagedArgs a) {
             const int i = qw + j * QG;
             if (KI % QG != 0 && i >= KI) break;
             const int dim = (i * 64 + lane) / VC, pc = lane % VC;
-            const int sw = F32 ? dim & 7 : (dim >> 2) & 3;
+            const int sw = F32 ? dim & 7 : (dim >> 1) & 3;
             const int key = k0 + (16 / ES) * (pc ^ sw);             // the slot's first key
             if (key + 16 / ES <= end) continue;
             u32x4_t* slot = (u32x4_t*)(base + i * 1024 + lane * 16);
@@ -362,7 +362,7 @@ attn_paged_kernel(PagedArgs a) {
 #pragma unroll
                 for (int u = 0; u < NV; ++u) {
                     const int dim = 16 * dt + r;
-                    const int sw = F32 ? dim & 7 : (dim >> 2) & 3;
+                    const int sw = F32 ? dim & 7 : (dim >> 1) & 3;
                     vf[w][dt][u] = *(const u32x4_t*)(buf + w * SBUF + KPLANE + dim * (32 * ES) + (((4 * u + g) ^ sw) << 4));
                 }
         __builtin_amdgcn_sched_barrier(0);
