@@ -17,6 +17,9 @@
 //   S^T (16 keys x 16 rows) = K tile (A) * Q^T (B),   O^T (16 dims x 16 rows) += V^T tile (A) * P^T (B).
 //   16-bit types, 32 keys a step: key tile t takes keys 8 (r / 4) + 4 t + r % 4, so that lane group g ends
 //   up with the probabilities of keys 8g .. 8g+7, which is the B operand of a 32-key product.
+//   16-bit types, 32 x 32 tiles (16 deep): key tile row m takes key 16 (m / 16) + 8 (m / 4 % 2) + 4 (m / 8 %
+//   2) + m % 4; a lane's 16 scores are then keys 16 j + 8g .. + 7 for j = 0, 1, the operands of
+//   two 16-key products.
 //   fp32 (4 keys a product): key tile t takes keys 16 t + r; lane group g has keys 16 t + 4g + i and
 //   product i takes exactly key i of every group.  Dims of a 16-dim step go 4g + i the same way.
 #pragma once
@@ -58,17 +61,29 @@ __device__ __forceinline__ int row_seq(const int* row0, int B, int r) {
     return lo;
 }
 
-// Element type: one product step, and the rounding of the probabilities.
+// Element type: one product step of a 16 x 16 or 32 x 32 tile (with 16-bit types 32 or 16 deep).
+typedef float f32x16_t __attribute__((ext_vector_type(16)));
+template <int RT> struct PagedAcc { using type = f32x4_t; };
+template <> struct PagedAcc<32> { using type = f32x16_t; };
 template <typename T> struct PagedElem;
 template <> struct PagedElem<_Float16> {
+    template <int RT> using Acc = typename PagedAcc<RT>::type;
     using x2 = _Float16 __attribute__((ext_vector_type(2)));
     static __device__ __forceinline__ f32x4_t mfma(const u32x4_t& a, const u32x4_t& b, f32x4_t c) { return mfma_f16(a, b, c); }
+    static __device__ __forceinline__ f32x16_t mfma(const u32x4_t& a, const u32x4_t& b, f32x16_t c) {
+        return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8_t, a), __builtin_bit_cast(f16x8_t, b), c, 0, 0, 0);
+    }
 };
 template <> struct PagedElem<__bf16> {
+    template <int RT> using Acc = typename PagedAcc<RT>::type;
     using x2 = __bf16 __attribute__((ext_vector_type(2)));
     static __device__ __forceinline__ f32x4_t mfma(const u32x4_t& a, const u32x4_t& b, f32x4_t c) { return mfma_bf16(a, b, c); }
+    static __device__ __forceinline__ f32x16_t mfma(const u32x4_t& a, const u32x4_t& b, f32x16_t c) {
+        return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, a), __builtin_bit_cast(bf16x8_t, b), c, 0, 0, 0);
+    }
 };
 template <> struct PagedElem<float> {
+    template <int RT> using Acc = typename PagedAcc<RT>::type;
     using x2 = float __attribute__((ext_vector_type(2)));
     static __device__ __forceinline__ f32x4_t mfma(const u32x4_t& a, const u32x4_t& b, f32x4_t c) {
 #pragma unroll
@@ -77,42 +92,53 @@ template <> struct PagedElem<float> {
     }
 };
 
+// Swizzles of a block's LDS rows (16-byte columns): the 16 lanes of one LDS cycle of a 16-byte read, which are
+// lanes 0-7 and 16-23 (and so on), read distinct banks.
 __device__ __forceinline__ int swz_paged(int key) { return (key & 3) | (((key >> 3) & 3) << 2); }
+template <bool F32, int RT> __device__ __forceinline__ int swz_v(int dim) {
+    return F32 ? dim & 7 : (RT == 32 ? ((dim >> 1) & 3) ^ ((dim >> 4) & 1) : (dim >> 1) & 3);
+}
 
 constexpr int MAX_ATTN_SPLITS = 64;           // key splits of a part
 
 // log2-domain slack of the lazily moved reference: probabilities <= 2^8 (fits fp16)
 constexpr float PAGED_SLACK = 8.f;
 
-// Workgroup = (part, K/V head, key split, tile of QG x QT x 16 virtual rows), QG waves of QT
-// 16-row tiles.  The split's 32-key blocks are staged in LDS with direct global->LDS loads
+// Workgroup = (part, K/V head, key split, tile of QG x RT virtual rows), QG waves of an RT-row
+// tile.  The split's 32-key blocks are staged in LDS with direct global->LDS loads
 // in a ring of NB buffers and read from there by all waves.  LDS rows are swizzled in 16-byte
 // columns so that the 16 rows of a fragment read lie in different banks.  Lane i holds the
 // page of block 64 n + i, so a block's page is one lane read.
-template <typename T, int DH, int QG, int QT, int NB, int SUB>
+template <typename T, int DH, int QG, int RT, int NB, int SUB>
 __global__ void __launch_bounds__(QG * 64)
 __attribute__((amdgpu_waves_per_eu(QG * (160 * 1024 / (NB * SUB * 64 * DH * (int)sizeof(T))) >= 8 ? 2 : 1)))
 attn_paged_kernel(PagedArgs a) {
     using E = PagedElem<T>;
     constexpr bool F32 = sizeof(T) == 4;
     constexpr int ES = sizeof(T);
-    constexpr int CD = F32 ? 16 : 32;         // dims of one 16-byte K fragment step (4 lane groups)
+    constexpr bool R32 = RT == 32;
+    constexpr int NG = 64 / RT;               // lane groups of RT lanes
+    constexpr int CD = 16 / ES * NG;          // dims of one 16-byte K fragment step
     constexpr int NC = DH / CD;
-    constexpr int ND = DH / 16;               // 16-dim output tiles
-    constexpr int NV = F32 ? 2 : 1;           // V^T fragments of a block per output tile
+    constexpr int NU = 32 / RT;               // key tiles of a block
+    constexpr int NS = RT / 2;                // scores of a block per lane
+    constexpr int ND = DH / RT;               // output tiles
+    constexpr int NV = F32 || R32 ? 2 : 1;    // V^T fragments of a block per output tile
+    using Acc = typename E::template Acc<RT>;
+    constexpr int NA = RT * RT / 64;          // accumulators of a tile per lane
     constexpr int KC = DH * ES / 16;          // 16-byte columns of a key's row
     constexpr int VC = 32 * ES / 16;          // and of a dim's row of V^T
     constexpr int KPLANE = 32 * DH * ES, SBUF = 2 * KPLANE, BUF = SUB * SBUF;
     constexpr int KI = KPLANE / 1024;         // 1 KiB wave loads per plane
     constexpr int LPW = SUB * 2 * (KI / QG);  // loads each wave issues per staged step, at least
     static_assert(64 % SUB == 0, "a step's pages lie in one chunk");
-    constexpr int TM = 16 * QG * QT;          // virtual rows of a workgroup
+    constexpr int TM = RT * QG;               // virtual rows of a workgroup
     static_assert(KI * 1024 == KPLANE, "planes must be whole wave loads");
     static_assert(TM <= 256, "at most four virtual rows per lane");
     __shared__ __attribute__((aligned(1024))) char lds[NB * BUF];
 
     const int lane = threadIdx.x & 63, qw = QG == 1 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int r = lane & 15, g = lane >> 4;
+    const int r = lane % RT, g = lane / RT;
 
     // Which item.  The dispatcher deals consecutive workgroups to the 8 XCDs in turn; XCD x
     // takes the x-th of 8 shares, so that tiles that read the same K/V share one L2.
@@ -192,7 +218,7 @@ attn_paged_kernel(PagedArgs a) {
                 const int i = qw + j * QG;
                 if (KI % QG != 0 && i >= KI) break;
                 const int dim = (i * 64 + lane) / VC, pc = lane % VC;
-                const int sw = F32 ? dim & 7 : (dim >> 1) & 3;
+                const int sw = swz_v<F32, RT>(dim);
                 buffer_to_lds16(Vp, ((dim << a.page_shift) * ES) + ((pc ^ sw) << 4), off * ES, base + KPLANE + i * 1024);
             }
         }
@@ -205,7 +231,7 @@ attn_paged_kernel(PagedArgs a) {
             const int i = qw + j * QG;
             if (KI % QG != 0 && i >= KI) break;
             const int dim = (i * 64 + lane) / VC, pc = lane % VC;
-            const int sw = F32 ? dim & 7 : (dim >> 1) & 3;
+            const int sw = swz_v<F32, RT>(dim);
             const int key = k0 + (16 / ES) * (pc ^ sw);             // the slot's first key
             if (key + 16 / ES <= end) continue;
             u32x4_t* slot = (u32x4_t*)(base + i * 1024 + lane * 16);
@@ -235,24 +261,23 @@ attn_paged_kernel(PagedArgs a) {
         const int n = own || short_len >= ke ? ke : min(ke, a.len[row_seq(a.row0, a.B, row)]);
         return a.lim != nullptr ? min(n, a.lim[row]) : n;
     };
-    u32x4_t qf[QT][NC];
-    int lim[QT];
-#pragma unroll
-    for (int q = 0; q < QT; ++q) {
-        // rows past the last repeat it (the rescale below is decided over a tile's 16 rows)
-        const int f = min(f0 + 16 * (QT * qw + q) + r, nv - 1);
+    u32x4_t qf[NC];
+    int lim;
+    {
+        // rows past the last repeat it (the rescale below is decided over a tile's rows)
+        const int f = min(f0 + RT * qw + r, nv - 1);
         const int row = R0 + f / a.G, h = hk * a.G + f % a.G;
         const T* src = (const T*)a.q + row * a.ld_q + h * DH + (16 / ES) * g;
 #pragma unroll
         for (int c = 0; c < NC; ++c) {
-            qf[q][c] = ldg16(src + CD * c);
+            qf[c] = ldg16(src + CD * c);
             if (a.qmul != 1.f) {
                 constexpr uint32_t sign = F32 ? 0x80000000u : 0x80008000u;
 #pragma unroll
-                for (int e = 0; e < 4; ++e) qf[q][c][e] = a.qmul == 0.f ? 0u : qf[q][c][e] ^ sign;
+                for (int e = 0; e < 4; ++e) qf[c][e] = a.qmul == 0.f ? 0u : qf[c][e] ^ sign;
             }
         }
-        lim[q] = row_limit(f);
+        lim = row_limit(f);
     }
     // The largest limit of the tile's rows ends its keys: what lies behind may be anything.
     int ktop = ks;
@@ -278,27 +303,29 @@ attn_paged_kernel(PagedArgs a) {
     // smallest limit of the wave's rows: blocks below it need no per-key mask
     int lim_w = ktop;
 #pragma unroll
-    for (int q = 0; q < QT; ++q)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) lim_w = min(lim_w, __builtin_amdgcn_readlane(lim[q], i));
+    for (int i = 0; i < RT; ++i) lim_w = min(lim_w, __builtin_amdgcn_readlane(lim, i));
 
-    float mrun[QT], lrun[QT];
-    f32x4_t oacc[QT][ND];
+    float mrun = -INFINITY, lrun = 0.f;
+    Acc oacc[ND];
 #pragma unroll
-    for (int q = 0; q < QT; ++q) {
-        mrun[q] = -INFINITY;
-        lrun[q] = 0.f;
+    for (int dt = 0; dt < ND; ++dt)
 #pragma unroll
-        for (int dt = 0; dt < ND; ++dt) oacc[q][dt] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-    }
-    const int krow0 = F32 ? r : 8 * (r >> 2) + (r & 3);     // the key this lane reads for tile 0
-    constexpr int KT = F32 ? 16 : 4;                        // and the step to tile 1
+        for (int i = 0; i < NA; ++i) oacc[dt][i] = 0.f;
+    // the key that this lane reads for key tile u, and the key of its score e (see above)
+    auto krow = [&](int u) {
+        if constexpr (R32) return 16 * (r >> 4) + 8 * ((r >> 2) & 1) + 4 * ((r >> 3) & 1) + (r & 3);
+        else return F32 ? r + 16 * u : 8 * (r >> 2) + (r & 3) + 4 * u;
+    };
+    auto key_of = [&](int e) {
+        if constexpr (R32) return 16 * (e >> 3) + 8 * g + (e & 7);
+        else return F32 ? 16 * (e >> 2) + 4 * g + (e & 3) : 8 * g + e;
+    };
 
     // no scalar load outstanding past here: the compiler does not see the waits in the loop's
     // asm and would otherwise wait for all LDS reads at each use
     __builtin_amdgcn_s_waitcnt(0xC07F);
     // a wave without rows of its own only stages
-    const bool busy = f0 + 16 * QT * qw < nv;
+    const bool busy = f0 + RT * qw < nv;
     for (int t = 0; t < rounds; ++t) {
         const int cur = t % NB;
         const int k0 = ks + 32 * (kb0 + SUB * t);
@@ -330,148 +357,144 @@ attn_paged_kernel(PagedArgs a) {
         // all of the step's K fragments are read before the first product, its V^T fragments between
         // the scores and the softmax, which covers their latency
         const char* buf = lds + cur * BUF;
-        u32x4_t kf[SUB][NC][2], vf[SUB][ND][NV];
+        u32x4_t kf[SUB][NC][NU], vf[SUB][ND][NV];
 #pragma unroll
         for (int w = 0; w < SUB; ++w)
 #pragma unroll
             for (int c = 0; c < NC; ++c)
 #pragma unroll
-                for (int u = 0; u < 2; ++u) {
-                    const int key = krow0 + KT * u;
+                for (int u = 0; u < NU; ++u) {
+                    const int key = krow(u);
                     const int sw = F32 ? key & 15 : swz_paged(key);
-                    kf[w][c][u] = *(const u32x4_t*)(buf + w * SBUF + key * (DH * ES) + (((4 * c + g) ^ (sw & (KC - 1))) << 4));
+                    kf[w][c][u] = *(const u32x4_t*)(buf + w * SBUF + key * (DH * ES) + (((NG * c + g) ^ (sw & (KC - 1))) << 4));
                 }
         __builtin_amdgcn_sched_barrier(0);
-        f32x4_t s[QT][SUB][2];
+        Acc s[SUB][NU];
 #pragma unroll
-        for (int q = 0; q < QT; ++q)
+        for (int w = 0; w < SUB; ++w)
 #pragma unroll
-            for (int w = 0; w < SUB; ++w) s[q][w][0] = s[q][w][1] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+            for (int u = 0; u < NU; ++u)
+#pragma unroll
+                for (int i = 0; i < NA; ++i) s[w][u][i] = 0.f;
 #pragma unroll
         for (int w = 0; w < SUB; ++w)
 #pragma unroll
             for (int c = 0; c < NC; ++c)
 #pragma unroll
-                for (int q = 0; q < QT; ++q)
-#pragma unroll
-                    for (int u = 0; u < 2; ++u) s[q][w][u] = E::mfma(kf[w][c][u], qf[q][c], s[q][w][u]);
+                for (int u = 0; u < NU; ++u) s[w][u] = E::mfma(kf[w][c][u], qf[c], s[w][u]);
 #pragma unroll
         for (int w = 0; w < SUB; ++w)
 #pragma unroll
             for (int dt = 0; dt < ND; ++dt)
 #pragma unroll
                 for (int u = 0; u < NV; ++u) {
-                    const int dim = 16 * dt + r;
-                    const int sw = F32 ? dim & 7 : (dim >> 1) & 3;
-                    vf[w][dt][u] = *(const u32x4_t*)(buf + w * SBUF + KPLANE + dim * (32 * ES) + (((4 * u + g) ^ sw) << 4));
+                    const int dim = RT * dt + r;
+                    const int sw = swz_v<F32, RT>(dim);
+                    vf[w][dt][u] = *(const u32x4_t*)(buf + w * SBUF + KPLANE + dim * (32 * ES) + (((NG * u + g) ^ sw) << 4));
                 }
         __builtin_amdgcn_sched_barrier(0);
 
-        u32x4_t pf[QT][SUB][NV];
-#pragma unroll
-        for (int q = 0; q < QT; ++q) {
-            // sv[8w + 4u + i]: the score of key k0 + 32w + (16-bit) 8g + 4u + i, (fp32) 16u + 4g + i
-            float sv[8 * SUB];
-#pragma unroll
-            for (int w = 0; w < SUB; ++w)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    sv[8 * w + i] = s[q][w][0][i];
-                    sv[8 * w + 4 + i] = s[q][w][1][i];
-                }
-            if (k0 + 32 * SUB > lim_w || !whole) {
-#pragma unroll
-                for (int w = 0; w < SUB; ++w) {
-                    const int e = (there >> w) & 1 ? lim[q] : 0;
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const int key0 = k0 + 32 * w + (F32 ? 4 : 8) * g + i;
-                        if (key0 >= e) sv[8 * w + i] = -INFINITY;
-                        if (key0 + KT >= e) sv[8 * w + 4 + i] = -INFINITY;
-                    }
-                }
-            }
-            // the row's maximum over the step and its four lane groups (max is symmetric: a swap hands
-            // a lane its partner's value)
-            float bm = sv[0];
-#pragma unroll
-            for (int e = 1; e < 8 * SUB; ++e) bm = fmaxf(bm, sv[e]);
-            const auto w32 = __builtin_amdgcn_permlane32_swap(__float_as_uint(bm), __float_as_uint(bm), false, false);
-            bm = fmaxf(__uint_as_float(w32[0]), __uint_as_float(w32[1]));
-            const auto w16 = __builtin_amdgcn_permlane16_swap(__float_as_uint(bm), __float_as_uint(bm), false, false);
-            bm = fmaxf(__uint_as_float(w16[0]), __uint_as_float(w16[1]));
-            const float bms = bm * a.sl2;
-            // the reference moves only when some row of the tile exceeds it by PAGED_SLACK: O, sum and
-            // merge are exact for any reference, and most steps skip the rescale
-            if (__builtin_expect(__builtin_amdgcn_ballot_w64(bms > mrun[q] + PAGED_SLACK) != 0, 0)) {
-                const float mnew = fmaxf(mrun[q], bms);
-                const float alpha = (mnew == -INFINITY) ? 1.f : __builtin_amdgcn_exp2f(mrun[q] - mnew);
-                lrun[q] *= alpha;
-#pragma unroll
-                for (int dt = 0; dt < ND; ++dt)
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) oacc[q][dt][i] *= alpha;
-                mrun[q] = mnew;
-            }
-            const float mref = (mrun[q] == -INFINITY) ? 0.f : mrun[q];
-            float p[8 * SUB], sum = 0.f;
-#pragma unroll
-            for (int e = 0; e < 8 * SUB; ++e) p[e] = __builtin_amdgcn_exp2f(fmaf(sv[e], a.sl2, -mref));
-#pragma unroll
-            for (int e = 0; e < 8 * SUB; e += 4) sum += (p[e] + p[e + 1]) + (p[e + 2] + p[e + 3]);
-            lrun[q] += sum;
-#pragma unroll
-            for (int w = 0; w < SUB; ++w) {
-                if constexpr (F32) {
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) pf[q][w][e >> 2][e & 3] = __float_as_uint(p[8 * w + e]);
-                } else {
-                    // rounded to nearest for the product with V (half a step of T a probability: as much as
-                    // the output's own rounding); the sum keeps fp32
-#pragma unroll
-                    for (int e = 0; e < 4; ++e)
-                        pf[q][w][0][e] = __builtin_bit_cast(uint32_t, (typename E::x2){(T)p[8 * w + 2 * e], (T)p[8 * w + 2 * e + 1]});
-                }
-            }
-        }
+        float sv[SUB][NS];
 #pragma unroll
         for (int w = 0; w < SUB; ++w)
 #pragma unroll
+            for (int e = 0; e < NS; ++e) sv[w][e] = s[w][e / NA][e % NA];
+        if (k0 + 32 * SUB > lim_w || !whole) {
+#pragma unroll
+            for (int w = 0; w < SUB; ++w) {
+                const int end = (there >> w) & 1 ? lim : 0;
+#pragma unroll
+                for (int e = 0; e < NS; ++e)
+                    if (k0 + 32 * w + key_of(e) >= end) sv[w][e] = -INFINITY;
+            }
+        }
+        // the row's maximum over the step and its lane groups (max is symmetric: a swap hands a lane its
+        // partner's value)
+        float bm = sv[0][0];
+#pragma unroll
+        for (int w = 0; w < SUB; ++w)
+#pragma unroll
+            for (int e = 0; e < NS; ++e) bm = fmaxf(bm, sv[w][e]);
+        const auto w32 = __builtin_amdgcn_permlane32_swap(__float_as_uint(bm), __float_as_uint(bm), false, false);
+        bm = fmaxf(__uint_as_float(w32[0]), __uint_as_float(w32[1]));
+        if constexpr (!R32) {
+            const auto w16 = __builtin_amdgcn_permlane16_swap(__float_as_uint(bm), __float_as_uint(bm), false, false);
+            bm = fmaxf(__uint_as_float(w16[0]), __uint_as_float(w16[1]));
+        }
+        const float bms = bm * a.sl2;
+        // the reference moves only when some row of the tile exceeds it by PAGED_SLACK: O, sum and merge are
+        // exact for any reference, and most steps skip the rescale
+        if (__builtin_expect(__builtin_amdgcn_ballot_w64(bms > mrun + PAGED_SLACK) != 0, 0)) {
+            const float mnew = fmaxf(mrun, bms);
+            const float alpha = (mnew == -INFINITY) ? 1.f : __builtin_amdgcn_exp2f(mrun - mnew);
+            lrun *= alpha;
+#pragma unroll
             for (int dt = 0; dt < ND; ++dt)
 #pragma unroll
-                for (int q = 0; q < QT; ++q)
+                for (int i = 0; i < NA; ++i) oacc[dt][i] *= alpha;
+            mrun = mnew;
+        }
+        const float mref = (mrun == -INFINITY) ? 0.f : mrun;
+        u32x4_t pf[SUB][NV];
+        float sum = 0.f;
 #pragma unroll
-                    for (int u = 0; u < NV; ++u) oacc[q][dt] = E::mfma(vf[w][dt][u], pf[q][w][u], oacc[q][dt]);
+        for (int w = 0; w < SUB; ++w) {
+            float p[NS];
+#pragma unroll
+            for (int e = 0; e < NS; ++e) p[e] = __builtin_amdgcn_exp2f(fmaf(sv[w][e], a.sl2, -mref));
+#pragma unroll
+            for (int e = 0; e < NS; e += 4) sum += (p[e] + p[e + 1]) + (p[e + 2] + p[e + 3]);
+            if constexpr (F32) {
+#pragma unroll
+                for (int e = 0; e < NS; ++e) pf[w][e >> 2][e & 3] = __float_as_uint(p[e]);
+            } else {
+                // rounded to nearest for the product with V (half a step of T a probability: as much as the
+                // output's own rounding); the sum keeps fp32
+#pragma unroll
+                for (int e = 0; e < NS / 2; ++e)
+                    pf[w][e >> 2][e & 3] = __builtin_bit_cast(uint32_t, (typename E::x2){(T)p[2 * e], (T)p[2 * e + 1]});
+            }
+        }
+        lrun += sum;
+#pragma unroll
+        for (int w = 0; w < SUB; ++w)
+#pragma unroll
+            for (int u = 0; u < NV; ++u)
+#pragma unroll
+                for (int dt = 0; dt < ND; ++dt) oacc[dt] = E::mfma(vf[w][dt][u], pf[w][u], oacc[dt]);
     }
 
+    float l = lrun + __shfl_xor(lrun, 32);
+    if constexpr (!R32) l += __shfl_xor(l, 16);
+    const int f = f0 + RT * qw + r;
+    if (f >= nv) return;
+    const int row = R0 + f / a.G, h = hk * a.G + f % a.G;
+    // (accumulators 4j .. 4j + 3 are consecutive dims)
+    auto dim_of = [&](int dt, int j) { return RT * dt + (R32 ? 8 * j + 4 * g : 4 * g); };
+    if (a.direct) {
+        const float inv = l > 0.f ? 1.f / l : 0.f;
+        T* op = (T*)a.out + row * a.ld_out + h * DH;
 #pragma unroll
-    for (int q = 0; q < QT; ++q) {
-        float l = lrun[q] + __shfl_xor(lrun[q], 16);
-        l += __shfl_xor(l, 32);
-        const int f = f0 + 16 * (QT * qw + q) + r;
-        if (f >= nv) continue;
-        const int row = R0 + f / a.G, h = hk * a.G + f % a.G;
-        if (a.direct) {
-            const float inv = l > 0.f ? 1.f / l : 0.f;
-            T* op = (T*)a.out + row * a.ld_out + h * DH;
+        for (int dt = 0; dt < ND; ++dt)
 #pragma unroll
-            for (int dt = 0; dt < ND; ++dt) {
+            for (int j = 0; j < NA / 4; ++j) {
                 T e[4];
 #pragma unroll
-                for (int i = 0; i < 4; ++i) e[i] = elem_from_f32<T>(oacc[q][dt][i] * inv);
-                __builtin_memcpy(__builtin_assume_aligned(op + 16 * dt + 4 * g, 4 * ES), e, sizeof(e));
+                for (int i = 0; i < 4; ++i) e[i] = elem_from_f32<T>(oacc[dt][4 * j + i] * inv);
+                __builtin_memcpy(__builtin_assume_aligned(op + dim_of(dt, j), 4 * ES), e, sizeof(e));
             }
-        } else {
-            const size_t rec = ((size_t)part * a.T + row) * a.H + h;
-            if (rounds > 0) {
-                float* op = a.opart + rec * DH;
+    } else {
+        const size_t rec = ((size_t)part * a.T + row) * a.H + h;
+        if (rounds > 0) {
+            float* op = a.opart + rec * DH;
 #pragma unroll
-                for (int dt = 0; dt < ND; ++dt)
-                    *(float4*)(op + 16 * dt + 4 * g) =
-                        make_float4(oacc[q][dt][0], oacc[q][dt][1], oacc[q][dt][2], oacc[q][dt][3]);
-            }
-            if (g == 0) *(float2*)(a.mlpart + rec * 2) = make_float2(mrun[q], l);
+            for (int dt = 0; dt < ND; ++dt)
+#pragma unroll
+                for (int j = 0; j < NA / 4; ++j)
+                    *(float4*)(op + dim_of(dt, j)) = make_float4(oacc[dt][4 * j], oacc[dt][4 * j + 1], oacc[dt][4 * j + 2],
+                                                                 oacc[dt][4 * j + 3]);
         }
+        if (g == 0) *(float2*)(a.mlpart + rec * 2) = make_float2(mrun, l);
     }
 }
 

@@ -170,7 +170,7 @@ template <typename T, int DH>
 void launch_attn_dh(PagedArgs a, const AttnPlan& p, hipStream_t s) {
     constexpr int SUB = sizeof(T) == 4 ? 1 : 2;
     const dim3 grid((unsigned)(p.wgs_s + p.wgs_o));
-#define ATTN(QG_, QT_) hipLaunchKernelGGL((attn_paged_kernel<T, DH, QG_, QT_, 2, SUB>), grid, dim3(QG_ * 64), 0, s, a)
+#define ATTN(QG_, QT_) hipLaunchKernelGGL((attn_paged_kernel<T, DH, QG_, 16 * QT_, 2, SUB>), grid, dim3(QG_ * 64), 0, s, a)
     if constexpr (sizeof(T) == 2) {
         if (p.qt == 2) ATTN(4, 2);
     }
