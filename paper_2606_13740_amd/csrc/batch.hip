@@ -166,6 +166,31 @@ size_t attn_ws_bytes(const dllm_attn_args* g, const AttnPlan& p) {
     return (size_t)(p.ns_s + p.ns_o) * g->n_rows * g->n_heads * (g->head_dim + 2) * 4;
 }
 
+// Every check of an attention call's sizes.
+int check_attn(const dllm_attn_args* g, int& shift) {
+    if (!g) return fail(DLLM_E_INVAL, "args is NULL");
+    if (int rc = check_dtype(g->dtype)) return rc;
+    if (int rc = check_heads(g->n_heads, g->n_kv_heads, g->head_dim)) return rc;
+    if (g->dtype != DLLM_F32 && g->head_dim == 32) return fail(DLLM_E_DTYPE, "head_dim 32 needs DLLM_F32");
+    if (g->n_rows < 0 || g->n_rows > MAX_BATCH_ROWS) return fail(DLLM_E_INVAL, "n_rows must be in [0, 2^24]");
+    if (g->n_seqs < 1 || g->n_seqs > DLLM_MAX_SEQS) return fail(DLLM_E_INVAL, "n_seqs must be in [1, DLLM_MAX_SEQS]");
+    if ((shift = page_shift(g->page, g->n_pages)) < 0) return DLLM_E_INVAL;
+    if (g->table_ld < 1 || (long)g->table_ld * g->page >= (1l << 31))
+        return fail(DLLM_E_INVAL, "table_ld must be >= 1 and table_ld * page < 2^31");
+    if (g->max_len < 0 || g->max_len > g->table_ld * g->page)
+        return fail(DLLM_E_INVAL, "max_len must be in [0, table_ld * page]");
+    if (g->max_rows < 0) return fail(DLLM_E_INVAL, "max_rows must be >= 0");
+    if (g->shared_len < 0 || g->shared_len % g->page != 0 || g->shared_len > g->table_ld * g->page)
+        return fail(DLLM_E_INVAL, "shared_len must be a multiple of page in [0, table_ld * page]");
+    if (!std::isfinite(g->scale)) return fail(DLLM_E_INVAL, "scale must be finite");
+    if ((long)g->n_rows * (g->n_heads / g->n_kv_heads) >= (1l << 31))
+        return fail(DLLM_E_INVAL, "n_rows times the query heads of a K/V head must be < 2^31");
+    const AttnPlan p = attn_plan(g);
+    if (p.wgs_s + p.wgs_o > 0x7FFFFFFF || (long)g->n_rows * g->n_heads > 0x7FFFFFFF)
+        return fail(DLLM_E_INVAL, "n_seqs, max_rows and n_rows need too many workgroups");
+    return DLLM_OK;
+}
+
 template <typename T, int DH>
 void launch_attn_dh(PagedArgs a, const AttnPlan& p, hipStream_t s) {
     constexpr int SUB = sizeof(T) == 4 ? 1 : 2;
@@ -189,26 +214,6 @@ void launch_attn(const PagedArgs& a, const AttnPlan& p, int Dh, hipStream_t s) {
     if (Dh == 128) launch_attn_dh<T, 128>(a, p, s);
     else if (Dh == 64) launch_attn_dh<T, 64>(a, p, s);
     else if constexpr (sizeof(T) == 4) launch_attn_dh<T, 32>(a, p, s);
-}
-
-// Every check of an attention call but the workspace's size.
-int check_attn(const dllm_attn_args* g, int& shift) {
-    if (!g) return fail(DLLM_E_INVAL, "args is NULL");
-    if (int rc = check_dtype(g->dtype)) return rc;
-    if (int rc = check_heads(g->n_heads, g->n_kv_heads, g->head_dim)) return rc;
-    if (g->dtype != DLLM_F32 && g->head_dim == 32) return fail(DLLM_E_DTYPE, "head_dim 32 needs DLLM_F32");
-    if (g->n_rows < 0 || g->n_rows > MAX_BATCH_ROWS) return fail(DLLM_E_INVAL, "n_rows must be in [0, 2^24]");
-    if (g->n_seqs < 1 || g->n_seqs > DLLM_MAX_SEQS) return fail(DLLM_E_INVAL, "n_seqs must be in [1, DLLM_MAX_SEQS]");
-    if ((shift = page_shift(g->page, g->n_pages)) < 0) return DLLM_E_INVAL;
-    if (g->table_ld < 1 || (long)g->table_ld * g->page >= (1l << 31))
-        return fail(DLLM_E_INVAL, "table_ld must be >= 1 and table_ld * page < 2^31");
-    if (g->max_len < 0 || g->max_len > g->table_ld * g->page)
-        return fail(DLLM_E_INVAL, "max_len must be in [0, table_ld * page]");
-    if (g->max_rows < 0) return fail(DLLM_E_INVAL, "max_rows must be >= 0");
-    if (g->shared_len < 0 || g->shared_len % g->page != 0 || g->shared_len > g->table_ld * g->page)
-        return fail(DLLM_E_INVAL, "shared_len must be a multiple of page in [0, table_ld * page]");
-    if (!std::isfinite(g->scale)) return fail(DLLM_E_INVAL, "scale must be finite");
-    return DLLM_OK;
 }
 
 // Ranges of SEL_IDS ids, and rows of a workgroup: as many as keep a sequence's tables and still leave
@@ -302,7 +307,6 @@ int dllm_attention_paged(const dllm_attn_args* g, dllm_stream stream) {
     if (g->n_rows == 0) return DLLM_OK;
     const AttnPlan p = attn_plan(g);
     const size_t need = attn_ws_bytes(g, p);
-    if (p.wgs_s + p.wgs_o > 0x7FFFFFFF) return fail(DLLM_E_INVAL, "n_seqs, max_rows and n_rows need too many workgroups");
     if (need > 0 && (!g->d_ws || !aligned(g->d_ws, 16))) return fail(DLLM_E_INVAL, "workspace: NULL or not 16-byte aligned");
     if (need > g->ws_bytes)
         return fail(DLLM_E_CAPACITY, "the call needs " + std::to_string(need) + " bytes of workspace");

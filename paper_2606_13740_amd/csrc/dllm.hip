@@ -1205,6 +1205,9 @@ int dllm_batch_step(dllm_model* m, void* d_pages, size_t bytes, const dllm_batch
     if (bytes < need) return fail(DLLM_E_CAPACITY, "pages smaller than dllm_batch_bytes()");
     if (((uintptr_t)d_pages & 15) != 0) return fail(DLLM_E_INVAL, "pages must be 16-byte aligned");
     if (!b->d_table || !b->d_row0 || !b->d_pos || !b->d_slot || !b->d_len) return fail(DLLM_E_INVAL, "rows: NULL array");
+    const void* arrays[] = {b->d_table, b->d_row0, b->d_pos, b->d_slot, b->d_len, b->d_lim, d_tok, d_out_id, d_out_conf};
+    for (const void* p : arrays)
+        if (((uintptr_t)p & 3) != 0) return fail(DLLM_E_INVAL, "arrays must be 4-byte aligned");
     if (b->n_rows < 1) return fail(DLLM_E_INVAL, "n_rows must be >= 1");
     if (b->max_len > m->cfg.max_pos) return fail(DLLM_E_CAPACITY, "max_len exceeds the model's max_pos");
     if ((d_out_id == nullptr) != (d_out_conf == nullptr))

@@ -107,6 +107,30 @@ def test_select_refusals(dl, change, code):
     assert dl.lib().dllm_select_ws(ctypes.byref(a), None) == dl.DLLM_E_INVAL
 
 
+def test_workspace_is_checked(dl):
+    L, n = dl.lib(), ctypes.c_size_t()
+    a = fill(dl.dllm_attn_args, **dict(ATTN, table_ld=200, max_len=6000, n_pages=4000, shared_len=0, d_ws=None, ws_bytes=0))
+    assert L.dllm_attention_paged_ws(ctypes.byref(a), ctypes.byref(n)) == 0 and n.value > 0
+    assert L.dllm_attention_paged(ctypes.byref(a), None) == dl.DLLM_E_INVAL             # NULL
+    a.d_ws, a.ws_bytes = P, n.value - 1
+    assert L.dllm_attention_paged(ctypes.byref(a), None) == dl.DLLM_E_CAPACITY
+    a.d_ws, a.ws_bytes = P + 8, n.value
+    assert L.dllm_attention_paged(ctypes.byref(a), None) == dl.DLLM_E_INVAL             # misaligned
+    s = fill(dl.dllm_select_args, **dict(SELECT, vocab=5000, mask_id=-1, ld=5000, allow_ld=200, d_ws=None, ws_bytes=0))
+    assert L.dllm_select_ws(ctypes.byref(s), ctypes.byref(n)) == 0 and n.value > 0
+    assert L.dllm_select(ctypes.byref(s), None) == dl.DLLM_E_INVAL
+    s.d_ws, s.ws_bytes = P, n.value - 1
+    assert L.dllm_select(ctypes.byref(s), None) == dl.DLLM_E_CAPACITY
+
+
+@pytest.mark.parametrize("change", [dict(n_rows=1 << 24, n_heads=1024, n_kv_heads=1, ld_q=1 << 16, ld_out=1 << 16),
+                                    dict(n_seqs=4096, max_rows=1 << 24, n_rows=1 << 24, n_heads=32, n_kv_heads=32, ld_q=2048, ld_out=2048)])
+def test_attention_refuses_launches_past_the_grid(dl, change):
+    a, n = fill(dl.dllm_attn_args, **dict(ATTN, **change)), ctypes.c_size_t()
+    assert dl.lib().dllm_attention_paged_ws(ctypes.byref(a), ctypes.byref(n)) == dl.DLLM_E_INVAL
+    assert dl.lib().dllm_attention_paged(ctypes.byref(a), None) == dl.DLLM_E_INVAL
+
+
 def test_binding_refuses_tensors_that_are_not_on_the_gpu(dl):
     import torch
     z = lambda n: torch.zeros(n, dtype=torch.int32)  # noqa: E731

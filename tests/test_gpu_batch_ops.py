@@ -319,6 +319,85 @@ def test_attention_strided_rows_longer_bounds_and_repeats(dl):
         assert torch.equal(out[:, H * D:].reshape(R, H, D), plain) and out[:, :H * D].eq(7.0).all()
 
 
+@pytest.mark.parametrize("shared", [0, 64])
+def test_attention_rows_before_the_first_sequence(dl, shared):
+    """row0 that does not begin at 0: the rows before it, like those behind the last, are left as they were."""
+    import torch
+    c = attn_case(np.random.default_rng(15), "f16", [20, 9], [210, 190], 4, 2, 64, 32, shared, extra_rows=5)
+    args = (c["kt"], c["vt"], i32(c["table"]))
+    out, moved = (torch.full_like(c["qt"], 7.0) for _ in range(2))
+    dl.dllm_attention_paged(c["qt"], *args, i32(c["row0"]), i32(c["lens"]), out, 20, 210, shared_len=shared)
+    dl.dllm_attention_paged(c["qt"].roll(3, 0), *args, i32(c["row0"] + 3), i32(c["lens"]), moved, 20, 210, shared_len=shared)
+    torch.cuda.synchronize()
+    assert torch.equal(moved[3:32], out[:29]) and moved[:3].eq(7.0).all() and moved[32:].eq(7.0).all()
+
+
+def test_attention_on_another_stream_with_a_workspace(dl):
+    """Two calls at once, each on its own stream with a workspace of its own."""
+    import ctypes
+    import torch
+    cs = [attn_case(np.random.default_rng(16 + i), "bf16", [32, 32, 32], [1500, 1300, 900], 4, 2, 128, 32, 640) for i in range(2)]
+    calls = [(c["qt"], c["kt"], c["vt"], i32(c["table"]), i32(c["row0"]), i32(c["lens"])) for c in cs]
+    want = [torch.full_like(c["qt"], 7.0) for c in cs]
+    for x, o in zip(calls, want):
+        dl.dllm_attention_paged(*x, o, 32, 1500, shared_len=640)
+    a, n = dl.dllm_attn_args(4, 98, 3, 4, 2, 128, 32, cs[0]["n_pages"], cs[0]["table"].shape[1], 640, 32, 1500, 0.1), ctypes.c_size_t()
+    assert dl.lib().dllm_attention_paged_ws(ctypes.byref(a), ctypes.byref(n)) == 0
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    spaces = [torch.full((n.value,), 255, dtype=torch.uint8, device="cuda") for _ in range(2)]
+    got = [torch.full_like(w, 7.0) for w in want]
+    torch.cuda.synchronize()
+    for _ in range(3):
+        for x, o, st, ws in zip(calls, got, streams, spaces):
+            dl.dllm_attention_paged(*x, o, 32, 1500, shared_len=640, ws=ws, stream=st)
+    torch.cuda.synchronize()
+    assert all(torch.equal(g, w) for g, w in zip(got, want))
+
+
+def test_offsets_past_32_bits(dl):
+    """A pool of more than 2^31 elements a plane: the same bits from its last pages as from a small pool's."""
+    import torch
+    H, Hk, D, page, T = 8, 4, 128, 64, 70
+    per = Hk * page * D
+    n_big = 2 ** 31 // per + 8
+    shift = n_big - 8                                        # page p of the small pool is page p + shift of the large one
+    g = torch.Generator(device="cuda")
+    g.manual_seed(5)
+    mk = lambda *s: torch.empty(s, dtype=torch.bfloat16, device="cuda").normal_(generator=g)  # noqa: E731
+    small = (mk(8, Hk, page, D), mk(8, Hk, D, page))
+    big = (torch.empty(n_big, Hk, page, D, dtype=torch.bfloat16, device="cuda"),
+           torch.empty(n_big, Hk, D, page, dtype=torch.bfloat16, device="cuda"))
+    for b, s in zip(big, small):
+        b[shift:] = s
+    qkv, rope = mk(T, (H + 2 * Hk) * D), torch.empty(400, D // 2, 2, device="cuda")
+    dl.dllm_rope_table(rope, D, 10000.0)
+    q, k, v = qkv.split([H * D, Hk * D, Hk * D], 1)
+    pos = np.arange(300, 300 + T)
+    table = np.array([[3, 0, 5, 1, 7, 2]])
+    slot = table[0][pos // page] * page + pos % page
+    outs = []
+    for (kp, vp), s in ((small, 0), (big, shift)):
+        qo, out = (torch.zeros(T, H, D, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+        dl.dllm_qk_norm_rope(q, k, v, rope, i32(pos), i32(slot + s * page), qo, kp, vp)
+        dl.dllm_attention_paged(qo, kp, vp, i32(table + s), i32([0, T]), i32([300 + T]), out, T, 6 * page)
+        outs.append((qo, out))
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(*outs))
+    assert all(torch.equal(b[shift:], s) for b, s in zip(big, small))
+    del big, small
+    V, R = 152064, 2 ** 31 // 152064 + 60                    # logits of more than 2^31 elements
+    x = torch.empty(R, V, dtype=torch.bfloat16, device="cuda")
+    x[-50:] = mk(50, V)
+    x[:-50] = x[-1]
+    ids, conf = torch.zeros(R, dtype=torch.int32, device="cuda"), torch.zeros(R, device="cuda")
+    dl.dllm_select(x, ids, conf, mask_id=5)
+    last = torch.zeros(50, dtype=torch.int32, device="cuda"), torch.zeros(50, device="cuda")
+    dl.dllm_select(x[-50:].clone(), *last, mask_id=5)
+    torch.cuda.synchronize()
+    assert torch.equal(ids[-50:], last[0]) and torch.allclose(conf[-50:], last[1], rtol=1e-6, atol=0)
+    assert ids[:-50].eq(last[0][-1]).all()
+
+
 # ---------------------------------------------------------------------------- select
 
 
