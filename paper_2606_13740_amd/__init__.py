@@ -162,17 +162,16 @@ def _ptr(t) -> Optional[int]:
 _raw_stream = None
 
 
-def _stream(stream):
-    """The stream's handle; None: the current stream of the current device."""
+def _stream(stream, device: Optional[int] = None):
+    """The stream's handle; None: the current stream of the current device (`device`, where the caller knows it)."""
     global _raw_stream
     if stream is None:
+        import torch
         if _raw_stream is None:
-            import torch
             # the handle without the Stream object around it (2.7 us a call), where torch has it
-            raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
-            device = torch.cuda.current_device
-            _raw_stream = (lambda: raw(device())) if raw else (lambda: torch.cuda.current_stream().cuda_stream)
-        return _raw_stream()
+            _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (
+                lambda dev: torch.cuda.current_stream(dev).cuda_stream)
+        return _raw_stream(torch.cuda.current_device() if device is None else device)
     return stream if isinstance(stream, int) else stream.cuda_stream
 
 
@@ -397,7 +396,8 @@ def dllm_batch_plan(length, new, owned, owned_out, table, free, n_free, n_free_o
                     pos, slot, seq, lim, status, stream=None):
     """The row arrays' common length is the plan's max_rows; free has an entry per page of the pool."""
     f, B, ld, R, N = "dllm_batch_plan", length.numel(), table.shape[-1], pos.numel(), free.numel()
-    _plain(f, _gpu(f, length), _Types.i32, (length, new, owned, owned_out, table, free, n_free, n_free_out, row0, pos, slot,
+    dev = _gpu(f, length)
+    _plain(f, dev, _Types.i32, (length, new, owned, owned_out, table, free, n_free, n_free_out, row0, pos, slot,
                                             seq, lim, status),
            "length new owned owned_out table free n_free n_free_out row0 pos slot seq lim status")
     if (new.numel() < B or owned.numel() < B or owned_out.numel() < B or slot.numel() < R or seq.numel() < R or
@@ -408,7 +408,7 @@ def dllm_batch_plan(length, new, owned, owned_out, table, free, n_free, n_free_o
     rc = lib().dllm_batch_plan(length.data_ptr(), new.data_ptr(), owned.data_ptr(), owned_out.data_ptr(), B,
                                table.data_ptr(), ld, free.data_ptr(), n_free.data_ptr(), n_free_out.data_ptr(), N, page,
                                shared_pages, R, row0.data_ptr(), pos.data_ptr(), slot.data_ptr(), seq.data_ptr(),
-                               lim.data_ptr(), status.data_ptr(), _stream(stream))
+                               lim.data_ptr(), status.data_ptr(), _stream(stream, dev))
     if rc:
         _check(rc, f)
 
@@ -444,7 +444,7 @@ def dllm_qk_norm_rope(q, k, v, rope, pos, slot, q_out, k_pages, v_pages, q_gain=
                      k.data_ptr(), v.data_ptr(), ld_q, ld_k, ld_v, None if q_gain is None else q_gain.data_ptr(),
                      None if k_gain is None else k_gain.data_ptr(), rope.data_ptr(), pos.data_ptr(), slot.data_ptr(),
                      q_out.data_ptr(), k_pages.data_ptr(), v_pages.data_ptr())
-    rc = lib().dllm_qk_norm_rope(ctypes.byref(a), _stream(stream))
+    rc = lib().dllm_qk_norm_rope(ctypes.byref(a), _stream(stream, dev))
     if rc:
         _check(rc, f)
 
@@ -490,7 +490,7 @@ def dllm_attention_paged(q, k_pages, v_pages, table, row0, length, out, max_rows
                        None if lim is None else lim.data_ptr(), out.data_ptr(), ld_out)
     L = lib()
     keep = _workspace(L.dllm_attention_paged_ws, a, ws, stream, dev, f)
-    rc = L.dllm_attention_paged(ctypes.byref(a), _stream(stream))
+    rc = L.dllm_attention_paged(ctypes.byref(a), _stream(stream, dev))
     if rc:
         _check(rc, f)
     del keep

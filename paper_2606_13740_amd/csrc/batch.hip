@@ -80,8 +80,9 @@ int dllm_batch_plan(const int32_t* d_len, const int32_t* d_new, const int32_t* d
     if (max_rows < 1 || max_rows > MAX_BATCH_ROWS) return fail(DLLM_E_INVAL, "max_rows must be in [1, 2^24]");
     PlanArgs a{d_len, d_new, d_owned, d_owned_out, n_seqs, d_table, table_ld, d_free, d_n_free, d_n_free_out,
                n_pages, shift, shared_pages, max_rows, d_row0, d_pos, d_slot, d_seq, d_lim, d_status};
-    const int wgs = std::min(256, std::max(1, ceil_div(max_rows, PLAN_NT)));
-    hipLaunchKernelGGL(batch_plan_kernel, dim3(wgs), dim3(PLAN_NT), 0, (hipStream_t)stream, a);
+    const int row_wgs = std::min(192, ceil_div(max_rows, PLAN_NT));
+    const int seq_wgs = std::min(64, ceil_div(std::max(n_seqs, n_pages), PLAN_NT));   // a CU for every workgroup
+    hipLaunchKernelGGL(batch_plan_kernel, dim3(row_wgs + seq_wgs), dim3(PLAN_NT), 0, (hipStream_t)stream, a, row_wgs);
     HIP_TRY(hipGetLastError());
     return DLLM_OK;
 }

@@ -37,13 +37,14 @@ __device__ __forceinline__ PlanSum operator+(const PlanSum& a, const PlanSum& b)
 // stands, in its table: takers write their tables only at [owned, need), givers' entries
 // [need, owned) and stack entries below n_free are never written, so no workgroup reads
 // what another writes, every workgroup repeats the scan (three loads a sequence, L2) and one launch
-// does all.
+// does all: the first row_wgs workgroups the rows, the others the sequences, tables and stack.
 //
 // What bounds it: launch and the chain of dependent loads (lengths, scan, table or stack
-// entry, slot).
+// entry, slot): 4.7 us for 4 sequences of one row, 8.1 for 2048 of 32 (9.4 where each workgroup did
+// its share of both kinds, one after the other), of which an empty launch is 2 to 3.
 constexpr int PLAN_NT = 512;
 constexpr int PLAN_MAXB = 4096;
-__global__ void __launch_bounds__(PLAN_NT) batch_plan_kernel(PlanArgs a) {
+__global__ void __launch_bounds__(PLAN_NT) batch_plan_kernel(PlanArgs a, int row_wgs) {
     constexpr int NW = PLAN_NT / 64, PER = PLAN_MAXB / PLAN_NT;
     __shared__ int row0[PLAN_MAXB + 1], t0[PLAN_MAXB + 1], g0[PLAN_MAXB + 1], len_s[PLAN_MAXB], own_s[PLAN_MAXB];
     __shared__ PlanSum wsum[NW];
@@ -132,9 +133,11 @@ __global__ void __launch_bounds__(PLAN_NT) batch_plan_kernel(PlanArgs a) {
         return a.table[(size_t)b * a.ld + own_s[b] - (g0[b + 1] - g0[b]) + (k - g0[b])];
     };
     const int n_stack = stack;
-    const int gtid = blockIdx.x * PLAN_NT + tid, gn = gridDim.x * PLAN_NT;
+    const bool rows = (int)blockIdx.x < row_wgs;
+    const int gtid = (rows ? blockIdx.x : blockIdx.x - row_wgs) * PLAN_NT + tid;
+    const int gn = (rows ? row_wgs : gridDim.x - row_wgs) * PLAN_NT;
 
-    for (int r = gtid; r < a.max_rows; r += gn) {
+    for (int r = rows ? gtid : a.max_rows; r < a.max_rows; r += gn) {
         int pos = 0, slot = -1, seq = -1, lim = 0;
         if (r < row0[a.B]) {
             seq = find(row0, r);
@@ -150,6 +153,7 @@ __global__ void __launch_bounds__(PLAN_NT) batch_plan_kernel(PlanArgs a) {
         a.seq[r] = seq;
         a.lim[r] = lim;
     }
+    if (rows) return;
     for (int b = gtid; b <= a.B; b += gn) a.row0[b] = row0[b];
     for (int b = gtid; b < a.B; b += gn)
         a.owned_out[b] = own_s[b] + (ok ? (t0[b + 1] - t0[b]) - (g0[b + 1] - g0[b]) : 0);
