@@ -471,7 +471,8 @@ int dllm_rope_table(float* d_table, int32_t max_pos, int32_t head_dim, float rop
  * d_slot[row] of the planes, each rounded to `dtype` once (fp16 saturates at +-65504).
  * A row with a slot outside [0, n_pages * page) writes no K/V; two rows must not have
  * the same slot.  ld_*: row strides in elements.  Head_dim is 32, 64 or 128.  E_INVAL
- * unless all pointers and row strides are multiples of 16 bytes (integer arrays: 4). */
+ * unless all pointers and row strides are multiples of 16 bytes (integer arrays: 4), and
+ * for launches past 2^32 threads. */
 typedef struct dllm_qk_args {
     int32_t dtype;
     int32_t n_rows;
@@ -506,14 +507,16 @@ int dllm_qk_norm_rope(const dllm_qk_args* args, dllm_stream stream);
  * the same pages for all sequences: they are read through the table of sequence 0, once
  * for all rows.  Scores, softmax and sums are fp32; the probabilities are rounded to
  * `dtype` for their product with V.  Keys past e, and pages whose table entry is no page
- * id, are never used, whatever they hold.  Rows from d_row0[n_seqs] on are left as they
+ * id, are never used, whatever they hold; an infinity or NaN in a key that a row sees is
+ * in that row's result alone.  Rows from d_row0[n_seqs] on are left as they
  * were.  max_rows and max_len bound the rows and keys (d_len) of any sequence: they size
  * the launch; a sequence beyond them gets wrong values, but no access is out of bounds.
  * n_rows bounds d_row0[n_seqs].  The workspace of dllm_attention_paged_ws() bytes is the
  * caller's; calls that may overlap, and captured graphs that may, need one each.  E_INVAL for
  * NULL pointers, sizes out of range, pointers or row strides that are not multiples of
- * 16 bytes (integer arrays: 4); E_DTYPE for another type or head_dim (32, 64, 128; 32 only
- * DLLM_F32); E_CAPACITY for a workspace too small. */
+ * 16 bytes (integer arrays: 4), and where max_len exceeds 2^30 or the launch 2^32 threads;
+ * E_DTYPE for another type or head_dim (32, 64, 128; 32 only DLLM_F32); E_CAPACITY for a
+ * workspace too small. */
 typedef struct dllm_attn_args {
     int32_t dtype;
     int32_t n_rows;

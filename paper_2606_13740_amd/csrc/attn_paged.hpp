@@ -99,6 +99,47 @@ template <bool F32, int RT> __device__ __forceinline__ int swz_v(int dim) {
     return F32 ? dim & 7 : (RT == 32 ? ((dim >> 1) & 3) ^ ((dim >> 4) & 1) : (dim >> 1) & 3);
 }
 
+// Classes of V's elements, in the element type: what is not finite, so that sums of up to 64 of them tell
+// which there are (0, 1 a +inf, 128 a -inf, 16384 a NaN: exact in every type and in an fp32 sum).
+template <typename T> struct PagedClass;
+template <> struct PagedClass<_Float16> { static constexpr uint32_t exp = 0x7C00u, one = 0x3C00u, c128 = 0x5800u, c16384 = 0x7400u; };
+template <> struct PagedClass<__bf16> { static constexpr uint32_t exp = 0x7F80u, one = 0x3F80u, c128 = 0x4300u, c16384 = 0x4680u; };
+template <> struct PagedClass<float> { static constexpr uint32_t exp = 0x7F800000u, one = 0x3F800000u, c128 = 0x43000000u, c16384 = 0x46800000u; };
+// f of every element's bits
+template <typename T, typename F> __device__ __forceinline__ u32x4_t map_elems(const u32x4_t& v, F f) {
+    u32x4_t out;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) out[i] = sizeof(T) == 4 ? f(v[i]) : f(v[i] & 0xFFFFu) | (f(v[i] >> 16) << 16);
+    return out;
+}
+template <typename T> __device__ __forceinline__ u32x4_t finite_or_zero(const u32x4_t& v) {
+    return map_elems<T>(v, [](uint32_t e) { return (e & PagedClass<T>::exp) == PagedClass<T>::exp ? 0u : e; });
+}
+template <typename T> __device__ __forceinline__ u32x4_t class_of(const u32x4_t& v) {
+    using C = PagedClass<T>;
+    constexpr uint32_t sign = sizeof(T) == 4 ? 0x80000000u : 0x8000u;
+    return map_elems<T>(v, [](uint32_t e) {
+        const uint32_t inf = (e & sign) != 0 ? C::c128 : C::one, nan = (e & (C::exp ^ (sign - 1))) != 0 ? C::c16384 : inf;
+        return (e & C::exp) == C::exp ? nan : 0u;
+    });
+}
+template <typename T> __device__ __forceinline__ bool any_odd(const u32x4_t& v) {
+    const u32x4_t c = v ^ finite_or_zero<T>(v);
+    return (c[0] | c[1] | c[2] | c[3]) != 0;
+}
+// o with a sum of classes added
+__device__ __forceinline__ float add_classes(float o, float c) {
+    const int n = (int)c, pos = n & 127, neg = (n >> 7) & 127;
+    if (n >= 16384 || (pos && neg)) return __builtin_nanf("");
+    return pos ? o + INFINITY : (neg ? o - INFINITY : o);
+}
+
+// An output: finite sums saturate in fp16 (rounded probabilities can carry a mean of values near the largest past
+// it), infinities stay.
+template <typename T> __device__ __forceinline__ T attn_out(float o) {
+    return __builtin_fabsf(o) == INFINITY ? (T)o : elem_from_f32<T>(o);
+}
+
 constexpr int MAX_ATTN_SPLITS = 64;           // key splits of a part
 
 // log2-domain slack of the lazily moved reference: probabilities <= 2^8 (fits fp16)
@@ -223,8 +264,11 @@ attn_paged_kernel(PagedArgs a) {
             }
         }
     };
-    // zero the V^T values of keys >= end in the slots of a block that this wave staged
-    auto zero_tail = [&](int k0, int end, char* sub) {
+    // In the slots of a block that this wave staged, zeroes for the V^T values of keys >= end, and for the
+    // infinities and NaNs of those from kz on: a key that one row of the workgroup sees and another
+    // does not, whose probability of 0 would not silence them.  Returns whether there were any.
+    auto clean_tail = [&](int k0, int end, int kz, char* sub) {
+        bool any = false;
         char* base = sub + KPLANE;
 #pragma unroll
         for (int j = 0; j < (KI + QG - 1) / QG; ++j) {
@@ -233,7 +277,7 @@ attn_paged_kernel(PagedArgs a) {
             const int dim = (i * 64 + lane) / VC, pc = lane % VC;
             const int sw = swz_v<F32, RT>(dim);
             const int key = k0 + (16 / ES) * (pc ^ sw);             // the slot's first key
-            if (key + 16 / ES <= end) continue;
+            if (key + 16 / ES <= end && key < kz) continue;
             u32x4_t* slot = (u32x4_t*)(base + i * 1024 + lane * 16);
             u32x4_t v = *slot;
 #pragma unroll
@@ -241,8 +285,13 @@ attn_paged_kernel(PagedArgs a) {
                 if (F32) v[e] = key + e >= end ? 0u : v[e];
                 else v[e] &= (key + 2 * e >= end ? 0u : 0x0000FFFFu) | (key + 2 * e + 1 >= end ? 0u : 0xFFFF0000u);
             }
+            if (key >= kz) {
+                any |= any_odd<T>(v);
+                v = finite_or_zero<T>(v);
+            }
             *slot = v;
         }
+        return __builtin_amdgcn_ballot_w64(any);
     };
 
     const int most = min(SUB * bps, ((ke - ks + 31) >> 5) - kb0);      // blocks of the split, at most
@@ -279,18 +328,28 @@ attn_paged_kernel(PagedArgs a) {
         }
         lim = row_limit(f);
     }
-    // The largest limit of the tile's rows ends its keys: what lies behind may be anything.
-    int ktop = ks;
+    // The largest limit of the tile's rows ends its keys: what lies behind may be anything.  Keys from the
+    // smallest on (kz: its 16-byte slot of V^T) are seen by some rows only.
+    int ktop = ks, lim_lo;
     if (a.lim == nullptr && (own || short_len >= ke)) {
-        ktop = max(ks, ke);
+        lim_lo = ktop = max(ks, ke);
     } else {
+        lim_lo = 0x7FFFFFFF;
 #pragma unroll
-        for (int i = 0; i < (TM + 63) / 64; ++i)
-            if (lane + 64 * i < TM) ktop = max(ktop, row_limit(min(f0 + lane + 64 * i, nv - 1)));
+        for (int i = 0; i < (TM + 63) / 64; ++i) {
+            const int n = row_limit(min(f0 + (TM < 64 ? lane % TM : lane) + 64 * i, nv - 1));
+            ktop = max(ktop, n);
+            lim_lo = min(lim_lo, n);
+        }
 #pragma unroll
-        for (int o = 32; o > 0; o >>= 1) ktop = max(ktop, __shfl_xor(ktop, o));
+        for (int o = 32; o > 0; o >>= 1) {
+            ktop = max(ktop, __shfl_xor(ktop, o));
+            lim_lo = min(lim_lo, __shfl_xor(lim_lo, o));
+        }
         ktop = __builtin_amdgcn_readfirstlane(ktop);
+        lim_lo = min(ktop, max(ks, __builtin_amdgcn_readfirstlane(lim_lo)));
     }
+    const int kz = lim_lo == ktop ? 0x7FFFFFFF : lim_lo & ~(16 / ES - 1);
     const int blocks = max(0, min((ktop - ks + 31) >> 5, kb0 + SUB * bps) - kb0);
     const int rounds = (blocks + SUB - 1) / SUB;
     auto chunk_have = [&](int n) { return __builtin_amdgcn_ballot_w64(pgv >= 0 && 64 * n + lane < blocks); };
@@ -324,6 +383,7 @@ attn_paged_kernel(PagedArgs a) {
     // no scalar load outstanding past here: the compiler does not see the waits in the loop's
     // asm and would otherwise wait for all LDS reads at each use
     __builtin_amdgcn_s_waitcnt(0xC07F);
+    uint64_t odd = 0;
     // a wave without rows of its own only stages
     const bool busy = f0 + RT * qw < nv;
     for (int t = 0; t < rounds; ++t) {
@@ -336,11 +396,11 @@ attn_paged_kernel(PagedArgs a) {
         // This wave's loads of step t have landed once at most LPW of the step staged after it are
         // outstanding (loads complete in issue order; a chunk's pages wait for all); the barrier makes
         // every wave's visible and frees the buffer that round t - 1 read.
-        if (!whole || k0 + 32 * SUB > ktop) {
+        if (!whole || k0 + 32 * SUB > lim_lo) {
             asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
 #pragma unroll
             for (int u = 0; u < SUB; ++u)
-                zero_tail(k0 + 32 * u, (there >> u) & 1 ? ktop : 0, lds + cur * BUF + u * SBUF);
+                odd |= clean_tail(k0 + 32 * u, (there >> u) & 1 ? ktop : 0, kz, lds + cur * BUF + u * SBUF);
         }
         if (NB > 2 && t + 1 < rounds) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(LPW) : "memory");
         else asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
@@ -464,6 +524,45 @@ attn_paged_kernel(PagedArgs a) {
                 for (int dt = 0; dt < ND; ++dt) oacc[dt] = E::mfma(vf[w][dt][u], pf[w][u], oacc[dt]);
     }
 
+    // What clean_tail took out, for the rows that see it: sums of classes over each block's keys, V^T
+    // straight from its page (a fragment's 16 bytes are consecutive keys of a dim).
+    if (lim_lo < ktop) {
+        __syncthreads();                                                // (the last round's reads)
+        if (lane == 0) ((int*)lds)[qw] = odd != 0;
+        __syncthreads();
+        int any = 0;
+#pragma unroll
+        for (int w = 0; w < QG; ++w) any |= ((const int*)lds)[w];
+        odd = __builtin_amdgcn_readfirstlane(any);
+    }
+    if (odd != 0) {
+        for (int blk = kz > ks + 32 * kb0 ? (kz - ks) / 32 - kb0 : 0; blk < blocks; ++blk) {
+            const int k0 = ks + 32 * (kb0 + blk), pg = trow[k0 >> a.page_shift];
+            if (pg < 0 || pg >= a.n_pages) continue;
+            const T* Vp = (const T*)a.vp + ((long)pg * a.Hk + hk) * page_elems + (k0 & ((1 << a.page_shift) - 1));
+#pragma unroll
+            for (int dt = 0; dt < ND; ++dt) {
+                Acc c;
+#pragma unroll
+                for (int i = 0; i < NA; ++i) c[i] = 0.f;
+#pragma unroll
+                for (int u = 0; u < NV; ++u) {
+                    const u32x4_t v = ldg16(Vp + ((long)(RT * dt + r) << a.page_shift) + (16 / ES) * (NG * u + g));
+                    auto sees = [&](int e) {
+                        const int key = k0 + key_of(16 / ES * u + e);
+                        return key >= kz && key < lim ? PagedClass<T>::one : 0u;
+                    };
+                    u32x4_t seen;
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) seen[i] = F32 ? sees(i) : sees(2 * i) | (sees(2 * i + 1) << 16);
+                    c = E::mfma(class_of<T>(v), seen, c);
+                }
+#pragma unroll
+                for (int i = 0; i < NA; ++i) oacc[dt][i] = add_classes(oacc[dt][i], c[i]);
+            }
+        }
+    }
+
     float l = lrun + __shfl_xor(lrun, 32);
     if constexpr (!R32) l += __shfl_xor(l, 16);
     const int f = f0 + RT * qw + r;
@@ -472,7 +571,7 @@ attn_paged_kernel(PagedArgs a) {
     // (accumulators 4j .. 4j + 3 are consecutive dims)
     auto dim_of = [&](int dt, int j) { return RT * dt + (R32 ? 8 * j + 4 * g : 4 * g); };
     if (a.direct) {
-        const float inv = l > 0.f ? 1.f / l : 0.f;
+        const float inv = l != 0.f ? 1.f / l : 0.f;          // (a NaN stays one)
         T* op = (T*)a.out + row * a.ld_out + h * DH;
 #pragma unroll
         for (int dt = 0; dt < ND; ++dt)
@@ -480,7 +579,7 @@ attn_paged_kernel(PagedArgs a) {
             for (int j = 0; j < NA / 4; ++j) {
                 T e[4];
 #pragma unroll
-                for (int i = 0; i < 4; ++i) e[i] = elem_from_f32<T>(oacc[dt][4 * j + i] * inv);
+                for (int i = 0; i < 4; ++i) e[i] = attn_out<T>(oacc[dt][4 * j + i] * inv);
                 __builtin_memcpy(__builtin_assume_aligned(op + dim_of(dt, j), 4 * ES), e, sizeof(e));
             }
     } else {
@@ -534,7 +633,7 @@ __global__ void __launch_bounds__(256) attn_paged_merge_kernel(PagedArgs a) {
     for (int o = 1; o < LPP; o <<= 1) M = fmaxf(M, __shfl_xor(M, o));
 #pragma unroll
     for (int i = 0; i < MAXW; ++i) {
-        m[i] = l[i] > 0.f ? exp2f(m[i] - M) : 0.f;                     // the part's weight
+        m[i] = l[i] != 0.f ? exp2f(m[i] - M) : 0.f;                    // the part's weight (a NaN sum stays one)
         L += l[i] * m[i];
     }
 #pragma unroll
@@ -552,9 +651,8 @@ __global__ void __launch_bounds__(256) attn_paged_merge_kernel(PagedArgs a) {
         }
     }
     if (R0 + pair / a.H >= R1) return;
-    const float inv = L > 0.f ? 1.f / L : 0.f;
-    T e[4] = {elem_from_f32<T>(o.x * inv), elem_from_f32<T>(o.y * inv), elem_from_f32<T>(o.z * inv),
-              elem_from_f32<T>(o.w * inv)};
+    const float inv = L != 0.f ? 1.f / L : 0.f;
+    T e[4] = {attn_out<T>(o.x * inv), attn_out<T>(o.y * inv), attn_out<T>(o.z * inv), attn_out<T>(o.w * inv)};
     __builtin_memcpy(__builtin_assume_aligned((T*)a.out + row * a.ld_out + h * DH + 4 * li, 4 * sizeof(T)), e, sizeof(e));
 }
 

@@ -51,6 +51,9 @@ bool row_stride_ok(const void* p, int64_t ld, int64_t width, int es) {
     return aligned(p, 16) && ld >= width && ld <= (1ll << 40) && (ld * es) % 16 == 0;
 }
 
+// A launch has fewer than 2^32 threads (here with a workgroup to spare).
+bool grid_ok(long wgs, int threads) { return wgs < ((1l << 32) - 1024) / threads; }
+
 constexpr int MAX_BATCH_ROWS = 1 << 24;
 constexpr int N_CU = 256;
 
@@ -93,15 +96,21 @@ namespace {
 
 // Heads a lane group takes one after another: as many as leave 16384 groups (eight waves for every CU's
 // worth of 8-lane groups), at most eight.
+int qk_heads_per(long T, int H, int Hk) { return (int)std::min<long>(8, std::max<long>(1, T * (H + Hk) / 16384)); }
+// Workgroups for Q and K, and with those for V.
+long qk_wgs(long T, int H, int Hk, int Dh) {
+    const int hp = qk_heads_per(T, H, Hk), per_wg = 256 / (Dh / 16);
+    return (T * (ceil_div(H, hp) + ceil_div(Hk, hp)) + per_wg - 1) / per_wg;
+}
+long qk_grid(long T, int H, int Hk, int Dh) { return qk_wgs(T, H, Hk, Dh) + (long)ceil_div(T, QK_VROWS) * Hk; }
+
 template <typename T>
 void launch_qk(const QkArgs& a, int Dh, hipStream_t s) {
-    const int hp = (int)std::min<long>(8, std::max<long>(1, (long)a.T * (a.H + a.Hk) / 16384));
-    const long groups = (long)a.T * (ceil_div(a.H, hp) + ceil_div(a.Hk, hp));
-    const int qk_wgs = ceil_div(groups, 256 / (Dh / 16));
-    const dim3 grid((unsigned)(qk_wgs + (long)ceil_div(a.T, QK_VROWS) * a.Hk));
-    if (Dh == 128) hipLaunchKernelGGL((qk_norm_rope_kernel<T, 128>), grid, dim3(256), 0, s, a, qk_wgs, hp);
-    else if (Dh == 64) hipLaunchKernelGGL((qk_norm_rope_kernel<T, 64>), grid, dim3(256), 0, s, a, qk_wgs, hp);
-    else hipLaunchKernelGGL((qk_norm_rope_kernel<T, 32>), grid, dim3(256), 0, s, a, qk_wgs, hp);
+    const int hp = qk_heads_per(a.T, a.H, a.Hk), wgs = (int)qk_wgs(a.T, a.H, a.Hk, Dh);
+    const dim3 grid((unsigned)qk_grid(a.T, a.H, a.Hk, Dh));
+    if (Dh == 128) hipLaunchKernelGGL((qk_norm_rope_kernel<T, 128>), grid, dim3(256), 0, s, a, wgs, hp);
+    else if (Dh == 64) hipLaunchKernelGGL((qk_norm_rope_kernel<T, 64>), grid, dim3(256), 0, s, a, wgs, hp);
+    else hipLaunchKernelGGL((qk_norm_rope_kernel<T, 32>), grid, dim3(256), 0, s, a, wgs, hp);
 }
 
 // Launch of an attention call.  Both parts (the shared prefix for all rows, and the sequences' own
@@ -178,8 +187,8 @@ int check_attn(const dllm_attn_args* g, int& shift) {
     if ((shift = page_shift(g->page, g->n_pages)) < 0) return DLLM_E_INVAL;
     if (g->table_ld < 1 || (long)g->table_ld * g->page >= (1l << 31))
         return fail(DLLM_E_INVAL, "table_ld must be >= 1 and table_ld * page < 2^31");
-    if (g->max_len < 0 || g->max_len > g->table_ld * g->page)
-        return fail(DLLM_E_INVAL, "max_len must be in [0, table_ld * page]");
+    if (g->max_len < 0 || g->max_len > std::min(g->table_ld * g->page, 1 << 30))
+        return fail(DLLM_E_INVAL, "max_len must be in [0, table_ld * page] and at most 2^30");
     if (g->max_rows < 0) return fail(DLLM_E_INVAL, "max_rows must be >= 0");
     if (g->shared_len < 0 || g->shared_len % g->page != 0 || g->shared_len > g->table_ld * g->page)
         return fail(DLLM_E_INVAL, "shared_len must be a multiple of page in [0, table_ld * page]");
@@ -187,7 +196,7 @@ int check_attn(const dllm_attn_args* g, int& shift) {
     if ((long)g->n_rows * (g->n_heads / g->n_kv_heads) >= (1l << 31))
         return fail(DLLM_E_INVAL, "n_rows times the query heads of a K/V head must be < 2^31");
     const AttnPlan p = attn_plan(g);
-    if (p.wgs_s + p.wgs_o > 0x7FFFFFFF || (long)g->n_rows * g->n_heads > 0x7FFFFFFF)
+    if (!grid_ok(p.wgs_s + p.wgs_o, p.qg * 64) || !grid_ok((long)g->n_rows * g->n_heads, g->head_dim / 4))
         return fail(DLLM_E_INVAL, "n_seqs, max_rows and n_rows need too many workgroups");
     return DLLM_OK;
 }
@@ -273,6 +282,8 @@ int dllm_qk_norm_rope(const dllm_qk_args* g, dllm_stream stream) {
         !aligned(g->d_slot, 4))
         return fail(DLLM_E_INVAL, "pointers must be 16-byte aligned (integer arrays: 4)");
     if (g->d_q_out == g->d_q && g->ld_q != wq) return fail(DLLM_E_INVAL, "q_out may be q only if q is contiguous");
+    if (!grid_ok(qk_grid(g->n_rows, g->n_heads, g->n_kv_heads, g->head_dim), 256))
+        return fail(DLLM_E_INVAL, "n_rows and n_heads need too many workgroups");
     if (g->n_rows == 0) return DLLM_OK;
     QkArgs a{g->d_q, g->d_k, g->d_v, g->ld_q, g->ld_k, g->ld_v, g->d_q_gain, g->d_k_gain, (const float2*)g->d_rope,
              g->d_pos, g->d_slot, g->d_q_out, g->d_k_pages, g->d_v_pages, g->n_rows, g->n_heads, g->n_kv_heads, shift,
@@ -367,7 +378,7 @@ int dllm_select(const dllm_select_args* g, dllm_stream stream) {
         if (!aligned(p, 4)) return fail(DLLM_E_INVAL, "arrays of 32-bit values must be 4-byte aligned");
     if (g->n_rows == 0) return DLLM_OK;
     const size_t need = select_ws_bytes(g);
-    if ((long)select_ranges(g->vocab) * ceil_div(g->n_rows, 2) > 0x7FFFFFFF)
+    if (!grid_ok((long)select_ranges(g->vocab) * ceil_div(g->n_rows, select_rows_per(g->n_rows, select_ranges(g->vocab))), SEL_NT))
         return fail(DLLM_E_INVAL, "n_rows and vocab need too many workgroups");
     if (need > 0 && (!g->d_ws || !aligned(g->d_ws, 16))) return fail(DLLM_E_INVAL, "workspace: NULL or not 16-byte aligned");
     if (need > g->ws_bytes)

@@ -41,7 +41,7 @@ __device__ __forceinline__ PlanSum operator+(const PlanSum& a, const PlanSum& b)
 //
 // What bounds it: launch and the chain of dependent loads (lengths, scan, table or stack
 // entry, slot): 4.7 us for 4 sequences of one row, 8.1 for 2048 of 32 (9.4 where each workgroup did
-// its share of both kinds, one after the other), of which an empty launch is 2 to 3.
+// its share of both kinds, one after the other).
 constexpr int PLAN_NT = 512;
 constexpr int PLAN_MAXB = 4096;
 __global__ void __launch_bounds__(PLAN_NT) batch_plan_kernel(PlanArgs a, int row_wgs) {

@@ -124,11 +124,17 @@ def test_workspace_is_checked(dl):
 
 
 @pytest.mark.parametrize("change", [dict(n_rows=1 << 24, n_heads=1024, n_kv_heads=1, ld_q=1 << 16, ld_out=1 << 16),
-                                    dict(n_seqs=4096, max_rows=1 << 24, n_rows=1 << 24, n_heads=32, n_kv_heads=32, ld_q=2048, ld_out=2048)])
+                                    dict(n_seqs=4096, max_rows=1 << 24, n_rows=1 << 24, n_heads=32, n_kv_heads=32, ld_q=2048, ld_out=2048),
+                                    dict(table_ld=1 << 25, max_len=(1 << 30) + 1), dict(n_rows=1 << 24, max_rows=1, n_heads=512, n_kv_heads=64, ld_q=1 << 16, ld_out=1 << 16)])
 def test_attention_refuses_launches_past_the_grid(dl, change):
     a, n = fill(dl.dllm_attn_args, **dict(ATTN, **change)), ctypes.c_size_t()
     assert dl.lib().dllm_attention_paged_ws(ctypes.byref(a), ctypes.byref(n)) == dl.DLLM_E_INVAL
     assert dl.lib().dllm_attention_paged(ctypes.byref(a), None) == dl.DLLM_E_INVAL
+
+
+def test_qk_refuses_launches_past_the_grid(dl):
+    wide = dict(n_rows=1 << 24, n_heads=1024, n_kv_heads=1024, ld_q=1 << 16, ld_k=1 << 16, ld_v=1 << 16)
+    assert dl.lib().dllm_qk_norm_rope(ctypes.byref(fill(dl.dllm_qk_args, **dict(QK, **wide))), None) == dl.DLLM_E_INVAL
 
 
 def test_binding_refuses_tensors_that_are_not_on_the_gpu(dl):

@@ -284,6 +284,80 @@ def test_attention_ignores_what_it_must_not_see(dl, dtype):
     check_attn(dl, c, dtype)
 
 
+def run_attn(dl, c, lim):
+    import torch
+    out = torch.full_like(c["qt"], 7.0)
+    dl.dllm_attention_paged(c["qt"], c["kt"], c["vt"], i32(c["table"]), i32(c["row0"]), i32(c["lens"]), out, max(c["rows"]),
+                            int(max(c["lens"])), shared_len=c["shared"], lim=i32(lim))
+    torch.cuda.synchronize()
+    return out.float().cpu().numpy()
+
+
+@pytest.mark.parametrize("dtype,rows,lens,H,Hk,D,shared", [
+    ("f32", [1, 9, 30], [40, 70, 131], 4, 2, 32, 0), ("f32", [20, 25], [300, 250], 2, 1, 128, 64),
+    ("f16", [1, 8], [64, 200], 2, 2, 64, 0), ("f16", [40, 33, 5], [300, 271, 100], 4, 2, 128, 128),
+    ("bf16", [30], [190], 4, 4, 128, 0), ("bf16", [20, 64, 3], [130, 400, 60], 8, 2, 64, 128),
+    ("f16", [64] * 8, [4200] * 7 + [4100], 28, 4, 128, 4096), ("bf16", [64] * 8, [4200] * 7 + [1500], 56, 8, 64, 4096)])
+def test_attention_infinities_and_nans_that_only_some_rows_see(dl, dtype, rows, lens, H, Hk, D, shared):
+    """Causal rows over V with a few infinities and NaNs (the last two cases: 128-row tiles).  Rows that see such a value
+    get what a sum with it is; everything else keeps the bits it has with zeros in these places."""
+    rng = np.random.default_rng(21)
+    c = attn_case(rng, dtype, rows, lens, H, Hk, D, 32, shared)
+    lim = np.concatenate([np.arange(n - w + 1, n + 1) for w, n in zip(rows, lens)] + [[1, 1]])
+    spots = []                                          # (sequences, position, K/V head, dim, value)
+    for b, (w, n) in enumerate(zip(rows, lens)):
+        for p in rng.integers(max(n - w - 3, min(shared, n - 1)), n, 5):
+            spots.append(([b], int(p), int(rng.integers(Hk)), int(rng.integers(D)), [np.inf, -np.inf, np.nan][rng.integers(3)]))
+        spots += [([b], n - 1, 0, 3, np.inf), ([b], max(n - 2, 0), 0, 3, -np.inf)]
+    if shared:                                          # sequences that end inside the shared part see less of it
+        short = min(lens)
+        spots += [([b for b in range(len(rows))], p, 0, 1, -np.inf) for p in (shared - 1, min(short, shared - 1), 0)]
+    want_class = np.zeros((3, sum(rows), H, D), bool)   # +inf, -inf, NaN
+    for clean in (True, False):
+        for seqs, p, hk, d, x in spots:
+            b = seqs[0] if p >= shared else 0
+            if p < lens[b] or p < shared:
+                page = c["table"][b, p // 32] if p >= shared else c["table"][0, p // 32]
+                c["vt"][int(page), hk, d, p % 32] = 0.0 if clean else x
+        if clean:
+            base = run_attn(dl, c, lim)
+    got = run_attn(dl, c, lim)
+    for seqs, p, hk, d, x in spots:
+        for b in seqs if p >= shared else range(len(rows)):
+            for r in range(c["row0"][b], c["row0"][b + 1]):
+                if p < min(lim[r], lens[b]):
+                    cls = 2 if np.isnan(x) else int(x < 0)
+                    want_class[cls, r, hk * (H // Hk):(hk + 1) * (H // Hk), d] = True
+    pos, neg, nan = want_class
+    nan = nan | (pos & neg)
+    T = sum(rows)
+    assert np.isfinite(base).all() and pos.any() and neg.any()
+    assert (np.isnan(got[:T]) == nan).all()
+    assert (got[:T][pos & ~nan] == np.inf).all() and (got[:T][neg & ~nan] == -np.inf).all()
+    plain = ~(pos | neg | nan)
+    assert plain.any() and (got[:T][plain] == base[:T][plain]).all() and (got[T:] == 7.0).all()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+def test_attention_nan_keys(dl, dtype):
+    """A NaN in K: NaN for the rows that see the key, in one part of the keys or all, and nothing for the others."""
+    rng = np.random.default_rng(22)
+    rows, lens = [30, 20], [230, 1100]
+    c = attn_case(rng, dtype, rows, lens, 4, 2, 64, 32, 0)
+    lim = np.concatenate([np.arange(n - w + 1, n + 1) for w, n in zip(rows, lens)] + [[1, 1]])
+    ref = attention(c["q"], c["kp"], c["vp"], c["table"], c["row0"], c["lens"], lim, 0, 32, 64 ** -0.5, dtype)
+    for b, p in ((0, 215), (1, 1090)):
+        c["kt"][int(c["table"][b, p // 32]), 0, p % 32, 5] = float("nan")
+    got = run_attn(dl, c, lim)
+    for r, (o, bound) in ref.items():
+        sees = lim[r] > (215 if r < 30 else 1090)
+        for h in range(4):
+            if sees and h < 2:
+                assert np.isnan(got[r, h]).all(), (r, h)
+            else:
+                assert (abs(got[r, h] - o[h]) <= bound[h] + 1e-30).all(), (r, h)
+
+
 @pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
 def test_attention_no_keys_at_all(dl, dtype):
     c = attn_case(np.random.default_rng(11), dtype, [3, 2], [0, 40], 2, 2, 64, 32, 0)
