@@ -145,14 +145,20 @@ constexpr int MAX_ATTN_SPLITS = 64;           // key splits of a part
 // log2-domain slack of the lazily moved reference: probabilities <= 2^8 (fits fp16)
 constexpr float PAGED_SLACK = 8.f;
 
-// Workgroup = (part, K/V head, key split, tile of QG x RT virtual rows), QG waves of an RT-row
-// tile.  The split's 32-key blocks are staged in LDS with direct global->LDS loads
-// in a ring of NB buffers and read from there by all waves.  LDS rows are swizzled in 16-byte
-// columns so that the 16 rows of a fragment read lie in different banks.  Lane i holds the
-// page of block 64 n + i, so a block's page is one lane read.
-template <typename T, int DH, int QG, int RT, int NB, int SUB>
-__global__ void __launch_bounds__(QG * 64)
-__attribute__((amdgpu_waves_per_eu(QG * (160 * 1024 / (NB * SUB * 64 * DH * (int)sizeof(T))) >= 8 ? 2 : 1)))
+// Workgroup = (part, K/V head, key split, tile of QG x RT virtual rows): QG row tiles of KG waves each.
+// A step is SUB blocks of 32 keys, which direct global->LDS loads stage in one of two buffers while
+// the other is read; a row tile's waves take SUB / KG of the blocks each and join at the end.
+// LDS rows are swizzled in 16-byte columns so that the lanes of an LDS cycle read distinct banks (no conflicts
+// counted).  Lane i holds the page of block 64 n + i, so a block's page is one lane read.
+//
+// What bounds it: many rows, the chain of products and exponentials of the two waves that a SIMD holds
+// (16 sequences of 64 rows, 28 heads over 4, behind 16384 bf16 keys: 136 us and 9 for the merge, 900
+// TFLOP/s where a large library product reaches 1100); rows enough for the prefix only, LDS reads and the K/V
+// themselves (8 x 32 rows of 32 fp16 heads behind 4096: 37 us and 6, 115 MB); few rows, latency (8 x 1 rows
+// behind 1564: 9.6 us and 4.6).
+template <typename T, int DH, int QG, int RT, int KG, int SUB>
+__global__ void __launch_bounds__(QG * KG * 64)
+__attribute__((amdgpu_waves_per_eu(QG * KG * (160 * 1024 / (2 * SUB * 64 * DH * (int)sizeof(T))) >= 8 ? 2 : 1)))
 attn_paged_kernel(PagedArgs a) {
     using E = PagedElem<T>;
     constexpr bool F32 = sizeof(T) == 4;
@@ -171,14 +177,16 @@ attn_paged_kernel(PagedArgs a) {
     constexpr int VC = 32 * ES / 16;          // and of a dim's row of V^T
     constexpr int KPLANE = 32 * DH * ES, SBUF = 2 * KPLANE, BUF = SUB * SBUF;
     constexpr int KI = KPLANE / 1024;         // 1 KiB wave loads per plane
-    constexpr int LPW = SUB * 2 * (KI / QG);  // loads each wave issues per staged step, at least
-    static_assert(64 % SUB == 0, "a step's pages lie in one chunk");
+    constexpr int NW = QG * KG;               // waves
+    constexpr int SW = SUB / KG;              // blocks of a step per wave
+    static_assert(64 % SUB == 0 && SUB % KG == 0, "a step's pages lie in one chunk, its blocks are dealt evenly");
     constexpr int TM = RT * QG;               // virtual rows of a workgroup
     static_assert(KI * 1024 == KPLANE, "planes must be whole wave loads");
     static_assert(TM <= 256, "at most four virtual rows per lane");
-    __shared__ __attribute__((aligned(1024))) char lds[NB * BUF];
+    __shared__ __attribute__((aligned(1024))) char lds[2 * BUF];
 
-    const int lane = threadIdx.x & 63, qw = QG == 1 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int lane = threadIdx.x & 63, wave = NW == 1 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int qw = wave % QG, kw = wave / QG;  // row tile, and the step's blocks that are this wave's
     const int r = lane % RT, g = lane / RT;
 
     // Which item.  The dispatcher deals consecutive workgroups to the 8 XCDs in turn; XCD x
@@ -217,9 +225,8 @@ attn_paged_kernel(PagedArgs a) {
     }
     const int kb0 = SUB * split * bps;        // the split's first 32-key block
 
-    // Pages of the 64 blocks of a chunk: lane i has block 64 n + i's (-1: no page).  Blocks are staged
-    // up to NB - 1 steps ahead of their use, so the chunk before keeps a bit a block: whether it
-    // has a page.  The first chunk, and with it the first step's K/V, is asked for before the
+    // Pages of the 64 blocks of a chunk: lane i has block 64 n + i's (-1: no page), and `have` a
+    // bit a block.  The first chunk, and with it the first step's K/V, is asked for before the
     // rows and their limits are known (a table row has table_ld entries whatever the length).
     const int* trow = a.table + (size_t)b * a.table_ld;
     auto chunk_pages = [&](int n) {
@@ -235,7 +242,7 @@ attn_paged_kernel(PagedArgs a) {
     if (f0 >= nv) return;
 
     // Stage step t: wave load i of a plane is its bytes [1024 i, 1024 i + 1024), taken by wave
-    // i % QG.  A block without a page is staged from page 0 (and not used).
+    // i % NW.  A block without a page is staged from page 0 (and not used).
     auto stage = [&](int t, int buf) {
 #pragma unroll
         for (int u = 0; u < SUB; ++u) {
@@ -247,17 +254,17 @@ attn_paged_kernel(PagedArgs a) {
             const T* Vp = (const T*)a.vp + head;
             char* base = lds + buf * BUF + u * SBUF;
 #pragma unroll
-            for (int j = 0; j < (KI + QG - 1) / QG; ++j) {
-                const int i = qw + j * QG;
-                if (KI % QG != 0 && i >= KI) break;
+            for (int j = 0; j < (KI + NW - 1) / NW; ++j) {
+                const int i = wave + j * NW;
+                if (KI % NW != 0 && i >= KI) break;
                 const int key = (i * 64 + lane) / KC, pc = lane % KC;
                 const int sw = F32 ? key & 15 : swz_paged(key);
                 buffer_to_lds16(Kp, key * (DH * ES) + ((pc ^ (sw & (KC - 1))) << 4), off * (DH * ES), base + i * 1024);
             }
 #pragma unroll
-            for (int j = 0; j < (KI + QG - 1) / QG; ++j) {
-                const int i = qw + j * QG;
-                if (KI % QG != 0 && i >= KI) break;
+            for (int j = 0; j < (KI + NW - 1) / NW; ++j) {
+                const int i = wave + j * NW;
+                if (KI % NW != 0 && i >= KI) break;
                 const int dim = (i * 64 + lane) / VC, pc = lane % VC;
                 const int sw = swz_v<F32, RT>(dim);
                 buffer_to_lds16(Vp, ((dim << a.page_shift) * ES) + ((pc ^ sw) << 4), off * ES, base + KPLANE + i * 1024);
@@ -271,9 +278,9 @@ attn_paged_kernel(PagedArgs a) {
         bool any = false;
         char* base = sub + KPLANE;
 #pragma unroll
-        for (int j = 0; j < (KI + QG - 1) / QG; ++j) {
-            const int i = qw + j * QG;
-            if (KI % QG != 0 && i >= KI) break;
+        for (int j = 0; j < (KI + NW - 1) / NW; ++j) {
+            const int i = wave + j * NW;
+            if (KI % NW != 0 && i >= KI) break;
             const int dim = (i * 64 + lane) / VC, pc = lane % VC;
             const int sw = swz_v<F32, RT>(dim);
             const int key = k0 + (16 / ES) * (pc ^ sw);             // the slot's first key
@@ -353,11 +360,7 @@ attn_paged_kernel(PagedArgs a) {
     const int blocks = max(0, min((ktop - ks + 31) >> 5, kb0 + SUB * bps) - kb0);
     const int rounds = (blocks + SUB - 1) / SUB;
     auto chunk_have = [&](int n) { return __builtin_amdgcn_ballot_w64(pgv >= 0 && 64 * n + lane < blocks); };
-    uint64_t have = chunk_have(0), have_before = 0;
-
-#pragma unroll
-    for (int j = 1; j < NB - 1; ++j)
-        if (j < rounds) stage(j, j);
+    uint64_t have = chunk_have(0);
 
     // smallest limit of the wave's rows: blocks below it need no per-key mask
     int lim_w = ktop;
@@ -387,39 +390,34 @@ attn_paged_kernel(PagedArgs a) {
     // a wave without rows of its own only stages
     const bool busy = f0 + RT * qw < nv;
     for (int t = 0; t < rounds; ++t) {
-        const int cur = t % NB;
-        const int k0 = ks + 32 * (kb0 + SUB * t);
-        // which blocks have a page (the chunk moves on with the step staged in the round before)
-        const bool before = ((SUB * t) >> 6) != ((SUB * min(t + NB - 2, rounds - 1)) >> 6);
-        const uint32_t there = (uint32_t)((before ? have_before : have) >> ((SUB * t) & 63)) & ((1u << SUB) - 1);
+        const int k0 = ks + 32 * (kb0 + SUB * t), k0w = k0 + 32 * kw * SW;
+        char* cur = lds + (t & 1) * BUF;
+        const uint32_t there = (uint32_t)(have >> ((SUB * t) & 63)) & ((1u << SUB) - 1);      // which blocks have a page
         const bool whole = there == (1u << SUB) - 1;
-        // This wave's loads of step t have landed once at most LPW of the step staged after it are
-        // outstanding (loads complete in issue order; a chunk's pages wait for all); the barrier makes
-        // every wave's visible and frees the buffer that round t - 1 read.
+        // This wave's loads of step t have landed; the barrier makes every wave's visible and frees the buffer
+        // that round t - 1 read, for step t + 1.
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
         if (!whole || k0 + 32 * SUB > lim_lo) {
-            asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
 #pragma unroll
             for (int u = 0; u < SUB; ++u)
-                odd |= clean_tail(k0 + 32 * u, (there >> u) & 1 ? ktop : 0, kz, lds + cur * BUF + u * SBUF);
+                odd |= clean_tail(k0 + 32 * u, (there >> u) & 1 ? ktop : 0, kz, cur + u * SBUF);
         }
-        if (NB > 2 && t + 1 < rounds) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(LPW) : "memory");
-        else asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
-        if (t + NB - 1 < rounds) {
-            if (((SUB * (t + NB - 1)) & 63) == 0) {
-                pgv = chunk_pages((SUB * (t + NB - 1)) >> 6);
-                have_before = have;
-                have = chunk_have((SUB * (t + NB - 1)) >> 6);
+        asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+        if (t + 1 < rounds) {
+            if (((SUB * (t + 1)) & 63) == 0) {
+                pgv = chunk_pages((SUB * (t + 1)) >> 6);
+                have = chunk_have((SUB * (t + 1)) >> 6);
             }
-            stage(t + NB - 1, (t + NB - 1) % NB);
+            stage(t + 1, (t + 1) & 1);
         }
         if (!busy) continue;
 
         // all of the step's K fragments are read before the first product, its V^T fragments between
         // the scores and the softmax, which covers their latency
-        const char* buf = lds + cur * BUF;
-        u32x4_t kf[SUB][NC][NU], vf[SUB][ND][NV];
+        const char* buf = cur + kw * SW * SBUF;
+        u32x4_t kf[SW][NC][NU], vf[SW][ND][NV];
 #pragma unroll
-        for (int w = 0; w < SUB; ++w)
+        for (int w = 0; w < SW; ++w)
 #pragma unroll
             for (int c = 0; c < NC; ++c)
 #pragma unroll
@@ -429,21 +427,21 @@ attn_paged_kernel(PagedArgs a) {
                     kf[w][c][u] = *(const u32x4_t*)(buf + w * SBUF + key * (DH * ES) + (((NG * c + g) ^ (sw & (KC - 1))) << 4));
                 }
         __builtin_amdgcn_sched_barrier(0);
-        Acc s[SUB][NU];
+        Acc s[SW][NU];
 #pragma unroll
-        for (int w = 0; w < SUB; ++w)
+        for (int w = 0; w < SW; ++w)
 #pragma unroll
             for (int u = 0; u < NU; ++u)
 #pragma unroll
                 for (int i = 0; i < NA; ++i) s[w][u][i] = 0.f;
 #pragma unroll
-        for (int w = 0; w < SUB; ++w)
+        for (int w = 0; w < SW; ++w)
 #pragma unroll
             for (int c = 0; c < NC; ++c)
 #pragma unroll
                 for (int u = 0; u < NU; ++u) s[w][u] = E::mfma(kf[w][c][u], qf[c], s[w][u]);
 #pragma unroll
-        for (int w = 0; w < SUB; ++w)
+        for (int w = 0; w < SW; ++w)
 #pragma unroll
             for (int dt = 0; dt < ND; ++dt)
 #pragma unroll
@@ -454,25 +452,25 @@ attn_paged_kernel(PagedArgs a) {
                 }
         __builtin_amdgcn_sched_barrier(0);
 
-        float sv[SUB][NS];
+        float sv[SW][NS];
 #pragma unroll
-        for (int w = 0; w < SUB; ++w)
+        for (int w = 0; w < SW; ++w)
 #pragma unroll
             for (int e = 0; e < NS; ++e) sv[w][e] = s[w][e / NA][e % NA];
-        if (k0 + 32 * SUB > lim_w || !whole) {
+        if (k0w + 32 * SW > lim_w || !whole) {
 #pragma unroll
-            for (int w = 0; w < SUB; ++w) {
-                const int end = (there >> w) & 1 ? lim : 0;
+            for (int w = 0; w < SW; ++w) {
+                const int end = (there >> (kw * SW + w)) & 1 ? lim : 0;
 #pragma unroll
                 for (int e = 0; e < NS; ++e)
-                    if (k0 + 32 * w + key_of(e) >= end) sv[w][e] = -INFINITY;
+                    if (k0w + 32 * w + key_of(e) >= end) sv[w][e] = -INFINITY;
             }
         }
         // the row's maximum over the step and its lane groups (max is symmetric: a swap hands a lane its
         // partner's value)
         float bm = sv[0][0];
 #pragma unroll
-        for (int w = 0; w < SUB; ++w)
+        for (int w = 0; w < SW; ++w)
 #pragma unroll
             for (int e = 0; e < NS; ++e) bm = fmaxf(bm, sv[w][e]);
         const auto w32 = __builtin_amdgcn_permlane32_swap(__float_as_uint(bm), __float_as_uint(bm), false, false);
@@ -495,10 +493,10 @@ attn_paged_kernel(PagedArgs a) {
             mrun = mnew;
         }
         const float mref = (mrun == -INFINITY) ? 0.f : mrun;
-        u32x4_t pf[SUB][NV];
+        u32x4_t pf[SW][NV];
         float sum = 0.f;
 #pragma unroll
-        for (int w = 0; w < SUB; ++w) {
+        for (int w = 0; w < SW; ++w) {
             float p[NS];
 #pragma unroll
             for (int e = 0; e < NS; ++e) p[e] = __builtin_amdgcn_exp2f(fmaf(sv[w][e], a.sl2, -mref));
@@ -517,7 +515,7 @@ attn_paged_kernel(PagedArgs a) {
         }
         lrun += sum;
 #pragma unroll
-        for (int w = 0; w < SUB; ++w)
+        for (int w = 0; w < SW; ++w)
 #pragma unroll
             for (int u = 0; u < NV; ++u)
 #pragma unroll
@@ -528,17 +526,18 @@ attn_paged_kernel(PagedArgs a) {
     // straight from its page (a fragment's 16 bytes are consecutive keys of a dim).
     if (lim_lo < ktop) {
         __syncthreads();                                                // (the last round's reads)
-        if (lane == 0) ((int*)lds)[qw] = odd != 0;
+        if (lane == 0) ((int*)lds)[wave] = odd != 0;
         __syncthreads();
         int any = 0;
 #pragma unroll
-        for (int w = 0; w < QG; ++w) any |= ((const int*)lds)[w];
+        for (int w = 0; w < NW; ++w) any |= ((const int*)lds)[w];
         odd = __builtin_amdgcn_readfirstlane(any);
+        if (KG > 1) __syncthreads();                                    // (written again below)
     }
     if (odd != 0) {
         for (int blk = kz > ks + 32 * kb0 ? (kz - ks) / 32 - kb0 : 0; blk < blocks; ++blk) {
             const int k0 = ks + 32 * (kb0 + blk), pg = trow[k0 >> a.page_shift];
-            if (pg < 0 || pg >= a.n_pages) continue;
+            if ((KG > 1 && blk % SUB / SW != kw) || pg < 0 || pg >= a.n_pages) continue;
             const T* Vp = (const T*)a.vp + ((long)pg * a.Hk + hk) * page_elems + (k0 & ((1 << a.page_shift) - 1));
 #pragma unroll
             for (int dt = 0; dt < ND; ++dt) {
@@ -560,6 +559,45 @@ attn_paged_kernel(PagedArgs a) {
 #pragma unroll
                 for (int i = 0; i < NA; ++i) oacc[dt][i] = add_classes(oacc[dt][i], c[i]);
             }
+        }
+    }
+
+    // the waves' key groups merge as the parts do
+    if constexpr (KG > 1) {
+        constexpr int REC = ND * NA / 4 + 1;                            // 16-byte records of a lane
+        static_assert((KG - 1) * QG * REC * 1024 <= 2 * BUF, "the groups' sums must fit the buffers");
+        __syncthreads();
+        float4* rec = (float4*)lds + qw * REC * 64 + lane;
+        if (kw > 0) {
+            rec += (kw - 1) * QG * REC * 64;
+#pragma unroll
+            for (int dt = 0; dt < ND; ++dt)
+#pragma unroll
+                for (int j = 0; j < NA / 4; ++j)
+                    rec[(dt * NA / 4 + j) * 64] = make_float4(oacc[dt][4 * j], oacc[dt][4 * j + 1], oacc[dt][4 * j + 2],
+                                                              oacc[dt][4 * j + 3]);
+            rec[(REC - 1) * 64] = make_float4(mrun, lrun, 0.f, 0.f);
+        }
+        __syncthreads();
+        if (kw > 0) return;
+#pragma unroll
+        for (int k = 0; k < KG - 1; ++k, rec += QG * REC * 64) {
+            const float4 ml = rec[(REC - 1) * 64];
+            const float M = fmaxf(mrun, ml.x);
+            const float w0 = mrun == M ? 1.f : __builtin_amdgcn_exp2f(mrun - M);
+            const float w1 = ml.x == M ? 1.f : __builtin_amdgcn_exp2f(ml.x - M);
+            mrun = M;
+            lrun = lrun * w0 + ml.y * w1;
+#pragma unroll
+            for (int dt = 0; dt < ND; ++dt)
+#pragma unroll
+                for (int j = 0; j < NA / 4; ++j) {
+                    const float4 o = rec[(dt * NA / 4 + j) * 64];
+                    oacc[dt][4 * j] = oacc[dt][4 * j] * w0 + o.x * w1;
+                    oacc[dt][4 * j + 1] = oacc[dt][4 * j + 1] * w0 + o.y * w1;
+                    oacc[dt][4 * j + 2] = oacc[dt][4 * j + 2] * w0 + o.z * w1;
+                    oacc[dt][4 * j + 3] = oacc[dt][4 * j + 3] * w0 + o.w * w1;
+                }
         }
     }
 

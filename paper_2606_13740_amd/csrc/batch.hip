@@ -114,8 +114,9 @@ void launch_qk(const QkArgs& a, int Dh, hipStream_t s) {
 }
 
 // Launch of an attention call.  Both parts (the shared prefix for all rows, and the sequences' own
-// keys) run in one launch of one tile shape, QG waves of QT 16-row tiles; waves without rows only
-// help staging.
+// keys) run in one launch of one tile shape: QG row tiles of 16 QT rows (qt 2: one 32 x 32 tile a wave),
+// a wave or, with up to two 16-row tiles of a 16-bit type, two waves each, which take a step's
+// two blocks; waves without rows only help staging.
 struct AttnPlan {
     int qg, qt;
     int shared;           // positions taken as the shared part
@@ -132,14 +133,19 @@ constexpr int ATTN_SLOTS = 512;
 //  - shared part or not: 16 x 1 rows behind 8192 keys 49 and 255; 16 x 3 behind 9984 26 and 38; 4 x 8 behind 2048
 //    (13 MB that the sequences would read again) 16.7 and 17.8; 16 x 48 rows, 4 heads of 64, behind 512 (8 MB) equal;
 //    8 x 1 behind 64 15.0 and 14.8.  With one sequence it is that sequence's own.
-//  - tile: 64 rows against 128: 12 x 40 rows behind 1024 36 and 41, 16 x 3 behind 9984 26.2 and 28.2, 6 x 20 rows
-//    of 16 heads of 64 behind 2976 13.7 and 15.5; from 12 steps of 128 rows a slot on 128 rows, which halve the LDS
-//    reads per product: 16 x 64 behind 16384 (56 steps) 150 and 186.  fp32 is bound by its products, where idle
-//    waves cost: by the rows of one sequence (6 x 24 rows of 32 heads behind 1024: 32 rows 62, 64 rows 66).
+//  - tile: 64 rows against 128 (32 x 32 tiles): 12 x 40 rows of 32 heads behind 1024 37 and 40, 16 x 3 behind 9984 25.6
+//    and 27.2, 6 x 20 rows of 16 heads of 64 behind 2976 13.6 and 14.8, 8 x 32 of 32 heads behind 4096 51.5 and 49.2;
+//    from 12 steps of 128 rows a slot on 128 rows, which halve the LDS reads per product: 16 x 64 behind 16384
+//    (56 steps) 145 and 186.  fp32 is bound by its products, where idle waves cost: by the rows of one sequence
+//    (6 x 24 rows of 32 heads behind 1024: 32 rows 62, 64 rows 66).
+//  - waves of a row tile, for tiles of 32 rows and fewer: two against one 46.5 and 48.7 (16 x 1 rows of 32 heads behind
+//    8192), 20.9 and 22.8 (1 x 32 of 32 heads behind 4096), 5.6 and 6.2 (3 x 1 of 4 heads of 64 behind 80), 14.9 and 14.7
+//    (8 x 1 behind 1564); 64 rows as two 32 x 32 tiles of two waves each against four of 16 rows: 50 and 51, 36.1
+//    and 36.6, 25.7 and 25.6, 14.0 and 13.6 in the calls above: not taken.
 //  - steps of a workgroup: all the call's steps (and two for each workgroup's start) over the slots, so that one
 //    round takes them, rounded towards fewer workgroups: 16 x 64 behind 16384 in 4 splits (448 workgroups) 150, 3 174,
 //    5 190; 8 x 32 of 32 heads behind 4096 in 3 splits 50, 2 62, 4 54; and at least four (two for tiles of 16 rows
-//    and in fp32), since a split is written and merged: 4 x 8 behind 2048 in 8 splits of 4 steps 16.7, in 16 of 2 19.0.
+//    and in fp32), since a split is written and merged: 4 x 8 behind 2048 in 8 splits of 4 steps 16.2, in 16 of 2 19.0.
 AttnPlan attn_plan(const dllm_attn_args* g) {
     const int G = g->n_heads / g->n_kv_heads, es = esize(g->dtype), step = es == 4 ? 32 : 64;
     AttnPlan p{};
@@ -196,7 +202,7 @@ int check_attn(const dllm_attn_args* g, int& shift) {
     if ((long)g->n_rows * (g->n_heads / g->n_kv_heads) >= (1l << 31))
         return fail(DLLM_E_INVAL, "n_rows times the query heads of a K/V head must be < 2^31");
     const AttnPlan p = attn_plan(g);
-    if (!grid_ok(p.wgs_s + p.wgs_o, p.qg * 64) || !grid_ok((long)g->n_rows * g->n_heads, g->head_dim / 4))
+    if (!grid_ok(p.wgs_s + p.wgs_o, 256) || !grid_ok((long)g->n_rows * g->n_heads, g->head_dim / 4))
         return fail(DLLM_E_INVAL, "n_seqs, max_rows and n_rows need too many workgroups");
     return DLLM_OK;
 }
@@ -205,14 +211,18 @@ template <typename T, int DH>
 void launch_attn_dh(PagedArgs a, const AttnPlan& p, hipStream_t s) {
     constexpr int SUB = sizeof(T) == 4 ? 1 : 2;
     const dim3 grid((unsigned)(p.wgs_s + p.wgs_o));
-#define ATTN(QG_, QT_) hipLaunchKernelGGL((attn_paged_kernel<T, DH, QG_, 16 * QT_, 2, SUB>), grid, dim3(QG_ * 64), 0, s, a)
+#define ATTN(QG_, RT_, KG_) \
+    hipLaunchKernelGGL((attn_paged_kernel<T, DH, QG_, RT_, KG_, SUB>), grid, dim3(QG_ * KG_ * 64), 0, s, a)
     if constexpr (sizeof(T) == 2) {
-        if (p.qt == 2) ATTN(4, 2);
+        if (p.qt == 2) ATTN(4, 32, 1);
+        else if (p.qg == 4) ATTN(4, 16, 1);
+        else if (p.qg == 2) ATTN(2, 16, 2);
+        else ATTN(1, 16, 2);
+    } else {
+        if (p.qg == 4) ATTN(4, 16, 1);
+        else if (p.qg == 2) ATTN(2, 16, 1);
+        else ATTN(1, 16, 1);
     }
-    if (p.qt == 2) {
-    } else if (p.qg == 4) ATTN(4, 1);
-    else if (p.qg == 2) ATTN(2, 1);
-    else ATTN(1, 1);
 #undef ATTN
     if (!a.direct)
         hipLaunchKernelGGL((attn_paged_merge_kernel<T, DH>), dim3(ceil_div((long)a.T * a.H, 256 / (DH / 4))), dim3(256), 0,
