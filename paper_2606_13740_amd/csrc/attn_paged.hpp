@@ -152,7 +152,7 @@ constexpr float PAGED_SLACK = 8.f;
 // counted).  Lane i holds the page of block 64 n + i, so a block's page is one lane read.
 //
 // What bounds it: many rows, the chain of products and exponentials of the two waves that a SIMD holds
-// (16 sequences of 64 rows, 28 heads over 4, behind 16384 bf16 keys: 136 us and 9 for the merge, 900
+// (16 sequences of 64 rows, 28 heads over 4, behind 16384 bf16 keys: 145 us with the merge, 900
 // TFLOP/s where a large library product reaches 1100); rows enough for the prefix only, LDS reads and the K/V
 // themselves (8 x 32 rows of 32 fp16 heads behind 4096: 37 us and 6, 115 MB); few rows, latency (8 x 1 rows
 // behind 1564: 9.6 us and 4.6).

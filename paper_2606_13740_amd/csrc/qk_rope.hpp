@@ -5,11 +5,6 @@
 
 namespace dllm {
 
-// Element types of the batch operators.
-struct ElemF32 { using T = float; };
-struct ElemF16 { using T = _Float16; };
-struct ElemBF16 { using T = __bf16; };
-
 template <typename T> __device__ __forceinline__ float elem_to_f32(T v) { return (float)v; }
 template <typename T> __device__ __forceinline__ T elem_from_f32(float v) { return (T)v; }
 // fp16 saturates, as the library's caches do
@@ -53,7 +48,8 @@ template <typename T> __device__ __forceinline__ void store8(T* p, const float (
 // an aligned one (groups are cut at the slots' alignment, taken from the tile's first row),
 // else one by one.
 //
-// What bounds it: HBM, each element read and written once.
+// What bounds it: HBM, each element read and written once: 16384 rows of 28 + 2 x 4 fp16 heads of 128 in 65 us,
+// 4.7 TB/s, the rate of a large copy (4.76).  A window's rows are launch and latency: 4 to 256 rows 6 to 7.5 us.
 constexpr int QK_VROWS = 64;
 template <typename T, int DH>
 __global__ void __launch_bounds__(256) qk_norm_rope_kernel(QkArgs a, int qk_wgs, int hp) {
