@@ -9,6 +9,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+import struct
 from typing import Optional
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
@@ -83,6 +84,16 @@ class dllm_select_args(ctypes.Structure):
                 _fields(_vp, "d_out_id d_out_conf d_ws") + [("ws_bytes", _sz)])
 
 
+def _packer(cls):
+    """Packs values, in the order of the fields, into the bytes of a struct: a quarter of its constructor's time."""
+    fmt = "@" + "".join({_i32: "i", _f32: "f", _i64: "q", _vp: "P", _sz: "N"}[t] for _, t in cls._fields_)
+    return struct.Struct(fmt + "x" * (ctypes.sizeof(cls) - struct.calcsize(fmt))).pack
+
+
+_pack_qk, _pack_attn, _pack_select = _packer(dllm_qk_args), _packer(dllm_attn_args), _packer(dllm_select_args)
+_pack_ws = struct.Struct("@PN").pack          # the last two fields of the latter
+
+# (the batch operators' args are pointers to their structs: a struct by reference, or its bytes)
 _SIGNATURES = {
     "dllm_last_error": ([], ctypes.c_char_p),
     "dllm_version": ([], ctypes.c_char_p),
@@ -117,15 +128,14 @@ _SIGNATURES = {
     "dllm_quantize_int8": ([_vp, _i32, _i32, _i32, _vp, _vp, _vp], ctypes.c_int),
     "dllm_batch_plan": ([_vp] * 4 + [_i32, _vp, _i32] + [_vp] * 3 + [_i32] * 4 + [_vp] * 7, ctypes.c_int),
     "dllm_rope_table": ([_vp, _i32, _i32, _f32, _vp], ctypes.c_int),
-    "dllm_qk_norm_rope": ([ctypes.POINTER(dllm_qk_args), _vp], ctypes.c_int),
-    "dllm_attention_paged_ws": ([ctypes.POINTER(dllm_attn_args), ctypes.POINTER(_sz)], ctypes.c_int),
-    "dllm_attention_paged": ([ctypes.POINTER(dllm_attn_args), _vp], ctypes.c_int),
-    "dllm_select_ws": ([ctypes.POINTER(dllm_select_args), ctypes.POINTER(_sz)], ctypes.c_int),
-    "dllm_select": ([ctypes.POINTER(dllm_select_args), _vp], ctypes.c_int),
+    "dllm_qk_norm_rope": ([_vp, _vp], ctypes.c_int),
+    "dllm_attention_paged_ws": ([_vp, ctypes.POINTER(_sz)], ctypes.c_int),
+    "dllm_attention_paged": ([_vp, _vp], ctypes.c_int),
+    "dllm_select_ws": ([_vp, ctypes.POINTER(_sz)], ctypes.c_int),
+    "dllm_select": ([_vp, _vp], ctypes.c_int),
     "dllm_model_set_qk_norm": ([_vp, ctypes.POINTER(_vp), ctypes.POINTER(_vp), _vp], ctypes.c_int),
     "dllm_batch_bytes": ([_vp, _i32, _i32, ctypes.POINTER(_sz)], ctypes.c_int),
-    "dllm_batch_step": ([_vp, _vp, _sz, ctypes.POINTER(dllm_batch_rows), _vp, _vp, ctypes.POINTER(dllm_select_args), _vp, _vp,
-                         _vp], ctypes.c_int),
+    "dllm_batch_step": ([_vp, _vp, _sz, ctypes.POINTER(dllm_batch_rows), _vp, _vp, _vp, _vp, _vp, _vp], ctypes.c_int),
     "dllm_commit_staged": ([_vp, _vp, _vp, _vp, _vp, _i32, _i32, ctypes.c_float, ctypes.c_float, _vp, _vp, _vp],
                            ctypes.c_int),
 }
@@ -162,16 +172,21 @@ def _ptr(t) -> Optional[int]:
 _raw_stream = None
 
 
+def _current_device() -> int:
+    import torch
+    return torch.cuda.current_device()
+
+
 def _stream(stream, device: Optional[int] = None):
     """The stream's handle; None: the current stream of the current device (`device`, where the caller knows it)."""
     global _raw_stream
     if stream is None:
-        import torch
         if _raw_stream is None:
+            import torch
             # the handle without the Stream object around it (2.7 us a call), where torch has it
             _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (
                 lambda dev: torch.cuda.current_stream(dev).cuda_stream)
-        return _raw_stream(torch.cuda.current_device() if device is None else device)
+        return _raw_stream(_current_device() if device is None else device)
     return stream if isinstance(stream, int) else stream.cuda_stream
 
 
@@ -352,6 +367,10 @@ def _refuse(func: str, msg: str):
     raise DllmError(DLLM_E_INVAL, func, msg)
 
 
+_NO_FIT = (struct.error, OverflowError)
+_NO_FIT_MSG = "an argument is no number of its field's range"
+
+
 def _gpu(func: str, ref) -> int:
     """The current GPU's index, which ref must be on."""
     if _Types.torch is None:
@@ -440,33 +459,35 @@ def dllm_qk_norm_rope(q, k, v, rope, pos, slot, q_out, k_pages, v_pages, q_gain=
             (k_gain is not None and k_gain.numel() < dim)):
         _refuse(f, "v_pages must be [n_pages][kv_heads][head_dim][page], q_out [rows][heads][dim], pos and slot have an entry "
                    "per row, gains head_dim")
-    a = dllm_qk_args(_Types.elem.get(dt, -1), T, H, kv, dim, page, n_pages, rope.numel() // dim, eps, q.data_ptr(),
-                     k.data_ptr(), v.data_ptr(), ld_q, ld_k, ld_v, None if q_gain is None else q_gain.data_ptr(),
-                     None if k_gain is None else k_gain.data_ptr(), rope.data_ptr(), pos.data_ptr(), slot.data_ptr(),
+    try:
+        a = _pack_qk(_Types.elem.get(dt, -1), T, H, kv, dim, page, n_pages, rope.numel() // dim, eps, q.data_ptr(),
+                     k.data_ptr(), v.data_ptr(), ld_q, ld_k, ld_v, 0 if q_gain is None else q_gain.data_ptr(),
+                     0 if k_gain is None else k_gain.data_ptr(), rope.data_ptr(), pos.data_ptr(), slot.data_ptr(),
                      q_out.data_ptr(), k_pages.data_ptr(), v_pages.data_ptr())
-    rc = lib().dllm_qk_norm_rope(ctypes.byref(a), _stream(stream, dev))
+    except _NO_FIT:
+        _refuse(f, _NO_FIT_MSG)
+    rc = lib().dllm_qk_norm_rope(a, _stream(stream, dev))
     if rc:
         _check(rc, f)
 
 
 def _workspace(query, a, ws, stream, dev: int, f: str):
-    """Sets a's workspace: `ws`, or memory of the call's own (on the current stream; freed once the call has been made)."""
+    """(args with their workspace, `ws` or memory of the call's own: on the current stream, freed once the call has been
+    made)."""
     if ws is None:
         n = _sz()
-        rc = query(ctypes.byref(a), ctypes.byref(n))
+        rc = query(a, n)
         if rc:
             _check(rc, f + "_ws")
         if not n.value:
-            return None
+            return a, None
         if stream is not None:
             _refuse(f, "a call on a given stream needs a workspace of the caller's")
         ws = _Types.torch.empty(n.value, dtype=_Types.torch.uint8, device=dev)
-        a.d_ws, a.ws_bytes = ws.data_ptr(), n.value
-    else:
-        if ws.get_device() != dev or not ws.is_contiguous():
-            _refuse(f, "ws must be a contiguous tensor on the same GPU")
-        a.d_ws, a.ws_bytes = ws.data_ptr(), ws.numel() * ws.element_size()
-    return ws
+        return a[:-16] + _pack_ws(ws.data_ptr(), n.value), ws
+    if ws.get_device() != dev or not ws.is_contiguous():
+        _refuse(f, "ws must be a contiguous tensor on the same GPU")
+    return a[:-16] + _pack_ws(ws.data_ptr(), ws.numel() * ws.element_size()), ws
 
 
 def dllm_attention_paged(q, k_pages, v_pages, table, row0, length, out, max_rows: int, max_len: int,
@@ -484,13 +505,16 @@ def dllm_attention_paged(q, k_pages, v_pages, table, row0, length, out, max_rows
             (lim is not None and lim.numel() < T)):
         _refuse(f, "v_pages must be [n_pages][kv_heads][head_dim][page], table must have a row and row0 an entry per sequence "
                    "(row0: one more), lim an entry per row")
-    a = dllm_attn_args(_Types.elem.get(dt, -1), T, B, H, kv, dim, page, n_pages, ld, shared_len, max_rows, max_len,
+    try:
+        a = _pack_attn(_Types.elem.get(dt, -1), T, B, H, kv, dim, page, n_pages, ld, shared_len, max_rows, max_len,
                        dim ** -0.5 if scale is None else scale, q.data_ptr(), ld_q, k_pages.data_ptr(),
                        v_pages.data_ptr(), table.data_ptr(), row0.data_ptr(), length.data_ptr(),
-                       None if lim is None else lim.data_ptr(), out.data_ptr(), ld_out)
+                       0 if lim is None else lim.data_ptr(), out.data_ptr(), ld_out, 0, 0)
+    except _NO_FIT:
+        _refuse(f, _NO_FIT_MSG)
     L = lib()
-    keep = _workspace(L.dllm_attention_paged_ws, a, ws, stream, dev, f)
-    rc = L.dllm_attention_paged(ctypes.byref(a), _stream(stream, dev))
+    a, keep = _workspace(L.dllm_attention_paged_ws, a, ws, stream, dev, f)
+    rc = L.dllm_attention_paged(a, _stream(stream, dev))
     if rc:
         _check(rc, f)
     del keep
@@ -499,66 +523,72 @@ def dllm_attention_paged(q, k_pages, v_pages, table, row0, length, out, max_rows
 def _select_args(f, logits, out_id, out_conf, mask_id=-1, row0=None, hist=None, hist0=None, n_prompt=None, repetition=None,
                  presence=None, frequency=None, bias_id=None, bias=None, bias0=None, allow=None, allow_row=None,
                  out_logits=None, ws=None, stream=None):
-    """(struct, what keeps its workspace alive) of a selection."""
+    """(args, what keeps its workspace alive, the GPU) of a selection."""
     dev, (T, V), dt = _gpu(f, logits), logits.shape, logits.dtype
     B = row0.numel() - 1 if row0 is not None else 1
-    a = dllm_select_args(_Types.elem.get(dt, -1), T, V, mask_id, B, logits.data_ptr(), logits.stride(0) if T > 1 else V)
     i32, f32 = [out_id], [out_conf]
     ok = out_id.numel() >= T and out_conf.numel() >= T and (V == 1 or logits.stride(1) == 1)
+    p_row0 = p_hist = p_hist0 = p_prompt = p_rep = p_pres = p_freq = p_bias_id = p_bias = p_bias0 = p_allow = 0
+    p_allow_row = p_out = n_allow = allow_ld = ld_out = 0
     if row0 is not None:
         i32.append(row0)
-        a.d_row0 = row0.data_ptr()
+        p_row0 = row0.data_ptr()
     if hist is not None:
         i32 += [hist, hist0]
         ok = ok and hist0.numel() > B
-        a.d_hist, a.d_hist0 = hist.data_ptr(), hist0.data_ptr()
+        p_hist, p_hist0 = hist.data_ptr(), hist0.data_ptr()
     if n_prompt is not None:
         i32.append(n_prompt)
         ok = ok and n_prompt.numel() >= B
-        a.d_n_prompt = n_prompt.data_ptr()
+        p_prompt = n_prompt.data_ptr()
     if repetition is not None:
         f32.append(repetition)
-        a.d_repetition = repetition.data_ptr()
+        p_rep = repetition.data_ptr()
     if presence is not None:
         f32.append(presence)
-        a.d_presence = presence.data_ptr()
+        p_pres = presence.data_ptr()
     if frequency is not None:
         f32.append(frequency)
-        a.d_frequency = frequency.data_ptr()
+        p_freq = frequency.data_ptr()
     for t in f32[1:]:
         ok = ok and t.numel() >= B
     if bias is not None:
         i32 += [bias_id, bias0]
         f32.append(bias)
         ok = ok and bias0.numel() > B and bias.numel() >= bias_id.numel()
-        a.d_bias_id, a.d_bias, a.d_bias0 = bias_id.data_ptr(), bias.data_ptr(), bias0.data_ptr()
+        p_bias_id, p_bias, p_bias0 = bias_id.data_ptr(), bias.data_ptr(), bias0.data_ptr()
     if allow is not None:
         i32.append(allow)
-        a.d_allow = allow.data_ptr()
-        a.n_allow, a.allow_ld = allow.shape
+        p_allow = allow.data_ptr()
+        n_allow, allow_ld = allow.shape
     if allow_row is not None:
         i32.append(allow_row)
         ok = ok and allow_row.numel() >= T
-        a.d_allow_row = allow_row.data_ptr()
+        p_allow_row = allow_row.data_ptr()
     if out_logits is not None:
         ok = ok and (out_logits.shape == logits.shape and out_logits.dtype is dt and out_logits.get_device() == dev and
                      (V == 1 or out_logits.stride(1) == 1))
-        a.d_out_logits, a.ld_out = out_logits.data_ptr(), out_logits.stride(0) if T > 1 else V
+        p_out, ld_out = out_logits.data_ptr(), out_logits.stride(0) if T > 1 else V
     _plain(f, dev, _Types.i32, i32, "array " * len(i32))
     _plain(f, dev, _Types.f32, f32, "array " * len(f32))
     if not ok:
         _refuse(f, "out_id, out_conf and allow_row must have an entry per row, n_prompt and the penalties one per sequence "
                    "(hist0, bias0: one more), out_logits be of the logits' shape and type, rows be whole")
-    a.d_out_id, a.d_out_conf = out_id.data_ptr(), out_conf.data_ptr()
-    return a, _workspace(lib().dllm_select_ws, a, ws, stream, dev, f)
+    try:
+        a = _pack_select(_Types.elem.get(dt, -1), T, V, mask_id, B, logits.data_ptr(), logits.stride(0) if T > 1 else V,
+                         p_row0, p_hist, p_hist0, p_prompt, p_rep, p_pres, p_freq, p_bias_id, p_bias, p_bias0, p_allow,
+                         n_allow, allow_ld, p_allow_row, p_out, ld_out, out_id.data_ptr(), out_conf.data_ptr(), 0, 0)
+    except _NO_FIT:
+        _refuse(f, _NO_FIT_MSG)
+    return _workspace(lib().dllm_select_ws, a, ws, stream, dev, f) + (dev,)
 
 
 def dllm_select(logits, out_id, out_conf, stream=None, **control):
     """logits (and out_logits): [rows][vocab], rows may be strided.  control: mask_id, row0, hist, hist0, n_prompt,
     repetition, presence, frequency, bias_id, bias, bias0, allow (int32 words [masks][words]), allow_row, out_logits, ws."""
     f = "dllm_select"
-    a, keep = _select_args(f, logits, out_id, out_conf, stream=stream, **control)
-    rc = lib().dllm_select(ctypes.byref(a), _stream(stream))
+    a, keep, dev = _select_args(f, logits, out_id, out_conf, stream=stream, **control)
+    rc = lib().dllm_select(a, _stream(stream, dev))
     if rc:
         _check(rc, f)
     del keep
@@ -595,8 +625,7 @@ def dllm_batch_step(model: int, pages, n_pages: int, page: int, tok, mask, table
                            pos.data_ptr(), slot.data_ptr(), length.data_ptr(), _ptr(lim))
     sel = keep = None
     if logits is not None:
-        a, keep = _select_args(f, logits, out_id, out_conf, stream=stream, **(control or {}))
-        sel = ctypes.byref(a)
+        sel, keep, _ = _select_args(f, logits, out_id, out_conf, stream=stream, **(control or {}))
     _check(lib().dllm_batch_step(model, pages.data_ptr(), pages.numel() * pages.element_size(), ctypes.byref(rows),
                                  tok.data_ptr(), _ptr(mask), sel, _ptr(out_id), _ptr(out_conf), _stream(stream)), f)
     del keep

@@ -146,6 +146,12 @@ def test_binding_refuses_tensors_that_are_not_on_the_gpu(dl):
         dl.dllm_select(torch.zeros(2, 9), z(2), torch.zeros(2))
 
 
+def test_packed_arguments_are_the_structs_bytes(dl):
+    for cls, pack in ((dl.dllm_qk_args, dl._pack_qk), (dl.dllm_attn_args, dl._pack_attn), (dl.dllm_select_args, dl._pack_select)):
+        v = [i + 0.5 if t is ctypes.c_float else i + 1 for i, (_, t) in enumerate(cls._fields_)]
+        assert pack(*v) == bytes(cls(*v))
+
+
 def test_argument_structs_have_the_headers_layout(dl, tmp_path):
     """The binding's structs against the header's, field by field, through the host compiler."""
     import os

@@ -428,6 +428,15 @@ def test_attention_on_another_stream_with_a_workspace(dl):
     assert all(torch.equal(g, w) for g, w in zip(got, want))
 
 
+@pytest.mark.parametrize("bad", [dict(max_len=2 ** 32 + 8), dict(max_rows=2 ** 31), dict(scale=1e300), dict(shared_len="64")])
+def test_attention_arguments_that_do_not_fit(dl, bad):
+    """Numbers past their field's range are refused, not cut to 32 bits."""
+    c = attn_case(np.random.default_rng(23), "f16", [4], [40], 2, 2, 64, 32, 0)
+    args = dict(dict(max_rows=4, max_len=40), **bad)
+    with pytest.raises(dl.DllmError):
+        dl.dllm_attention_paged(c["qt"], c["kt"], c["vt"], i32(c["table"]), i32(c["row0"]), i32(c["lens"]), c["qt"].clone(), **args)
+
+
 def test_offsets_past_32_bits(dl):
     """A pool of more than 2^31 elements a plane: the same bits from its last pages as from a small pool's."""
     import torch
