@@ -644,7 +644,10 @@ typedef struct dllm_batch_rows {
  * sel->d_logits (contiguous fp32 [n_rows][vocab], the caller's; MASK column -inf) and
  * dllm_select with its penalties, biases and masks gives the outputs instead (its d_out_id,
  * d_out_conf are this call's).  Workspaces grow at the first call of a size (the call then
- * synchronises the device); later ones can be captured.  E_INVAL, E_CAPACITY and E_DTYPE as
+ * synchronises the device); later ones can be captured.  They are the model's, as for every
+ * other call: its calls, and replays of graphs captured from them, must not overlap.  A graph
+ * stays valid when later calls need larger ones (what it uses is then kept until
+ * dllm_model_destroy).  E_INVAL, E_CAPACITY and E_DTYPE as
  * the operators' and dllm_denoise_step's; E_CAPACITY if max_len exceeds cfg.max_pos or
  * the pages are fewer than dllm_batch_bytes(). */
 int dllm_batch_step(dllm_model* m, void* d_pages, size_t bytes, const dllm_batch_rows* rows, const int32_t* d_tok,

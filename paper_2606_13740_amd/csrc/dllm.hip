@@ -116,6 +116,8 @@ struct dllm_model {
     bool rows_qkv = false;   // the workspace holds Q/K/V rows (heads' norm, batch steps)
     void* attn_ws = nullptr; // workspace of the paged attention (batch steps)
     size_t attn_ws_bytes = 0;
+    bool captured = false;      // a call has been captured into a graph, which keeps using the workspaces it saw
+    std::vector<void*> retired; // those of them that have been outgrown since
     Workspace ws;
     int n_lm_wg = 1;
     // probe
@@ -464,9 +466,10 @@ struct ProbeScope {
 // Workspace
 // ---------------------------------------------------------------------------
 
-void free_ws(Workspace& w) {
-    if (w.block) (void)hipFree(w.block);
-    w = Workspace{};
+// Memory that a larger workspace replaces: kept for the graphs captured before, if any (until the model is destroyed).
+void outgrown(dllm_model* m, void* p) {
+    if (p && m->captured) m->retired.push_back(p);
+    else if (p) (void)hipFree(p);
 }
 
 int alloc_zero(void** p, size_t bytes) {
@@ -497,7 +500,8 @@ int ensure_ws(dllm_model* m, int rows_needed) {
     if (m->ws.rows >= rows && m->ws.block && (m->ws.qkv || !m->rows_qkv)) return DLLM_OK;
     HIP_TRY(hipDeviceSynchronize());
     const int had = m->ws.rows;
-    free_ws(m->ws);
+    outgrown(m, m->ws.block);
+    m->ws = Workspace{};
     if (had > rows) return ensure_ws(m, had);     // grown for the Q/K/V rows only: never smaller than before
     const int wrows = (int)round_up(c.max_window, 64);
     const size_t part_floats = part_floats_for(m, rows, wrows);
@@ -967,6 +971,10 @@ int forward_t(dllm_model* m, dllm_kv* kv, const FwdArgs& a, hipStream_t s) {
 }
 
 int forward(dllm_model* m, dllm_kv* kv, const FwdArgs& a, hipStream_t s) {
+    if (!m->captured) {
+        hipStreamCaptureStatus st = hipStreamCaptureStatusNone;
+        m->captured = hipStreamIsCapturing(s, &st) == hipSuccess && st == hipStreamCaptureStatusActive;
+    }
     if (m->wt == WT_F32) return forward_t<WT_F32, float>(m, kv, a, s);
     if (m->wt == WT_BF16) return forward_t<WT_BF16, uint16_t>(m, kv, a, s);
     if (m->wt == WT_Q4) return forward_t<WT_Q4, uint16_t>(m, kv, a, s);
@@ -1152,8 +1160,8 @@ int dllm_model_create(const dllm_config* cfg, const dllm_weights* w, dllm_stream
 
 int dllm_model_destroy(dllm_model* m) {
     if (!m) return DLLM_OK;
-    free_ws(m->ws);
-    void* ptrs[] = {m->wpool, m->spool, m->qpool, m->gpool, m->bpool, m->embed, m->rope, m->hgpool, m->attn_ws};
+    for (void* p : m->retired) (void)hipFree(p);
+    void* ptrs[] = {m->ws.block, m->wpool, m->spool, m->qpool, m->gpool, m->bpool, m->embed, m->rope, m->hgpool, m->attn_ws};
     for (void* p : ptrs)
         if (p) (void)hipFree(p);
     for (auto e : m->ev_b) (void)hipEventDestroy(e);
@@ -1240,7 +1248,7 @@ int dllm_batch_step(dllm_model* m, void* d_pages, size_t bytes, const dllm_batch
     if ((rc = ensure_ws(m, b->n_rows))) return rc;
     if (aws > m->attn_ws_bytes) {
         HIP_TRY(hipDeviceSynchronize());
-        if (m->attn_ws) (void)hipFree(m->attn_ws);
+        outgrown(m, m->attn_ws);
         m->attn_ws = nullptr;
         m->attn_ws_bytes = 0;
         if (hipMalloc(&m->attn_ws, aws) != hipSuccess)

@@ -203,6 +203,53 @@ def test_batch_step_captured(dl):
         torch.cuda.synchronize()
 
 
+def test_captured_calls_keep_their_workspaces(dl):
+    """Graphs of a single-sequence step and of a batch step, replayed after calls that needed larger workspaces: the first
+    batch step at all, then a prompt of many rows, then the heads' norm's rows."""
+    import torch
+    shape = synth.SMALL_BF16
+    model, _, _ = build_pair(shape, "bf16", oracle_too=False)
+    kv = dl.KVCache(model, 128)
+    dl.dllm_prefill(model.handle, kv.handle, dev_i32(synth.prompt_ids(shape, 40)), 40)
+    tok, mask = synth.window(shape, 32, range(8, 32))
+    step = (model.handle, kv.handle, dev_i32(tok), dev_u8(mask), 32, torch.zeros(32, dtype=torch.int32, device="cuda"),
+            torch.zeros(32, device="cuda"))
+    graphs = []
+
+    def record(call, args, kw):
+        call(*args, **kw)
+        torch.cuda.synchronize()
+        outs = [x for x in args if isinstance(x, torch.Tensor)][-2:]
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            call(*args, **kw)
+        graphs.append((g, outs, [o.clone() for o in outs]))
+
+    def replay_all():
+        junk = [torch.full((1 << 20,), 3.0, device="cuda") for _ in range(64)]       # into what has been freed, if anything
+        for _ in range(3):
+            for g, outs, want in graphs:
+                for o in outs:
+                    o.fill_(7)
+                g.replay()
+                torch.cuda.synchronize()
+                assert all(torch.equal(o, w) for o, w in zip(outs, want))
+        del junk
+
+    record(dl.dllm_denoise_step, step, {})
+    prompt, own, win = scene(shape, 64, [40, 8], [32, 32], seed=9)
+    bt = Batch(dl, model, 2, prompt, n_pages=60)
+    replay_all()
+    bt.step(np.concatenate(own), None, np.array([40, 8]))
+    bt.step(np.concatenate([t for t, _ in win]), np.concatenate([m for _, m in win]), np.array([32, 32]), commit=False, out=True)
+    record(dl.dllm_batch_step, *bt.last)
+    replay_all()
+    many = np.random.default_rng(10).integers(0, shape.mask_id, 700).astype(np.int32)
+    other = Batch(dl, model, 2, many[:288], n_pages=80)
+    other.step(many[:348], None, np.array([148, 200]), commit=False)
+    replay_all()
+
+
 # ---------------------------------------------------------------------------- the heads' norm
 
 
