@@ -459,6 +459,8 @@ def dllm_qk_norm_rope(q, k, v, rope, pos, slot, q_out, k_pages, v_pages, q_gain=
             (k_gain is not None and k_gain.numel() < dim)):
         _refuse(f, "v_pages must be [n_pages][kv_heads][head_dim][page], q_out [rows][heads][dim], pos and slot have an entry "
                    "per row, gains head_dim")
+    if T == 0:                      # (empty tensors have no address)
+        return
     try:
         a = _pack_qk(_Types.elem.get(dt, -1), T, H, kv, dim, page, n_pages, rope.numel() // dim, eps, q.data_ptr(),
                      k.data_ptr(), v.data_ptr(), ld_q, ld_k, ld_v, 0 if q_gain is None else q_gain.data_ptr(),
@@ -505,6 +507,8 @@ def dllm_attention_paged(q, k_pages, v_pages, table, row0, length, out, max_rows
             (lim is not None and lim.numel() < T)):
         _refuse(f, "v_pages must be [n_pages][kv_heads][head_dim][page], table must have a row and row0 an entry per sequence "
                    "(row0: one more), lim an entry per row")
+    if T == 0:
+        return
     try:
         a = _pack_attn(_Types.elem.get(dt, -1), T, B, H, kv, dim, page, n_pages, ld, shared_len, max_rows, max_len,
                        dim ** -0.5 if scale is None else scale, q.data_ptr(), ld_q, k_pages.data_ptr(),
@@ -536,7 +540,8 @@ def _select_args(f, logits, out_id, out_conf, mask_id=-1, row0=None, hist=None, 
     if hist is not None:
         i32 += [hist, hist0]
         ok = ok and hist0.numel() > B
-        p_hist, p_hist0 = hist.data_ptr(), hist0.data_ptr()
+        p_hist0 = hist0.data_ptr()
+        p_hist = hist.data_ptr() or p_hist0          # (an empty tensor has no address; nothing is read through this one)
     if n_prompt is not None:
         i32.append(n_prompt)
         ok = ok and n_prompt.numel() >= B
@@ -556,7 +561,8 @@ def _select_args(f, logits, out_id, out_conf, mask_id=-1, row0=None, hist=None, 
         i32 += [bias_id, bias0]
         f32.append(bias)
         ok = ok and bias0.numel() > B and bias.numel() >= bias_id.numel()
-        p_bias_id, p_bias, p_bias0 = bias_id.data_ptr(), bias.data_ptr(), bias0.data_ptr()
+        p_bias0 = bias0.data_ptr()
+        p_bias_id, p_bias = bias_id.data_ptr() or p_bias0, bias.data_ptr() or p_bias0
     if allow is not None:
         i32.append(allow)
         p_allow = allow.data_ptr()
@@ -587,6 +593,8 @@ def dllm_select(logits, out_id, out_conf, stream=None, **control):
     """logits (and out_logits): [rows][vocab], rows may be strided.  control: mask_id, row0, hist, hist0, n_prompt,
     repetition, presence, frequency, bias_id, bias, bias0, allow (int32 words [masks][words]), allow_row, out_logits, ws."""
     f = "dllm_select"
+    if logits.shape[0] == 0:
+        return
     a, keep, dev = _select_args(f, logits, out_id, out_conf, stream=stream, **control)
     rc = lib().dllm_select(a, _stream(stream, dev))
     if rc:

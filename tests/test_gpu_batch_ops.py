@@ -598,6 +598,31 @@ def test_select_strides_in_place_and_no_sequences(dl):
 # ---------------------------------------------------------------------------- together, and captured
 
 
+def test_select_with_histories_and_biases_that_are_empty(dl):
+    """The first step of a batch: penalties are set, but no sequence has a history yet."""
+    import torch
+    x = torch.randn(5, 300, generator=torch.Generator().manual_seed(3)).cuda()
+    e, two = i32([]), torch.full((2,), 2.0, device="cuda")
+    outs = []
+    for control in ({}, dict(hist=e, hist0=i32([0, 0, 0]), repetition=two, presence=two, frequency=two, n_prompt=i32([0, 0]),
+                             bias_id=e, bias=torch.empty(0, device="cuda"), bias0=i32([0, 0, 0]))):
+        outs.append((torch.zeros(5, dtype=torch.int32, device="cuda"), torch.zeros(5, device="cuda")))
+        dl.dllm_select(x, *outs[-1], row0=i32([0, 3, 5]), **control)
+    torch.cuda.synchronize()
+    assert torch.equal(outs[0][0], x.argmax(1).int()) and all(torch.equal(a, b) for a, b in zip(*outs))
+
+
+def test_calls_without_rows(dl):
+    import torch
+    z = lambda *s, dt=torch.float16: torch.zeros(s, dtype=dt, device="cuda")  # noqa: E731
+    kp, vp = z(3, 2, 32, 64), z(3, 2, 64, 32)
+    dl.dllm_qk_norm_rope(z(0, 4, 64), z(0, 2, 64), z(0, 2, 64), z(8, 32, 2, dt=torch.float32), i32([]), i32([]), z(0, 4, 64), kp, vp)
+    dl.dllm_attention_paged(z(0, 4, 64), kp, vp, i32([[0, 1]]), i32([0, 0]), i32([40]), z(0, 4, 64), 1, 40)
+    dl.dllm_select(z(0, 100), i32([]), z(0, dt=torch.float32))
+    torch.cuda.synchronize()
+    assert not kp.any() and not vp.any()
+
+
 def test_operators_of_a_step_together_and_captured(dl):
     """plan -> norm, rotation, cache write -> attention -> select, eagerly and replayed from a graph whose lengths change."""
     import torch
