@@ -252,7 +252,9 @@ size_t select_ws_bytes(const dllm_select_args* g) {
 template <typename T>
 void launch_select(const SelectArgs& a, SelectPart* part, hipStream_t s) {
     const int n = select_ranges(a.V), per = select_rows_per(a.T, n);
-    hipLaunchKernelGGL(select_kernel<T>, dim3((unsigned)n * ceil_div(a.T, per)), dim3(SEL_NT), 0, s, a, part, n, per);
+    const long wgs = (long)n * ceil_div(a.T, per);
+    if (wgs <= 4 * N_CU) hipLaunchKernelGGL((select_kernel<T, 3>), dim3((unsigned)wgs), dim3(SEL_NT), 0, s, a, part, n, per);
+    else hipLaunchKernelGGL((select_kernel<T, 5>), dim3((unsigned)wgs), dim3(SEL_NT), 0, s, a, part, n, per);
     if (n > 1) hipLaunchKernelGGL(select_merge_kernel, dim3(ceil_div(a.T, 4)), dim3(256), 0, s, a, (const SelectPart*)part, n);
 }
 

@@ -116,8 +116,10 @@ template <class F> __device__ __forceinline__ uint32_t wave_fold2(uint32_t v0, u
 //
 // What bounds it: reading the logits (16 bytes a lane, also from rows that start at odd
 // elements: the hardware takes unaligned addresses) beside about 11 VALU instructions an id and
-// latency: five waves a SIMD (96 VGPRs) hide more of it than four of 109 or six with spills
-// (256 rows of 152064 bf16 logits, adjusted logits kept: 61, 70 and 73 us).
+// latency: five waves a SIMD (WPE 5: 96 VGPRs) hide more of it than four of 109 or six with spills
+// (256 rows of 152064 bf16 logits, adjusted logits kept: 52 us, 59, and 3 us more than the latter; a torch
+// copy of that size takes 45).  Where four a SIMD hold all workgroups, their registers save the spills (WPE 3, up to 123 VGPRs): 32 rows of
+// 126464 fp32 logits 11.3 and 12.6 us, of 1024 7.8 and 8.2.
 constexpr int SEL_NT = 256, SEL_PT = 8, SEL_IDS = SEL_NT * SEL_PT, SEL_RB = 4, SEL_MAX_ROWS = 16;
 struct alignas(16) SelectPart {
     float mx;
@@ -126,8 +128,8 @@ struct alignas(16) SelectPart {
     int pad;
 };
 
-template <typename T>
-__global__ void __launch_bounds__(SEL_NT) __attribute__((amdgpu_waves_per_eu(5))) select_kernel(SelectArgs a, SelectPart* part, int n_ranges, int rows_per) {
+template <typename T, int WPE>
+__global__ void __launch_bounds__(SEL_NT) __attribute__((amdgpu_waves_per_eu(WPE))) select_kernel(SelectArgs a, SelectPart* part, int n_ranges, int rows_per) {
     constexpr int NL = 16 / (int)sizeof(T), U = SEL_PT / NL;   // ids per 16-byte load, loads per row
     constexpr int HB = 4;                                      // history entries a thread loads at once
     __shared__ uint32_t adj_s[SEL_IDS], last_s[SEL_IDS];
