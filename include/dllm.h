@@ -510,7 +510,8 @@ int dllm_qk_norm_rope(const dllm_qk_args* args, dllm_stream stream);
  * id, are never used, whatever they hold; an infinity or NaN in a key that a row sees is
  * in that row's result alone.  Rows from d_row0[n_seqs] on are left as they
  * were.  max_rows and max_len bound the rows and keys (d_len) of any sequence: they size
- * the launch; a sequence beyond them gets wrong values, but no access is out of bounds.
+ * the launch; a sequence beyond them gets wrong values, but no access is out of bounds,
+ * whatever d_row0 holds.  max_rows past n_rows (2^31 - 1: no bound known) counts as n_rows.
  * n_rows bounds d_row0[n_seqs].  The workspace of dllm_attention_paged_ws() bytes is the
  * caller's; calls that may overlap, and captured graphs that may, need one each.  E_INVAL for
  * NULL pointers, sizes out of range, pointers or row strides that are not multiples of

@@ -24,6 +24,7 @@
 //   product i takes exactly key i of every group.  Dims of a 16-dim step go 4g + i the same way.
 #pragma once
 
+#include "batch_rules.hpp"
 #include "common.hpp"
 #include "qk_rope.hpp"
 
@@ -195,17 +196,18 @@ attn_paged_kernel(PagedArgs a) {
     const int n_items = own ? (int)gridDim.x - a.n_s : a.n_s;
     const int L = (int)blockIdx.x - (own ? a.n_s : 0), xcd = L & 7;
     const int item = xcd * (n_items >> 3) + min(xcd, n_items & 7) + (L >> 3);
-    int tile, split, hk, b, ks, ke, R0, R1, bps, part;
+    int tile, split, hk, b, ks, ke, first, behind, most_rows, bps, part;
     if (own) {
         tile = item % a.nt_o;
         const int i1 = item / a.nt_o, i2 = i1 / a.ns_o;
         split = i1 % a.ns_o;
         hk = i2 % a.Hk;
         b = i2 / a.Hk;
-        R0 = a.row0[b];
-        R1 = min(a.row0[b + 1], R0 + a.max_rows);
+        first = a.row0[b];
+        behind = a.row0[b + 1];
+        most_rows = a.max_rows;
         ks = a.shared;
-        ke = min(a.len[b], a.max_len);
+        ke = min(max(a.len[b], 0), a.max_len);
         // steps per split from the sequence's own length: a short one is still spread
         const int nst = (max(0, ke - ks) + 32 * SUB - 1) / (32 * SUB);
         bps = (nst + a.ns_o - 1) / a.ns_o;
@@ -216,8 +218,9 @@ attn_paged_kernel(PagedArgs a) {
         split = i1 % a.ns_s;
         hk = i1 / a.ns_s;
         b = 0;
-        R0 = a.row0[0];
-        R1 = a.row0[a.B];
+        first = a.row0[0];
+        behind = a.row0[a.B];
+        most_rows = a.T;
         ks = 0;
         ke = min(a.shared, a.max_len);
         bps = ((ke + 32 * SUB - 1) / (32 * SUB) + a.ns_s - 1) / a.ns_s;
@@ -235,9 +238,9 @@ attn_paged_kernel(PagedArgs a) {
     };
     int pgv = chunk_pages(0);
     const long page_elems = (long)DH << a.page_shift;
-    R0 = max(R0, 0);
-    R1 = min(R1, a.T);
-    const int nv = (R1 - R0) * a.G;           // virtual rows of the part
+    const RowRange rows = row_range(first, behind, most_rows, a.T);
+    const int R0 = rows.begin, R1 = rows.end;
+    const int nv = (R1 - R0) * a.G;           // virtual rows of the part (n_rows * G fits 32 bits)
     const int f0 = tile * TM;
     if (f0 >= nv) return;
 
@@ -644,7 +647,8 @@ template <typename T, int DH>
 __global__ void __launch_bounds__(256) attn_paged_merge_kernel(PagedArgs a) {
     constexpr int LPP = DH / 4, MAXW = 2 * MAX_ATTN_SPLITS / LPP;      // weights per lane
     const int pair = blockIdx.x * (256 / LPP) + threadIdx.x / LPP, li = threadIdx.x % LPP;
-    const int R0 = max(a.row0[0], 0), R1 = min(a.row0[a.B], a.T);
+    const RowRange rows = row_range(a.row0[0], a.row0[a.B], a.T, a.T);
+    const int R0 = rows.begin, R1 = rows.end;
     const int row = min(R0 + pair / a.H, a.T - 1), h = pair % a.H;
     const size_t rec = (size_t)row * a.H + h, step = (size_t)a.T * a.H;
     const int np = a.ns_s + a.ns_o;

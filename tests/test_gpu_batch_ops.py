@@ -437,6 +437,42 @@ def test_attention_arguments_that_do_not_fit(dl, bad):
         dl.dllm_attention_paged(c["qt"], c["kt"], c["vt"], i32(c["table"]), i32(c["row0"]), i32(c["lens"]), c["qt"].clone(), **args)
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("rows,lens,H,Hk,shared", [
+    ([3, 5, 0, 7], [90, 40, 64, 130], 2, 2, 0), ([3, 5, 0, 7], [90, 40, 64, 130], 4, 2, 0), ([20, 33, 17], [300, 250, 90], 7, 1, 64),
+    ([1] * 33, [540] * 32 + [500], 1, 1, 512)])
+def test_attention_without_a_bound_of_rows(dl, dtype, rows, lens, H, Hk, shared):
+    """max_rows = 2^31 - 1, no bound at all: the results of the tight one, and the rows behind the last as they were."""
+    import torch
+    c = attn_case(np.random.default_rng(24), dtype, rows, lens, H, Hk, 128, 32, shared, extra_rows=40)
+    want = check_attn(dl, c, dtype)
+    for bound in (max(rows) + 1, len(want), 2 ** 31 - max(rows), 2 ** 31 - 1):
+        out = torch.full((len(want) + 64, H, 128), 7.0, dtype=tdtype(dtype), device="cuda")
+        dl.dllm_attention_paged(c["qt"], c["kt"], c["vt"], i32(c["table"]), i32(c["row0"]), i32(c["lens"]), out[:len(want)], bound,
+                                int(max(lens)), shared_len=shared)
+        torch.cuda.synchronize()
+        T = sum(rows)
+        assert out[T:].eq(7.0).all(), bound
+        # (another bound may choose another tile: two results inside the same bound of the reference)
+        ref = attention(c["q"], c["kp"], c["vp"], c["table"], c["row0"], c["lens"], None, shared, 32, 128 ** -0.5, dtype)
+        got = out.double().cpu().numpy()
+        assert all((abs(got[r] - o) <= b + 1e-30).all() for r, (o, b) in ref.items()), bound
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_attention_negative_lengths_are_empty(dl, dtype):
+    """A sequence of a negative length sees nothing; the others are not touched by it."""
+    import torch
+    c = attn_case(np.random.default_rng(25), dtype, [3, 20, 4], [500, 430, 90], 4, 2, 64, 32, 64)
+    want = check_attn(dl, c, dtype)
+    for n in (-1, -2 ** 31):
+        got = torch.full_like(c["qt"], 7.0)
+        dl.dllm_attention_paged(c["qt"], c["kt"], c["vt"], i32(c["table"]), i32(c["row0"]), i32([500, n, 90]), got, 20, 500,
+                                shared_len=64)
+        torch.cuda.synchronize()
+        assert not got[3:23].any() and torch.equal(got[:3], want[:3]) and torch.equal(got[23:], want[23:])
+
+
 def test_offsets_past_32_bits(dl):
     """A pool of more than 2^31 elements a plane: the same bits from its last pages as from a small pool's."""
     import torch
