@@ -141,8 +141,6 @@ template <typename T> __device__ __forceinline__ T attn_out(float o) {
     return __builtin_fabsf(o) == INFINITY ? (T)o : elem_from_f32<T>(o);
 }
 
-constexpr int MAX_ATTN_SPLITS = 64;           // key splits of a part
-
 // log2-domain slack of the lazily moved reference: probabilities <= 2^8 (fits fp16)
 constexpr float PAGED_SLACK = 8.f;
 

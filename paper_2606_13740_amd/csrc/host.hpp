@@ -1,4 +1,4 @@
-// What the library's translation units share on the host: errors and small arithmetic.
+// What the library's translation units share on the host: errors and small arithmetic (arith.hpp).
 #pragma once
 
 #include <hip/hip_runtime.h>
@@ -6,6 +6,7 @@
 #include <string>
 
 #include "../../include/dllm.h"
+#include "arith.hpp"
 
 namespace dllm {
 
@@ -18,8 +19,5 @@ int fail(int code, const std::string& msg);
         if (_e != hipSuccess)                                                                   \
             return fail(DLLM_E_HIP, std::string(#expr) + ": " + hipGetErrorString(_e));        \
     } while (0)
-
-inline int ceil_div(long a, long b) { return (int)((a + b - 1) / b); }
-inline long round_up(long a, long b) { return (a + b - 1) / b * b; }
 
 }  // namespace dllm

@@ -1,6 +1,7 @@
 // Norm of every query and key head, rotation and cache write in one pass.
 #pragma once
 
+#include "batch_rules.hpp"
 #include "common.hpp"
 
 namespace dllm {
@@ -50,7 +51,6 @@ template <typename T> __device__ __forceinline__ void store8(T* p, const float (
 //
 // What bounds it: HBM, each element read and written once: 16384 rows of 28 + 2 x 4 fp16 heads of 128 in 65 us,
 // 4.7 TB/s, the rate of a large copy (4.76).  A window's rows are launch and latency: 4 to 256 rows 6 to 7.5 us.
-constexpr int QK_VROWS = 64;
 template <typename T, int DH>
 __global__ void __launch_bounds__(256) qk_norm_rope_kernel(QkArgs a, int qk_wgs, int hp) {
     constexpr int ES = sizeof(T);

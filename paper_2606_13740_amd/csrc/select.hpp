@@ -6,6 +6,7 @@
 #include <type_traits>
 
 #include "attn_paged.hpp"
+#include "batch_rules.hpp"
 #include "common.hpp"
 #include "qk_rope.hpp"
 
@@ -120,7 +121,6 @@ template <class F> __device__ __forceinline__ uint32_t wave_fold2(uint32_t v0, u
 // (256 rows of 152064 bf16 logits, adjusted logits kept: 52 us, 59, and 3 us more than the latter; a torch
 // copy of that size takes 45).  Where four a SIMD hold all workgroups, their registers save the spills (WPE 3, up to 123 VGPRs): 32 rows of
 // 126464 fp32 logits 11.3 and 12.6 us, of 1024 7.8 and 8.2.
-constexpr int SEL_NT = 256, SEL_PT = 8, SEL_IDS = SEL_NT * SEL_PT, SEL_RB = 4, SEL_MAX_ROWS = 16;
 struct alignas(16) SelectPart {
     float mx;
     int id;

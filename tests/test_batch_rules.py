@@ -5,6 +5,8 @@ import subprocess
 
 import pytest
 
+import batch_large
+
 ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 
 
@@ -43,3 +45,47 @@ int main() {
 }
 """)
     assert int(out) == 4 * 16 * 16 * 8
+
+
+def test_large_calls_get_the_launch_that_they_are_there_for(tmp_path):
+    """Tiles, shared part, workgroup rows and heads a lane group of batch_large's cases, from the rules themselves."""
+    body = r"""
+int main(int argc, char** argv) {
+    char kind;
+    while (scanf(" %c", &kind) == 1) {
+        if (kind == 'a') {
+            dllm_attn_args g{};
+            if (scanf("%d %d %d %d %d %d %d %d %d %d %d", &g.dtype, &g.n_rows, &g.n_seqs, &g.n_heads, &g.n_kv_heads, &g.head_dim,
+                      &g.page, &g.table_ld, &g.shared_len, &g.max_rows, &g.max_len) != 11) return 1;
+            const AttnPlan p = attn_plan(&g);
+            printf("%d %d\n", 16 * p.qg * p.qt, p.shared > 0 && p.ns_s > 0);
+        } else if (kind == 's') {
+            int T, V;
+            if (scanf("%d %d", &T, &V) != 2) return 1;
+            const int n = select_ranges(V);
+            printf("%d %d\n", select_rows_per(T, n), select_four_waves(select_wgs(T, n)));
+        } else {
+            int T, H, Hk;
+            if (scanf("%d %d %d", &T, &H, &Hk) != 3) return 1;
+            printf("%d 0\n", qk_heads_per(T, H, Hk));
+        }
+    }
+}
+"""
+    asked, want = [], []
+    for c in batch_large.ATTN:
+        for dtype in c.dtypes:
+            asked.append("a " + " ".join(map(str, c.plan_args(dtype))))
+            want.append((f"{c.name} {dtype}", (c.tile, int(c.shared))))
+    for *args, tile in batch_large.ODD:
+        asked.append("a " + " ".join(map(str, batch_large.odd_plan_args(*args))))
+        want.append((f"infinities {args[0]} {tile}", (tile, 1)))
+    for rows, V, _, _, _, per, four in batch_large.SELECT:
+        asked.append(f"s {sum(rows)} {V}")
+        want.append((f"select {sum(rows)}", (per, int(four))))
+    for T, H, Hk, _, _, heads in batch_large.QK:
+        asked.append(f"q {T} {H} {Hk}")
+        want.append((f"qk {T}", (heads, 0)))
+    out = run_cpp(tmp_path, body, stdin="\n".join(asked)).split("\n")
+    got = [(name, tuple(int(x) for x in line.split())) for (name, _), line in zip(want, out)]
+    assert got == want
