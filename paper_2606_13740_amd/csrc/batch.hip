@@ -181,6 +181,49 @@ int check_select(const dllm_select_args* g) {
 
 }  // namespace
 
+namespace dllm {
+
+// Every check of a selection.
+int select_check(const dllm_select_args* g) {
+    if (int rc = check_select(g)) return rc;
+    if (!g->d_logits || !g->d_out_id || !g->d_out_conf) return fail(DLLM_E_INVAL, "NULL argument");
+    if (!g->d_row0 && g->n_seqs != 1) return fail(DLLM_E_INVAL, "row0 may be NULL only for one sequence");
+    if (g->d_hist && !g->d_hist0) return fail(DLLM_E_INVAL, "hist needs hist0");
+    if (!g->d_hist && (g->d_repetition || g->d_presence || g->d_frequency || g->d_n_prompt))
+        return fail(DLLM_E_INVAL, "penalties need a history");
+    if ((g->d_bias == nullptr) != (g->d_bias_id == nullptr) || (g->d_bias == nullptr) != (g->d_bias0 == nullptr))
+        return fail(DLLM_E_INVAL, "bias, bias_id and bias0 must all be set or all be NULL");
+    if (g->d_allow) {
+        if (g->n_allow < 1 || g->allow_ld < 1) return fail(DLLM_E_INVAL, "n_allow and allow_ld must be >= 1");
+        if ((long)g->allow_ld * 32 < g->vocab) return fail(DLLM_E_INVAL, "allow_ld words do not cover the vocabulary");
+        if (!g->d_allow_row && g->n_allow < g->n_rows) return fail(DLLM_E_INVAL, "a mask per row needs n_allow >= n_rows");
+    } else if (g->d_allow_row) {
+        return fail(DLLM_E_INVAL, "allow_row needs allow");
+    }
+    const int es = esize(g->dtype);
+    if (g->ld < g->vocab || g->ld > (1ll << 40) || !aligned(g->d_logits, es))
+        return fail(DLLM_E_INVAL, "logits: stride of at least a row, pointer aligned to its elements");
+    if (g->d_out_logits && (g->ld_out < g->vocab || g->ld_out > (1ll << 40) || !aligned(g->d_out_logits, es)))
+        return fail(DLLM_E_INVAL, "out_logits: stride of at least a row, pointer aligned to its elements");
+    if (g->d_out_logits == g->d_logits && g->ld_out != g->ld)
+        return fail(DLLM_E_INVAL, "out_logits may be logits only with the same stride");
+    const void* ints[] = {g->d_row0, g->d_hist, g->d_hist0, g->d_n_prompt, g->d_repetition, g->d_presence,
+                          g->d_frequency, g->d_bias_id, g->d_bias, g->d_bias0, g->d_allow, g->d_allow_row,
+                          g->d_out_id, g->d_out_conf};
+    for (const void* p : ints)
+        if (!aligned(p, 4)) return fail(DLLM_E_INVAL, "arrays of 32-bit values must be 4-byte aligned");
+    if (g->n_rows == 0) return DLLM_OK;               // (no workspace, no launch)
+    const size_t need = select_ws_bytes(g);
+    if (!grid_ok(select_wgs(g->n_rows, select_ranges(g->vocab)), SEL_NT))
+        return fail(DLLM_E_INVAL, "n_rows and vocab need too many workgroups");
+    if (need > 0 && (!g->d_ws || !aligned(g->d_ws, 16))) return fail(DLLM_E_INVAL, "workspace: NULL or not 16-byte aligned");
+    if (need > g->ws_bytes)
+        return fail(DLLM_E_CAPACITY, "the call needs " + std::to_string(need) + " bytes of workspace");
+    return DLLM_OK;
+}
+
+}  // namespace dllm
+
 extern "C" {
 
 int dllm_qk_norm_rope(const dllm_qk_args* g, dllm_stream stream) {
@@ -272,40 +315,8 @@ int dllm_select_ws(const dllm_select_args* g, size_t* bytes) {
 }
 
 int dllm_select(const dllm_select_args* g, dllm_stream stream) {
-    if (int rc = check_select(g)) return rc;
-    if (!g->d_logits || !g->d_out_id || !g->d_out_conf) return fail(DLLM_E_INVAL, "NULL argument");
-    if (!g->d_row0 && g->n_seqs != 1) return fail(DLLM_E_INVAL, "row0 may be NULL only for one sequence");
-    if (g->d_hist && !g->d_hist0) return fail(DLLM_E_INVAL, "hist needs hist0");
-    if (!g->d_hist && (g->d_repetition || g->d_presence || g->d_frequency || g->d_n_prompt))
-        return fail(DLLM_E_INVAL, "penalties need a history");
-    if ((g->d_bias == nullptr) != (g->d_bias_id == nullptr) || (g->d_bias == nullptr) != (g->d_bias0 == nullptr))
-        return fail(DLLM_E_INVAL, "bias, bias_id and bias0 must all be set or all be NULL");
-    if (g->d_allow) {
-        if (g->n_allow < 1 || g->allow_ld < 1) return fail(DLLM_E_INVAL, "n_allow and allow_ld must be >= 1");
-        if ((long)g->allow_ld * 32 < g->vocab) return fail(DLLM_E_INVAL, "allow_ld words do not cover the vocabulary");
-        if (!g->d_allow_row && g->n_allow < g->n_rows) return fail(DLLM_E_INVAL, "a mask per row needs n_allow >= n_rows");
-    } else if (g->d_allow_row) {
-        return fail(DLLM_E_INVAL, "allow_row needs allow");
-    }
-    const int es = esize(g->dtype);
-    if (g->ld < g->vocab || g->ld > (1ll << 40) || !aligned(g->d_logits, es))
-        return fail(DLLM_E_INVAL, "logits: stride of at least a row, pointer aligned to its elements");
-    if (g->d_out_logits && (g->ld_out < g->vocab || g->ld_out > (1ll << 40) || !aligned(g->d_out_logits, es)))
-        return fail(DLLM_E_INVAL, "out_logits: stride of at least a row, pointer aligned to its elements");
-    if (g->d_out_logits == g->d_logits && g->ld_out != g->ld)
-        return fail(DLLM_E_INVAL, "out_logits may be logits only with the same stride");
-    const void* ints[] = {g->d_row0, g->d_hist, g->d_hist0, g->d_n_prompt, g->d_repetition, g->d_presence,
-                          g->d_frequency, g->d_bias_id, g->d_bias, g->d_bias0, g->d_allow, g->d_allow_row,
-                          g->d_out_id, g->d_out_conf};
-    for (const void* p : ints)
-        if (!aligned(p, 4)) return fail(DLLM_E_INVAL, "arrays of 32-bit values must be 4-byte aligned");
+    if (int rc = select_check(g)) return rc;
     if (g->n_rows == 0) return DLLM_OK;
-    const size_t need = select_ws_bytes(g);
-    if (!grid_ok(select_wgs(g->n_rows, select_ranges(g->vocab)), SEL_NT))
-        return fail(DLLM_E_INVAL, "n_rows and vocab need too many workgroups");
-    if (need > 0 && (!g->d_ws || !aligned(g->d_ws, 16))) return fail(DLLM_E_INVAL, "workspace: NULL or not 16-byte aligned");
-    if (need > g->ws_bytes)
-        return fail(DLLM_E_CAPACITY, "the call needs " + std::to_string(need) + " bytes of workspace");
     SelectArgs a{g->d_logits, g->ld, g->n_rows, g->vocab, g->mask_id, g->n_seqs, g->d_row0, g->d_hist, g->d_hist0,
                  g->d_n_prompt, g->d_repetition, g->d_presence, g->d_frequency, g->d_bias_id, g->d_bias, g->d_bias0,
                  g->d_allow, g->n_allow, g->allow_ld, g->d_allow_row, g->d_out_logits, g->ld_out, g->d_out_id,

@@ -1231,15 +1231,7 @@ int dllm_batch_step(dllm_model* m, void* d_pages, size_t bytes, const dllm_batch
         if (sa.mask_id != m->cfg.mask_id) return fail(DLLM_E_INVAL, "selection: mask_id must be the model's");
         sa.d_out_id = d_out_id;
         sa.d_out_conf = d_out_conf;
-        // (checked before any launch: a call without rows validates and queues nothing)
-        dllm_select_args probe = sa;
-        size_t ws = 0;
-        if ((rc = dllm_select_ws(&sa, &ws))) return rc;
-        if (sa.ws_bytes < ws) return fail(DLLM_E_CAPACITY, "selection: workspace smaller than dllm_select_ws()");
-        if (ws > 0 && !sa.d_ws) return fail(DLLM_E_INVAL, "selection: NULL workspace");
-        if (sa.d_allow && !sa.d_allow_row && sa.n_allow < sa.n_rows) return fail(DLLM_E_INVAL, "selection: a mask per row needs n_allow >= n_rows");
-        probe.n_rows = 0;
-        if ((rc = dllm_select(&probe, stream))) return rc;
+        if ((rc = select_check(&sa))) return rc;       // before any launch
     }
     dllm_attn_args ga = batch_attn_args(m, b);
     size_t aws = 0;

@@ -13,6 +13,9 @@ namespace dllm {
 // Records msg as the thread's dllm_last_error() and returns code (dllm.hip).
 int fail(int code, const std::string& msg);
 
+// Every check of a dllm_select call, without a launch (batch.hip).
+int select_check(const dllm_select_args* args);
+
 #define HIP_TRY(expr)                                                                           \
     do {                                                                                        \
         hipError_t _e = (expr);                                                                 \

@@ -1,0 +1,45 @@
+"""Batch calls that are refused, and what they leave behind."""
+import dataclasses
+
+import numpy as np
+import pytest
+
+import synth
+from gpu_util import build_pair, dev_i32
+from test_gpu_batch_step import Batch, scene
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def dl():
+    import paper_2606_13740_amd as pkg
+    return pkg
+
+
+def wide_batch(dl, V=5000):
+    """A batch of two sequences of a small model whose logits take a selection with a workspace, and a step's rows."""
+    shape = dataclasses.replace(synth.TINY, vocab=V, mask_id=V - 1)
+    model, _, _ = build_pair(shape, "f32", oracle_too=False)
+    prompt, own, win = scene(shape, 64, [10, 20], [9, 5], seed=5)
+    bt = Batch(dl, model, 2, prompt)
+    bt.step(np.concatenate(own), None, np.array([10, 20]))
+    return shape, model, bt, np.concatenate([t for t, _ in win]), np.concatenate([m for _, m in win])
+
+
+def test_a_step_with_a_refused_selection_does_nothing(dl):
+    """Every refusal of the selection comes before the step's first launch: no K/V, no outputs, no logits."""
+    import torch
+    shape, model, bt, tok, mask = wide_batch(dl)
+    logits = torch.full((14, shape.vocab), 3.0, device="cuda")
+    bt.step(tok, mask, np.array([9, 5]), commit=False, out=True, logits=logits, control=dict(mask_id=shape.mask_id))
+    args, kw = bt.last
+    args[-2].fill_(-5), args[-1].fill_(9.0), logits.fill_(3.0)
+    bt.pages.fill_(0x11)
+    before = bt.pages.clone()
+    ws = torch.zeros(4096, dtype=torch.uint8, device="cuda")
+    for bad in (dict(ws=ws[8:]), dict(ws=ws[:64]), dict(mask_id=5), dict(allow=dev_i32([[0] * 200])), dict(allow=dev_i32([[0] * 9] * 20))):
+        with pytest.raises(dl.DllmError):
+            dl.dllm_batch_step(*args, **dict(kw, control=dict(dict(mask_id=shape.mask_id), **bad)))
+        torch.cuda.synchronize()
+        assert args[-2].eq(-5).all() and args[-1].eq(9.0).all() and logits.eq(3.0).all() and torch.equal(bt.pages, before), bad
