@@ -484,9 +484,9 @@ int alloc_zero(void** p, size_t bytes) {
 // The buffers of a workspace for `rows` token rows (a multiple of 64), LM-head and
 // attention partials for `wrows` rows, and `part_floats` split-K partials, laid out
 // one after another (256-byte aligned) from `base`.  Returns the bytes they take; with
-// base == nullptr only the size is computed.  Every user of a workspace (the model's
+// base == nullptr only the size is computed.  qkv: with Q/K/V rows.  Every user of a workspace (the model's
 // own, grown on demand, and the no-allocation step's static scratch) is carved here.
-size_t ws_carve(const dllm_model* m, int rows, int wrows, size_t part_floats, char* base, Workspace* w);
+size_t ws_carve(const dllm_model* m, int rows, int wrows, size_t part_floats, bool qkv, char* base, Workspace* w);
 
 // Split-K partials: RES_SPLIT slices of the window rows (O and down of up to 64 rows), and
 // what the tiled layouts of up to `rows` rows plan with (QKV, O and down past 64 rows).
@@ -505,11 +505,11 @@ int ensure_ws(dllm_model* m, int rows_needed) {
     if (had > rows) return ensure_ws(m, had);     // grown for the Q/K/V rows only: never smaller than before
     const int wrows = (int)round_up(c.max_window, 64);
     const size_t part_floats = part_floats_for(m, rows, wrows);
-    const size_t bytes = ws_carve(m, rows, wrows, part_floats, nullptr, nullptr);
+    const size_t bytes = ws_carve(m, rows, wrows, part_floats, m->rows_qkv, nullptr, nullptr);
     void* blk = nullptr;
     int rc = alloc_zero(&blk, bytes);
     if (rc) return rc;
-    ws_carve(m, rows, wrows, part_floats, (char*)blk, &m->ws);
+    ws_carve(m, rows, wrows, part_floats, m->rows_qkv, (char*)blk, &m->ws);
     m->ws.block = blk;
     return DLLM_OK;
 }
@@ -518,7 +518,7 @@ int ensure_ws(dllm_model* m, int rows_needed) {
 // Weight prepacking
 // ---------------------------------------------------------------------------
 
-size_t ws_carve(const dllm_model* m, int rows, int wrows, size_t part_floats, char* base, Workspace* w) {
+size_t ws_carve(const dllm_model* m, int rows, int wrows, size_t part_floats, bool qkv, char* base, Workspace* w) {
     const dllm_config& c = m->cfg;
     const size_t d = c.d_model;
     const size_t xchunk = m->xf32 ? 1024 : 2048;   // an activation chunk: fp32, or bf16 hi + lo
@@ -555,7 +555,7 @@ size_t ws_carve(const dllm_model* m, int rows, int wrows, size_t part_floats, ch
     take(v.oid, (size_t)rows * 4);
     take(v.oconf, (size_t)rows * 4);
     take(v.need, (size_t)rows);
-    if (m->rows_qkv) take(v.qkv, (size_t)rows * m->layers[0].qkv.n_tiles * 16 * 4);
+    if (qkv) take(v.qkv, (size_t)rows * m->layers[0].qkv.n_tiles * 16 * 4);
     return off;
 }
 
@@ -1342,14 +1342,15 @@ int dllm_denoise_step_noalloc(dllm_model* m, dllm_kv* kv, const int32_t* d_tok, 
     if (!d_out_id || !d_out_conf) return fail(DLLM_E_INVAL, "output pointer is NULL");
     const int rows = (int)round_up(W, 64);
     const size_t part_floats = part_floats_for(m, rows, rows);
-    const size_t need = ws_carve(m, rows, rows, part_floats, nullptr, nullptr);
+    const bool qkv = m->hgpool != nullptr;                    // (batch steps before this one are none of its business)
+    const size_t need = ws_carve(m, rows, rows, part_floats, qkv, nullptr, nullptr);
     if (need > SCRATCH_BYTES)
         return fail(DLLM_E_CAPACITY, "the step needs " + std::to_string(need) + " bytes of scratch; the static scratch holds " +
                                          std::to_string(SCRATCH_BYTES));
     void* base = nullptr;
     if ((rc = scratch_ptr(&base))) return rc;
     Workspace w;
-    ws_carve(m, rows, rows, part_floats, (char*)base, &w);
+    ws_carve(m, rows, rows, part_floats, qkv, (char*)base, &w);
     // padding columns of the activation fragments (widths that are not whole chunks):
     // never written by the step, multiplied by zero weights, so they must be zeros
     const int kcol = m->xf32 ? 16 : 32;

@@ -5,7 +5,7 @@ import numpy as np
 import pytest
 
 import synth
-from gpu_util import build_pair, dev_i32
+from gpu_util import build_pair, dev_i32, dev_u8
 from test_gpu_batch_step import Batch, scene
 
 pytestmark = pytest.mark.gpu
@@ -43,3 +43,22 @@ def test_a_step_with_a_refused_selection_does_nothing(dl):
             dl.dllm_batch_step(*args, **dict(kw, control=dict(dict(mask_id=shape.mask_id), **bad)))
         torch.cuda.synchronize()
         assert args[-2].eq(-5).all() and args[-1].eq(9.0).all() and logits.eq(3.0).all() and torch.equal(bt.pages, before), bad
+
+
+def test_a_batch_step_takes_nothing_from_the_static_scratch(dl):
+    """A 256-row step that just fits the no-allocation step's 64 MiB (249 KB a row) fits them after a batch step too, whose
+    Q/K/V rows (24 KB a row) are in the model's own workspace."""
+    import torch
+    shape = dataclasses.replace(synth.SMALL_BF16, n_layers=1, d_model=2048, n_heads=16, d_ff=4096)
+    model, _, _ = build_pair(shape, "bf16", max_window=256, oracle_too=False)
+    kv = dl.KVCache(model, 512)
+    dl.dllm_prefill(model.handle, kv.handle, dev_i32(synth.prompt_ids(shape, 64)), 64)
+    tok, mask = (f(a) for f, a in zip((dev_i32, dev_u8), synth.window(shape, 256, range(8, 256))))
+    outs = []
+    for i in range(2):
+        ids, conf = torch.zeros(256, dtype=torch.int32, device="cuda"), torch.zeros(256, device="cuda")
+        dl.dllm_denoise_step_noalloc(model.handle, kv.handle, tok, mask, 256, ids, conf)
+        outs += [ids, conf]
+        if i == 0:
+            Batch(dl, model, 2, synth.prompt_ids(shape, 64))
+    assert torch.equal(outs[0], outs[2]) and torch.equal(outs[1], outs[3]) and outs[1].gt(0).all()
