@@ -472,11 +472,17 @@ void outgrown(dllm_model* m, void* p) {
     else if (p) (void)hipFree(p);
 }
 
-int alloc_zero(void** p, size_t bytes) {
+int alloc(void** p, size_t bytes) {
     if (hipMalloc(p, std::max<size_t>(bytes, 256)) != hipSuccess) {
         *p = nullptr;
+        (void)hipGetLastError();
         return fail(DLLM_E_NOMEM, "device allocation of " + std::to_string(bytes) + " bytes failed");
     }
+    return DLLM_OK;
+}
+
+int alloc_zero(void** p, size_t bytes) {
+    if (int rc = alloc(p, bytes)) return rc;
     HIP_TRY(hipMemset(*p, 0, std::max<size_t>(bytes, 256)));
     return DLLM_OK;
 }
@@ -1187,6 +1193,7 @@ int dllm_model_set_qk_norm(dllm_model* m, const float* const* d_q_gain, const fl
     }
     if (e == hipSuccess) e = hipStreamSynchronize(s);
     if (e != hipSuccess) {
+        (void)hipGetLastError();
         if (pool != m->hgpool) (void)hipFree(pool);
         return fail(DLLM_E_HIP, std::string("copying the heads' gains failed: ") + hipGetErrorString(e));
     }
@@ -1243,8 +1250,7 @@ int dllm_batch_step(dllm_model* m, void* d_pages, size_t bytes, const dllm_batch
         outgrown(m, m->attn_ws);
         m->attn_ws = nullptr;
         m->attn_ws_bytes = 0;
-        if (hipMalloc(&m->attn_ws, aws) != hipSuccess)
-            return fail(DLLM_E_NOMEM, "device allocation of " + std::to_string(aws) + " bytes failed");
+        if ((rc = alloc(&m->attn_ws, aws))) return rc;
         m->attn_ws_bytes = aws;
     }
     FwdArgs a{};

@@ -16,11 +16,15 @@ int fail(int code, const std::string& msg);
 // Every check of a dllm_select call, without a launch (batch.hip).
 int select_check(const dllm_select_args* args);
 
+// An error that a call reports is taken from the runtime, so that the next call (or another library) does not
+// find it and report it again.
 #define HIP_TRY(expr)                                                                           \
     do {                                                                                        \
         hipError_t _e = (expr);                                                                 \
-        if (_e != hipSuccess)                                                                   \
+        if (_e != hipSuccess) {                                                                 \
+            (void)hipGetLastError();                                                            \
             return fail(DLLM_E_HIP, std::string(#expr) + ": " + hipGetErrorString(_e));        \
+        }                                                                                       \
     } while (0)
 
 }  // namespace dllm

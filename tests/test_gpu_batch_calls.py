@@ -62,3 +62,25 @@ def test_a_batch_step_takes_nothing_from_the_static_scratch(dl):
         if i == 0:
             Batch(dl, model, 2, synth.prompt_ids(shape, 64))
     assert torch.equal(outs[0], outs[2]) and torch.equal(outs[1], outs[3]) and outs[1].gt(0).all()
+
+
+def test_a_step_too_large_for_the_card_leaves_the_model_usable(dl):
+    """A workspace of more bytes than the card has (4 Mi rows of about 80 KB) is refused, and the next calls are what they
+    were before."""
+    import torch
+    shape = dataclasses.replace(synth.SMALL_BF16, n_layers=1, d_model=2048, n_heads=16, d_ff=4096)
+    model, _, _ = build_pair(shape, "bf16", oracle_too=False)
+    bt = Batch(dl, model, 2, synth.prompt_ids(shape, 64))
+    tok = np.arange(40, dtype=np.int32)
+    want = bt.step(tok, None, np.array([30, 10]), commit=False, out=True)
+    n = 1 << 22
+    z = torch.zeros(n, dtype=torch.int32, device="cuda")
+    row0, length = dev_i32([0, n, n]), dev_i32([0, 0])
+    for _ in range(2):
+        with pytest.raises(dl.DllmError) as e:
+            dl.dllm_batch_step(model.handle, bt.pages, bt.n_pages, 32, z, None, bt.table, row0, z, z, length, 1, 1)
+        assert e.value.code == dl.DLLM_E_NOMEM
+        kv = dl.KVCache(model, 128)
+        dl.dllm_prefill(model.handle, kv.handle, dev_i32(synth.prompt_ids(shape, 40)), 40)
+        got = bt.step(tok, None, np.array([30, 10]), commit=False, out=True)
+        assert all(np.array_equal(a, b) for a, b in zip(got, want))
