@@ -648,7 +648,8 @@ typedef struct dllm_batch_rows {
  * synchronises the device); later ones can be captured.  They are the model's, as for every
  * other call: its calls, and replays of graphs captured from them, must not overlap.  A graph
  * stays valid when later calls need larger ones (what it uses is then kept until
- * dllm_model_destroy).  E_INVAL, E_CAPACITY and E_DTYPE as
+ * dllm_model_destroy; workspaces at least double from then on, where memory allows, so that what
+ * is kept stays smaller than what is in use).  E_INVAL, E_CAPACITY and E_DTYPE as
  * the operators' and dllm_denoise_step's; E_CAPACITY if max_len exceeds cfg.max_pos or
  * the pages are fewer than dllm_batch_bytes(). */
 int dllm_batch_step(dllm_model* m, void* d_pages, size_t bytes, const dllm_batch_rows* rows, const int32_t* d_tok,

@@ -500,16 +500,9 @@ size_t part_floats_for(const dllm_model* m, int rows, int wrows) {
     return (size_t)std::max((long)RES_SPLIT * wrows, part_rows(rows)) * m->cfg.d_model;
 }
 
-int ensure_ws(dllm_model* m, int rows_needed) {
-    const dllm_config& c = m->cfg;
-    const int rows = (int)round_up(std::max(rows_needed, 1), 64);
-    if (m->ws.rows >= rows && m->ws.block && (m->ws.qkv || !m->rows_qkv)) return DLLM_OK;
-    HIP_TRY(hipDeviceSynchronize());
-    const int had = m->ws.rows;
-    outgrown(m, m->ws.block);
-    m->ws = Workspace{};
-    if (had > rows) return ensure_ws(m, had);     // grown for the Q/K/V rows only: never smaller than before
-    const int wrows = (int)round_up(c.max_window, 64);
+// A workspace of `rows` rows for a model that has none.
+int alloc_ws(dllm_model* m, int rows) {
+    const int wrows = (int)round_up(m->cfg.max_window, 64);
     const size_t part_floats = part_floats_for(m, rows, wrows);
     const size_t bytes = ws_carve(m, rows, wrows, part_floats, m->rows_qkv, nullptr, nullptr);
     void* blk = nullptr;
@@ -518,6 +511,20 @@ int ensure_ws(dllm_model* m, int rows_needed) {
     ws_carve(m, rows, wrows, part_floats, m->rows_qkv, (char*)blk, &m->ws);
     m->ws.block = blk;
     return DLLM_OK;
+}
+
+int ensure_ws(dllm_model* m, int rows_needed) {
+    int rows = (int)round_up(std::max(rows_needed, 1), 64);
+    if (m->ws.rows >= rows && m->ws.block && (m->ws.qkv || !m->rows_qkv)) return DLLM_OK;
+    HIP_TRY(hipDeviceSynchronize());
+    // Never smaller than before (it may grow for the Q/K/V rows only).  Where the one before is kept, twice its rows
+    // at least: all that are kept then hold fewer rows than the one in use.
+    const int had = m->ws.rows, twice = m->captured && rows > had ? 2 * had : 0;
+    rows = std::max(rows, had);
+    outgrown(m, m->ws.block);
+    m->ws = Workspace{};
+    if (twice > rows && alloc_ws(m, twice) == DLLM_OK) return DLLM_OK;
+    return alloc_ws(m, rows);
 }
 
 // ---------------------------------------------------------------------------
@@ -1247,11 +1254,13 @@ int dllm_batch_step(dllm_model* m, void* d_pages, size_t bytes, const dllm_batch
     if ((rc = ensure_ws(m, b->n_rows))) return rc;
     if (aws > m->attn_ws_bytes) {
         HIP_TRY(hipDeviceSynchronize());
+        const size_t twice = m->captured ? 2 * m->attn_ws_bytes : 0;      // (as in ensure_ws)
         outgrown(m, m->attn_ws);
         m->attn_ws = nullptr;
         m->attn_ws_bytes = 0;
-        if ((rc = alloc(&m->attn_ws, aws))) return rc;
-        m->attn_ws_bytes = aws;
+        size_t take = std::max(aws, twice);
+        if (alloc(&m->attn_ws, take) != DLLM_OK && (rc = alloc(&m->attn_ws, take = aws))) return rc;
+        m->attn_ws_bytes = take;
     }
     FwdArgs a{};
     a.M = b->n_rows; a.tok = d_tok; a.mask = d_mask; a.pos = b->d_pos; a.n_layers = m->cfg.n_layers;

@@ -84,3 +84,42 @@ def test_a_step_too_large_for_the_card_leaves_the_model_usable(dl):
         dl.dllm_prefill(model.handle, kv.handle, dev_i32(synth.prompt_ids(shape, 40)), 40)
         got = bt.step(tok, None, np.array([30, 10]), commit=False, out=True)
         assert all(np.array_equal(a, b) for a, b in zip(got, want))
+
+
+def test_workspaces_kept_for_graphs_stay_few(dl):
+    """Prompts that get longer 64 rows at a time after a capture: what is kept for the graph and the workspace in use take less
+    than four times the workspace that the longest prompt needs, and the graph gives the same ids."""
+    import torch
+    shape = dataclasses.replace(synth.SMALL_BF16, n_layers=1, d_model=1024, n_heads=8, d_ff=2048)
+    top, taken = 1536, []
+
+    def used():
+        torch.cuda.synchronize()
+        torch.cuda.empty_cache()
+        free, total = torch.cuda.mem_get_info()
+        return total - free
+
+    ids = dev_i32(synth.prompt_ids(shape, top))
+    for lengths in ([top], range(64, top + 64, 64)):
+        model, _, _ = build_pair(shape, "bf16", max_pos=2048, oracle_too=False)
+        bt = Batch(dl, model, 2, synth.prompt_ids(shape, 64), n_pages=140)
+        want = bt.step(np.arange(40, dtype=np.int32), None, np.array([30, 10]), commit=False, out=True)
+        args, kw = bt.last
+        g = torch.cuda.CUDAGraph()
+        if len(lengths) > 1:
+            with torch.cuda.graph(g):
+                dl.dllm_batch_step(*args, **kw)
+        before = used()
+        for n in lengths:
+            kv = dl.KVCache(model, top)
+            dl.dllm_prefill(model.handle, kv.handle, ids[:n], n)
+            del kv
+        taken.append(used() - before)
+        if len(lengths) > 1:
+            for _ in range(3):
+                args[-2].fill_(-5)
+                g.replay()
+                torch.cuda.synchronize()
+                assert np.array_equal(args[-2].cpu().numpy(), want[0])
+    print(f"  longest prompt alone {taken[0] >> 20} MiB, grown to it {taken[1] >> 20} MiB", flush=True)
+    assert 0 < taken[0] and taken[1] < 4 * taken[0]
