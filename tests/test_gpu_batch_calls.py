@@ -6,7 +6,7 @@ import pytest
 
 import synth
 from gpu_util import build_pair, dev_i32, dev_u8
-from test_gpu_batch_step import Batch, scene
+from test_gpu_batch_step import Batch, gains, scene
 
 pytestmark = pytest.mark.gpu
 
@@ -123,3 +123,32 @@ def test_workspaces_kept_for_graphs_stay_few(dl):
                 assert np.array_equal(args[-2].cpu().numpy(), want[0])
     print(f"  longest prompt alone {taken[0] >> 20} MiB, grown to it {taken[1] >> 20} MiB", flush=True)
     assert 0 < taken[0] and taken[1] < 4 * taken[0]
+
+
+def test_allocations_on_a_stream_of_its_own(dl):
+    """Model, heads' gains, first prompt and first batch step (each allocates zeroed memory) on a stream that does not wait for
+    the default one: the results of the default stream."""
+    import torch
+    shape = dataclasses.replace(synth.SMALL_BF16, n_layers=1, d_model=1024, n_heads=8, d_ff=2048)
+    tok = np.arange(40, dtype=np.int32)
+
+    def life():
+        model, _, _ = build_pair(shape, "bf16", oracle_too=False)
+        dl.dllm_model_set_qk_norm(model.handle, *gains(shape)[1])
+        kv = dl.KVCache(model, 512)
+        dl.dllm_prefill(model.handle, kv.handle, dev_i32(synth.prompt_ids(shape, 300)), 300)
+        ids, conf = torch.zeros(32, dtype=torch.int32, device="cuda"), torch.zeros(32, device="cuda")
+        dl.dllm_denoise_step(model.handle, kv.handle, dev_i32(tok[:32]), None, 32, ids, conf)
+        bt = Batch(dl, model, 2, synth.prompt_ids(shape, 400))
+        out = bt.step(tok, None, np.array([30, 10]), commit=False, out=True)
+        return [ids.cpu().numpy(), conf.cpu().numpy(), *out]
+
+    want = life()
+    assert (want[1] > 0).all()
+    for _ in range(3):
+        side = torch.cuda.Stream()
+        side.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(side):
+            got = life()
+        side.synchronize()
+        assert all(np.array_equal(a, b) for a, b in zip(got, want))
