@@ -632,6 +632,8 @@ def dllm_batch_step(model: int, pages, n_pages: int, page: int, tok, mask, table
     rows = dllm_batch_rows(R, B, page, n_pages, ld, shared_len, max_rows, max_len, table.data_ptr(), row0.data_ptr(),
                            pos.data_ptr(), slot.data_ptr(), length.data_ptr(), _ptr(lim))
     sel = keep = None
+    if (control and logits is None) or (logits is not None and (out_id is None or out_conf is None)):
+        _refuse(f, "control needs logits, and logits need out_id and out_conf")
     if logits is not None:
         sel, keep, _ = _select_args(f, logits, out_id, out_conf, stream=stream, **(control or {}))
     _check(lib().dllm_batch_step(model, pages.data_ptr(), pages.numel() * pages.element_size(), ctypes.byref(rows),

@@ -152,3 +152,16 @@ def test_allocations_on_a_stream_of_its_own(dl):
             got = life()
         side.synchronize()
         assert all(np.array_equal(a, b) for a, b in zip(got, want))
+
+
+def test_a_control_that_could_not_act_is_refused(dl):
+    """Logits without ids to write, and a control without logits (it was dropped without a word)."""
+    import torch
+    shape, model, bt, tok, mask = wide_batch(dl)
+    bt.step(tok, mask, np.array([9, 5]), commit=False, out=True)
+    args, kw = bt.last
+    logits, control = torch.zeros(14, shape.vocab, device="cuda"), dict(mask_id=shape.mask_id)
+    for a, more in ((args[:-2], dict(logits=logits, control=control)), (args[:-2], dict(logits=logits)), (args, dict(control=control)),
+                    (args[:-1], dict(logits=logits, control=control)), (args[:-2], dict(control=control))):
+        with pytest.raises(dl.DllmError):
+            dl.dllm_batch_step(*a, **dict(kw, **more))
