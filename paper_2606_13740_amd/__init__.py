@@ -367,6 +367,7 @@ def _refuse(func: str, msg: str):
     raise DllmError(DLLM_E_INVAL, func, msg)
 
 
+_NO_SHAPE = (ValueError, IndexError, ZeroDivisionError)
 _NO_FIT = (struct.error, OverflowError)
 _NO_FIT_MSG = "an argument is no number of its field's range"
 
@@ -397,6 +398,9 @@ def _at_least(func: str, n: int, tensors, names: str):
         if t is not None and t.numel() < n:
             bad = names.split()[[u is t for u in tensors].index(True)]
             _refuse(func, f"{bad} must have at least {n} entries")
+
+
+_PAGES_MSG = "k_pages must be [n_pages][kv_heads][page][head_dim], q and q_out [rows][heads][head_dim] or [rows][heads * head_dim]"
 
 
 def _row_stride(func: str, name: str, t, dtype, dev: int, rows: int, heads: int, dim: int) -> int:
@@ -446,9 +450,12 @@ def dllm_qk_norm_rope(q, k, v, rope, pos, slot, q_out, k_pages, v_pages, q_gain=
     """q, k, v: [rows][heads][dim] or [rows][heads * dim], rows may be strided (slices of one projection's output);
     k_pages [n_pages][kv_heads][page][dim], v_pages [n_pages][kv_heads][dim][page]."""
     f, dt = "dllm_qk_norm_rope", q.dtype
-    dev, T, qs = _gpu(f, q), q.shape[0], q_out.shape
-    n_pages, kv, page, dim = k_pages.shape
-    H = qs[1] if len(qs) == 3 else qs[1] // dim
+    dev, qs = _gpu(f, q), q_out.shape
+    try:
+        T, (n_pages, kv, page, dim) = q.shape[0], k_pages.shape
+        H = qs[1] if len(qs) == 3 else qs[1] // dim
+    except _NO_SHAPE:
+        _refuse(f, _PAGES_MSG)
     ld_q, ld_k = _row_stride(f, "q", q, dt, dev, T, H, dim), _row_stride(f, "k", k, dt, dev, T, kv, dim)
     ld_v = _row_stride(f, "v", v, dt, dev, T, kv, dim)
     _plain(f, dev, dt, (k_pages, v_pages, q_out), "k_pages v_pages q_out")
@@ -497,9 +504,12 @@ def dllm_attention_paged(q, k_pages, v_pages, table, row0, length, out, max_rows
     """q, out: [rows][heads][dim] or [rows][heads * dim], rows may be strided; scale: 1 / sqrt(dim) if None;
     k_pages [n_pages][kv_heads][page][dim], v_pages [n_pages][kv_heads][dim][page]."""
     f, dt, sh = "dllm_attention_paged", q.dtype, q.shape
-    dev, T, B, ld = _gpu(f, q), sh[0], length.numel(), table.shape[-1]
-    n_pages, kv, page, dim = k_pages.shape
-    H = sh[1] if len(sh) == 3 else sh[1] // dim
+    dev, B = _gpu(f, q), length.numel()
+    try:
+        T, ld, (n_pages, kv, page, dim) = sh[0], table.shape[-1], k_pages.shape
+        H = sh[1] if len(sh) == 3 else sh[1] // dim
+    except _NO_SHAPE:
+        _refuse(f, _PAGES_MSG)
     ld_q, ld_out = _row_stride(f, "q", q, dt, dev, T, H, dim), _row_stride(f, "out", out, dt, dev, T, H, dim)
     _plain(f, dev, dt, (k_pages, v_pages), "k_pages v_pages")
     _plain(f, dev, _Types.i32, (table, row0, length, lim), "table row0 length lim")
@@ -528,7 +538,12 @@ def _select_args(f, logits, out_id, out_conf, mask_id=-1, row0=None, hist=None, 
                  presence=None, frequency=None, bias_id=None, bias=None, bias0=None, allow=None, allow_row=None,
                  out_logits=None, ws=None, stream=None):
     """(args, what keeps its workspace alive, the GPU) of a selection."""
-    dev, (T, V), dt = _gpu(f, logits), logits.shape, logits.dtype
+    dev, dt = _gpu(f, logits), logits.dtype
+    if logits.dim() != 2 or (allow is not None and allow.dim() != 2):
+        _refuse(f, "logits must be [rows][vocab], allow [masks][words]")
+    if (hist is not None and hist0 is None) or (bias is None) != (bias_id is None) or (bias is None) != (bias0 is None):
+        _refuse(f, "hist needs hist0; bias, bias_id and bias0 go together")
+    T, V = logits.shape
     B = row0.numel() - 1 if row0 is not None else 1
     i32, f32 = [out_id], [out_conf]
     ok = out_id.numel() >= T and out_conf.numel() >= T and (V == 1 or logits.stride(1) == 1)
@@ -593,7 +608,7 @@ def dllm_select(logits, out_id, out_conf, stream=None, **control):
     """logits (and out_logits): [rows][vocab], rows may be strided.  control: mask_id, row0, hist, hist0, n_prompt,
     repetition, presence, frequency, bias_id, bias, bias0, allow (int32 words [masks][words]), allow_row, out_logits, ws."""
     f = "dllm_select"
-    if logits.shape[0] == 0:
+    if logits.dim() == 2 and logits.shape[0] == 0:
         return
     a, keep, dev = _select_args(f, logits, out_id, out_conf, stream=stream, **control)
     rc = lib().dllm_select(a, _stream(stream, dev))

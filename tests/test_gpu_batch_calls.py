@@ -165,3 +165,29 @@ def test_a_control_that_could_not_act_is_refused(dl):
                     (args[:-1], dict(logits=logits, control=control)), (args[:-2], dict(control=control))):
         with pytest.raises(dl.DllmError):
             dl.dllm_batch_step(*a, **dict(kw, **more))
+
+
+def test_tensors_of_other_ranks_and_lists_without_their_parts_are_refused(dl):
+    """A refusal that says so, not an error of the unpacking, and no list that is silently dropped."""
+    import torch
+    z = lambda *s, dt=torch.float16: torch.zeros(s, dtype=dt, device="cuda")  # noqa: E731
+    i = lambda *s: z(*s, dt=torch.int32)  # noqa: E731
+    q, k, v, kp, vp = z(2, 4, 64), z(2, 2, 64), z(2, 2, 64), z(3, 2, 32, 64), z(3, 2, 64, 32)
+    rope = z(8, 32, 2, dt=torch.float32)
+    for a in ((q, k, v, rope, i(2), i(2), q.clone(), kp[0], vp), (q[0, 0, 0], k, v, rope, i(2), i(2), q.clone(), kp, vp),
+              (q, k, v, rope, i(2), i(2), z(64), kp, vp), (q, k, v, rope, i(2), i(2), q.view(2, 256).clone(), kp[..., :0], vp)):
+        with pytest.raises(dl.DllmError):
+            dl.dllm_qk_norm_rope(*a)
+    for a in ((q, kp[0], vp, i(1, 2), i(2), i(1), q.clone()), (z(64), kp, vp, i(1, 2), i(2), i(1), q.clone()),
+              (q, kp, vp, i(1, 2)[0, 0], i(2), i(1), q.clone()), (q.view(2, 256), kp[..., :0], vp, i(1, 2), i(2), i(1), q.clone())):
+        with pytest.raises(dl.DllmError):
+            dl.dllm_attention_paged(*a, 2, 32)
+    x, ids, conf = z(2, 50, dt=torch.float32), i(2), z(2, dt=torch.float32)
+    w = z(3, dt=torch.float32)
+    for control in (dict(hist=i(3)), dict(bias=w), dict(bias_id=i(3)), dict(bias0=i(2)), dict(bias=w, bias_id=i(3)),
+                    dict(bias_id=i(3), bias0=i(2)), dict(allow=i(2))):
+        with pytest.raises(dl.DllmError):
+            dl.dllm_select(x, ids, conf, **control)
+    for bad in (x[0], x[0, 0], x[None]):
+        with pytest.raises(dl.DllmError):
+            dl.dllm_select(bad, ids, conf)
