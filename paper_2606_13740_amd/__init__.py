@@ -91,7 +91,9 @@ def _packer(cls):
 
 
 _pack_qk, _pack_attn, _pack_select = _packer(dllm_qk_args), _packer(dllm_attn_args), _packer(dllm_select_args)
-_pack_ws = struct.Struct("@PN").pack          # the last two fields of the latter
+_pack_rows = _packer(dllm_batch_rows)
+_pack_ws = struct.Struct("@PN").pack          # the last two fields of attention's and selection's
+_pack_2i = struct.Struct("@2i").pack
 
 # (the batch operators' args are pointers to their structs: a struct by reference, or its bytes)
 _SIGNATURES = {
@@ -135,7 +137,7 @@ _SIGNATURES = {
     "dllm_select": ([_vp, _vp], ctypes.c_int),
     "dllm_model_set_qk_norm": ([_vp, ctypes.POINTER(_vp), ctypes.POINTER(_vp), _vp], ctypes.c_int),
     "dllm_batch_bytes": ([_vp, _i32, _i32, ctypes.POINTER(_sz)], ctypes.c_int),
-    "dllm_batch_step": ([_vp, _vp, _sz, ctypes.POINTER(dllm_batch_rows), _vp, _vp, _vp, _vp, _vp, _vp], ctypes.c_int),
+    "dllm_batch_step": ([_vp, _vp, _sz, _vp, _vp, _vp, _vp, _vp, _vp, _vp], ctypes.c_int),
     "dllm_commit_staged": ([_vp, _vp, _vp, _vp, _vp, _i32, _i32, ctypes.c_float, ctypes.c_float, _vp, _vp, _vp],
                            ctypes.c_int),
 }
@@ -382,6 +384,14 @@ def _gpu(func: str, ref) -> int:
     return dev
 
 
+def _fits(func: str, a, b):
+    """Two numbers that go through ctypes, which cuts them to 32 bits without a word."""
+    try:
+        _pack_2i(a, b)
+    except _NO_FIT:
+        _refuse(func, _NO_FIT_MSG)
+
+
 # The checks below run for every call, beside launches of 3 us: they test first and look for names only to refuse.
 
 
@@ -428,6 +438,7 @@ def dllm_batch_plan(length, new, owned, owned_out, table, free, n_free, n_free_o
             not n_free_out.numel()):
         _refuse(f, "new, owned and owned_out must have an entry and table a row per sequence (row0: one entry more), slot, seq "
                    "and lim as many as pos, status 3, n_free 1")
+    _fits(f, page, shared_pages)
     rc = lib().dllm_batch_plan(length.data_ptr(), new.data_ptr(), owned.data_ptr(), owned_out.data_ptr(), B,
                                table.data_ptr(), ld, free.data_ptr(), n_free.data_ptr(), n_free_out.data_ptr(), N, page,
                                shared_pages, R, row0.data_ptr(), pos.data_ptr(), slot.data_ptr(), seq.data_ptr(),
@@ -440,7 +451,8 @@ def dllm_rope_table(table, head_dim: int, rope_base: float, stream=None):
     """table: float32 [max_pos][head_dim / 2][2]."""
     f = "dllm_rope_table"
     _plain(f, _gpu(f, table), _Types.f32, (table,), "table")
-    if table.numel() % head_dim != 0:
+    _fits(f, head_dim, table.numel() // max(head_dim, 1))
+    if head_dim < 1 or table.numel() % head_dim != 0:
         _refuse(f, "table must be [max_pos][head_dim / 2][2]")
     _check(lib().dllm_rope_table(table.data_ptr(), table.numel() // head_dim, head_dim, rope_base, _stream(stream)), f)
 
@@ -627,6 +639,7 @@ def dllm_model_set_qk_norm(model: int, q_gains, k_gains, stream=None):
 
 def dllm_batch_bytes(model: int, n_pages: int, page: int) -> int:
     n = _sz()
+    _fits("dllm_batch_bytes", n_pages, page)
     _check(lib().dllm_batch_bytes(model, n_pages, page, ctypes.byref(n)), "dllm_batch_bytes")
     return n.value
 
@@ -644,15 +657,18 @@ def dllm_batch_step(model: int, pages, n_pages: int, page: int, tok, mask, table
     _at_least(f, R, (pos, slot, lim, mask, out_id, out_conf), "pos slot lim mask out_id out_conf")
     if table.numel() < B * ld or row0.numel() < B + 1 or pages.get_device() != dev or not pages.is_contiguous():
         _refuse(f, "table must have a row and row0 an entry per sequence (row0: one more), pages be on the same GPU")
-    rows = dllm_batch_rows(R, B, page, n_pages, ld, shared_len, max_rows, max_len, table.data_ptr(), row0.data_ptr(),
-                           pos.data_ptr(), slot.data_ptr(), length.data_ptr(), _ptr(lim))
+    try:
+        rows = _pack_rows(R, B, page, n_pages, ld, shared_len, max_rows, max_len, table.data_ptr(), row0.data_ptr(),
+                          pos.data_ptr(), slot.data_ptr(), length.data_ptr(), _ptr(lim) or 0)
+    except _NO_FIT:
+        _refuse(f, _NO_FIT_MSG)
     sel = keep = None
     if (control and logits is None) or (logits is not None and (out_id is None or out_conf is None)):
         _refuse(f, "control needs logits, and logits need out_id and out_conf")
     if logits is not None:
         sel, keep, _ = _select_args(f, logits, out_id, out_conf, stream=stream, **(control or {}))
-    _check(lib().dllm_batch_step(model, pages.data_ptr(), pages.numel() * pages.element_size(), ctypes.byref(rows),
-                                 tok.data_ptr(), _ptr(mask), sel, _ptr(out_id), _ptr(out_conf), _stream(stream)), f)
+    _check(lib().dllm_batch_step(model, pages.data_ptr(), pages.numel() * pages.element_size(), rows, tok.data_ptr(),
+                                 _ptr(mask), sel, _ptr(out_id), _ptr(out_conf), _stream(stream)), f)
     del keep
 
 

@@ -191,3 +191,26 @@ def test_tensors_of_other_ranks_and_lists_without_their_parts_are_refused(dl):
     for bad in (x[0], x[0, 0], x[None]):
         with pytest.raises(dl.DllmError):
             dl.dllm_select(bad, ids, conf)
+
+
+def test_numbers_past_32_bits_are_refused(dl):
+    """Not cut to their low 32 bits, in the calls that do not go through the packed structs either."""
+    import torch
+    shape, model, bt, tok, mask = wide_batch(dl)
+    for n_pages, page in ((2 ** 32 + 1, 32), (4, 2 ** 32 + 32), (-2 ** 32 + 4, 32), (4.5, 32), ("4", 32)):
+        with pytest.raises(dl.DllmError):
+            dl.dllm_batch_bytes(model.handle, n_pages, page)
+    bt.step(tok, mask, np.array([9, 5]), commit=False, out=True)
+    args, kw = bt.last
+    for at, bad in ((2, 2 ** 32 + bt.n_pages), (3, 2 ** 32 + 32), (11, 2 ** 32 + 9), (12, 2 ** 32 + 100)):
+        with pytest.raises(dl.DllmError):
+            dl.dllm_batch_step(*args[:at], bad, *args[at + 1:], **kw)
+    with pytest.raises(dl.DllmError):
+        dl.dllm_batch_step(*args, **dict(kw, shared_len=2 ** 32))
+    i = lambda *s: torch.zeros(s, dtype=torch.int32, device="cuda")  # noqa: E731
+    for page, shared in ((2 ** 32 + 32, 0), (32, 2 ** 32), (32, -2 ** 32)):
+        with pytest.raises(dl.DllmError):
+            dl.dllm_batch_plan(i(2), i(2), i(2), i(2), i(2, 4), i(8), i(1), i(1), page, shared, i(3), i(5), i(5), i(5), i(5), i(3))
+    for head_dim in (0, -64, 2 ** 32 + 64):
+        with pytest.raises(dl.DllmError):
+            dl.dllm_rope_table(torch.zeros(4, 32, 2, device="cuda"), head_dim, 10000.0)
