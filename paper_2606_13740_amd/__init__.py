@@ -197,14 +197,19 @@ def _stream(stream, device: Optional[int] = None):
 # ----------------------------------------------------------------------------
 
 
+_gain_sizes = {}          # of a model's handle: (layers, head_dim), what dllm_model_set_qk_norm reads
+
+
 def dllm_model_create(cfg: dllm_config, weights: dllm_weights, stream=None) -> int:
     h = _vp()
     _check(lib().dllm_model_create(ctypes.byref(cfg), ctypes.byref(weights), _stream(stream), ctypes.byref(h)),
            "dllm_model_create")
+    _gain_sizes[h.value] = (cfg.n_layers, cfg.head_dim)
     return h.value
 
 
 def dllm_model_destroy(model: int):
+    _gain_sizes.pop(model, None)
     _check(lib().dllm_model_destroy(model), "dllm_model_destroy")
 
 
@@ -632,6 +637,11 @@ def dllm_select(logits, out_id, out_conf, stream=None, **control):
 def dllm_model_set_qk_norm(model: int, q_gains, k_gains, stream=None):
     """q_gains, k_gains: one float32 [head_dim] tensor per layer."""
     f = "dllm_model_set_qk_norm"
+    layers, dim = _gain_sizes.get(model, (len(q_gains), 1))
+    if not len(q_gains) == len(k_gains) == layers or layers == 0:
+        _refuse(f, f"q_gains and k_gains must have a tensor for each of the model's {layers} layers")
+    if any(t.numel() != dim for t in (*q_gains, *k_gains)) and model in _gain_sizes:
+        _refuse(f, f"a gain must have the model's head_dim of {dim} entries")
     _plain(f, _gpu(f, q_gains[0]), _Types.f32, tuple(q_gains) + tuple(k_gains), "gain " * (len(q_gains) + len(k_gains)))
     q, k = ((_vp * len(g))(*[t.data_ptr() for t in g]) for g in (q_gains, k_gains))
     _check(lib().dllm_model_set_qk_norm(model, q, k, _stream(stream)), f)

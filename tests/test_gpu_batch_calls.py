@@ -214,3 +214,17 @@ def test_numbers_past_32_bits_are_refused(dl):
     for head_dim in (0, -64, 2 ** 32 + 64):
         with pytest.raises(dl.DllmError):
             dl.dllm_rope_table(torch.zeros(4, 32, 2, device="cuda"), head_dim, 10000.0)
+
+
+def test_gains_of_another_number_or_size_are_refused(dl):
+    """The library reads a pointer a layer and head_dim floats behind each: fewer of either must not reach it."""
+    import torch
+    model, _, _ = build_pair(synth.TINY, "f32", oracle_too=False)
+    n, d = synth.TINY.n_layers, synth.TINY.head_dim
+    one = lambda size: torch.ones(size, device="cuda")  # noqa: E731
+    good = [one(d)] * n
+    for q, k in ((good[1:], good), (good, good[1:]), (good[1:], good[1:]), ([], []), (good + good, good + good),
+                 (good, [one(d - 1)] * n), ([one(d)] * (n - 1) + [one(1)], good), (good, [one(2 * d)] * n)):
+        with pytest.raises(dl.DllmError):
+            dl.dllm_model_set_qk_norm(model.handle, q, k)
+    dl.dllm_model_set_qk_norm(model.handle, good, good)
