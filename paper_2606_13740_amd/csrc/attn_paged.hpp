@@ -46,6 +46,7 @@ struct PagedArgs {
     int nt_s, nt_o;               // row tiles of the shared part and of a sequence
     int n_s;                      // workgroups of the shared part (the first ones)
     int direct;                   // one part in all: the output is written here, not merged
+    int out_f32;                  // out holds floats whatever T is (a batch step's, for the O projection's operand)
     float* opart;                 // [ns_s + ns_o][T][H][Dh] unnormalised partial outputs
     float* mlpart;                // [ns_s + ns_o][T][H][2]  (reference in log2 units, sum)
 };
@@ -143,6 +144,18 @@ template <typename T> __device__ __forceinline__ T attn_out(float o) {
 
 // log2-domain slack of the lazily moved reference: probabilities <= 2^8 (fits fp16)
 constexpr float PAGED_SLACK = 8.f;
+
+// Four consecutive outputs from element `at` of a.out on.
+template <typename T> __device__ __forceinline__ void store_out4(const PagedArgs& a, size_t at, const float (&o)[4]) {
+    if (sizeof(T) == 4 || a.out_f32) {
+        *(float4*)((float*)a.out + at) = make_float4(o[0], o[1], o[2], o[3]);
+    } else {
+        T e[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) e[i] = attn_out<T>(o[i]);
+        __builtin_memcpy(__builtin_assume_aligned((T*)a.out + at, 4 * sizeof(T)), e, sizeof(e));
+    }
+}
 
 // Workgroup = (part, K/V head, key split, tile of QG x RT virtual rows): QG row tiles of KG waves each.
 // A step is SUB blocks of 32 keys, which direct global->LDS loads stage in one of two buffers while
@@ -611,15 +624,15 @@ attn_paged_kernel(PagedArgs a) {
     auto dim_of = [&](int dt, int j) { return RT * dt + (R32 ? 8 * j + 4 * g : 4 * g); };
     if (a.direct) {
         const float inv = l != 0.f ? 1.f / l : 0.f;          // (a NaN stays one)
-        T* op = (T*)a.out + row * a.ld_out + h * DH;
+        const size_t at = row * a.ld_out + h * DH;
 #pragma unroll
         for (int dt = 0; dt < ND; ++dt)
 #pragma unroll
             for (int j = 0; j < NA / 4; ++j) {
-                T e[4];
+                float o[4];
 #pragma unroll
-                for (int i = 0; i < 4; ++i) e[i] = attn_out<T>(oacc[dt][4 * j + i] * inv);
-                __builtin_memcpy(__builtin_assume_aligned(op + dim_of(dt, j), 4 * ES), e, sizeof(e));
+                for (int i = 0; i < 4; ++i) o[i] = oacc[dt][4 * j + i] * inv;
+                store_out4<T>(a, at + dim_of(dt, j), o);
             }
     } else {
         const size_t rec = ((size_t)part * a.T + row) * a.H + h;
@@ -692,8 +705,8 @@ __global__ void __launch_bounds__(256) attn_paged_merge_kernel(PagedArgs a) {
     }
     if (R0 + pair / a.H >= R1) return;
     const float inv = L != 0.f ? 1.f / L : 0.f;
-    T e[4] = {attn_out<T>(o.x * inv), attn_out<T>(o.y * inv), attn_out<T>(o.z * inv), attn_out<T>(o.w * inv)};
-    __builtin_memcpy(__builtin_assume_aligned((T*)a.out + row * a.ld_out + h * DH + 4 * li, 4 * sizeof(T)), e, sizeof(e));
+    const float e[4] = {o.x * inv, o.y * inv, o.z * inv, o.w * inv};
+    store_out4<T>(a, row * a.ld_out + h * DH + 4 * li, e);
 }
 
 }  // namespace dllm

@@ -222,6 +222,43 @@ int select_check(const dllm_select_args* g) {
     return DLLM_OK;
 }
 
+int attention_paged(const dllm_attn_args* g, bool out_f32, hipStream_t s) {
+    int shift = 0;
+    if (int rc = check_attn(g, shift)) return rc;
+    if (!g->d_q || !g->d_k_pages || !g->d_v_pages || !g->d_table || !g->d_row0 || !g->d_len || !g->d_out)
+        return fail(DLLM_E_INVAL, "NULL argument");
+    const int es = esize(g->dtype);
+    const int64_t w = (int64_t)g->n_heads * g->head_dim;
+    if (!row_stride_ok(g->d_q, g->ld_q, w, es) || !row_stride_ok(g->d_out, g->ld_out, w, out_f32 ? 4 : es))
+        return fail(DLLM_E_INVAL, "q, out: pointers and row strides must be multiples of 16 bytes, strides at least a row");
+    if (!aligned(g->d_k_pages, 16) || !aligned(g->d_v_pages, 16) || !aligned(g->d_table, 4) || !aligned(g->d_row0, 4) ||
+        !aligned(g->d_len, 4) || !aligned(g->d_lim, 4))
+        return fail(DLLM_E_INVAL, "pages must be 16-byte aligned, integer arrays 4-byte");
+    if (g->n_rows == 0) return DLLM_OK;
+    const AttnPlan p = attn_plan(g);
+    const size_t need = attn_ws_bytes(g, p);
+    if (need > 0 && (!g->d_ws || !aligned(g->d_ws, 16))) return fail(DLLM_E_INVAL, "workspace: NULL or not 16-byte aligned");
+    if (need > g->ws_bytes)
+        return fail(DLLM_E_CAPACITY, "the call needs " + std::to_string(need) + " bytes of workspace");
+    PagedArgs a{};
+    a.q = g->d_q; a.ld_q = g->ld_q; a.kp = g->d_k_pages; a.vp = g->d_v_pages; a.table = g->d_table; a.table_ld = g->table_ld;
+    a.row0 = g->d_row0; a.len = g->d_len; a.lim = g->d_lim; a.out = g->d_out; a.ld_out = g->ld_out;
+    a.T = g->n_rows; a.B = g->n_seqs; a.H = g->n_heads; a.Hk = g->n_kv_heads; a.G = a.H / a.Hk; a.page_shift = shift;
+    a.n_pages = g->n_pages; a.shared = p.shared; a.max_rows = g->max_rows; a.max_len = g->max_len;
+    a.sl2 = g->scale == 0.f ? 1.f : std::fabs(g->scale) * 1.4426950408889634f;
+    a.qmul = g->scale == 0.f ? 0.f : (g->scale < 0.f ? -1.f : 1.f);
+    a.opart = (float*)g->d_ws;
+    a.mlpart = a.opart + (size_t)(p.ns_s + p.ns_o) * a.T * a.H * g->head_dim;
+    a.ns_s = p.ns_s; a.nt_s = p.nt_s; a.ns_o = p.ns_o; a.nt_o = p.nt_o; a.n_s = (int)p.wgs_s;
+    a.direct = p.direct();
+    a.out_f32 = out_f32;
+    if (g->dtype == DLLM_F32) launch_attn<float>(a, p, g->head_dim, s);
+    else if (g->dtype == DLLM_F16) launch_attn<_Float16>(a, p, g->head_dim, s);
+    else launch_attn<__bf16>(a, p, g->head_dim, s);
+    HIP_TRY(hipGetLastError());
+    return DLLM_OK;
+}
+
 }  // namespace dllm
 
 extern "C" {
@@ -270,42 +307,7 @@ int dllm_attention_paged_ws(const dllm_attn_args* g, size_t* bytes) {
     return DLLM_OK;
 }
 
-int dllm_attention_paged(const dllm_attn_args* g, dllm_stream stream) {
-    int shift = 0;
-    if (int rc = check_attn(g, shift)) return rc;
-    if (!g->d_q || !g->d_k_pages || !g->d_v_pages || !g->d_table || !g->d_row0 || !g->d_len || !g->d_out)
-        return fail(DLLM_E_INVAL, "NULL argument");
-    const int es = esize(g->dtype);
-    const int64_t w = (int64_t)g->n_heads * g->head_dim;
-    if (!row_stride_ok(g->d_q, g->ld_q, w, es) || !row_stride_ok(g->d_out, g->ld_out, w, es))
-        return fail(DLLM_E_INVAL, "q, out: pointers and row strides must be multiples of 16 bytes, strides at least a row");
-    if (!aligned(g->d_k_pages, 16) || !aligned(g->d_v_pages, 16) || !aligned(g->d_table, 4) || !aligned(g->d_row0, 4) ||
-        !aligned(g->d_len, 4) || !aligned(g->d_lim, 4))
-        return fail(DLLM_E_INVAL, "pages must be 16-byte aligned, integer arrays 4-byte");
-    if (g->n_rows == 0) return DLLM_OK;
-    const AttnPlan p = attn_plan(g);
-    const size_t need = attn_ws_bytes(g, p);
-    if (need > 0 && (!g->d_ws || !aligned(g->d_ws, 16))) return fail(DLLM_E_INVAL, "workspace: NULL or not 16-byte aligned");
-    if (need > g->ws_bytes)
-        return fail(DLLM_E_CAPACITY, "the call needs " + std::to_string(need) + " bytes of workspace");
-    PagedArgs a{};
-    a.q = g->d_q; a.ld_q = g->ld_q; a.kp = g->d_k_pages; a.vp = g->d_v_pages; a.table = g->d_table; a.table_ld = g->table_ld;
-    a.row0 = g->d_row0; a.len = g->d_len; a.lim = g->d_lim; a.out = g->d_out; a.ld_out = g->ld_out;
-    a.T = g->n_rows; a.B = g->n_seqs; a.H = g->n_heads; a.Hk = g->n_kv_heads; a.G = a.H / a.Hk; a.page_shift = shift;
-    a.n_pages = g->n_pages; a.shared = p.shared; a.max_rows = g->max_rows; a.max_len = g->max_len;
-    a.sl2 = g->scale == 0.f ? 1.f : std::fabs(g->scale) * 1.4426950408889634f;
-    a.qmul = g->scale == 0.f ? 0.f : (g->scale < 0.f ? -1.f : 1.f);
-    a.opart = (float*)g->d_ws;
-    a.mlpart = a.opart + (size_t)(p.ns_s + p.ns_o) * a.T * a.H * g->head_dim;
-    a.ns_s = p.ns_s; a.nt_s = p.nt_s; a.ns_o = p.ns_o; a.nt_o = p.nt_o; a.n_s = (int)p.wgs_s;
-    a.direct = p.direct();
-    hipStream_t s = (hipStream_t)stream;
-    if (g->dtype == DLLM_F32) launch_attn<float>(a, p, g->head_dim, s);
-    else if (g->dtype == DLLM_F16) launch_attn<_Float16>(a, p, g->head_dim, s);
-    else launch_attn<__bf16>(a, p, g->head_dim, s);
-    HIP_TRY(hipGetLastError());
-    return DLLM_OK;
-}
+int dllm_attention_paged(const dllm_attn_args* g, dllm_stream stream) { return attention_paged(g, false, (hipStream_t)stream); }
 
 int dllm_select_ws(const dllm_select_args* g, size_t* bytes) {
     if (!bytes) return fail(DLLM_E_INVAL, "bytes is NULL");

@@ -121,17 +121,13 @@ __global__ void __launch_bounds__(256) qkv_rows_kernel(QkvRows a, int qk_wgs) {
     }
 }
 
-// Attention rows [M][d] into the O projection's operand fragments; padding rows up to gridDim.x get zeros.
+// Attention rows [M][d], floats, into the O projection's operand fragments; padding rows up to gridDim.x get zeros.
 template <bool XF32>
-__global__ void __launch_bounds__(256) attn_operand_kernel(const void* rows, int M, int d, void* frag, int KCx) {
-    using T = typename std::conditional<XF32, float, _Float16>::type;
+__global__ void __launch_bounds__(256) attn_operand_kernel(const float* rows, int M, int d, void* frag, int KCx) {
     const int m = blockIdx.x;
     for (int n = 4 * threadIdx.x; n < d; n += 4 * 256) {
         float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-        if (m < M) {
-            const T* p = (const T*)rows + (size_t)m * d + n;
-            v = make_float4((float)p[0], (float)p[1], (float)p[2], (float)p[3]);
-        }
+        if (m < M) v = *(const float4*)(rows + (size_t)m * d + n);
         xfrag_store4<XF32>(frag, m, n, KCx, v);
     }
 }

@@ -860,8 +860,9 @@ int forward_t(dllm_model* m, dllm_kv* kv, const FwdArgs& a, hipStream_t s) {
             g.d_q = w.q; g.d_k_pages = Kc; g.d_v_pages = Vt;
             g.d_out = w.qkv;                       // the Q/K/V rows are spent
             ProbeScope ps(m, DLLM_K_ATTN, s);
-            if ((rc = dllm_attention_paged(&g, (dllm_stream)s))) return rc;
-            hipLaunchKernelGGL(attn_operand_kernel<XF32>, dim3(Mc), dim3(256), 0, s, (const void*)w.qkv, a.M, d, w.of,
+            // (rows of d floats, which the operand splits into its pair: no rounding to the cache's type between)
+            if ((rc = attention_paged(&g, true, s))) return rc;
+            hipLaunchKernelGGL(attn_operand_kernel<XF32>, dim3(Mc), dim3(256), 0, s, (const float*)w.qkv, a.M, d, w.of,
                                m->KCx_d);
         }
         // attention over [0, T) (+ split merge)

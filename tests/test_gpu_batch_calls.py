@@ -5,7 +5,7 @@ import numpy as np
 import pytest
 
 import synth
-from gpu_util import build_pair, dev_i32, dev_u8
+from gpu_util import GLOBALS, build_pair, dev_i32, dev_u8, gpu_logits
 from test_gpu_batch_step import Batch, gains, scene
 
 pytestmark = pytest.mark.gpu
@@ -228,3 +228,29 @@ def test_gains_of_another_number_or_size_are_refused(dl):
         with pytest.raises(dl.DllmError):
             dl.dllm_model_set_qk_norm(model.handle, q, k)
     dl.dllm_model_set_qk_norm(model.handle, good, good)
+
+
+def test_attention_rows_reach_the_projection_unrounded(dl):
+    """With W_k = 0 every key weighs the same: Q's and the probabilities' roundings do nothing, and a batch step differs from the
+    single sequence's only in how the attention's rows reach the O projection.  W_o times 16, so that the logits follow
+    them: rows rounded to fp16 would be off by 2^-11 / sqrt(12) RMS, about 2^-13 of the largest logit; as pairs of
+    bf16 of the fp32 sums (half a step 2^-17, in both calls, beside sums of 96 values in two orders) by 2^-17."""
+    import torch
+    shape = dataclasses.replace(synth.SMALL_BF16, n_layers=1)
+    w = synth.all_weights(shape, "bf16", 0)
+    layer = dict(w["layers"][0])
+    layer["wk"] = np.zeros_like(layer["wk"])
+    layer["wo"] = layer["wo"] + np.uint16(4 << 7)                       # bf16: four steps of the exponent
+    model = dl.Model(shape, "bf16", {k: w[k] for k in GLOBALS}, lambda l: layer, max_window=64, max_pos=256)
+    prompt = synth.prompt_ids(shape, 64)
+    tok, mask = synth.window(shape, 32, range(8, 32))
+    kv = dl.KVCache(model, 128)
+    dl.dllm_prefill(model.handle, kv.handle, dev_i32(prompt), 64)
+    want, _, _ = gpu_logits(model, kv, tok, mask)
+    bt = Batch(dl, model, 1, prompt)
+    logits = torch.zeros(32, shape.vocab, device="cuda")
+    bt.step(tok, mask, np.array([32]), commit=False, out=True, logits=logits, control=dict(mask_id=shape.mask_id))
+    got, fin = logits.double().cpu().numpy(), np.isfinite(want)
+    off, top = abs(got[fin] - want[fin]).max(), abs(want[fin]).max()
+    print(f"  off by 2^{np.log2(off / top + 1e-30):.1f} of the largest logit", flush=True)
+    assert off <= 2.0 ** -15 * top
