@@ -159,7 +159,8 @@ __global__ void __launch_bounds__(SEL_NT) __attribute__((amdgpu_waves_per_eu(WPE
     auto enter = [&](int b) {
         const int h0 = a.hist ? a.hist0[b] : 0, h1 = a.hist ? a.hist0[b + 1] : 0;
         const int i0 = a.bias ? a.bias0[b] : 0, i1 = a.bias ? a.bias0[b + 1] : 0;
-        const int hp = a.n_prompt ? h0 + a.n_prompt[b] : h0;
+        // (a prompt longer than the history, 2^31 - 1 as "all of it", is the history: no sum past 32 bits)
+        const int hp = a.n_prompt ? h0 + min(max(a.n_prompt[b], 0), max(h1 - h0, 0)) : h0;
         pres = a.pres ? a.pres[b] : 0.f;
         freq = a.freq ? a.freq[b] : 0.f;
         rep = a.rep ? a.rep[b] : 1.f;

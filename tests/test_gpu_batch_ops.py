@@ -648,6 +648,18 @@ def test_select_with_histories_and_biases_that_are_empty(dl):
     assert torch.equal(outs[0][0], x.argmax(1).int()) and all(torch.equal(a, b) for a, b in zip(*outs))
 
 
+@pytest.mark.parametrize("n_prompt", [2 ** 31 - 1, 2 ** 30, 5, 0, -1, -2 ** 31])
+def test_select_with_prompts_of_any_length(dl, n_prompt):
+    """More prompt entries than the history has: nothing was generated.  Fewer than none: everything was."""
+    rng = np.random.default_rng(8)
+    c = select_case(rng, "f32", [3, 4], 700, 300, 0, 0)
+    c["hist0"] = np.array([0, 120, 250])
+    c["hist"] = rng.integers(0, 40, 250)
+    c["n_prompt"] = np.array([7, n_prompt])
+    c["pres"], c["freq"] = np.array([0.5, 0.75], np.float32), np.array([0.25, 0.5], np.float32)
+    check_select(dl, c, "f32")
+
+
 def test_calls_without_rows(dl):
     import torch
     z = lambda *s, dt=torch.float16: torch.zeros(s, dtype=dt, device="cuda")  # noqa: E731
