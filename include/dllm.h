@@ -551,7 +551,8 @@ int dllm_attention_paged(const dllm_attn_args* args, dllm_stream stream);
 /* Penalties, biases and masks on logits, then the id and its confidence: what
  * dllm_denoise_step's LM head reports, for logits the caller controls.  For row r of
  * sequence b (d_row0; NULL: one sequence has all rows) and id v, in fp32 and in this order:
- *   - l = l > 0 ? l / repetition : l * repetition where v is in the sequence's history,
+ *   - l = l > 0 ? l / repetition : l * repetition where v is in the sequence's history (a
+ *     subnormal repetition counts as 0),
  *   - l -= frequency * c and, where c > 0, l -= presence, c the times v occurs in the
  *     history past its first d_n_prompt[b] entries,
  *   - l += bias where v is in the sequence's bias list (listed twice: its last entry),

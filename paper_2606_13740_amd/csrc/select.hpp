@@ -46,13 +46,13 @@ __device__ __forceinline__ Best best_merge(const Best& a, const Best& b) {
 
 // A logit after its sequence's penalties and bias (0: none); e: the id's table entry.  Separate
 // roundings (no fused multiply-add), so that equal logits with equal adjustments stay equal.  l / rep by
-// 1 / rep and one step of the remainder, which is the rounded quotient (but for the last bit of
-// results near the underflow).
+// rcp = 1 / rep and one step of the remainder, which is the rounded quotient (but for the last bit of
+// results near the underflow); div is rep there, but 0 for an infinite rep, whose rcp of 0 would make the step a NaN.
 constexpr uint32_t SEL_SEEN = 0x80000000u, SEL_BIAS = 0x40000000u, SEL_COUNT = 0x3FFFFFFFu;
-__device__ __forceinline__ float adjust_logit(float l, uint32_t e, float bias, float rep, float rcp, float pres, float freq) {
+__device__ __forceinline__ float adjust_logit(float l, uint32_t e, float bias, float rep, float div, float rcp, float pres, float freq) {
 #pragma clang fp contract(off)
     const float up = l * rep, q = l * rcp;
-    const float d = fmaf(fmaf(-q, rep, l), rcp, q);
+    const float d = fmaf(fmaf(-q, div, l), rcp, q);
     const float down = fabsf(q) < INFINITY ? d : q;
     l = (e & SEL_SEEN) ? (l > 0.f ? down : up) : l;
     const uint32_t made = e & SEL_COUNT;
@@ -146,7 +146,7 @@ __global__ void __launch_bounds__(SEL_NT) __attribute__((amdgpu_waves_per_eu(WPE
 
     // bit j: of valid, this thread's j-th id may be picked; of jmask, some lane's j-th id has an adjustment
     uint32_t valid = 0, jmask = 0, adj[SEL_PT];
-    float bias[SEL_PT], rep = 1.f, rcp = 1.f, pres = 0.f, freq = 0.f;
+    float bias[SEL_PT], rep = 1.f, div = 1.f, rcp = 1.f, pres = 0.f, freq = 0.f;
 #pragma unroll
     for (int j = 0; j < SEL_PT; ++j) {
         const int v = id_of(j / NL) + j % NL;
@@ -164,6 +164,8 @@ __global__ void __launch_bounds__(SEL_NT) __attribute__((amdgpu_waves_per_eu(WPE
         pres = a.pres ? a.pres[b] : 0.f;
         freq = a.freq ? a.freq[b] : 0.f;
         rep = a.rep ? a.rep[b] : 1.f;
+        rep = fabsf(rep) < FLT_MIN ? copysignf(0.f, rep) : rep;      // (1 / a subnormal one overflows; a NaN stays)
+        div = fabsf(rep) == INFINITY ? 0.f : rep;
         rcp = __fdiv_rn(1.f, rep);
         if (h0 >= h1 && i0 >= i1) {
             jmask = 0;
@@ -284,7 +286,7 @@ __global__ void __launch_bounds__(SEL_NT) __attribute__((amdgpu_waves_per_eu(WPE
                     if (jmask != 0) {
 #pragma unroll
                         for (int j = 0; j < SEL_PT; ++j)
-                            if (jmask >> j & 1) l[i][j] = adjust_logit(l[i][j], adj[j], bias[j], rep, rcp, pres, freq);
+                            if (jmask >> j & 1) l[i][j] = adjust_logit(l[i][j], adj[j], bias[j], rep, div, rcp, pres, freq);
                     }
                     // NaN counts as -inf: the median instruction returns the least of the others if one is a NaN
                     // (the bound is hidden from the compiler, which would drop it)

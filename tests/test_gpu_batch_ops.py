@@ -660,6 +660,40 @@ def test_select_with_prompts_of_any_length(dl, n_prompt):
     check_select(dl, c, "f32")
 
 
+REPETITIONS = [float("inf"), -float("inf"), float("nan"), 0.0, -0.0, 1e-40, 2.0 ** -126, 2.0 ** -125, 1e-30, 1e30, 2.0 ** 126,
+               2.0 ** 127, 3.4e38, -1.7, 1.0000001, 0.9999999]
+
+
+def test_select_repetition_of_any_size(dl):
+    """Quotients and products by any float, rounded once; where the quotient is below 2^-100 its last bits may differ.  A
+    subnormal factor counts as 0."""
+    import torch
+    rng = np.random.default_rng(9)
+    B, V = len(REPETITIONS), 600
+    c = select_case(rng, "f32", [2] * B, V, 40, 0, 0)
+    n = 300
+    c["hist0"], c["hist"] = np.arange(B + 1) * n, rng.integers(0, V, B * n)
+    c["n_prompt"], c["pres"], c["freq"] = np.full(B, n), np.zeros(B, np.float32), np.zeros(B, np.float32)
+    c["rep"] = np.array(REPETITIONS, np.float32)
+    x = c["x"]
+    x *= np.exp2(rng.integers(-20, 20, x.shape))
+    x[:, ::50], x[:, 1::50], x[:, 2::50], x[:, 3::50], x[:, 4::50], x[:, 5::50] = 0.0, np.inf, -np.inf, 3e38, -3e38, 1e-44
+    c["xt"] = torch.from_numpy(x.astype(np.float32)).cuda()
+    c["x"] = x.astype(np.float32).astype(np.float64)
+    ids, conf, out = (torch.zeros(s, dtype=t, device="cuda") for s, t in ((2 * B, torch.int32), (2 * B, torch.float32), ((2 * B, V), torch.float32)))
+    dl.dllm_select(c["xt"], ids, conf, mask_id=V - 1, row0=i32(c["row0"]), hist=i32(c["hist"]), hist0=i32(c["hist0"]),
+                   n_prompt=i32(c["n_prompt"]), repetition=to_gpu(c["rep"]), out_logits=out)
+    torch.cuda.synchronize()
+    with np.errstate(divide="ignore"):
+        rep = np.where(abs(c["rep"]) < np.finfo(np.float32).tiny, np.copysign(0, c["rep"]), c["rep"]).astype(np.float32)
+        want, rid, _ = select(c["x"], V, V - 1, c["row0"], c["hist"], c["hist0"], c["n_prompt"], rep, None, None, None, None, None,
+                              None, None)
+    got = out.cpu().numpy()
+    fine = (got == want) | ((abs(want) < 2.0 ** -100) & (abs(got - want) <= 2.0 ** -148))
+    assert fine.all(), [(REPETITIONS[r // 2], float(c["x"][r, v]), float(got[r, v]), float(want[r, v])) for r, v in np.argwhere(~fine)[:8]]
+    assert np.array_equal(ids.cpu().numpy(), rid)
+
+
 def test_calls_without_rows(dl):
     import torch
     z = lambda *s, dt=torch.float16: torch.zeros(s, dtype=dt, device="cuda")  # noqa: E731
