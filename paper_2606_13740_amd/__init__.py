@@ -556,16 +556,20 @@ def _select_args(f, logits, out_id, out_conf, mask_id=-1, row0=None, hist=None, 
                  out_logits=None, ws=None, stream=None):
     """(args, what keeps its workspace alive, the GPU) of a selection."""
     dev, dt = _gpu(f, logits), logits.dtype
-    if logits.dim() != 2 or (allow is not None and allow.dim() != 2):
-        _refuse(f, "logits must be [rows][vocab], allow [masks][words]")
     if (hist is not None and hist0 is None) or (bias is None) != (bias_id is None) or (bias is None) != (bias0 is None):
         _refuse(f, "hist needs hist0; bias, bias_id and bias0 go together")
-    T, V = logits.shape
+    n_allow = allow_ld = 0
+    try:
+        T, V = logits.shape
+        if allow is not None:
+            n_allow, allow_ld = allow.shape
+    except ValueError:
+        _refuse(f, "logits must be [rows][vocab], allow [masks][words]")
     B = row0.numel() - 1 if row0 is not None else 1
     i32, f32 = [out_id], [out_conf]
     ok = out_id.numel() >= T and out_conf.numel() >= T and (V == 1 or logits.stride(1) == 1)
     p_row0 = p_hist = p_hist0 = p_prompt = p_rep = p_pres = p_freq = p_bias_id = p_bias = p_bias0 = p_allow = 0
-    p_allow_row = p_out = n_allow = allow_ld = ld_out = 0
+    p_allow_row = p_out = ld_out = 0
     if row0 is not None:
         i32.append(row0)
         p_row0 = row0.data_ptr()
@@ -598,7 +602,6 @@ def _select_args(f, logits, out_id, out_conf, mask_id=-1, row0=None, hist=None, 
     if allow is not None:
         i32.append(allow)
         p_allow = allow.data_ptr()
-        n_allow, allow_ld = allow.shape
     if allow_row is not None:
         i32.append(allow_row)
         ok = ok and allow_row.numel() >= T
@@ -625,7 +628,8 @@ def dllm_select(logits, out_id, out_conf, stream=None, **control):
     """logits (and out_logits): [rows][vocab], rows may be strided.  control: mask_id, row0, hist, hist0, n_prompt,
     repetition, presence, frequency, bias_id, bias, bias0, allow (int32 words [masks][words]), allow_row, out_logits, ws."""
     f = "dllm_select"
-    if logits.dim() == 2 and logits.shape[0] == 0:
+    sh = logits.shape
+    if len(sh) == 2 and sh[0] == 0:
         return
     a, keep, dev = _select_args(f, logits, out_id, out_conf, stream=stream, **control)
     rc = lib().dllm_select(a, _stream(stream, dev))
