@@ -128,6 +128,9 @@ def attn_reference(c, x, dtype, lim):
         a, e, n = int(x["row0"][b]), int(x["row0"][b + 1]), int(x["lens"][b])
         if a == e:
             continue
+        if n <= 0:
+            res.update({r: (np.zeros((c.H, c.D)), np.zeros((c.H, c.D))) for r in range(a, e)})
+            continue
         pages = -(-n // c.page)
         ids = np.where(np.arange(pages) < sp, x["table"][0, :pages], x["table"][b, :pages])
         there = torch.from_numpy(np.repeat((ids >= 0) & (ids < n_pages), c.page)[:n]).cuda()
