@@ -254,3 +254,38 @@ def test_attention_rows_reach_the_projection_unrounded(dl):
     off, top = abs(got[fin] - want[fin]).max(), abs(want[fin]).max()
     print(f"  off by 2^{np.log2(off / top + 1e-30):.1f} of the largest logit", flush=True)
     assert off <= 2.0 ** -15 * top
+
+
+@pytest.mark.parametrize("shape,dtype,rtol", [(synth.TINY_GQA, "f32", 1e-3), (synth.SMALL_BF16, "bf16", 0.1)])
+def test_heads_norm_in_the_merged_and_the_windowed_step(dl, shape, dtype, rtol):
+    """Refresh, append and step in one pass, and a window behind kept positions with selective outputs: what the calls one by one
+    give for a model with the heads' norm (confidences as closely as the merged step's own test asks)."""
+    import torch
+    model, _, _ = build_pair(shape, dtype, oracle_too=False)
+    rng, W, P = np.random.default_rng(3), 20, 40
+    block, pos, new = (dev_i32(a) for a in (rng.integers(0, 900, 32), [3, 17, 39], [5, 6, 7]))
+    tok, mask = (f(a) for f, a in zip((dev_i32, dev_u8), synth.window(shape, W, range(4, W))))
+
+    def life(merged):
+        kv = dl.KVCache(model, 160)
+        dl.dllm_prefill(model.handle, kv.handle, dev_i32(synth.prompt_ids(shape, P)), P)
+        ids, conf = torch.zeros(W, dtype=torch.int32, device="cuda"), torch.zeros(W, device="cuda")
+        if merged:
+            dl.dllm_step_merged(model.handle, kv.handle, pos, new, 3, block, 32, tok, mask, W, ids, conf)
+        else:
+            dl.dllm_refresh_kv(model.handle, kv.handle, pos, new, 3)
+            dl.dllm_append_prefix_kv(model.handle, kv.handle, block, 32)
+            dl.dllm_denoise_step(model.handle, kv.handle, tok, mask, W, ids, conf)
+        need = torch.ones(W, dtype=torch.uint8, device="cuda")
+        wid, wconf = torch.zeros_like(ids), torch.zeros_like(conf)
+        (dl.dllm_denoise_window_sls(model.handle, kv.handle, P + 32, tok, mask, need, W, W, wid, wconf) if merged else
+         dl.dllm_denoise_window(model.handle, kv.handle, P + 32, tok, mask, W, wid, wconf))
+        torch.cuda.synchronize()
+        return [t.cpu().numpy() for t in (conf, wconf)]
+
+    plain = life(False)
+    dl.dllm_model_set_qk_norm(model.handle, *gains(shape)[1])
+    one, all_ = life(False), life(True)
+    for a, b, c in zip(one, all_, plain):
+        np.testing.assert_allclose(b, a, rtol=rtol)
+        assert not np.allclose(a, c, rtol=1e-6)
