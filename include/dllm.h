@@ -415,7 +415,9 @@ int dllm_quantize_int8(const void* d_src, int32_t src_dtype, int32_t rows, int32
  * prompt, several candidate continuations or requests), apart from its matrix
  * products: the plan of the step's rows, Q/K normalisation with rotation and the cache
  * write, the attention, and the selection from the logits.  dllm_batch_step runs a
- * whole step of a model with them; each can be called on its own.  None keeps state,
+ * whole step of a model over a plan's rows with the attention and the selection (its Q,
+ * K and V, sums of its own GEMM, are finished as by the second); each can be called on
+ * its own.  None keeps state,
  * allocates or synchronises; all can be captured into a HIP graph.
  *
  * Paged cache: a pool of n_pages pages of `page` positions (32, 64, 128 or 256).  One
@@ -640,9 +642,10 @@ typedef struct dllm_batch_rows {
  * per layer.  Row r feeds the MASK id where d_mask[r] != 0 (d_mask nullable), else
  * d_tok[r]; its K/V are written to its slot before the layer's attention.  A sequence's
  * rows are, value for value up to rounding, dllm_denoise_step's over a cache of its own
- * (Q is one fp16 value here, not a pair).  With outputs (both set): every row's argmax
- * id and confidence, at most cfg.max_window rows.  Without: only the K/V, any number
- * of rows (prompts, finished blocks).  `sel` (nullable): the logits are written to
+ * (Q is one fp16 value here, not a pair, and so are the attention's probabilities; its
+ * rows reach the O projection in fp32).  With outputs (both set): every row's argmax id
+ * and confidence, at most cfg.max_window rows.  Without: only the K/V, any number of
+ * rows (prompts, finished blocks).  `sel` (nullable): the logits are written to
  * sel->d_logits (contiguous fp32 [n_rows][vocab], the caller's; MASK column -inf) and
  * dllm_select with its penalties, biases and masks gives the outputs instead (its d_out_id,
  * d_out_conf are this call's).  Workspaces grow at the first call of a size (the call then

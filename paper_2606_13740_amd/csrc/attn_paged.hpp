@@ -161,13 +161,13 @@ template <typename T> __device__ __forceinline__ void store_out4(const PagedArgs
 // A step is SUB blocks of 32 keys, which direct global->LDS loads stage in one of two buffers while
 // the other is read; a row tile's waves take SUB / KG of the blocks each and join at the end.
 // LDS rows are swizzled in 16-byte columns so that the lanes of an LDS cycle read distinct banks (no conflicts
-// counted).  Lane i holds the page of block 64 n + i, so a block's page is one lane read.
+// counted in either tile's loop).  Lane i holds the page of block 64 n + i, so a block's page is one lane read.
 //
 // What bounds it: many rows, the chain of products and exponentials of the two waves that a SIMD holds
-// (16 sequences of 64 rows, 28 heads over 4, behind 16384 bf16 keys: 145 us with the merge, 900
-// TFLOP/s where a large library product reaches 1100); rows enough for the prefix only, LDS reads and the K/V
+// (16 sequences of 64 rows, 28 heads over 4, behind 16384 bf16 keys: 145-153 us with the merge, 850 to 900
+// TFLOP/s where a large library product reaches 1100; waiting 22% of the wave cycles); rows enough for the prefix only, LDS reads and the K/V
 // themselves (8 x 32 rows of 32 fp16 heads behind 4096: 37 us and 6, 115 MB); few rows, latency (8 x 1 rows
-// behind 1564: 9.6 us and 4.6).
+// behind 1564: 9.8 us and 4.8, 288 workgroups of three steps, each asked for when the one before has landed).
 template <typename T, int DH, int QG, int RT, int KG, int SUB>
 __global__ void __launch_bounds__(QG * KG * 64)
 __attribute__((amdgpu_waves_per_eu(QG * KG * (160 * 1024 / (2 * SUB * 64 * DH * (int)sizeof(T))) >= 8 ? 2 : 1)))

@@ -59,9 +59,9 @@ constexpr int ATTN_SLOTS = 512;
 //    (13 MB that the sequences would read again) 16.7 and 17.8; 16 x 48 rows, 4 heads of 64, behind 512 (8 MB) equal;
 //    8 x 1 behind 64 15.0 and 14.8.  With one sequence it is that sequence's own.
 //  - tile: 64 rows against 128 (32 x 32 tiles): 12 x 40 rows of 32 heads behind 1024 37 and 40, 16 x 3 behind 9984 25.6
-//    and 27.2, 6 x 20 rows of 16 heads of 64 behind 2976 13.6 and 14.8, 8 x 32 of 32 heads behind 4096 51.5 and 49.2;
-//    from 12 steps of 128 rows a slot on 128 rows, which halve the LDS reads per product: 16 x 64 behind 16384
-//    (56 steps) 145 and 186.  fp32 is bound by its products, where idle waves cost: by the rows of one sequence
+//    and 27.2, 6 x 20 rows of 16 heads of 64 behind 2976 13.6 and 14.8; from 12 steps of 128 rows a slot on
+//    128 rows, which halve the LDS reads per product: 16 x 64 behind 16384 (56 steps) 186 and 145.  The border
+//    lies lower for some calls: 8 x 32 of 32 heads behind 4096 (8 steps) 51.5 and 49.2, where the rule keeps 64 rows.  fp32 is bound by its products, where idle waves cost: by the rows of one sequence
 //    (6 x 24 rows of 32 heads behind 1024: 32 rows 62, 64 rows 66).
 //  - waves of a row tile, for tiles of 32 rows and fewer: two against one 46.5 and 48.7 (16 x 1 rows of 32 heads behind
 //    8192), 20.9 and 22.8 (1 x 32 of 32 heads behind 4096), 5.6 and 6.2 (3 x 1 of 4 heads of 64 behind 80), 14.9 and 14.7

@@ -27,7 +27,10 @@ struct QkvRows {
 };
 
 // DH / 16 lanes per (row, Q or K head): lane i has pairs 8i .. 8i+7, which are dims 8i + e and 8i + e +
-// DH / 2; the V values follow, one per thread.  Reads 4 bytes a value once, launch-bound at a window's rows.
+// DH / 2; the V values follow, one per thread.  Reads 4 bytes a value once, launch-bound at a window's rows
+// (four layers of the 8B widths, 32 rows behind 512: the heads' norm through it 644 us against 639 without, where the GEMM's
+// epilogue does the work).  V^T goes out in single elements a page or cache row apart: a prompt of 4096 rows 12.6
+// against 12.1 ms.
 template <bool XF32, int DH>
 __global__ void __launch_bounds__(256) qkv_rows_kernel(QkvRows a, int qk_wgs) {
     using T = typename std::conditional<XF32, float, _Float16>::type;

@@ -116,11 +116,12 @@ template <class F> __device__ __forceinline__ uint32_t wave_fold2(uint32_t v0, u
 // vocabularies) the workgroup writes the result.
 //
 // What bounds it: reading the logits (16 bytes a lane, also from rows that start at odd
-// elements: the hardware takes unaligned addresses) beside about 11 VALU instructions an id and
-// latency: five waves a SIMD (WPE 5: 96 VGPRs) hide more of it than four of 109 or six with spills
+// elements: the hardware takes unaligned addresses) beside 31 VALU instructions an id (counted; 31 us of issue
+// for 256 rows of 152064) and latency: five waves a SIMD (WPE 5: 96 VGPRs) hide more of it than four of 109 or six with spills
 // (256 rows of 152064 bf16 logits, adjusted logits kept: 52 us, 59, and 3 us more than the latter; a torch
 // copy of that size takes 45).  Where four a SIMD hold all workgroups, their registers save the spills (WPE 3, up to 123 VGPRs): 32 rows of
-// 126464 fp32 logits 11.3 and 12.6 us, of 1024 7.8 and 8.2.
+// 126464 fp32 logits 11.3 and 12.6 us, of 1024 7.8 and 8.2.  In fp32 five waves spill 26 registers (16-bit types 2 to 4): 256 rows
+// of 126464, adjusted logits kept, 90 us a call where the bytes take 54, 128 rows not kept 37 and 14.
 struct alignas(16) SelectPart {
     float mx;
     int id;
