@@ -158,10 +158,11 @@ __global__ void __launch_bounds__(SEL_NT) __attribute__((amdgpu_waves_per_eu(WPE
 
     // the tables of sequence b's history and biases at this workgroup's ids
     auto enter = [&](int b) {
-        const int h0 = a.hist ? a.hist0[b] : 0, h1 = a.hist ? a.hist0[b + 1] : 0;
-        const int i0 = a.bias ? a.bias0[b] : 0, i1 = a.bias ? a.bias0[b + 1] : 0;
+        // (unsigned: the threads' indexes go up to a step past the end, which may be 2^31 - 1)
+        const uint32_t h0 = a.hist ? a.hist0[b] : 0, h1 = a.hist ? a.hist0[b + 1] : 0;
+        const uint32_t i0 = a.bias ? a.bias0[b] : 0, i1 = a.bias ? a.bias0[b + 1] : 0;
         // (a prompt longer than the history, 2^31 - 1 as "all of it", is the history: no sum past 32 bits)
-        const int hp = a.n_prompt ? h0 + min(max(a.n_prompt[b], 0), max(h1 - h0, 0)) : h0;
+        const uint32_t hp = a.n_prompt ? h0 + min(max(a.n_prompt[b], 0), max((int)(h1 - h0), 0)) : h0;
         pres = a.pres ? a.pres[b] : 0.f;
         freq = a.freq ? a.freq[b] : 0.f;
         rep = a.rep ? a.rep[b] : 1.f;
@@ -176,10 +177,10 @@ __global__ void __launch_bounds__(SEL_NT) __attribute__((amdgpu_waves_per_eu(WPE
         // the first entries of both lists are asked for before the tables are cleared
         int hv[HB], bv = -1;
         float bw = 0.f;
-        auto load_hist = [&](int at) {
+        auto load_hist = [&](uint32_t at) {
 #pragma unroll
             for (int k = 0; k < HB; ++k) {
-                const int i = at + k * SEL_NT;
+                const uint32_t i = at + k * SEL_NT;
                 hv[k] = i < h1 ? slot(a.hist[i]) : -1;
             }
         };
@@ -189,7 +190,7 @@ __global__ void __launch_bounds__(SEL_NT) __attribute__((amdgpu_waves_per_eu(WPE
 #pragma unroll
         for (int i = 0; i < SEL_IDS / SEL_NT; ++i) { adj_s[tid + i * SEL_NT] = 0; last_s[tid + i * SEL_NT] = 0; }
         __syncthreads();
-        for (int at = h0 + tid; at < h1; at += HB * SEL_NT) {
+        for (uint32_t at = h0 + tid; at < h1; at += HB * SEL_NT) {
             if (at != h0 + tid) load_hist(at);
 #pragma unroll
             for (int k = 0; k < HB; ++k) {
@@ -201,9 +202,9 @@ __global__ void __launch_bounds__(SEL_NT) __attribute__((amdgpu_waves_per_eu(WPE
         }
         if (i0 < i1) {
             if (bv >= 0) atomicMax(&last_s[bv], (uint32_t)tid + 1u);
-            for (int i = i0 + tid + SEL_NT; i < i1; i += SEL_NT) {
+            for (uint32_t i = i0 + tid + SEL_NT; i < i1; i += SEL_NT) {
                 const int k = slot(a.bias_id[i]);
-                if (k >= 0) atomicMax(&last_s[k], (uint32_t)(i - i0) + 1u);
+                if (k >= 0) atomicMax(&last_s[k], i - i0 + 1u);
             }
             __syncthreads();
             auto win = [&](int k, int i, float w) {            // the last entry of an id: one thread
@@ -212,7 +213,7 @@ __global__ void __launch_bounds__(SEL_NT) __attribute__((amdgpu_waves_per_eu(WPE
                 atomicOr(&adj_s[k], SEL_BIAS);
             };
             win(bv, tid, bw);
-            for (int i = i0 + tid + SEL_NT; i < i1; i += SEL_NT) win(slot(a.bias_id[i]), i - i0, a.bias[i]);
+            for (uint32_t i = i0 + tid + SEL_NT; i < i1; i += SEL_NT) win(slot(a.bias_id[i]), i - i0, a.bias[i]);
         }
         __syncthreads();
         jmask = 0;
