@@ -660,6 +660,148 @@ int dllm_batch_step(dllm_model* m, void* d_pages, size_t bytes, const dllm_batch
                     const uint8_t* d_mask, const dllm_select_args* sel, int32_t* d_out_id, float* d_out_conf,
                     dllm_stream stream);
 
+/* ------------------------------------------------------------------------------
+ * Branches: trees of drafted rows, candidates side by side, forks of sequences
+ *
+ * A step whose sequences draft more than one continuation: the rows of a sequence form a
+ * tree (or several windows side by side) behind its cached positions, each row attends to
+ * the cached positions and to the rows its mask has, the drafts are judged by their log
+ * probabilities, the accepted path's K/V move up behind the text, and sequences go on as
+ * copies of others.  As the batch operators, none keeps state, allocates or
+ * synchronises, and all can be captured into a HIP graph.
+ *
+ * A cache is all layers' planes as dllm_batch_bytes lays them out: [n_layers][K, V^T]
+ * [n_pages][n_kv_heads][page * head_dim].
+ * ------------------------------------------------------------------------------ */
+#define DLLM_MAX_TOP 64       /* most probable ids that dllm_logprobs reports of a row */
+#define DLLM_MAX_TREE 1024    /* rows of a sequence's tree in dllm_tree_plan, entries of a path */
+
+/* Plan of trees: positions and masks from parents.  Row i of sequence b (rows
+ * [d_row0[b], d_row0[b + 1]), i counted from d_row0[b]) follows its parent, the sequence's
+ * row d_parent[row], or the cached text where that is -1.  (A parent that is not a row before i
+ * counts as -1.)
+ *     d_mask [n_rows][mask_ld]  bit j % 32 of word j / 32: row j is i or an ancestor of it
+ *     d_pos [n_rows]            d_len[b] - rows of b + number of ancestors
+ * with d_len[b] the sequence's positions, its new rows included (dllm_batch_step's); rows go to
+ * the cache in their order, row i at position d_len[b] - rows of b + i (dllm_batch_plan's
+ * slots), whatever position they stand for in the text.  Rows of no sequence, and those of a
+ * sequence past its first 32 * mask_ld, are left as they were.  E_INVAL unless mask_ld is
+ * in [1, 32], for NULL pointers and sizes out of range. */
+int dllm_tree_plan(const int32_t* d_parent, const int32_t* d_row0, const int32_t* d_len, int32_t n_rows, int32_t n_seqs,
+                   int32_t* d_pos, uint32_t* d_mask, int32_t mask_ld, dllm_stream stream);
+
+/* dllm_attention_paged with a mask for every row: row r of sequence b sees the positions
+ * before its sequence's rows, [0, d_len[b] - rows of b), and of the rows i behind them those whose
+ * bit i % 32 of word i / 32 of d_mask[r] is set (rows past 32 * mask_ld: none), all of it
+ * below its limit.  A row that sees nothing gets zeros.  Everything else, the workspace and the
+ * refusals are dllm_attention_paged's (a shared prefix reaches into a sequence's rows only
+ * if the caller says so: the masks then hold there too).  E_INVAL unless mask_ld is in [1,
+ * 2^24] and d_mask 4-byte aligned. */
+int dllm_attention_tree(const dllm_attn_args* args, const uint32_t* d_mask, int32_t mask_ld, dllm_stream stream);
+
+/* dllm_batch_step with a mask for every row (dllm_tree_plan's d_mask; rows->d_pos its
+ * d_pos): the rows attend as in dllm_attention_tree. */
+int dllm_batch_step_tree(dllm_model* m, void* d_pages, size_t bytes, const dllm_batch_rows* rows, const uint32_t* d_tree,
+                         int32_t tree_ld, const int32_t* d_tok, const uint8_t* d_mask, const dllm_select_args* sel,
+                         int32_t* d_out_id, float* d_out_conf, dllm_stream stream);
+
+/* Log probabilities: with l_v a row's logits and lse = log sum_v e^(l_v), all in fp32,
+ *     d_logp[i]          l - lse of token d_tok[i] in row d_tok_row[i] (NULL: row i)
+ *     d_entropy[r]       lse - sum_v e^(l_v - lse) l_v (nullable)
+ *     d_top_id [r][top], d_top_logp [r][top]
+ *                        the `top` most probable ids, the most probable first (equal logits: the
+ *                        lower id first), and their l - lse
+ * NaN counts as -inf, values above the largest float as that, mask_id (-1: none) as -inf.
+ * An id of -inf, a token outside the vocabulary and one of a row that there is not have log
+ * probability -inf; where fewer than `top` ids are left the others are -1 and -inf; a row
+ * with none left has entropy 0.  The same token may be given any number of times, in
+ * any order.  The workspace of dllm_logprobs_ws() bytes is the caller's; calls that may overlap, and
+ * captured graphs that may, need one each.  E_INVAL for NULL pointers, pointers not aligned to
+ * their elements and sizes out of range (top in [0, DLLM_MAX_TOP]); E_DTYPE for another type;
+ * E_CAPACITY for a workspace too small. */
+typedef struct dllm_logprobs_args {
+    int32_t dtype;
+    int32_t n_rows;
+    int32_t vocab;
+    int32_t mask_id;            /* -1: none */
+    int32_t n_tok;
+    int32_t top;
+    const void* d_logits;       /* [n_rows][vocab], row stride ld elements */
+    int64_t ld;
+    const int32_t* d_tok;       /* [n_tok] */
+    const int32_t* d_tok_row;   /* [n_tok] or NULL (n_tok <= n_rows) */
+    float* d_logp;              /* [n_tok] */
+    float* d_entropy;           /* [n_rows] or NULL */
+    int32_t* d_top_id;          /* [n_rows][top] */
+    float* d_top_logp;          /* [n_rows][top] */
+    void* d_ws;
+    size_t ws_bytes;
+} dllm_logprobs_args;
+int dllm_logprobs_ws(const dllm_logprobs_args* args, size_t* bytes);
+int dllm_logprobs(const dllm_logprobs_args* args, dllm_stream stream);
+
+/* A paged cache of all layers. */
+typedef struct dllm_cache {
+    int32_t dtype;        /* DLLM_F32, or DLLM_BF16 / DLLM_F16: 16-bit values, moved as they are */
+    int32_t n_layers;
+    int32_t n_kv_heads;
+    int32_t head_dim;
+    int32_t page;
+    int32_t n_pages;
+    void* d_pages;
+} dllm_cache;
+
+/* Accepted rows behind the text: in every layer, K and V of sequence b's position
+ * d_base[b] + d_path[b][i] move to position d_base[b] + i, for i < d_n[b] (d_path rows of
+ * path_ld entries).  A path ascends (a row's ancestors come before it); an entry that is not
+ * above the one before it, is negative or lies past the table ends it, and it counts as path_ld entries
+ * at most.  Where either position has no page nothing is moved, and a sequence with a
+ * negative base stays as it is.  Positions behind the path keep what they hold.  The pages from
+ * position d_base[b] on must be the sequence's alone.  E_INVAL for NULL pointers
+ * and sizes out of range (path_ld in [1, DLLM_MAX_TREE], table_ld as dllm_batch_plan's). */
+int dllm_cache_compact(const dllm_cache* cache, const int32_t* d_table, int32_t table_ld, const int32_t* d_base,
+                       const int32_t* d_path, int32_t path_ld, const int32_t* d_n, int32_t n_seqs, dllm_stream stream);
+
+/* Forks: afterwards sequence b holds the first d_keep[b] positions of what was sequence
+ * d_src[b] (itself to go on or to be cut; 0 positions: it ends), in ceil(d_keep[b] / page)
+ * pages.  Whole pages are shared by all that keep them.  A last page that is kept in part will be
+ * written to, so only one sequence may go on with it: the first in order, if no sequence
+ * keeps it whole; the others get a page of their own with the kept positions copied, in every layer.
+ * Pages in the old tables that no sequence keeps any more are given back.  The first
+ * shared_pages of a table belong to all and are never counted, copied or given back.  In order:
+ * pages given back are pushed onto the stack d_free[0 .. *d_n_free), the lowest id first, then
+ * the copies' pages are popped off its top, for the lowest sequence first.
+ * d_table_out, d_owned_out and d_n_free_out receive the new tables and counts and must be other
+ * memory; table entries past a sequence's pages, the stack past its top and positions past the
+ * kept ones are left as they were.  d_status [3]: pages copied, pages short, and 0 if granted.
+ * A fork is refused (1) as a whole if pages are short, a source or count is out of range or
+ * a sequence keeps more than its source has pages for (then none is counted as copied): the new
+ * tables and counts are the old ones and no page is copied.
+ * Sequences that share pages are cut and ended by this call: dllm_batch_plan gives
+ * back the pages of a sequence that it cuts, whoever else may hold them.  The workspace of
+ * dllm_batch_fork_ws() bytes is the caller's; calls that may overlap, and captured graphs that may,
+ * need one each.  E_INVAL for NULL pointers and sizes out of range (as dllm_batch_plan's);
+ * E_CAPACITY for a workspace too small. */
+typedef struct dllm_fork_args {
+    int32_t n_seqs;
+    int32_t table_ld;
+    int32_t shared_pages;
+    const int32_t* d_src;       /* [n_seqs] */
+    const int32_t* d_keep;      /* [n_seqs] */
+    const int32_t* d_owned;     /* [n_seqs] */
+    int32_t* d_owned_out;       /* [n_seqs] */
+    const int32_t* d_table;     /* [n_seqs][table_ld] */
+    int32_t* d_table_out;       /* [n_seqs][table_ld] */
+    int32_t* d_free;            /* [n_pages of the cache] */
+    const int32_t* d_n_free;
+    int32_t* d_n_free_out;
+    int32_t* d_status;          /* [3] */
+    void* d_ws;
+    size_t ws_bytes;
+} dllm_fork_args;
+int dllm_batch_fork_ws(int32_t n_seqs, int32_t n_pages, size_t* bytes);
+int dllm_batch_fork(const dllm_cache* cache, const dllm_fork_args* args, dllm_stream stream);
+
 /* Measurement helper: one launch of a plain streaming read over `bytes` bytes of
  * the device buffer d_buf (16-byte aligned; bytes a multiple of 16), the same
  * 16-byte-per-lane non-temporal loads the GEMMs stream weights with.  The caller

@@ -19,6 +19,7 @@ DLLM_OK, DLLM_E_INVAL, DLLM_E_CAPACITY, DLLM_E_DTYPE, DLLM_E_HIP, DLLM_E_UNIMPL,
 DLLM_F32, DLLM_BF16, DLLM_W8, DLLM_Q4 = 0, 1, 2, 3
 DLLM_F16 = 4                      # element type of the batch operators
 DLLM_MAX_SEQS = 4096
+DLLM_MAX_TOP, DLLM_MAX_TREE = 64, 1024
 K_QKV, K_ATTN, K_OPROJ, K_GATEUP, K_DOWN, K_LMHEAD = range(6)
 KERNEL_CLASSES = {"qkv": K_QKV, "attn": K_ATTN, "oproj": K_OPROJ, "gateup": K_GATEUP, "down": K_DOWN,
                   "lmhead": K_LMHEAD}
@@ -84,6 +85,21 @@ class dllm_select_args(ctypes.Structure):
                 _fields(_vp, "d_out_id d_out_conf d_ws") + [("ws_bytes", _sz)])
 
 
+class dllm_logprobs_args(ctypes.Structure):
+    _fields_ = (_fields(_i32, "dtype n_rows vocab mask_id n_tok top") + [("d_logits", _vp), ("ld", _i64)] +
+                _fields(_vp, "d_tok d_tok_row d_logp d_entropy d_top_id d_top_logp d_ws") + [("ws_bytes", _sz)])
+
+
+class dllm_cache(ctypes.Structure):
+    _fields_ = _fields(_i32, "dtype n_layers n_kv_heads head_dim page n_pages") + [("d_pages", _vp)]
+
+
+class dllm_fork_args(ctypes.Structure):
+    _fields_ = (_fields(_i32, "n_seqs table_ld shared_pages") +
+                _fields(_vp, "d_src d_keep d_owned d_owned_out d_table d_table_out d_free d_n_free d_n_free_out d_status d_ws") +
+                [("ws_bytes", _sz)])
+
+
 def _packer(cls):
     """Packs values, in the order of the fields, into the bytes of a struct: a quarter of its constructor's time."""
     fmt = "@" + "".join({_i32: "i", _f32: "f", _i64: "q", _vp: "P", _sz: "N"}[t] for _, t in cls._fields_)
@@ -92,7 +108,8 @@ def _packer(cls):
 
 _pack_qk, _pack_attn, _pack_select = _packer(dllm_qk_args), _packer(dllm_attn_args), _packer(dllm_select_args)
 _pack_rows = _packer(dllm_batch_rows)
-_pack_ws = struct.Struct("@PN").pack          # the last two fields of attention's and selection's
+_pack_logprobs, _pack_cache, _pack_fork = _packer(dllm_logprobs_args), _packer(dllm_cache), _packer(dllm_fork_args)
+_pack_ws = struct.Struct("@PN").pack          # the last two fields of every struct with a workspace
 _pack_2i = struct.Struct("@2i").pack
 
 # (the batch operators' args are pointers to their structs: a struct by reference, or its bytes)
@@ -138,6 +155,14 @@ _SIGNATURES = {
     "dllm_model_set_qk_norm": ([_vp, ctypes.POINTER(_vp), ctypes.POINTER(_vp), _vp], ctypes.c_int),
     "dllm_batch_bytes": ([_vp, _i32, _i32, ctypes.POINTER(_sz)], ctypes.c_int),
     "dllm_batch_step": ([_vp, _vp, _sz, _vp, _vp, _vp, _vp, _vp, _vp, _vp], ctypes.c_int),
+    "dllm_tree_plan": ([_vp, _vp, _vp, _i32, _i32, _vp, _vp, _i32, _vp], ctypes.c_int),
+    "dllm_attention_tree": ([_vp, _vp, _i32, _vp], ctypes.c_int),
+    "dllm_batch_step_tree": ([_vp, _vp, _sz, _vp, _vp, _i32, _vp, _vp, _vp, _vp, _vp, _vp], ctypes.c_int),
+    "dllm_logprobs_ws": ([_vp, ctypes.POINTER(_sz)], ctypes.c_int),
+    "dllm_logprobs": ([_vp, _vp], ctypes.c_int),
+    "dllm_cache_compact": ([_vp, _vp, _i32, _vp, _vp, _i32, _vp, _i32, _vp], ctypes.c_int),
+    "dllm_batch_fork_ws": ([_i32, _i32, ctypes.POINTER(_sz)], ctypes.c_int),
+    "dllm_batch_fork": ([_vp, _vp, _vp], ctypes.c_int),
     "dllm_commit_staged": ([_vp, _vp, _vp, _vp, _vp, _i32, _i32, ctypes.c_float, ctypes.c_float, _vp, _vp, _vp],
                            ctypes.c_int),
 }
@@ -516,11 +541,9 @@ def _workspace(query, a, ws, stream, dev: int, f: str):
     return a[:-16] + _pack_ws(ws.data_ptr(), ws.numel() * ws.element_size()), ws
 
 
-def dllm_attention_paged(q, k_pages, v_pages, table, row0, length, out, max_rows: int, max_len: int,
-                         shared_len: int = 0, lim=None, scale: Optional[float] = None, ws=None, stream=None):
-    """q, out: [rows][heads][dim] or [rows][heads * dim], rows may be strided; scale: 1 / sqrt(dim) if None;
-    k_pages [n_pages][kv_heads][page][dim], v_pages [n_pages][kv_heads][dim][page]."""
-    f, dt, sh = "dllm_attention_paged", q.dtype, q.shape
+def _attention(f, q, k_pages, v_pages, table, row0, length, out, max_rows, max_len, shared_len, lim, scale, ws, stream,
+               mask=None):
+    dt, sh = q.dtype, q.shape
     dev, B = _gpu(f, q), length.numel()
     try:
         T, ld, (n_pages, kv, page, dim) = sh[0], table.shape[-1], k_pages.shape
@@ -534,6 +557,10 @@ def dllm_attention_paged(q, k_pages, v_pages, table, row0, length, out, max_rows
             (lim is not None and lim.numel() < T)):
         _refuse(f, "v_pages must be [n_pages][kv_heads][head_dim][page], table must have a row and row0 an entry per sequence "
                    "(row0: one more), lim an entry per row")
+    if mask is not None:
+        _plain(f, dev, _Types.i32, (mask,), "mask")
+        if mask.dim() != 2 or mask.shape[0] < T:
+            _refuse(f, "mask must be [rows][words]")
     if T == 0:
         return
     try:
@@ -545,10 +572,21 @@ def dllm_attention_paged(q, k_pages, v_pages, table, row0, length, out, max_rows
         _refuse(f, _NO_FIT_MSG)
     L = lib()
     a, keep = _workspace(L.dllm_attention_paged_ws, a, ws, stream, dev, f)
-    rc = L.dllm_attention_paged(a, _stream(stream, dev))
+    if mask is None:
+        rc = L.dllm_attention_paged(a, _stream(stream, dev))
+    else:
+        rc = L.dllm_attention_tree(a, mask.data_ptr(), mask.shape[1], _stream(stream, dev))
     if rc:
         _check(rc, f)
     del keep
+
+
+def dllm_attention_paged(q, k_pages, v_pages, table, row0, length, out, max_rows: int, max_len: int,
+                         shared_len: int = 0, lim=None, scale: Optional[float] = None, ws=None, stream=None):
+    """q, out: [rows][heads][dim] or [rows][heads * dim], rows may be strided; scale: 1 / sqrt(dim) if None;
+    k_pages [n_pages][kv_heads][page][dim], v_pages [n_pages][kv_heads][dim][page]."""
+    _attention("dllm_attention_paged", q, k_pages, v_pages, table, row0, length, out, max_rows, max_len, shared_len, lim,
+               scale, ws, stream)
 
 
 def _select_args(f, logits, out_id, out_conf, mask_id=-1, row0=None, hist=None, hist0=None, n_prompt=None, repetition=None,
@@ -658,12 +696,8 @@ def dllm_batch_bytes(model: int, n_pages: int, page: int) -> int:
     return n.value
 
 
-def dllm_batch_step(model: int, pages, n_pages: int, page: int, tok, mask, table, row0, pos, slot, length, max_rows: int,
-                    max_len: int, out_id=None, out_conf=None, shared_len: int = 0, lim=None, logits=None, control=None,
-                    stream=None):
-    """tok's length is the number of rows.  logits (float32 [rows][vocab]) with control, a dict of dllm_select's options:
-    the outputs come from the controlled logits."""
-    f = "dllm_batch_step"
+def _batch_step(f, model, pages, n_pages, page, tok, mask, table, row0, pos, slot, length, max_rows, max_len, out_id, out_conf,
+                shared_len, lim, logits, control, stream, tree=None):
     dev, R, B, ld = _gpu(f, tok), tok.numel(), length.numel(), table.shape[-1]
     _plain(f, dev, _Types.i32, (tok, table, row0, pos, slot, length, lim, out_id), "tok table row0 pos slot length lim out_id")
     _plain(f, dev, _Types.torch.uint8, (mask,), "mask")
@@ -671,6 +705,10 @@ def dllm_batch_step(model: int, pages, n_pages: int, page: int, tok, mask, table
     _at_least(f, R, (pos, slot, lim, mask, out_id, out_conf), "pos slot lim mask out_id out_conf")
     if table.numel() < B * ld or row0.numel() < B + 1 or pages.get_device() != dev or not pages.is_contiguous():
         _refuse(f, "table must have a row and row0 an entry per sequence (row0: one more), pages be on the same GPU")
+    if tree is not None:
+        _plain(f, dev, _Types.i32, (tree,), "tree")
+        if tree.dim() != 2 or tree.shape[0] < R:
+            _refuse(f, "tree must be [rows][words]")
     try:
         rows = _pack_rows(R, B, page, n_pages, ld, shared_len, max_rows, max_len, table.data_ptr(), row0.data_ptr(),
                           pos.data_ptr(), slot.data_ptr(), length.data_ptr(), _ptr(lim) or 0)
@@ -681,9 +719,161 @@ def dllm_batch_step(model: int, pages, n_pages: int, page: int, tok, mask, table
         _refuse(f, "control needs logits, and logits need out_id and out_conf")
     if logits is not None:
         sel, keep, _ = _select_args(f, logits, out_id, out_conf, stream=stream, **(control or {}))
-    _check(lib().dllm_batch_step(model, pages.data_ptr(), pages.numel() * pages.element_size(), rows, tok.data_ptr(),
-                                 _ptr(mask), sel, _ptr(out_id), _ptr(out_conf), _stream(stream)), f)
+    head, tail = (model, pages.data_ptr(), pages.numel() * pages.element_size(), rows), (
+        tok.data_ptr(), _ptr(mask), sel, _ptr(out_id), _ptr(out_conf), _stream(stream))
+    if tree is None:
+        _check(lib().dllm_batch_step(*head, *tail), f)
+    else:
+        _check(lib().dllm_batch_step_tree(*head, tree.data_ptr(), tree.shape[1], *tail), f)
     del keep
+
+
+def dllm_batch_step(model: int, pages, n_pages: int, page: int, tok, mask, table, row0, pos, slot, length, max_rows: int,
+                    max_len: int, out_id=None, out_conf=None, shared_len: int = 0, lim=None, logits=None, control=None,
+                    stream=None):
+    """tok's length is the number of rows.  logits (float32 [rows][vocab]) with control, a dict of dllm_select's options:
+    the outputs come from the controlled logits."""
+    _batch_step("dllm_batch_step", model, pages, n_pages, page, tok, mask, table, row0, pos, slot, length, max_rows, max_len,
+                out_id, out_conf, shared_len, lim, logits, control, stream)
+
+
+# ----------------------------------------------------------------------------
+# Branches: trees of drafted rows, their log probabilities, accepted paths and forks
+# ----------------------------------------------------------------------------
+
+
+def dllm_tree_plan(parent, row0, length, pos, mask, stream=None):
+    """parent and pos: an entry per row; mask: int32 words [rows][words]."""
+    f, B = "dllm_tree_plan", length.numel()
+    dev = _gpu(f, length)
+    _plain(f, dev, _Types.i32, (parent, row0, length, pos, mask), "parent row0 length pos mask")
+    if mask.dim() != 2:
+        _refuse(f, "mask must be [rows][words]")
+    T, ld = mask.shape
+    if row0.numel() <= B or parent.numel() < T or pos.numel() < T:
+        _refuse(f, "row0 must have an entry per sequence and one more, parent and pos an entry per row of mask")
+    if T == 0:
+        return
+    _fits(f, T, ld)
+    rc = lib().dllm_tree_plan(parent.data_ptr(), row0.data_ptr(), length.data_ptr(), T, B, pos.data_ptr(), mask.data_ptr(), ld,
+                              _stream(stream, dev))
+    if rc:
+        _check(rc, f)
+
+
+def dllm_attention_tree(q, k_pages, v_pages, table, row0, length, mask, out, max_rows: int, max_len: int,
+                        shared_len: int = 0, lim=None, scale: Optional[float] = None, ws=None, stream=None):
+    """As dllm_attention_paged, with mask: int32 words [rows][words]."""
+    if mask is None:
+        _refuse("dllm_attention_tree", "mask must be [rows][words]")
+    _attention("dllm_attention_tree", q, k_pages, v_pages, table, row0, length, out, max_rows, max_len, shared_len, lim, scale,
+               ws, stream, mask)
+
+
+def dllm_batch_step_tree(model: int, pages, n_pages: int, page: int, tok, mask, tree, table, row0, pos, slot, length,
+                         max_rows: int, max_len: int, out_id=None, out_conf=None, shared_len: int = 0, lim=None, logits=None,
+                         control=None, stream=None):
+    """As dllm_batch_step, with tree: int32 words [rows][words], and pos: dllm_tree_plan's."""
+    if tree is None:
+        _refuse("dllm_batch_step_tree", "tree must be [rows][words]")
+    _batch_step("dllm_batch_step_tree", model, pages, n_pages, page, tok, mask, table, row0, pos, slot, length, max_rows, max_len,
+                out_id, out_conf, shared_len, lim, logits, control, stream, tree)
+
+
+def dllm_logprobs(logits, tok=None, tok_row=None, logp=None, entropy=None, top_id=None, top_logp=None, mask_id: int = -1,
+                  ws=None, stream=None):
+    """logits: [rows][vocab], rows may be strided; tok, tok_row and logp: an entry per token; entropy: one per row;
+    top_id and top_logp: [rows][top]."""
+    f = "dllm_logprobs"
+    dev, dt = _gpu(f, logits), logits.dtype
+    if logits.dim() != 2:
+        _refuse(f, "logits must be [rows][vocab]")
+    T, V = logits.shape
+    if (tok is None) != (logp is None) or (tok is None and tok_row is not None) or (top_id is None) != (top_logp is None):
+        _refuse(f, "tok and logp, top_id and top_logp go together; tok_row needs tok")
+    _plain(f, dev, _Types.i32, (tok, tok_row, top_id), "tok tok_row top_id")
+    _plain(f, dev, _Types.f32, (logp, entropy, top_logp), "logp entropy top_logp")
+    n = 0 if tok is None else tok.numel()
+    top = 0
+    if top_id is not None:
+        if top_id.dim() != 2 or top_id.shape[0] != T or top_logp.shape != top_id.shape:
+            _refuse(f, "top_id and top_logp must be [rows][top]")
+        top = top_id.shape[1]
+    if ((V > 1 and logits.stride(1) != 1) or (n and logp.numel() < n) or (tok_row is not None and tok_row.numel() < n) or
+            (entropy is not None and entropy.numel() < T)):
+        _refuse(f, "rows must be whole, logp and tok_row have an entry per token, entropy one per row")
+    if T == 0 and n == 0:
+        return
+    try:
+        a = _pack_logprobs(_Types.elem.get(dt, -1), T, V, mask_id, n, top, logits.data_ptr(), logits.stride(0) if T > 1 else V,
+                           tok.data_ptr() if n else 0, tok_row.data_ptr() if n and tok_row is not None else 0,
+                           logp.data_ptr() if n else 0, 0 if entropy is None else entropy.data_ptr(),
+                           top_id.data_ptr() if top else 0, top_logp.data_ptr() if top else 0, 0, 0)
+    except _NO_FIT:
+        _refuse(f, _NO_FIT_MSG)
+    L = lib()
+    a, keep = _workspace(L.dllm_logprobs_ws, a, ws, stream, dev, f)
+    rc = L.dllm_logprobs(a, _stream(stream, dev))
+    if rc:
+        _check(rc, f)
+    del keep
+
+
+def _cache(f, dev, pages, page) -> bytes:
+    """The dllm_cache of pages [layers][2][n_pages][kv_heads][page * head_dim]."""
+    sh = pages.shape
+    if pages.get_device() != dev or not pages.is_contiguous():
+        _refuse(f, "pages must be a contiguous tensor on the same GPU")
+    if len(sh) != 5 or sh[1] != 2 or page < 1 or sh[4] % page != 0:
+        _refuse(f, "pages must be [layers][2][n_pages][kv_heads][page * head_dim]")
+    try:
+        return _pack_cache(_Types.elem.get(pages.dtype, -1), sh[0], sh[3], sh[4] // page, page, sh[2], pages.data_ptr())
+    except _NO_FIT:
+        _refuse(f, _NO_FIT_MSG)
+
+
+def dllm_cache_compact(pages, page: int, table, base, path, n, stream=None):
+    """pages: [layers][2][n_pages][kv_heads][page * head_dim], as dllm_batch_step's; base and n: an entry per
+    sequence; path: [sequences][entries]."""
+    f, B = "dllm_cache_compact", base.numel()
+    dev = _gpu(f, base)
+    c = _cache(f, dev, pages, page)
+    _plain(f, dev, _Types.i32, (table, base, path, n), "table base path n")
+    if path.dim() != 2 or path.shape[0] < B or n.numel() < B or table.numel() < B * table.shape[-1]:
+        _refuse(f, "path must be [sequences][entries], n have an entry and table a row per sequence")
+    _fits(f, table.shape[-1], path.shape[1])
+    rc = lib().dllm_cache_compact(c, table.data_ptr(), table.shape[-1], base.data_ptr(), path.data_ptr(), path.shape[1],
+                                  n.data_ptr(), B, _stream(stream, dev))
+    if rc:
+        _check(rc, f)
+
+
+def dllm_batch_fork(src, keep, owned, owned_out, table, table_out, free, n_free, n_free_out, shared_pages: int, pages,
+                    page: int, status, ws=None, stream=None):
+    """src, keep, owned and owned_out: an entry, table and table_out: a row per sequence; free: an entry per page of
+    pages, [layers][2][n_pages][kv_heads][page * head_dim]."""
+    f, B, ld = "dllm_batch_fork", src.numel(), table.shape[-1]
+    dev = _gpu(f, src)
+    c = _cache(f, dev, pages, page)
+    _plain(f, dev, _Types.i32, (src, keep, owned, owned_out, table, table_out, free, n_free, n_free_out, status),
+           "src keep owned owned_out table table_out free n_free n_free_out status")
+    if (keep.numel() < B or owned.numel() < B or owned_out.numel() < B or table.numel() < B * ld or
+            table_out.shape != table.shape or free.numel() < pages.shape[2] or not n_free.numel() or not n_free_out.numel() or
+            status.numel() < 3):
+        _refuse(f, "keep, owned and owned_out must have an entry, table and table_out a row per sequence, free an entry per page, "
+                   "status 3, n_free 1")
+    try:
+        a = _pack_fork(B, ld, shared_pages, src.data_ptr(), keep.data_ptr(), owned.data_ptr(), owned_out.data_ptr(),
+                       table.data_ptr(), table_out.data_ptr(), free.data_ptr(), n_free.data_ptr(), n_free_out.data_ptr(),
+                       status.data_ptr(), 0, 0)
+    except _NO_FIT:
+        _refuse(f, _NO_FIT_MSG)
+    L, n_pages = lib(), pages.shape[2]
+    a, hold = _workspace(lambda _, out: L.dllm_batch_fork_ws(B, n_pages, out), a, ws, stream, dev, f)
+    rc = L.dllm_batch_fork(c, a, _stream(stream, dev))
+    if rc:
+        _check(rc, f)
+    del hold
 
 
 # ----------------------------------------------------------------------------

@@ -47,6 +47,8 @@ struct PagedArgs {
     int n_s;                      // workgroups of the shared part (the first ones)
     int direct;                   // one part in all: the output is written here, not merged
     int out_f32;                  // out holds floats whatever T is (a batch step's, for the O projection's operand)
+    const uint32_t* mask;         // [T][mask_ld]: which of its sequence's rows a row sees (TREE)
+    int mask_ld;
     float* opart;                 // [ns_s + ns_o][T][H][Dh] unnormalised partial outputs
     float* mlpart;                // [ns_s + ns_o][T][H][2]  (reference in log2 units, sum)
 };
@@ -62,6 +64,19 @@ __device__ __forceinline__ int row_seq(const int* row0, int B, int r) {
     }
     return lo;
 }
+
+// First position of sequence b that one of the call's rows has; those before it are cached.
+__device__ __forceinline__ int seq_base(const PagedArgs& a, int b) {
+    const RowRange n = row_range(a.row0[b], a.row0[b + 1], a.T, a.T);
+    return max(a.len[b], 0) - (n.end - n.begin);
+}
+// Word i of a row's mask; the cached positions before it count as set bits.
+__device__ __forceinline__ uint32_t mask_word(const uint32_t* words, int ld, int i) {
+    const uint32_t w = words[min(max(i, 0), ld - 1)];
+    return i < 0 ? 0xFFFFFFFFu : (i < ld ? w : 0u);
+}
+// The 32 bits from bit t on, of the words t / 32 and the one behind it.
+__device__ __forceinline__ uint32_t mask_bits(uint32_t w0, uint32_t w1, int t) { return __builtin_amdgcn_alignbit(w1, w0, t & 31); }
 
 // Element type: one product step of a 16 x 16 or 32 x 32 tile (with 16-bit types 32 or 16 deep).
 typedef float f32x16_t __attribute__((ext_vector_type(16)));
@@ -168,7 +183,11 @@ template <typename T> __device__ __forceinline__ void store_out4(const PagedArgs
 // TFLOP/s where a large library product reaches 1100; waiting 22% of the wave cycles); rows enough for the prefix only, LDS reads and the K/V
 // themselves (8 x 32 rows of 32 fp16 heads behind 4096: 37 us and 6, 115 MB); few rows, latency (8 x 1 rows
 // behind 1564: 9.8 us and 4.8, 288 workgroups of three steps, each asked for when the one before has landed).
-template <typename T, int DH, int QG, int RT, int KG, int SUB>
+//
+// TREE: a row sees the cached positions and, of its sequence's rows, those that its mask has.  Steps whose keys are all
+// cached run as without; in the others a lane takes the 32 bits of its row for a block from two words, which are
+// asked for beside the step's K/V one step ahead (a load waited for inside a step would wait for the staging behind it).
+template <typename T, int DH, int QG, int RT, int KG, int SUB, bool TREE>
 __global__ void __launch_bounds__(QG * KG * 64)
 __attribute__((amdgpu_waves_per_eu(QG * KG * (160 * 1024 / (2 * SUB * 64 * DH * (int)sizeof(T))) >= 8 ? 2 : 1)))
 attn_paged_kernel(PagedArgs a) {
@@ -207,7 +226,7 @@ attn_paged_kernel(PagedArgs a) {
     const int n_items = own ? (int)gridDim.x - a.n_s : a.n_s;
     const int L = (int)blockIdx.x - (own ? a.n_s : 0), xcd = L & 7;
     const int item = xcd * (n_items >> 3) + min(xcd, n_items & 7) + (L >> 3);
-    int tile, split, hk, b, ks, ke, first, behind, most_rows, bps, part;
+    int tile, split, hk, b, ks, ke, first, behind, most_rows, bps, part, base_own = 0;
     if (own) {
         tile = item % a.nt_o;
         const int i1 = item / a.nt_o, i2 = i1 / a.ns_o;
@@ -223,6 +242,7 @@ attn_paged_kernel(PagedArgs a) {
         const int nst = (max(0, ke - ks) + 32 * SUB - 1) / (32 * SUB);
         bps = (nst + a.ns_o - 1) / a.ns_o;
         part = a.ns_s + split;
+        if constexpr (TREE) base_own = seq_base(a, b);
     } else {
         tile = item % a.nt_s;
         const int i1 = item / a.nt_s;
@@ -322,7 +342,7 @@ attn_paged_kernel(PagedArgs a) {
     // sequence ends inside it.
     int short_len = 0x7FFFFFFF;
     if (!own) {
-        for (int i = lane; i < a.B; i += 64) short_len = min(short_len, a.len[i]);
+        for (int i = lane; i < a.B; i += 64) short_len = min(short_len, TREE ? seq_base(a, i) : a.len[i]);
 #pragma unroll
         for (int o = 32; o > 0; o >>= 1) short_len = min(short_len, __shfl_xor(short_len, o));
     }
@@ -331,8 +351,13 @@ attn_paged_kernel(PagedArgs a) {
         const int n = own || short_len >= ke ? ke : min(ke, a.len[row_seq(a.row0, a.B, row)]);
         return a.lim != nullptr ? min(n, a.lim[row]) : n;
     };
+    // (TREE: short_len is the least number of cached positions) the first key of virtual row f that its mask decides
+    auto row_low = [&](int f) {
+        return own ? base_own : (short_len >= ke ? ke : seq_base(a, row_seq(a.row0, a.B, R0 + f / a.G)));
+    };
     u32x4_t qf[NC];
-    int lim;
+    int lim, low = 0;
+    const uint32_t* words = nullptr;
     {
         // rows past the last repeat it (the rescale below is decided over a tile's rows)
         const int f = min(f0 + RT * qw + r, nv - 1);
@@ -348,19 +373,26 @@ attn_paged_kernel(PagedArgs a) {
             }
         }
         lim = row_limit(f);
+        if constexpr (TREE) {
+            low = row_low(f);
+            words = a.mask + (size_t)row * a.mask_ld;
+        }
     }
     // The largest limit of the tile's rows ends its keys: what lies behind may be anything.  Keys from the
     // smallest on (kz: its 16-byte slot of V^T) are seen by some rows only.
     int ktop = ks, lim_lo;
     if (a.lim == nullptr && (own || short_len >= ke)) {
         lim_lo = ktop = max(ks, ke);
+        if constexpr (TREE) {
+            if (own) lim_lo = min(ktop, max(ks, base_own));
+        }
     } else {
         lim_lo = 0x7FFFFFFF;
 #pragma unroll
         for (int i = 0; i < (TM + 63) / 64; ++i) {
-            const int n = row_limit(min(f0 + (TM < 64 ? lane % TM : lane) + 64 * i, nv - 1));
+            const int f = min(f0 + (TM < 64 ? lane % TM : lane) + 64 * i, nv - 1), n = row_limit(f);
             ktop = max(ktop, n);
-            lim_lo = min(lim_lo, n);
+            lim_lo = min(lim_lo, TREE ? min(n, row_low(f)) : n);
         }
 #pragma unroll
         for (int o = 32; o > 0; o >>= 1) {
@@ -376,10 +408,29 @@ attn_paged_kernel(PagedArgs a) {
     auto chunk_have = [&](int n) { return __builtin_amdgcn_ballot_w64(pgv >= 0 && 64 * n + lane < blocks); };
     uint64_t have = chunk_have(0);
 
-    // smallest limit of the wave's rows: blocks below it need no per-key mask
+    // smallest limit of the wave's rows (or first key that a mask decides): blocks below it need no per-key mask
     int lim_w = ktop;
+    const int lim_m = TREE ? min(lim, low) : lim;
 #pragma unroll
-    for (int i = 0; i < RT; ++i) lim_w = min(lim_w, __builtin_amdgcn_readlane(lim, i));
+    for (int i = 0; i < RT; ++i) lim_w = min(lim_w, __builtin_amdgcn_readlane(lim_m, i));
+
+    // the mask words of this wave's blocks of step t
+    uint32_t w0[SW], w1[SW];
+    auto first_key = [&](int t) { return ks + 32 * (kb0 + SUB * t + kw * SW); };
+    auto load_words = [&](int t) {
+        if (first_key(t) + 32 * SW <= lim_w) return;
+#pragma unroll
+        for (int w = 0; w < SW; ++w) {
+            const int i = (first_key(t) + 32 * w - low) >> 5;
+            w0[w] = mask_word(words, a.mask_ld, i);
+            w1[w] = mask_word(words, a.mask_ld, i + 1);
+        }
+    };
+    if constexpr (TREE) {
+#pragma unroll
+        for (int w = 0; w < SW; ++w) w0[w] = w1[w] = 0xFFFFFFFFu;
+        load_words(0);
+    }
 
     float mrun = -INFINITY, lrun = 0.f;
     Acc oacc[ND];
@@ -411,6 +462,15 @@ attn_paged_kernel(PagedArgs a) {
         // This wave's loads of step t have landed; the barrier makes every wave's visible and frees the buffer
         // that round t - 1 read, for step t + 1.
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        // (before the next loads go out, which a use of these words would else wait for)
+        uint32_t seen[SW];
+        if constexpr (TREE) {
+#pragma unroll
+            for (int w = 0; w < SW; ++w) {
+                seen[w] = mask_bits(w0[w], w1[w], k0w + 32 * w - low);
+                asm volatile("" : "+v"(seen[w]));
+            }
+        }
         if (!whole || k0 + 32 * SUB > lim_lo) {
 #pragma unroll
             for (int u = 0; u < SUB; ++u)
@@ -423,6 +483,7 @@ attn_paged_kernel(PagedArgs a) {
                 have = chunk_have((SUB * (t + 1)) >> 6);
             }
             stage(t + 1, (t + 1) & 1);
+            if constexpr (TREE) load_words(t + 1);
         }
         if (!busy) continue;
 
@@ -475,9 +536,17 @@ attn_paged_kernel(PagedArgs a) {
 #pragma unroll
             for (int w = 0; w < SW; ++w) {
                 const int end = (there >> (kw * SW + w)) & 1 ? lim : 0;
+                if constexpr (TREE) {
+                    const int n = end - (k0w + 32 * w);                 // keys of the block before the limit
+                    const uint32_t vis = (n >= 32 ? seen[w] : (n > 0 ? seen[w] & ((1u << n) - 1) : 0u)) >> key_of(0);
 #pragma unroll
-                for (int e = 0; e < NS; ++e)
-                    if (k0w + 32 * w + key_of(e) >= end) sv[w][e] = -INFINITY;
+                    for (int e = 0; e < NS; ++e)
+                        if (!(vis >> (key_of(e) - key_of(0)) & 1)) sv[w][e] = -INFINITY;
+                } else {
+#pragma unroll
+                    for (int e = 0; e < NS; ++e)
+                        if (k0w + 32 * w + key_of(e) >= end) sv[w][e] = -INFINITY;
+                }
             }
         }
         // the row's maximum over the step and its lane groups (max is symmetric: a swap hands a lane its
@@ -553,6 +622,11 @@ attn_paged_kernel(PagedArgs a) {
             const int k0 = ks + 32 * (kb0 + blk), pg = trow[k0 >> a.page_shift];
             if ((KG > 1 && blk % SUB / SW != kw) || pg < 0 || pg >= a.n_pages) continue;
             const T* Vp = (const T*)a.vp + ((long)pg * a.Hk + hk) * page_elems + (k0 & ((1 << a.page_shift) - 1));
+            uint32_t vis = 0xFFFFFFFFu;
+            if constexpr (TREE) {
+                const int t = k0 - low;
+                vis = mask_bits(mask_word(words, a.mask_ld, t >> 5), mask_word(words, a.mask_ld, (t >> 5) + 1), t);
+            }
 #pragma unroll
             for (int dt = 0; dt < ND; ++dt) {
                 Acc c;
@@ -562,8 +636,8 @@ attn_paged_kernel(PagedArgs a) {
                 for (int u = 0; u < NV; ++u) {
                     const u32x4_t v = ldg16(Vp + ((long)(RT * dt + r) << a.page_shift) + (16 / ES) * (NG * u + g));
                     auto sees = [&](int e) {
-                        const int key = k0 + key_of(16 / ES * u + e);
-                        return key >= kz && key < lim ? PagedClass<T>::one : 0u;
+                        const int o = key_of(16 / ES * u + e), key = k0 + o;
+                        return key >= kz && key < lim && (!TREE || (vis >> o & 1)) ? PagedClass<T>::one : 0u;
                     };
                     u32x4_t seen;
 #pragma unroll

@@ -6,7 +6,8 @@
 #include <string>
 
 #include "../../include/dllm.h"
-#include "attn_paged.hpp"
+#include "attn_launch.hpp"
+#include "batch_host.hpp"
 #include "batch_plan.hpp"
 #include "batch_rules.hpp"
 #include "common.hpp"
@@ -15,47 +16,6 @@
 #include "select.hpp"
 
 using namespace dllm;
-
-namespace {
-
-bool aligned(const void* p, size_t n) { return ((uintptr_t)p & (n - 1)) == 0; }
-
-int check_dtype(int dtype) {
-    if (dtype != DLLM_F32 && dtype != DLLM_BF16 && dtype != DLLM_F16)
-        return fail(DLLM_E_DTYPE, "dtype must be DLLM_F32, DLLM_BF16 or DLLM_F16");
-    return DLLM_OK;
-}
-
-// A page size and count: shift of the page size, or -1 (recorded).
-int page_shift(int page, int n_pages) {
-    if (page != 32 && page != 64 && page != 128 && page != 256) {
-        fail(DLLM_E_INVAL, "page must be 32, 64, 128 or 256");
-        return -1;
-    }
-    if (n_pages < 1 || (long)n_pages * page >= (1l << 31)) {
-        fail(DLLM_E_INVAL, "n_pages must be >= 1 and n_pages * page < 2^31");
-        return -1;
-    }
-    return page == 32 ? 5 : (page == 64 ? 6 : (page == 128 ? 7 : 8));
-}
-
-int check_heads(int H, int Hk, int Dh) {
-    if (H < 1 || H > 1024 || Hk < 1 || Hk > H || H % Hk != 0)
-        return fail(DLLM_E_INVAL, "n_heads must be in [1, 1024] and n_kv_heads divide it");
-    if (Dh != 32 && Dh != 64 && Dh != 128) return fail(DLLM_E_DTYPE, "head_dim must be 32, 64 or 128");
-    return DLLM_OK;
-}
-
-bool row_stride_ok(const void* p, int64_t ld, int64_t width, int es) {
-    return aligned(p, 16) && ld >= width && ld <= (1ll << 40) && (ld * es) % 16 == 0;
-}
-
-// A launch has fewer than 2^32 threads (here with a workgroup to spare).
-bool grid_ok(long wgs, int threads) { return wgs < ((1l << 32) - 1024) / threads; }
-
-constexpr int MAX_BATCH_ROWS = 1 << 24;
-
-}  // namespace
 
 extern "C" {
 
@@ -126,33 +86,12 @@ int check_attn(const dllm_attn_args* g, int& shift) {
     return DLLM_OK;
 }
 
-template <typename T, int DH>
-void launch_attn_dh(PagedArgs a, const AttnPlan& p, hipStream_t s) {
-    constexpr int SUB = sizeof(T) == 4 ? 1 : 2;
-    const dim3 grid((unsigned)(p.wgs_s + p.wgs_o));
-#define ATTN(QG_, RT_, KG_) \
-    hipLaunchKernelGGL((attn_paged_kernel<T, DH, QG_, RT_, KG_, SUB>), grid, dim3(QG_ * KG_ * 64), 0, s, a)
-    if constexpr (sizeof(T) == 2) {
-        if (p.qt == 2) ATTN(4, 32, 1);
-        else if (p.qg == 4) ATTN(4, 16, 1);
-        else if (p.qg == 2) ATTN(2, 16, 2);
-        else ATTN(1, 16, 2);
-    } else {
-        if (p.qg == 4) ATTN(4, 16, 1);
-        else if (p.qg == 2) ATTN(2, 16, 1);
-        else ATTN(1, 16, 1);
-    }
-#undef ATTN
-    if (!a.direct)
-        hipLaunchKernelGGL((attn_paged_merge_kernel<T, DH>), dim3(ceil_div((long)a.T * a.H, 256 / (DH / 4))), dim3(256), 0,
-                           s, a);
-}
-
 template <typename T>
-void launch_attn(const PagedArgs& a, const AttnPlan& p, int Dh, hipStream_t s) {
-    if (Dh == 128) launch_attn_dh<T, 128>(a, p, s);
-    else if (Dh == 64) launch_attn_dh<T, 64>(a, p, s);
-    else if constexpr (sizeof(T) == 4) launch_attn_dh<T, 32>(a, p, s);
+void merge_attn(const PagedArgs& a, int Dh, hipStream_t s) {
+    const dim3 grid(ceil_div((long)a.T * a.H, 256 / (Dh / 4)));
+    if (Dh == 128) hipLaunchKernelGGL((attn_paged_merge_kernel<T, 128>), grid, dim3(256), 0, s, a);
+    else if (Dh == 64) hipLaunchKernelGGL((attn_paged_merge_kernel<T, 64>), grid, dim3(256), 0, s, a);
+    else if constexpr (sizeof(T) == 4) hipLaunchKernelGGL((attn_paged_merge_kernel<T, 32>), grid, dim3(256), 0, s, a);
 }
 
 size_t select_ws_bytes(const dllm_select_args* g) {
@@ -222,7 +161,7 @@ int select_check(const dllm_select_args* g) {
     return DLLM_OK;
 }
 
-int attention_paged(const dllm_attn_args* g, bool out_f32, hipStream_t s) {
+int attention_paged(const dllm_attn_args* g, const uint32_t* d_mask, int mask_ld, bool out_f32, hipStream_t s) {
     int shift = 0;
     if (int rc = check_attn(g, shift)) return rc;
     if (!g->d_q || !g->d_k_pages || !g->d_v_pages || !g->d_table || !g->d_row0 || !g->d_len || !g->d_out)
@@ -252,9 +191,14 @@ int attention_paged(const dllm_attn_args* g, bool out_f32, hipStream_t s) {
     a.ns_s = p.ns_s; a.nt_s = p.nt_s; a.ns_o = p.ns_o; a.nt_o = p.nt_o; a.n_s = (int)p.wgs_s;
     a.direct = p.direct();
     a.out_f32 = out_f32;
-    if (g->dtype == DLLM_F32) launch_attn<float>(a, p, g->head_dim, s);
-    else if (g->dtype == DLLM_F16) launch_attn<_Float16>(a, p, g->head_dim, s);
-    else launch_attn<__bf16>(a, p, g->head_dim, s);
+    a.mask = d_mask; a.mask_ld = mask_ld;
+    if (d_mask) launch_attn_tree(g->dtype, a, p, g->head_dim, s);
+    else launch_attn<false>(g->dtype, a, p, g->head_dim, s);
+    if (!a.direct) {
+        if (g->dtype == DLLM_F32) merge_attn<float>(a, g->head_dim, s);
+        else if (g->dtype == DLLM_F16) merge_attn<_Float16>(a, g->head_dim, s);
+        else merge_attn<__bf16>(a, g->head_dim, s);
+    }
     HIP_TRY(hipGetLastError());
     return DLLM_OK;
 }
@@ -307,7 +251,7 @@ int dllm_attention_paged_ws(const dllm_attn_args* g, size_t* bytes) {
     return DLLM_OK;
 }
 
-int dllm_attention_paged(const dllm_attn_args* g, dllm_stream stream) { return attention_paged(g, false, (hipStream_t)stream); }
+int dllm_attention_paged(const dllm_attn_args* g, dllm_stream stream) { return attention_paged(g, nullptr, 0, false, (hipStream_t)stream); }
 
 int dllm_select_ws(const dllm_select_args* g, size_t* bytes) {
     if (!bytes) return fail(DLLM_E_INVAL, "bytes is NULL");

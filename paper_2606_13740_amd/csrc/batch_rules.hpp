@@ -121,4 +121,30 @@ inline int select_rows_per(int T, int n_ranges) {
 inline long select_wgs(int T, int n_ranges) { return (long)n_ranges * ceil_div(T, select_rows_per(T, n_ranges)); }
 inline bool select_four_waves(long wgs) { return wgs <= 4 * N_CU; }
 
+// Rows of a sequence's tree: bits of a mask row that the plan of trees keeps in LDS.
+constexpr int TREE_MAX_LD = 32;
+inline size_t tree_lds_bytes(int ld) { return (size_t)32 * ld * (ld + 3) * 4; }
+
+// Threads of a log probability workgroup, logits of a lane, ids of a wave's block.
+constexpr int LP_NT = 256, LP_PT = 32, LP_BLOCK = 64 * LP_PT, LP_MAX_TOP = 64;
+
+// Blocks of a part of a row: whole rounds of the four waves, as many as leave 1024 workgroups (four for every CU).
+inline int lp_per(int T, int vocab) {
+    const int blocks = ceil_div(vocab, LP_BLOCK), waves = LP_NT / 64;
+    const long parts = std::max<long>(1, 4 * N_CU / std::max(T, 1));
+    return waves * ceil_div(ceil_div(blocks, parts), waves);
+}
+inline int lp_parts(int T, int vocab) { return ceil_div(ceil_div(vocab, LP_BLOCK), lp_per(T, vocab)); }
+inline size_t lp_ws_bytes(int T, int vocab, int top) {
+    const int parts = lp_parts(T, vocab);
+    return parts == 1 ? 0 : (size_t)T * parts * (16 + 8 * (size_t)top);
+}
+
+// Threads of a fork's workgroup, and pages whose marks its LDS holds (beside 32 KB of the sequences').
+constexpr int FORK_NT = 1024, FORK_LDS_PAGES = 31 * 1024;
+// The copies' count (16 bytes), their list, and the marks where they do not fit.
+inline size_t fork_ws_bytes(int n_seqs, int n_pages) {
+    return 16 + (size_t)n_seqs * 16 + (n_pages > FORK_LDS_PAGES ? (size_t)n_pages * 4 : 0);
+}
+
 }  // namespace dllm

@@ -660,6 +660,8 @@ struct FwdArgs {
     Workspace* ws = nullptr;  // a caller-provided workspace (no growth), else the model's
     const dllm_batch_rows* batch = nullptr;   // rows of several sequences over a paged cache
     void* pages = nullptr;                    // that cache
+    const uint32_t* tree = nullptr;           // masks of the batch's rows [M][tree_ld], or none
+    int tree_ld = 0;
 };
 
 // O / down projection: split-K GEMM into partials, then the reduction that adds
@@ -861,7 +863,7 @@ int forward_t(dllm_model* m, dllm_kv* kv, const FwdArgs& a, hipStream_t s) {
             g.d_out = w.qkv;                       // the Q/K/V rows are spent
             ProbeScope ps(m, DLLM_K_ATTN, s);
             // (rows of d floats, which the operand splits into its pair: no rounding to the cache's type between)
-            if ((rc = attention_paged(&g, true, s))) return rc;
+            if ((rc = attention_paged(&g, a.tree, a.tree_ld, true, s))) return rc;
             hipLaunchKernelGGL(attn_operand_kernel<XF32>, dim3(Mc), dim3(256), 0, s, (const float*)w.qkv, a.M, d, w.of,
                                m->KCx_d);
         }
@@ -1222,9 +1224,9 @@ int dllm_batch_bytes(const dllm_model* m, int32_t n_pages, int32_t page, size_t*
     return DLLM_OK;
 }
 
-int dllm_batch_step(dllm_model* m, void* d_pages, size_t bytes, const dllm_batch_rows* b, const int32_t* d_tok,
-                    const uint8_t* d_mask, const dllm_select_args* sel, int32_t* d_out_id, float* d_out_conf,
-                    dllm_stream stream) {
+static int batch_step(dllm_model* m, void* d_pages, size_t bytes, const dllm_batch_rows* b, const uint32_t* d_tree,
+                      int32_t tree_ld, const int32_t* d_tok, const uint8_t* d_mask, const dllm_select_args* sel,
+                      int32_t* d_out_id, float* d_out_conf, dllm_stream stream) {
     if (!m || !d_pages || !b || !d_tok) return fail(DLLM_E_INVAL, "NULL argument");
     size_t need = 0;
     int rc = dllm_batch_bytes(m, b->n_pages, b->page, &need);
@@ -1270,9 +1272,24 @@ int dllm_batch_step(dllm_model* m, void* d_pages, size_t bytes, const dllm_batch
     FwdArgs a{};
     a.M = b->n_rows; a.tok = d_tok; a.mask = d_mask; a.pos = b->d_pos; a.n_layers = m->cfg.n_layers;
     a.lm = d_out_id != nullptr; a.out_id = d_out_id; a.out_conf = d_out_conf; a.batch = b; a.pages = d_pages;
+    a.tree = d_tree; a.tree_ld = tree_ld;
     if (sel) a.logits = (float*)sa.d_logits;
     if ((rc = forward(m, nullptr, a, (hipStream_t)stream))) return rc;
     return sel ? dllm_select(&sa, stream) : DLLM_OK;
+}
+
+int dllm_batch_step(dllm_model* m, void* d_pages, size_t bytes, const dllm_batch_rows* rows, const int32_t* d_tok,
+                    const uint8_t* d_mask, const dllm_select_args* sel, int32_t* d_out_id, float* d_out_conf,
+                    dllm_stream stream) {
+    return batch_step(m, d_pages, bytes, rows, nullptr, 0, d_tok, d_mask, sel, d_out_id, d_out_conf, stream);
+}
+
+int dllm_batch_step_tree(dllm_model* m, void* d_pages, size_t bytes, const dllm_batch_rows* rows, const uint32_t* d_tree,
+                         int32_t tree_ld, const int32_t* d_tok, const uint8_t* d_mask, const dllm_select_args* sel,
+                         int32_t* d_out_id, float* d_out_conf, dllm_stream stream) {
+    if (!d_tree || ((uintptr_t)d_tree & 3) != 0) return fail(DLLM_E_INVAL, "tree: NULL or not 4-byte aligned");
+    if (tree_ld < 1 || tree_ld > (1 << 24)) return fail(DLLM_E_INVAL, "tree_ld must be in [1, 2^24]");
+    return batch_step(m, d_pages, bytes, rows, d_tree, tree_ld, d_tok, d_mask, sel, d_out_id, d_out_conf, stream);
 }
 
 static int cs_of(int capacity) { return (int)round_up(capacity, 32); }

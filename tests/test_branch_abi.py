@@ -1,0 +1,124 @@
+"""Refusals of the branching operators on the host, and the launch rules of their kernels (no GPU here)."""
+import ctypes
+
+import pytest
+
+from test_batch_abi import ATTN, P, dl, fill  # noqa: F401
+from test_batch_rules import run_cpp
+
+TREE = dict(d_parent=P, d_row0=P, d_len=P, n_rows=8, n_seqs=2, d_pos=2 * P, d_mask=P, mask_ld=1)
+
+
+@pytest.mark.parametrize("change", [dict(d_parent=None), dict(d_mask=None), dict(d_pos=P + 2), dict(d_pos=P), dict(n_rows=-1),
+                                    dict(n_rows=(1 << 24) + 1), dict(n_seqs=0), dict(n_seqs=4097), dict(mask_ld=0), dict(mask_ld=33)])
+def test_tree_plan_refusals(dl, change):  # noqa: F811
+    a = dict(TREE, **change)
+    assert dl.lib().dllm_tree_plan(*a.values(), None) == dl.DLLM_E_INVAL and dl.lib().dllm_last_error()
+
+
+@pytest.mark.parametrize("change,mask,ld,code", [
+    ({}, None, 1, -1), ({}, P + 2, 1, -1), ({}, P, 0, -1), ({}, P, (1 << 24) + 1, -1), (dict(dtype=3), P, 1, -3),
+    (dict(head_dim=96), P, 1, -3), (dict(d_q=None), P, 1, -1), (dict(max_len=129), P, 1, -1), (dict(ld_out=258), P, 1, -1)])
+def test_attention_tree_refusals(dl, change, mask, ld, code):  # noqa: F811
+    a = fill(dl.dllm_attn_args, **dict(ATTN, **change))
+    assert dl.lib().dllm_attention_tree(ctypes.byref(a), mask, ld, None) == code and dl.lib().dllm_last_error()
+    assert dl.lib().dllm_attention_tree(None, P, 1, None) == dl.DLLM_E_INVAL
+
+
+def test_batch_step_tree_refusals(dl):  # noqa: F811
+    for tree, ld in ((None, 1), (P + 1, 1), (P, 0), (P, 1)):           # (the last: no model)
+        assert dl.lib().dllm_batch_step_tree(None, P, 1 << 20, None, tree, ld, P, None, None, None, None, None) == dl.DLLM_E_INVAL
+
+
+LOGP = dict(dtype=0, n_rows=4, vocab=5000, mask_id=99, n_tok=3, top=2, d_logits=P, ld=5000, d_tok=P, d_tok_row=P, d_logp=P,
+            d_entropy=P, d_top_id=P, d_top_logp=P, d_ws=P, ws_bytes=1 << 40)
+
+
+@pytest.mark.parametrize("change,code", [
+    (dict(dtype=2), -3), (dict(n_rows=-1), -1), (dict(vocab=0), -1), (dict(vocab=(1 << 24) + 1), -1), (dict(mask_id=-2), -1),
+    (dict(mask_id=5000), -1), (dict(top=-1), -1), (dict(top=65), -1), (dict(n_tok=-1), -1), (dict(n_tok=(1 << 24) + 1), -1),
+    (dict(d_logits=None), -1), (dict(d_tok=None), -1), (dict(d_logp=None), -1), (dict(d_tok_row=None, n_tok=5), -1),
+    (dict(d_top_id=None), -1), (dict(d_top_logp=None), -1), (dict(ld=4999), -1), (dict(d_logits=P + 2), -1), (dict(d_tok=P + 1), -1),
+    (dict(d_entropy=P + 2), -1), (dict(n_rows=0), -1)])
+def test_logprobs_refusals(dl, change, code):  # noqa: F811
+    a = fill(dl.dllm_logprobs_args, **dict(LOGP, **change))
+    assert dl.lib().dllm_logprobs(ctypes.byref(a), None) == code and dl.lib().dllm_last_error()
+    assert dl.lib().dllm_logprobs(None, None) == dl.DLLM_E_INVAL
+
+
+def test_workspaces_are_checked(dl):  # noqa: F811
+    L, n = dl.lib(), ctypes.c_size_t()
+    assert L.dllm_logprobs_ws(None, ctypes.byref(n)) == dl.DLLM_E_INVAL
+    a = fill(dl.dllm_logprobs_args, **dict(LOGP, vocab=50000, ld=50000, d_ws=None, ws_bytes=0))
+    assert L.dllm_logprobs_ws(ctypes.byref(a), None) == dl.DLLM_E_INVAL
+    assert L.dllm_logprobs_ws(ctypes.byref(a), ctypes.byref(n)) == 0 and n.value > 0
+    assert L.dllm_logprobs(ctypes.byref(a), None) == dl.DLLM_E_INVAL
+    a.d_ws, a.ws_bytes = P, n.value - 1
+    assert L.dllm_logprobs(ctypes.byref(a), None) == dl.DLLM_E_CAPACITY
+    a.d_ws, a.ws_bytes = P + 8, n.value
+    assert L.dllm_logprobs(ctypes.byref(a), None) == dl.DLLM_E_INVAL
+    assert L.dllm_batch_fork_ws(0, 8, ctypes.byref(n)) == dl.DLLM_E_INVAL
+    assert L.dllm_batch_fork_ws(4, 0, ctypes.byref(n)) == dl.DLLM_E_INVAL
+    assert L.dllm_batch_fork_ws(4, 8, None) == dl.DLLM_E_INVAL
+    assert L.dllm_batch_fork_ws(FORK["n_seqs"], CACHE["n_pages"], ctypes.byref(n)) == 0 and n.value > 0
+    c, f = fill(dl.dllm_cache, **CACHE), fill(dl.dllm_fork_args, **dict(FORK, ws_bytes=n.value - 1))
+    assert L.dllm_batch_fork(ctypes.byref(c), ctypes.byref(f), None) == dl.DLLM_E_CAPACITY
+
+
+CACHE = dict(dtype=4, n_layers=2, n_kv_heads=2, head_dim=64, page=32, n_pages=8, d_pages=P)
+BAD_CACHE = [(dict(dtype=2), -3), (dict(n_layers=0), -1), (dict(n_layers=4097), -1), (dict(n_kv_heads=0), -1), (dict(n_kv_heads=1025), -1),
+             (dict(head_dim=48), -3), (dict(page=16), -1), (dict(n_pages=0), -1), (dict(n_pages=1 << 26), -1), (dict(d_pages=None), -1),
+             (dict(d_pages=P + 8), -1)]
+COMPACT = dict(d_table=P, table_ld=4, d_base=P, d_path=P, path_ld=8, d_n=P, n_seqs=3)
+
+
+@pytest.mark.parametrize("change,code", BAD_CACHE)
+def test_cache_refusals(dl, change, code):  # noqa: F811
+    c, f = fill(dl.dllm_cache, **dict(CACHE, **change)), fill(dl.dllm_fork_args, **FORK)
+    assert dl.lib().dllm_cache_compact(ctypes.byref(c), *COMPACT.values(), None) == code and dl.lib().dllm_last_error()
+    assert dl.lib().dllm_batch_fork(ctypes.byref(c), ctypes.byref(f), None) == code
+
+
+@pytest.mark.parametrize("change", [dict(d_table=None), dict(d_n=None), dict(d_base=P + 2), dict(table_ld=0), dict(table_ld=(1 << 18) + 1),
+                                    dict(path_ld=0), dict(path_ld=1025), dict(n_seqs=0), dict(n_seqs=4097)])
+def test_compact_refusals(dl, change):  # noqa: F811
+    c, a = fill(dl.dllm_cache, **CACHE), dict(COMPACT, **change)
+    assert dl.lib().dllm_cache_compact(ctypes.byref(c), *a.values(), None) == dl.DLLM_E_INVAL
+    assert dl.lib().dllm_cache_compact(None, *COMPACT.values(), None) == dl.DLLM_E_INVAL
+
+
+FORK = dict(n_seqs=3, table_ld=4, shared_pages=1, d_src=P, d_keep=P, d_owned=P, d_owned_out=2 * P, d_table=P, d_table_out=2 * P,
+            d_free=P, d_n_free=P, d_n_free_out=2 * P, d_status=P, d_ws=P, ws_bytes=1 << 40)
+
+
+@pytest.mark.parametrize("change", [
+    dict(n_seqs=0), dict(n_seqs=4097), dict(table_ld=0), dict(table_ld=(1 << 18) + 1), dict(shared_pages=-1), dict(shared_pages=5),
+    dict(d_src=None), dict(d_status=None), dict(d_keep=P + 2), dict(d_owned_out=P), dict(d_table_out=P), dict(d_n_free_out=P),
+    dict(d_ws=None), dict(d_ws=P + 8)])
+def test_fork_refusals(dl, change):  # noqa: F811
+    c, f = fill(dl.dllm_cache, **CACHE), fill(dl.dllm_fork_args, **dict(FORK, **change))
+    assert dl.lib().dllm_batch_fork(ctypes.byref(c), ctypes.byref(f), None) == dl.DLLM_E_INVAL and dl.lib().dllm_last_error()
+    assert dl.lib().dllm_batch_fork(ctypes.byref(c), None, None) == dl.DLLM_E_INVAL
+
+
+def test_rules_of_the_branching_operators(tmp_path):
+    """Parts of a row: every block in exactly one, none empty, whole rounds of a workgroup's waves; LDS within a CU's 160 KB."""
+    out = run_cpp(tmp_path, r"""
+int main() {
+    long n = 0;
+    for (int T : {0, 1, 2, 7, 32, 256, 1024, 1025, 4096, 1 << 24})
+        for (int V : {1, 2, 2047, 2048, 2049, 8192, 8193, 126464, 152064, 1 << 24}) {
+            const int blocks = (V + LP_BLOCK - 1) / LP_BLOCK, per = lp_per(T, V), parts = lp_parts(T, V);
+            if (per < 1 || per % (LP_NT / 64) || (long)parts * per < blocks || (long)(parts - 1) * per >= blocks) return 1;
+            if (T >= 4 * N_CU && parts != 1) return 2;
+            if (lp_ws_bytes(T, V, 64) != (parts == 1 ? 0 : (size_t)T * parts * 528)) return 3;
+            ++n;
+        }
+    for (int ld = 1; ld <= TREE_MAX_LD; ++ld)
+        if (tree_lds_bytes(ld) > 160 * 1024 || tree_lds_bytes(ld) != (size_t)(32 * ld) * ld * 4 + 3 * 128 * ld) return 4;
+    if ((size_t)FORK_LDS_PAGES * 4 + 2 * 4 * DLLM_MAX_SEQS + 1024 > 160 * 1024) return 5;
+    if (fork_ws_bytes(3, FORK_LDS_PAGES) != 64 || fork_ws_bytes(3, FORK_LDS_PAGES + 1) != 64 + 4 * (FORK_LDS_PAGES + 1)) return 6;
+    std::printf("%ld", n);
+}
+""")
+    assert out == "100"

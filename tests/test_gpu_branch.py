@@ -1,0 +1,560 @@
+"""The branching operators against plain 64-bit implementations: sizes, masks, paths and strides where they can go wrong."""
+import numpy as np
+import pytest
+
+from batch_util import rounded, tdtype, to_gpu
+from branch_util import ancestors, compact, fork, logprobs, tree_attention, trees, words
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def dl():
+    import paper_2606_13740_amd as pkg
+    return pkg
+
+
+def i32(a):
+    return to_gpu(np.asarray(a, dtype=np.int32))
+
+
+def starts(rows, first=0):
+    return np.concatenate([[first], first + np.cumsum(rows)])
+
+
+# ---------------------------------------------------------------------------- tree plan
+
+
+def check_tree(dl, parents, ld, first=0, behind=3, lens=None):
+    import torch
+    rows = [len(p) for p in parents]
+    row0, T = starts(rows, first), first + sum(rows) + behind
+    lens = [n + 7 * b for b, n in enumerate(rows)] if lens is None else lens
+    par = np.full(T, 5)
+    for b, p in enumerate(parents):
+        par[row0[b]:row0[b + 1]] = p
+    pos = torch.full((T,), -77, dtype=torch.int32, device="cuda")
+    mask = torch.full((T, ld), 0x55, dtype=torch.int32, device="cuda")
+    dl.dllm_tree_plan(i32(par), i32(row0), i32(lens), pos, mask)
+    want_p, want_m = np.full(T, -77), np.full((T, ld), 0x55)
+    for b, p in enumerate(parents):
+        sets = ancestors(p)[:32 * ld]
+        a = row0[b]
+        want_m[a:a + len(sets)] = words(sets, ld)
+        want_p[a:a + len(sets)] = [lens[b] - rows[b] + len(s) - 1 for s in sets]
+    assert np.array_equal(mask.cpu().numpy(), want_m)
+    assert np.array_equal(pos.cpu().numpy(), want_p)
+
+
+@pytest.mark.parametrize("rows,ld", [([1], 1), ([0, 5, 0, 32], 1), ([33, 1, 64], 2), ([100, 7], 4), ([31, 65, 0, 96, 3], 3),
+                                     ([1024, 1, 500], 32), ([700], 23), ([3] * 300, 1)])
+def test_tree_plan(dl, rows, ld):
+    rng = np.random.default_rng(sum(rows) + ld)
+    check_tree(dl, trees(rng, rows), ld, first=2)
+    check_tree(dl, trees(rng, rows, back=2000, roots=0.02), ld)
+
+
+@pytest.mark.parametrize("n", [1, 31, 32, 33, 64, 65, 1000, 1024])
+def test_tree_plan_chains_and_stars(dl, n):
+    ld = -(-n // 32)
+    check_tree(dl, [list(range(-1, n - 1)), [-1] * n, [-1] + [0] * (n - 1)], ld)
+
+
+def test_tree_plan_bad_parents_and_rows_past_the_mask(dl):
+    p = [-1, 1, 5, -9, 2 ** 31 - 1, -2 ** 31, 4, 3, 8]        # themselves, later ones, far ones: the text
+    check_tree(dl, [p], 1)
+    rng = np.random.default_rng(0)
+    check_tree(dl, trees(rng, [50, 90, 20]), 1)               # the rows from 32 on stay as they were
+    check_tree(dl, trees(rng, [70]), 2, lens=[0])             # (fewer positions than rows)
+
+
+# ---------------------------------------------------------------------------- attention
+
+
+def attn_case(rng, dtype, rows, cached, H, Hk, D, page, shared, behind=2, first=0):
+    B = len(rows)
+    lens = np.array([c + n for c, n in zip(cached, rows)])
+    sp = shared // page
+    counts = [max(sp, -(-int(n) // page)) for n in lens]
+    n_pages = sp + sum(c - sp for c in counts) + 2
+    perm, ld, at = rng.permutation(n_pages), max(counts) + 2, sp
+    table = np.full((B, ld), -1)
+    for b, c in enumerate(counts):
+        table[b, :sp] = perm[:sp]
+        table[b, sp:c] = perm[at:at + c - sp]
+        at += c - sp
+    row0 = starts(rows, first)
+    T = int(row0[-1]) + behind
+    q, qt = rounded(rng, (T, H, D), dtype, 2.0)
+    k, kt = rounded(rng, (n_pages, Hk, page, D), dtype)
+    v, vt = rounded(rng, (n_pages, Hk, D, page), dtype)
+    return dict(dtype=dtype, rows=rows, lens=lens, table=table, row0=row0, q=qt, k=kt, v=vt, shared=shared, page=page, T=T)
+
+
+def run_tree(dl, c, mask, lim=None, scale=None, q=None, max_rows=None, **kw):
+    import torch
+    out = torch.full(c["q"].shape, 77.0, dtype=c["q"].dtype, device="cuda")
+    dl.dllm_attention_tree(c["q"] if q is None else q, c["k"], c["v"], i32(c["table"]), i32(c["row0"]), i32(c["lens"]), mask, out,
+                           max_rows or max(c["rows"]), int(max(c["lens"])), shared_len=c["shared"],
+                           lim=None if lim is None else i32(lim), scale=scale, **kw)
+    return out
+
+
+def check_out(c, out, seen, lim=None, scale=None):
+    """out against the formula; rows of no sequence as they were."""
+    import torch
+    D = c["q"].shape[2]
+    scale = D ** -0.5 if scale is None else scale
+    got, done = out.double(), torch.zeros(c["T"], dtype=torch.bool, device="cuda")
+    for rows, want, bound in tree_attention(c["q"].double(), c["k"].double(), c["v"].double(), c["table"], c["row0"], c["lens"], lim, seen,
+                                            c["shared"], c["page"], scale, c["dtype"]):
+        err = (got[rows] - want).abs()
+        assert (err <= bound).all(), (rows, err.max().item(), (err / bound.clamp(min=1e-30)).max().item())
+        done[rows] = True
+    assert got[~done].eq(77).all()
+
+
+def random_sets(rng, rows, row0, p=0.4):
+    """Any masks at all, not only trees': {row: set}."""
+    return {int(row0[b]) + i: set(np.flatnonzero(rng.random(n) < p).tolist()) for b, n in enumerate(rows) for i in range(n)}
+
+
+def sets_to_mask(c, seen, ld):
+    s = [set()] * c["T"]
+    for r, v in seen.items():
+        s[r] = v
+    return i32(words(s, ld))
+
+
+SHAPES = [([1], [0], 2, 1, 64, 32, 0), ([1, 1, 1], [5, 0, 300], 4, 2, 64, 32, 0), ([5, 0, 17], [40, 9, 0], 4, 4, 128, 64, 0),
+          ([24, 3, 11, 20], [500, 800, 31, 33], 4, 2, 64, 32, 0), ([40, 64, 33], [1000, 2, 130], 28, 4, 128, 64, 0),
+          ([7, 33, 64, 1], [900, 640, 700, 800], 8, 8, 64, 128, 640), ([100, 70], [300, 4000], 4, 1, 128, 256, 0),
+          ([130], [70], 7, 7, 64, 32, 0)]
+
+
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("shape", SHAPES)
+def test_attention_tree(dl, dtype, shape):
+    rows, cached, H, Hk, D, page, shared = shape
+    rng = np.random.default_rng(sum(rows) + H)
+    c = attn_case(rng, dtype, rows, cached, H, Hk, D, page, shared, first=1)
+    ld = -(-max(rows) // 32)
+    seen = {int(c["row0"][b]) + i: s for b, p in enumerate(trees(rng, rows)) for i, s in enumerate(ancestors(p))}
+    check_out(c, run_tree(dl, c, sets_to_mask(c, seen, ld)), seen)
+    seen = random_sets(rng, rows, c["row0"])
+    check_out(c, run_tree(dl, c, sets_to_mask(c, seen, ld + 2)), seen)
+
+
+@pytest.mark.parametrize("shape", [([5, 9], [90, 40], 3, 3, 32, 32, 32), ([40, 50], [70, 0], 4, 1, 32, 32, 0)])
+def test_attention_tree_small_heads_fp32(dl, shape):
+    test_attention_tree(dl, "f32", shape)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+def test_attention_tree_full_and_causal_masks_are_the_paged_attention(dl, dtype):
+    """A row that sees all rows, and one that sees those up to itself: dllm_attention_paged without and with limits, up to
+    the last bit (the same tiles, the same order)."""
+    import torch
+    rng = np.random.default_rng(8)
+    rows, cached = [33, 64, 5], [700, 31, 96]
+    c = attn_case(rng, dtype, rows, cached, 4, 2, 64, 32, 0)
+    T, row0 = c["T"], c["row0"]
+    for causal in (False, True):
+        seen = {int(row0[b]) + i: set(range(i + 1 if causal else n)) for b, n in enumerate(rows) for i in range(n)}
+        lim = np.zeros(T, int)
+        for b, n in enumerate(rows):
+            lim[row0[b]:row0[b + 1]] = cached[b] + (np.arange(n) + 1 if causal else n)
+        out, ref = run_tree(dl, c, sets_to_mask(c, seen, 2)), torch.full_like(c["q"], 77.0)
+        dl.dllm_attention_paged(c["q"], c["k"], c["v"], i32(c["table"]), i32(row0), i32(c["lens"]), ref, 64, int(max(c["lens"])), lim=i32(lim))
+        assert torch.equal(out, ref)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+def test_attention_tree_rows_that_see_nothing(dl, dtype):
+    rng = np.random.default_rng(2)
+    rows, cached = [40, 8, 3], [0, 0, 50]
+    c = attn_case(rng, dtype, rows, cached, 4, 2, 64, 32, 0)
+    seen = random_sets(rng, rows, c["row0"], 0.2)
+    for r in (0, 3, 39, 41, 48):
+        seen[r] = set()
+    out = run_tree(dl, c, sets_to_mask(c, seen, 2))
+    check_out(c, out, seen)
+    assert out[[0, 3, 39, 41]].eq(0).all() and not out[48].eq(0).all()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("shared", [0, 64])
+def test_attention_tree_limits_and_short_masks(dl, dtype, shared):
+    """Limits below, inside and past the rows; masks with fewer words than a sequence has rows."""
+    rng = np.random.default_rng(4)
+    rows, cached = [50, 70, 33], [100, 64, 70]
+    c = attn_case(rng, dtype, rows, cached, 4, 2, 64, 32, shared)
+    seen = random_sets(rng, rows, c["row0"])
+    lim = rng.integers(0, 200, c["T"])
+    lim[:4] = [0, 1, 100, 2 ** 31 - 1]
+    check_out(c, run_tree(dl, c, sets_to_mask(c, seen, 3), lim=lim), seen, lim=lim)
+    short = {r: {j for j in s if j < 32} for r, s in seen.items()}
+    check_out(c, run_tree(dl, c, sets_to_mask(c, seen, 1)), short)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+def test_attention_tree_rows_inside_the_shared_prefix(dl, dtype):
+    """A shared prefix that reaches into the rows of some sequences: their masks hold there too (the sharing is the caller's)."""
+    rng = np.random.default_rng(6)
+    H, Hk, D, page, shared = 8, 8, 128, 32, 1024
+    rows, cached = [40, 33, 7] + [9] * 9, [1000, 1010, 1100] + [1024] * 9
+    c = attn_case(rng, dtype, rows, cached, H, Hk, D, page, shared)
+    seen = random_sets(rng, rows, c["row0"])
+    check_out(c, run_tree(dl, c, sets_to_mask(c, seen, 2)), seen)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("shape", [([24, 3], [500, 30], 4, 2, 64, 32, 0), ([1, 2], [70, 3], 8, 2, 128, 64, 0), ([64], [33], 16, 2, 64, 64, 0)])
+def test_attention_tree_infinities_and_nans_where_no_row_looks(dl, dtype, shape):
+    """Keys and values that only some rows see, or none: what stands there reaches those rows alone."""
+    import torch
+    rows, cached, H, Hk, D, page, shared = shape
+    rng = np.random.default_rng(12)
+    c = attn_case(rng, dtype, rows, cached, H, Hk, D, page, shared)
+    seen = random_sets(rng, rows, c["row0"], 0.6)
+    for b, n in enumerate(rows):
+        for i in range(n):
+            seen[int(c["row0"][b]) + i].discard(n - 1)         # nobody sees a sequence's last row, all others their own
+            if n > 2:
+                (seen[int(c["row0"][b]) + i].add if i % 2 else seen[int(c["row0"][b]) + i].discard)(n - 2)
+    where = lambda b, p: (int(c["table"][b, p // page]), p % page)  # noqa: E731
+    clean = dict(c, k=c["k"].clone(), v=c["v"].clone())
+    for b, n in enumerate(rows):
+        pg, o = where(b, int(c["lens"][b]) - 1)
+        for t in (c["k"][pg, :, o], c["v"][pg, :, :, o]):
+            t[:, 0::3], t[:, 1::3], t[:, 2::3] = float("nan"), float("inf"), -float("inf")
+        for p in range(int(c["lens"][b]), -(-int(c["lens"][b]) // page) * page):      # and behind the sequence
+            pg, o = where(b, p)
+            c["k"][pg, :, o], c["v"][pg, :, :, o] = float("nan"), float("inf")
+    mask = sets_to_mask(c, seen, -(-max(rows) // 32))
+    check_out(clean, run_tree(dl, c, mask), seen)
+    # an infinite value in a row that half of the rows see: theirs is infinite, the others' stay
+    if rows[0] > 2:
+        pg, o = where(0, int(c["lens"][0]) - 2)
+        c["v"][pg, :, 3, o] = float("inf")
+        out, odd = run_tree(dl, c, mask), torch.arange(rows[0], device="cuda") % 2 == 1
+        a = out[:rows[0]]
+        assert a[odd][:, :, 3].eq(float("inf")).all() and torch.isfinite(a[~odd]).all()
+        assert torch.isfinite(a[odd][:, :, [0, 1, 2, 4, 5]]).all()
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+def test_attention_tree_large_tiles(dl, dtype):
+    """Rows and keys enough for the 32 x 32 tiles, own keys alone and with a shared prefix."""
+    rng = np.random.default_rng(3)
+    for rows, cached, shared in (([64, 61, 64, 50, 64, 64, 33, 64], [4090] * 7 + [3000], 0), ([64] * 10 + [7, 64], [8192 + 100] * 12, 8192)):
+        c = attn_case(rng, dtype, rows, cached, 28, 4, 128, 64, shared)
+        seen = random_sets(rng, rows, c["row0"], 0.3)
+        check_out(c, run_tree(dl, c, sets_to_mask(c, seen, 2)), seen)
+
+
+def test_attention_tree_strided_rows_scales_and_bounds(dl):
+    import torch
+    rng = np.random.default_rng(9)
+    rows, cached = [20, 33], [100, 7]
+    c = attn_case(rng, "f16", rows, cached, 4, 2, 64, 32, 0)
+    seen = random_sets(rng, rows, c["row0"])
+    mask = sets_to_mask(c, seen, 2)
+    wide = torch.zeros(c["T"], 4 * 64 + 24, dtype=torch.float16, device="cuda")
+    wide[:, 8:8 + 256] = c["q"].reshape(c["T"], 256)
+    view = wide[:, 8:8 + 256]
+    ref = run_tree(dl, c, mask)
+    assert torch.equal(run_tree(dl, c, mask, q=view), ref)
+    for scale in (0.0, -0.05, 0.3):
+        check_out(c, run_tree(dl, c, mask, scale=scale), seen, scale=scale)
+    # no bound on the rows known
+    assert (run_tree(dl, c, mask, max_rows=2 ** 31 - 1).float() - ref.float()).abs().max() < 0.02
+    # row bounds that are none: nothing is read or written out of range
+    for row0 in ([-5, 20, 2 ** 31 - 1], [0, -2 ** 31, 40], [2 ** 31 - 1, 3, 9], [30, 10, 50]):
+        for ln in ([120, 40], [-2 ** 31, 2 ** 31 - 1], [0, -1]):
+            out = torch.zeros_like(c["q"])
+            dl.dllm_attention_tree(c["q"], c["k"], c["v"], i32(c["table"]), i32(row0), i32(ln), mask, out, 33, 120)
+    torch.cuda.synchronize()
+
+
+# ---------------------------------------------------------------------------- log probabilities
+
+
+def check_logprobs(dl, x, dtype, mask_id=-1, tok=None, tok_row=None, top=0, entropy=True, ld=None):
+    """x: [T, V] tensor on the CPU of the type."""
+    import torch
+    T, V = x.shape
+    ld = V if ld is None else ld
+    wide = torch.zeros(T, ld, dtype=x.dtype)
+    wide[:, :V] = x
+    g = wide.cuda()[:, :V]
+    z = lambda *s: torch.full(s, 77.0, device="cuda")  # noqa: E731
+    lp = None if tok is None else z(len(tok))
+    ent = z(T) if entropy else None
+    ids = torch.full((T, top), -77, dtype=torch.int32, device="cuda") if top else None
+    tl = z(T, top) if top else None
+    dl.dllm_logprobs(g, None if tok is None else i32(tok), None if tok_row is None else i32(tok_row), lp, ent, ids, tl, mask_id)
+    want = logprobs(x.double().numpy(), mask_id, tok, tok_row, top)
+    close = lambda got, ref, bound: np.array_equal(np.isneginf(got), np.isneginf(ref)) and (  # noqa: E731
+        abs(np.where(np.isneginf(ref), 0, got - np.where(np.isneginf(ref), 0, ref))) <= bound).all()
+    with np.errstate(invalid="ignore"):
+        if top:
+            assert np.array_equal(ids.cpu().numpy(), want[2])
+            assert close(tl.double().cpu().numpy(), want[3], want[6])
+        if tok is not None:
+            assert close(lp.double().cpu().numpy(), want[0], want[4])
+        if entropy:
+            got = ent.double().cpu().numpy()
+            assert np.isfinite(got).all() and (abs(got - want[1]) <= want[5]).all(), abs(got - want[1]).max()
+    return lp, ent, ids, tl
+
+
+def logits_of(rng, T, V, dtype, std=3.0):
+    import torch
+    x = torch.from_numpy(rng.normal(0, std, (T, V)).astype(np.float32))
+    for r in range(T):
+        x[r, rng.integers(0, V, 4)] += torch.from_numpy(rng.uniform(0, 16, 4).astype(np.float32))
+    return x.to(tdtype(dtype))
+
+
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("T,V,n,top", [(1, 1, 1, 1), (3, 5, 9, 8), (2, 64, 2, 64), (16, 1024, 15, 4), (5, 2047, 3, 1), (4, 2049, 40, 33),
+                                       (7, 8193, 0, 64), (300, 5000, 7, 20), (1, 126464, 1, 8), (33, 40001, 64, 20), (2, 152064, 5, 0)])
+def test_logprobs(dl, dtype, T, V, n, top):
+    rng = np.random.default_rng(T + V)
+    x = logits_of(rng, T, V, dtype)
+    tok, row = rng.integers(0, V, n), rng.integers(0, T, n)
+    check_logprobs(dl, x, dtype, mask_id=V // 2 if V > 1 else -1, tok=tok if n else None, tok_row=row if n else None, top=top, ld=V + 3)
+    if n:
+        k = min(n, T)
+        check_logprobs(dl, x, dtype, tok=tok[:k], top=min(top, 3), entropy=False)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+def test_logprobs_ties_go_to_the_lower_id(dl, dtype):
+    import torch
+    rng = np.random.default_rng(1)
+    V = 30011
+    x = torch.stack([torch.zeros(V), torch.from_numpy(rng.integers(0, 3, V).astype(np.float32)),
+                     torch.arange(V).float().div(4096).floor(), -torch.arange(V).float().div(4096).floor(),
+                     torch.where(torch.arange(V) % 7 == 0, 0.0, -0.0)]).to(tdtype(dtype))
+    for top in (1, 5, 64):
+        check_logprobs(dl, x, dtype, mask_id=3, top=top)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+def test_logprobs_sorted_logits(dl, dtype):
+    """Every logit larger than all before it, and the reverse."""
+    import torch
+    V = 50000
+    up = torch.linspace(-20, 30, V)
+    x = torch.stack([up, up.flip(0), up - 1000, up * 0.01]).to(tdtype(dtype))
+    check_logprobs(dl, x, dtype, top=64, tok=[V - 1, 0, 5, 7])
+
+
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("V", [40, 6000, 70001])
+def test_logprobs_infinities_nans_and_empty_rows(dl, dtype, V):
+    import torch
+    rng = np.random.default_rng(V)
+    x = logits_of(rng, 9, V, dtype)
+    inf, top = float("inf"), float(torch.finfo(tdtype(dtype)).max)
+    x[0, ::2], x[0, 1::3] = float("nan"), -inf
+    x[1] = -inf
+    x[2] = float("nan")
+    x[3], x[3, V // 2] = -inf, 1.5                     # one id left
+    x[4, 7], x[4, 9] = inf, inf                        # count as the largest float: a tie
+    x[5] = -top                                        # masks of the type's lowest value: a uniform row
+    x[6, : V - 1] = -top
+    x[7], x[7, V - 1] = -inf, 3.0                      # the only one is the MASK id
+    x[8, 1], x[8, 2] = top, -top
+    tok = np.tile([0, 1, 7, V // 2, V - 1, V, -1], 11)
+    row = np.repeat(np.arange(-1, 10), 7)
+    check_logprobs(dl, x, dtype, mask_id=V - 1, tok=tok, tok_row=row, top=6)
+
+
+def test_logprobs_far_logits_and_large_offsets(dl):
+    import torch
+    rng = np.random.default_rng(2)
+    x = torch.from_numpy(np.concatenate([rng.normal(0, 1, (1, 9000)) + 1e4, rng.normal(0, 1e30, (1, 9000)), rng.normal(0, 1, (1, 9000)) * 1e-30,
+                                         rng.normal(-3e38, 1e36, (1, 9000))]).astype(np.float32))
+    check_logprobs(dl, x, "f32", tok=[0, 1, 2, 3], top=10)
+
+
+# ---------------------------------------------------------------------------- moves in the cache
+
+
+def cache_of(rng, dtype, L, n_pages, Hk, D, page):
+    import torch
+    if dtype == "f32":
+        a = rng.integers(1, 1 << 20, (L, 2, n_pages, Hk, page * D)).astype(np.float32)
+        return a, torch.from_numpy(a).cuda()
+    a = rng.integers(1, 0x7BFF, (L, 2, n_pages, Hk, page * D)).astype(np.int16)
+    t = torch.from_numpy(a).cuda().view(torch.float16 if dtype == "f16" else torch.bfloat16)
+    return a, t
+
+
+def same(t, a):
+    import torch
+    return np.array_equal((t if t.dtype == torch.float32 else t.view(torch.int16)).cpu().numpy(), a)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("B,W,P,L,Hk,D,page", [(1, 1, 1, 1, 1, 32, 32), (2, 16, 5, 2, 2, 64, 32), (9, 64, 16, 3, 4, 128, 64), (3, 200, 150, 1, 1, 64, 128),
+                                               (5, 33, 33, 2, 1, 128, 256), (1, 1024, 1024, 1, 2, 32, 32)])
+def test_cache_compact(dl, dtype, B, W, P, L, Hk, D, page):
+    rng = np.random.default_rng(B + W)
+    ld = (2 * page + W) // page + 2
+    n_pages = B * ld + 1
+    table = rng.permutation(n_pages)[:B * ld].reshape(B, ld)
+    base = rng.integers(0, 2 * page, B)
+    n = rng.integers(0, min(P, W) + 1, B)
+    n[0] = min(P, W)
+    path = np.full((B, P), -3)
+    for b in range(B):
+        path[b, :n[b]] = np.sort(rng.permutation(W)[:n[b]])
+    if B > 2:
+        path[1, :n[1]] = np.arange(n[1])                          # already in place
+    a, t = cache_of(rng, dtype, L, n_pages, Hk, D, page)
+    dl.dllm_cache_compact(t, page, i32(table), i32(base), i32(path), i32(n))
+    assert same(t, compact(a, page, D, table, base, path, n))
+
+
+def test_cache_compact_what_ends_a_path_and_positions_without_a_page(dl):
+    rng = np.random.default_rng(5)
+    L, Hk, D, page, ld, B = 2, 2, 64, 32, 4, 9
+    n_pages = B * ld
+    table = rng.permutation(n_pages).reshape(B, ld)
+    table[4, 1], table[5, 2], table[6, 0] = -1, n_pages, 2 ** 31 - 1
+    base = np.array([5, 5, 5, 100, 20, 40, 20, -1, -2 ** 31])
+    path = np.array([[1, 3, 3, 9, 20, 21], [2, 9, 7, 30, 31, 32], [-1, 2, 3, 4, 5, 6], [1, 20, 27, 28, 29, 40], [3, 9, 30, 40, 41, 50],
+                     [2, 20, 23, 24, 25, 26], [3, 9, 14, 22, 23, 24], [1, 2, 3, 4, 5, 6], [1, 2, 3, 4, 5, 6]])
+    n = np.array([6, 6, 6, 6, 6, 9, 6, 6, 6])                     # (one past its entries)
+    a, t = cache_of(rng, "f16", L, n_pages, Hk, D, page)
+    dl.dllm_cache_compact(t, page, i32(table), i32(base), i32(path), i32(n))
+    want = compact(a, page, D, table, base, path, n)
+    assert same(t, want) and not np.array_equal(want, a)
+    n[:] = [-5, 0, 0, -2 ** 31, 0, 0, 0, 0, 0]
+    dl.dllm_cache_compact(t, page, i32(table), i32(base), i32(path), i32(n))
+    assert same(t, want)
+
+
+def fork_case(rng, B, ld, page, shared, spare, longest=None):
+    """A batch whose sequences share some whole pages, and which of them go on as what."""
+    sp = min(shared, ld)
+    longest = ld * page if longest is None else longest
+    lens, held, n_pages = [], [], sp
+    for b in range(B):
+        n = int(rng.integers(0, longest + 1)) if rng.random() < 0.9 else int(rng.integers(0, ld + 1)) * page
+        n = max(min(n, ld * page), sp * page)
+        need, h = -(-n // page), list(range(sp))
+        if b and rng.random() < 0.4:
+            h += held[b - 1][sp:min(n, lens[b - 1]) // page]
+        h += range(n_pages, n_pages + max(0, need - len(h)))
+        n_pages = max(n_pages, max(h, default=-1) + 1)
+        lens.append(n)
+        held.append(h[:need])
+    src = np.where(rng.random(B) < 0.5, np.arange(B), rng.integers(0, B, B))
+    keep = np.array([lens[s] if rng.random() < 0.7 else int(rng.integers(0, lens[s] + 1)) for s in src])
+    keep[rng.random(B) < 0.1] = 0
+    used, total = n_pages, n_pages + spare
+    perm = rng.permutation(total)
+    table = np.full((B, ld), -1)
+    for b in range(B):
+        table[b, :len(held[b])] = perm[held[b]]
+    free = np.full(total, -9)
+    free[:spare] = perm[used:]
+    return src, keep, np.array([len(h) for h in held]), table, free, spare, total
+
+
+def run_fork(dl, src, keep, owned, table, free, n_free, shared, page, t):
+    import torch
+    z = lambda n: torch.full((n,), 77, dtype=torch.int32, device="cuda")  # noqa: E731
+    o = dict(owned_out=z(len(src)), table_out=torch.full(table.shape, -6, dtype=torch.int32, device="cuda"), free=i32(free), n_free_out=z(1),
+             status=z(3))
+    tab = i32(table)
+    dl.dllm_batch_fork(i32(src), i32(keep), i32(owned), o["owned_out"], tab, o["table_out"], o["free"], i32([n_free]), o["n_free_out"], shared,
+                       t, page, o["status"])
+    torch.cuda.synchronize()
+    assert np.array_equal(tab.cpu().numpy(), table)
+    return {k: v.cpu().numpy() for k, v in o.items()}
+
+
+def check_fork(dl, src, keep, owned, table, free, n_free, shared, page, a, t, D):
+    got = run_fork(dl, src, keep, owned, table, free, n_free, shared, page, t)
+    want = fork(src, keep, owned, table, np.full(table.shape, -6), free, n_free, shared, page, a, D)
+    for k, v in want.items():
+        assert np.array_equal(got[k], v), (k, got[k], v)
+    assert same(t, a)
+    return want
+
+
+@pytest.mark.parametrize("dtype", ["f32", "f16"])
+@pytest.mark.parametrize("B,ld,page,shared,L,Hk,D", [(1, 3, 32, 0, 1, 1, 32), (2, 4, 64, 1, 2, 2, 64), (8, 7, 64, 2, 3, 2, 128), (64, 9, 32, 0, 1, 1, 64),
+                                                     (333, 5, 128, 1, 1, 1, 32), (40, 70, 32, 0, 1, 1, 32), (5, 2, 256, 0, 2, 1, 128)])
+def test_batch_fork(dl, dtype, B, ld, page, shared, L, Hk, D):
+    rng = np.random.default_rng(B + ld)
+    for _ in range(2):
+        src, keep, owned, table, free, n_free, n_pages = fork_case(rng, B, ld, page, shared, B + 3)
+        a, t = cache_of(rng, dtype, L, n_pages, Hk, D, page)
+        want = check_fork(dl, src, keep, owned, table, free, n_free, shared, page, a, t, D)
+        assert want["status"][2] == 0
+
+
+def test_batch_fork_many_sequences_and_pages_past_the_lds(dl):
+    rng = np.random.default_rng(7)
+    src, keep, owned, table, free, n_free, n_pages = fork_case(rng, 4096, 6, 32, 0, 4100, longest=190)
+    a, t = cache_of(rng, "f16", 1, n_pages, 1, 32, 32)
+    assert check_fork(dl, src, keep, owned, table, free, n_free, 0, 32, a, t, 32)["status"][2] == 0
+    src, keep, owned, table, free, n_free, n_pages = fork_case(rng, 50, 8, 32, 1, 40000)      # (marks in the workspace)
+    a, t = cache_of(rng, "f16", 1, n_pages, 1, 32, 32)
+    assert n_pages > 31 * 1024
+    assert check_fork(dl, src, keep, owned, table, free, n_free, 1, 32, a, t, 32)["status"][0] > 0
+
+
+def test_batch_fork_takes_pages_that_the_same_call_gives_back(dl):
+    rng = np.random.default_rng(3)
+    table = np.array([[4, 0, -1], [2, 1, 3], [6, 5, -1]])
+    a, t = cache_of(rng, "f16", 2, 7, 2, 64, 32)
+    # sequence 1 ends and goes on as 0, and so does 2, whose pages also go: 1, 2, 3, 5 and 6 are free, of which two are copies
+    want = check_fork(dl, np.array([0, 0, 0]), np.array([40, 50, 64]), np.array([2, 3, 2]), table, np.full(7, -9), 0, 0, 32, a, t, 64)
+    assert want["status"].tolist() == [2, 0, 0] and want["n_free_out"][0] == 3
+    assert want["table_out"][:, 1].tolist() == [6, 5, 0] and want["free"][:3].tolist() == [1, 2, 3]
+
+
+@pytest.mark.parametrize("what", ["pages", "source", "negative source", "keep", "negative keep", "owned", "n_free", "last page"])
+def test_batch_fork_refused_as_a_whole(dl, what):
+    rng = np.random.default_rng(9)
+    table = np.array([[4, 0, -1], [2, 1, 3], [6, 5, -1]])
+    src, keep, owned, free, n_free = np.array([0, 0, 2]), np.array([40, 50, 64]), np.array([2, 3, 2]), np.full(9, -9), 2
+    free[:2] = [7, 8]
+    if what == "pages":
+        src, keep, n_free = np.array([1, 1, 1]), np.array([70, 71, 72]), 0
+        owned = np.array([0, 3, 0])
+    elif what == "source":
+        src[1] = 3
+    elif what == "negative source":
+        src[0] = -1
+    elif what == "keep":
+        keep[2] = 65
+    elif what == "negative keep":
+        keep[2] = -1
+    elif what == "owned":
+        owned[0] = 4
+    elif what == "n_free":
+        n_free = 10
+    else:
+        keep[0] = 2 ** 31 - 1
+    a, t = cache_of(rng, "f32", 1, 9, 1, 32, 32)
+    want = check_fork(dl, src, keep, owned, table, free, n_free, 0, 32, a, t, 32)
+    assert want["status"][2] == 1 and want["status"][1] == (2 if what == "pages" else 0)
+
+
+def test_batch_fork_entries_that_are_no_pages(dl):
+    rng = np.random.default_rng(11)
+    table = np.array([[4, -1, 5], [2 ** 31 - 1, 1, 3], [6, 9, -7]])
+    free = np.full(9, -9)
+    free[:3] = [7, 8, 0]
+    a, t = cache_of(rng, "f32", 1, 9, 1, 32, 32)
+    check_fork(dl, np.array([0, 0, 2]), np.array([40, 70, 64]), np.array([3, 3, 3]), table, free, 3, 0, 32, a, t, 32)
+    check_fork(dl, np.array([1, 1, 2]), np.array([70, 70, 70]), np.array([3, 3, 3]), table, free, 3, 0, 32, a, t, 32)
