@@ -693,10 +693,11 @@ int dllm_tree_plan(const int32_t* d_parent, const int32_t* d_row0, const int32_t
 /* dllm_attention_paged with a mask for every row: row r of sequence b sees the positions
  * before its sequence's rows, [0, d_len[b] - rows of b), and of the rows i behind them those whose
  * bit i % 32 of word i / 32 of d_mask[r] is set (rows past 32 * mask_ld: none), all of it
- * below its limit.  A row that sees nothing gets zeros.  Everything else, the workspace and the
- * refusals are dllm_attention_paged's (a shared prefix reaches into a sequence's rows only
+ * below its limit.  A row that sees nothing gets zeros.  Everything else and the refusals are
+ * dllm_attention_paged's, but for the workspace's size, dllm_attention_tree_ws() bytes (a shared prefix reaches into a sequence's rows only
  * if the caller says so: the masks then hold there too).  E_INVAL unless mask_ld is in [1,
- * 2^24] and d_mask 4-byte aligned. */
+ * 2^24], n_rows * mask_ld < 2^29 and d_mask 4-byte aligned. */
+int dllm_attention_tree_ws(const dllm_attn_args* args, size_t* bytes);
 int dllm_attention_tree(const dllm_attn_args* args, const uint32_t* d_mask, int32_t mask_ld, dllm_stream stream);
 
 /* dllm_batch_step with a mask for every row (dllm_tree_plan's d_mask; rows->d_pos its

@@ -156,6 +156,7 @@ _SIGNATURES = {
     "dllm_batch_bytes": ([_vp, _i32, _i32, ctypes.POINTER(_sz)], ctypes.c_int),
     "dllm_batch_step": ([_vp, _vp, _sz, _vp, _vp, _vp, _vp, _vp, _vp, _vp], ctypes.c_int),
     "dllm_tree_plan": ([_vp, _vp, _vp, _i32, _i32, _vp, _vp, _i32, _vp], ctypes.c_int),
+    "dllm_attention_tree_ws": ([_vp, ctypes.POINTER(_sz)], ctypes.c_int),
     "dllm_attention_tree": ([_vp, _vp, _i32, _vp], ctypes.c_int),
     "dllm_batch_step_tree": ([_vp, _vp, _sz, _vp, _vp, _i32, _vp, _vp, _vp, _vp, _vp, _vp], ctypes.c_int),
     "dllm_logprobs_ws": ([_vp, ctypes.POINTER(_sz)], ctypes.c_int),
@@ -571,7 +572,7 @@ def _attention(f, q, k_pages, v_pages, table, row0, length, out, max_rows, max_l
     except _NO_FIT:
         _refuse(f, _NO_FIT_MSG)
     L = lib()
-    a, keep = _workspace(L.dllm_attention_paged_ws, a, ws, stream, dev, f)
+    a, keep = _workspace(L.dllm_attention_paged_ws if mask is None else L.dllm_attention_tree_ws, a, ws, stream, dev, f)
     if mask is None:
         rc = L.dllm_attention_paged(a, _stream(stream, dev))
     else:

@@ -70,13 +70,67 @@ __device__ __forceinline__ int seq_base(const PagedArgs& a, int b) {
     const RowRange n = row_range(a.row0[b], a.row0[b + 1], a.T, a.T);
     return max(a.len[b], 0) - (n.end - n.begin);
 }
-// Word i of a row's mask; the cached positions before it count as set bits.
-__device__ __forceinline__ uint32_t mask_word(const uint32_t* words, int ld, int i) {
-    const uint32_t w = words[min(max(i, 0), ld - 1)];
-    return i < 0 ? 0xFFFFFFFFu : (i < ld ? w : 0u);
+// The 32 bits of a row's mask from bit t on, w0 and w1 what stands at the words t / 32 and behind it (as far as there are ld):
+// the cached positions before the mask count as set bits, what lies past it as none.
+__device__ __forceinline__ uint32_t mask_bits(uint32_t w0, uint32_t w1, int t, int ld) {
+    const int i = t >> 5;
+    w0 = i < 0 ? 0xFFFFFFFFu : (i < ld ? w0 : 0u);
+    w1 = i < -1 ? 0xFFFFFFFFu : (i + 1 < ld ? w1 : 0u);
+    return __builtin_amdgcn_alignbit(w1, w0, t & 31);
 }
-// The 32 bits from bit t on, of the words t / 32 and the one behind it.
-__device__ __forceinline__ uint32_t mask_bits(uint32_t w0, uint32_t w1, int t) { return __builtin_amdgcn_alignbit(w1, w0, t & 31); }
+
+// Item L of the sequences' own parts in a call with masks (b = -1: none), for tiles of tm virtual rows.  Sequences
+// differ in their rows, and items without any must not stand between the others: the dispatcher deals workgroups to the
+// shader engines in turn and waits for one that is full, so that short-lived ones leave CUs unevenly filled, and
+// workgroups that would all have fitted start when the first have ended (16 trees of up to 64 rows, 28 heads over 4,
+// behind 8192 + 3000, the shared part in three: 142 us, 108 so).  Where there is more than one tile a sequence, the tiles
+// that have rows are counted (a wave's scan over the sequences, for up to 256 of them) and dealt as if there were no
+// others, XCD x taking the x-th share of (head, split, sequence, tile), which is the same number for each.
+// Otherwise the groups (sequence, head, split) go to the XCDs in turn, first tiles first.
+struct TreeItem {
+    int b, tile, split, hk;
+};
+constexpr int TREE_SCAN = 256;
+__device__ __forceinline__ TreeItem tree_item(const PagedArgs& a, int tm, int L, int n_items) {
+    const int xcd = L & 7, k = L >> 3, lane = threadIdx.x & 63;
+    if (a.nt_o == 1 || a.B > TREE_SCAN) {
+        const int groups = (n_items >> 3) / a.nt_o, tile = k / groups, i1 = xcd + 8 * (k - tile * groups);
+        if (i1 >= a.B * a.Hk * a.ns_o) return TreeItem{-1, 0, 0, 0};
+        const int i2 = i1 / a.ns_o;
+        return TreeItem{i2 / a.Hk, tile, i1 % a.ns_o, i2 % a.Hk};
+    }
+    constexpr int PER = TREE_SCAN / 64;
+    int at[PER + 1], tiles[PER], sum = 0;
+#pragma unroll
+    for (int i = 0; i <= PER; ++i) at[i] = a.row0[min(PER * lane + i, a.B)];
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+        const RowRange n = row_range(at[i], at[i + 1], a.max_rows, a.T);
+        tiles[i] = PER * lane + i < a.B ? ((n.end - n.begin) * a.G + tm - 1) / tm : 0;
+        sum += tiles[i];
+    }
+    int inc = sum;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+        const int up = __shfl_up(inc, o);
+        inc += lane >= o ? up : 0;
+    }
+    const int R = __builtin_amdgcn_readlane(inc, 63), N = R * a.Hk * a.ns_o;      // (N <= n_items)
+    const int i = xcd * (N >> 3) + min(xcd, N & 7) + k;
+    if (k >= (N >> 3) + (xcd < (N & 7))) return TreeItem{-1, 0, 0, 0};
+    const int u = i / R, r = i - u * R;
+    const int ln = __builtin_ctzll(__builtin_amdgcn_ballot_w64(inc > r));
+    int tile = r - (__builtin_amdgcn_readlane(inc, ln) - __builtin_amdgcn_readlane(sum, ln)), b = PER * ln;
+#pragma unroll
+    for (int j = 0; j < PER - 1; ++j) {
+        const int n = __builtin_amdgcn_readlane(tiles[j], ln);
+        if (b == PER * ln + j && tile >= n) {
+            tile -= n;
+            ++b;
+        }
+    }
+    return TreeItem{b, tile, u % a.ns_o, u / a.ns_o};
+}
 
 // Element type: one product step of a 16 x 16 or 32 x 32 tile (with 16-bit types 32 or 16 deep).
 typedef float f32x16_t __attribute__((ext_vector_type(16)));
@@ -185,8 +239,10 @@ template <typename T> __device__ __forceinline__ void store_out4(const PagedArgs
 // behind 1564: 9.8 us and 4.8, 288 workgroups of three steps, each asked for when the one before has landed).
 //
 // TREE: a row sees the cached positions and, of its sequence's rows, those that its mask has.  Steps whose keys are all
-// cached run as without; in the others a lane takes the 32 bits of its row for a block from two words, which are
-// asked for beside the step's K/V one step ahead (a load waited for inside a step would wait for the staging behind it).
+// cached run as without; in the others a lane takes the 32 bits of its row for a block from two words, which come to LDS
+// beside the step's K/V (a load waited for inside a step would wait for the staging behind it).  What a lane needs for
+// that waits in LDS too: kept in registers, the 32 x 32 tiles spilled three, and a spill's reload waits for the staging
+// in every step.
 template <typename T, int DH, int QG, int RT, int KG, int SUB, bool TREE>
 __global__ void __launch_bounds__(QG * KG * 64)
 __attribute__((amdgpu_waves_per_eu(QG * KG * (160 * 1024 / (2 * SUB * 64 * DH * (int)sizeof(T))) >= 8 ? 2 : 1)))
@@ -215,6 +271,8 @@ attn_paged_kernel(PagedArgs a) {
     static_assert(KI * 1024 == KPLANE, "planes must be whole wave loads");
     static_assert(TM <= 256, "at most four virtual rows per lane");
     __shared__ __attribute__((aligned(1024))) char lds[2 * BUF];
+    __shared__ uint32_t words_s[TREE ? 2 * NW * (SW + 1) * 64 : 1];      // [step & 1][wave][word][lane]
+    __shared__ int lane_s[TREE ? NW * 3 * 64 : 1];                       // [wave]: limit, first masked key, mask row
 
     const int lane = threadIdx.x & 63, wave = NW == 1 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int qw = wave % QG, kw = wave / QG;  // row tile, and the step's blocks that are this wave's
@@ -228,11 +286,20 @@ attn_paged_kernel(PagedArgs a) {
     const int item = xcd * (n_items >> 3) + min(xcd, n_items & 7) + (L >> 3);
     int tile, split, hk, b, ks, ke, first, behind, most_rows, bps, part, base_own = 0;
     if (own) {
-        tile = item % a.nt_o;
-        const int i1 = item / a.nt_o, i2 = i1 / a.ns_o;
-        split = i1 % a.ns_o;
-        hk = i2 % a.Hk;
-        b = i2 / a.Hk;
+        if (TREE) {
+            const TreeItem it = tree_item(a, TM, L, n_items);
+            if (it.b < 0) return;
+            tile = it.tile;
+            split = it.split;
+            hk = it.hk;
+            b = it.b;
+        } else {
+            tile = item % a.nt_o;
+            const int i1 = item / a.nt_o, i2 = i1 / a.ns_o;
+            split = i1 % a.ns_o;
+            hk = i2 % a.Hk;
+            b = i2 / a.Hk;
+        }
         first = a.row0[b];
         behind = a.row0[b + 1];
         most_rows = a.max_rows;
@@ -357,7 +424,7 @@ attn_paged_kernel(PagedArgs a) {
     };
     u32x4_t qf[NC];
     int lim, low = 0;
-    const uint32_t* words = nullptr;
+    int* mine = lane_s + (TREE ? wave * 3 * 64 + lane : 0);
     {
         // rows past the last repeat it (the rescale below is decided over a tile's rows)
         const int f = min(f0 + RT * qw + r, nv - 1);
@@ -375,7 +442,9 @@ attn_paged_kernel(PagedArgs a) {
         lim = row_limit(f);
         if constexpr (TREE) {
             low = row_low(f);
-            words = a.mask + (size_t)row * a.mask_ld;
+            mine[0] = lim;
+            mine[64] = low;
+            mine[128] = row * a.mask_ld;               // (n_rows * mask_ld < 2^29)
         }
     }
     // The largest limit of the tile's rows ends its keys: what lies behind may be anything.  Keys from the
@@ -415,22 +484,16 @@ attn_paged_kernel(PagedArgs a) {
     for (int i = 0; i < RT; ++i) lim_w = min(lim_w, __builtin_amdgcn_readlane(lim_m, i));
 
     // the mask words of this wave's blocks of step t
-    uint32_t w0[SW], w1[SW];
     auto first_key = [&](int t) { return ks + 32 * (kb0 + SUB * t + kw * SW); };
+    auto words_of = [&](int t) { return words_s + ((t & 1) * NW + wave) * (SW + 1) * 64; };
     auto load_words = [&](int t) {
         if (first_key(t) + 32 * SW <= lim_w) return;
+        const int i = (first_key(t) - mine[64]) >> 5, at = mine[128];
 #pragma unroll
-        for (int w = 0; w < SW; ++w) {
-            const int i = (first_key(t) + 32 * w - low) >> 5;
-            w0[w] = mask_word(words, a.mask_ld, i);
-            w1[w] = mask_word(words, a.mask_ld, i + 1);
-        }
+        for (int w = 0; w <= SW; ++w)
+            buffer_to_lds4(a.mask, (at + min(max(i + w, 0), a.mask_ld - 1)) * 4, 0, (char*)(words_of(t) + 64 * w));
     };
-    if constexpr (TREE) {
-#pragma unroll
-        for (int w = 0; w < SW; ++w) w0[w] = w1[w] = 0xFFFFFFFFu;
-        load_words(0);
-    }
+    if (TREE && rounds > 0) load_words(0);
 
     float mrun = -INFINITY, lrun = 0.f;
     Acc oacc[ND];
@@ -448,9 +511,10 @@ attn_paged_kernel(PagedArgs a) {
         else return F32 ? 16 * (e >> 2) + 4 * g + (e & 3) : 8 * g + e;
     };
 
-    // no scalar load outstanding past here: the compiler does not see the waits in the loop's
-    // asm and would otherwise wait for all LDS reads at each use
-    __builtin_amdgcn_s_waitcnt(0xC07F);
+    // no load outstanding past here: the compiler does not see the waits in the loop's asm and would wait again at
+    // each use: for all LDS reads where a scalar load could be left, and, for Q's loads, in every step until the step's own
+    // staging has landed
+    __builtin_amdgcn_s_waitcnt(0x0070);
     uint64_t odd = 0;
     // a wave without rows of its own only stages
     const bool busy = f0 + RT * qw < nv;
@@ -462,15 +526,6 @@ attn_paged_kernel(PagedArgs a) {
         // This wave's loads of step t have landed; the barrier makes every wave's visible and frees the buffer
         // that round t - 1 read, for step t + 1.
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-        // (before the next loads go out, which a use of these words would else wait for)
-        uint32_t seen[SW];
-        if constexpr (TREE) {
-#pragma unroll
-            for (int w = 0; w < SW; ++w) {
-                seen[w] = mask_bits(w0[w], w1[w], k0w + 32 * w - low);
-                asm volatile("" : "+v"(seen[w]));
-            }
-        }
         if (!whole || k0 + 32 * SUB > lim_lo) {
 #pragma unroll
             for (int u = 0; u < SUB; ++u)
@@ -533,16 +588,23 @@ attn_paged_kernel(PagedArgs a) {
 #pragma unroll
             for (int e = 0; e < NS; ++e) sv[w][e] = s[w][e / NA][e % NA];
         if (k0w + 32 * SW > lim_w || !whole) {
+            if constexpr (TREE) {
+                const int end0 = mine[0], t0 = k0w - mine[64];
+                const uint32_t* words = words_of(t) + lane;
+                const bool masked = k0w + 32 * SW > lim_w;              // (else the words are not there)
 #pragma unroll
-            for (int w = 0; w < SW; ++w) {
-                const int end = (there >> (kw * SW + w)) & 1 ? lim : 0;
-                if constexpr (TREE) {
-                    const int n = end - (k0w + 32 * w);                 // keys of the block before the limit
-                    const uint32_t vis = (n >= 32 ? seen[w] : (n > 0 ? seen[w] & ((1u << n) - 1) : 0u)) >> key_of(0);
+                for (int w = 0; w < SW; ++w) {
+                    const int n = ((there >> (kw * SW + w)) & 1 ? end0 : 0) - (k0w + 32 * w);      // keys before the limit
+                    uint32_t vis = masked ? mask_bits(words[64 * w], words[64 * w + 64], t0 + 32 * w, a.mask_ld) : 0xFFFFFFFFu;
+                    vis = (n >= 32 ? vis : (n > 0 ? vis & ((1u << n) - 1) : 0u)) >> key_of(0);
 #pragma unroll
                     for (int e = 0; e < NS; ++e)
                         if (!(vis >> (key_of(e) - key_of(0)) & 1)) sv[w][e] = -INFINITY;
-                } else {
+                }
+            } else {
+#pragma unroll
+                for (int w = 0; w < SW; ++w) {
+                    const int end = (there >> (kw * SW + w)) & 1 ? lim : 0;
 #pragma unroll
                     for (int e = 0; e < NS; ++e)
                         if (k0w + 32 * w + key_of(e) >= end) sv[w][e] = -INFINITY;
@@ -623,9 +685,12 @@ attn_paged_kernel(PagedArgs a) {
             if ((KG > 1 && blk % SUB / SW != kw) || pg < 0 || pg >= a.n_pages) continue;
             const T* Vp = (const T*)a.vp + ((long)pg * a.Hk + hk) * page_elems + (k0 & ((1 << a.page_shift) - 1));
             uint32_t vis = 0xFFFFFFFFu;
+            int end = lim;
             if constexpr (TREE) {
-                const int t = k0 - low;
-                vis = mask_bits(mask_word(words, a.mask_ld, t >> 5), mask_word(words, a.mask_ld, (t >> 5) + 1), t);
+                const int t = k0 - mine[64], i = t >> 5;
+                const uint32_t* words = a.mask + mine[128];
+                vis = mask_bits(words[min(max(i, 0), a.mask_ld - 1)], words[min(max(i + 1, 0), a.mask_ld - 1)], t, a.mask_ld);
+                end = mine[0];
             }
 #pragma unroll
             for (int dt = 0; dt < ND; ++dt) {
@@ -637,7 +702,7 @@ attn_paged_kernel(PagedArgs a) {
                     const u32x4_t v = ldg16(Vp + ((long)(RT * dt + r) << a.page_shift) + (16 / ES) * (NG * u + g));
                     auto sees = [&](int e) {
                         const int o = key_of(16 / ES * u + e), key = k0 + o;
-                        return key >= kz && key < lim && (!TREE || (vis >> o & 1)) ? PagedClass<T>::one : 0u;
+                        return key >= kz && key < end && (!TREE || (vis >> o & 1)) ? PagedClass<T>::one : 0u;
                     };
                     u32x4_t seen;
 #pragma unroll

@@ -62,7 +62,7 @@ void launch_qk(const QkArgs& a, int Dh, hipStream_t s) {
 }
 
 // Every check of an attention call's sizes.
-int check_attn(const dllm_attn_args* g, int& shift) {
+int check_attn(const dllm_attn_args* g, int& shift, bool tree) {
     if (!g) return fail(DLLM_E_INVAL, "args is NULL");
     if (int rc = check_dtype(g->dtype)) return rc;
     if (int rc = check_heads(g->n_heads, g->n_kv_heads, g->head_dim)) return rc;
@@ -80,7 +80,7 @@ int check_attn(const dllm_attn_args* g, int& shift) {
     if (!std::isfinite(g->scale)) return fail(DLLM_E_INVAL, "scale must be finite");
     if ((long)g->n_rows * (g->n_heads / g->n_kv_heads) >= (1l << 31))
         return fail(DLLM_E_INVAL, "n_rows times the query heads of a K/V head must be < 2^31");
-    const AttnPlan p = attn_plan(g);
+    const AttnPlan p = attn_plan(g, tree);
     if (!grid_ok(p.wgs_s + p.wgs_o, 256) || !grid_ok((long)g->n_rows * g->n_heads, g->head_dim / 4))
         return fail(DLLM_E_INVAL, "n_seqs, max_rows and n_rows need too many workgroups");
     return DLLM_OK;
@@ -161,9 +161,17 @@ int select_check(const dllm_select_args* g) {
     return DLLM_OK;
 }
 
+int attention_ws(const dllm_attn_args* g, bool tree, size_t* bytes) {
+    if (!bytes) return fail(DLLM_E_INVAL, "bytes is NULL");
+    int shift = 0;
+    if (int rc = check_attn(g, shift, tree)) return rc;
+    *bytes = attn_ws_bytes(g, attn_plan(g, tree));
+    return DLLM_OK;
+}
+
 int attention_paged(const dllm_attn_args* g, const uint32_t* d_mask, int mask_ld, bool out_f32, hipStream_t s) {
     int shift = 0;
-    if (int rc = check_attn(g, shift)) return rc;
+    if (int rc = check_attn(g, shift, d_mask != nullptr)) return rc;
     if (!g->d_q || !g->d_k_pages || !g->d_v_pages || !g->d_table || !g->d_row0 || !g->d_len || !g->d_out)
         return fail(DLLM_E_INVAL, "NULL argument");
     const int es = esize(g->dtype);
@@ -174,7 +182,7 @@ int attention_paged(const dllm_attn_args* g, const uint32_t* d_mask, int mask_ld
         !aligned(g->d_len, 4) || !aligned(g->d_lim, 4))
         return fail(DLLM_E_INVAL, "pages must be 16-byte aligned, integer arrays 4-byte");
     if (g->n_rows == 0) return DLLM_OK;
-    const AttnPlan p = attn_plan(g);
+    const AttnPlan p = attn_plan(g, d_mask != nullptr);
     const size_t need = attn_ws_bytes(g, p);
     if (need > 0 && (!g->d_ws || !aligned(g->d_ws, 16))) return fail(DLLM_E_INVAL, "workspace: NULL or not 16-byte aligned");
     if (need > g->ws_bytes)
@@ -243,13 +251,7 @@ int dllm_qk_norm_rope(const dllm_qk_args* g, dllm_stream stream) {
     return DLLM_OK;
 }
 
-int dllm_attention_paged_ws(const dllm_attn_args* g, size_t* bytes) {
-    if (!bytes) return fail(DLLM_E_INVAL, "bytes is NULL");
-    int shift = 0;
-    if (int rc = check_attn(g, shift)) return rc;
-    *bytes = attn_ws_bytes(g, attn_plan(g));
-    return DLLM_OK;
-}
+int dllm_attention_paged_ws(const dllm_attn_args* g, size_t* bytes) { return attention_ws(g, false, bytes); }
 
 int dllm_attention_paged(const dllm_attn_args* g, dllm_stream stream) { return attention_paged(g, nullptr, 0, false, (hipStream_t)stream); }
 

@@ -71,7 +71,10 @@ constexpr int ATTN_SLOTS = 512;
 //    round takes them, rounded towards fewer workgroups: 16 x 64 behind 16384 in 4 splits (448 workgroups) 150, 3 174,
 //    5 190; 8 x 32 of 32 heads behind 4096 in 3 splits 50, 2 62, 4 54; and at least four (two for tiles of 16 rows
 //    and in fp32), since a split is written and merged: 4 x 8 behind 2048 in 8 splits of 4 steps 16.2, in 16 of 2 19.0.
-inline AttnPlan attn_plan(const dllm_attn_args* g) {
+//
+// With masks (tree) the rows of a sequence are drafts, of which some sequences have many and some few or none: max_rows
+// makes nt_o tiles for each, n_rows says how many of them can have rows.
+inline AttnPlan attn_plan(const dllm_attn_args* g, bool tree = false) {
     const int G = g->n_heads / g->n_kv_heads, es = esize(g->dtype), step = es == 4 ? 32 : 64;
     AttnPlan p{};
     p.shared = std::min(g->shared_len, g->max_len);
@@ -89,7 +92,7 @@ inline AttnPlan attn_plan(const dllm_attn_args* g) {
     p.nt_s = ceil_div(rows_s, tm);
     p.nt_o = std::max(1, ceil_div(rows_o, tm));
     // (rows behind the last sequence make no work: rows_s / tm, not rounded up)
-    const double wgs_s = p.shared > 0 ? g->n_kv_heads * std::max(1.0, (double)rows_s / tm) : 0, wgs_o = (double)units_o * p.nt_o;
+    const double wgs_s = p.shared > 0 ? g->n_kv_heads * std::max(1.0, (double)rows_s / tm) : 0, wgs_o = tree ? g->n_kv_heads * std::min((double)g->n_seqs * p.nt_o, (double)rows_s / tm + 0.5 * g->n_seqs) : (double)units_o * p.nt_o;
     const double per = std::max((wgs_s * (steps_s + 2) + wgs_o * (steps_o + 2)) / ATTN_SLOTS, tm <= 16 || es == 4 ? 2.0 : 4.0);
     auto splits = [&](int steps) {
         const int ns = std::min(MAX_ATTN_SPLITS, std::max(1, (int)(steps / per + 0.25)));
@@ -98,7 +101,9 @@ inline AttnPlan attn_plan(const dllm_attn_args* g) {
     if (p.shared > 0) p.ns_s = splits(steps_s);
     p.ns_o = splits(steps_o);
     p.wgs_s = p.shared > 0 ? (long)g->n_kv_heads * p.nt_s * p.ns_s : 0;
-    p.wgs_o = units_o * p.nt_o * p.ns_o;
+    p.wgs_o = units_o * p.ns_o;
+    if (tree) p.wgs_o = (p.wgs_o + 7) / 8 * 8;                 // (dealt to the XCDs one by one)
+    p.wgs_o *= p.nt_o;
     return p;
 }
 

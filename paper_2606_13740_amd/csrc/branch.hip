@@ -100,8 +100,11 @@ int dllm_tree_plan(const int32_t* d_parent, const int32_t* d_row0, const int32_t
 int dllm_attention_tree(const dllm_attn_args* g, const uint32_t* d_mask, int32_t mask_ld, dllm_stream stream) {
     if (!d_mask || !aligned(d_mask, 4)) return fail(DLLM_E_INVAL, "mask: NULL or not 4-byte aligned");
     if (mask_ld < 1 || mask_ld > (1 << 24)) return fail(DLLM_E_INVAL, "mask_ld must be in [1, 2^24]");
+    if (g && (int64_t)g->n_rows * mask_ld >= (1ll << 29)) return fail(DLLM_E_INVAL, "n_rows * mask_ld must be < 2^29");
     return attention_paged(g, d_mask, mask_ld, false, (hipStream_t)stream);
 }
+
+int dllm_attention_tree_ws(const dllm_attn_args* g, size_t* bytes) { return attention_ws(g, true, bytes); }
 
 int dllm_logprobs_ws(const dllm_logprobs_args* g, size_t* bytes) {
     if (!bytes) return fail(DLLM_E_INVAL, "bytes is NULL");

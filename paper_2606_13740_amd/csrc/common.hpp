@@ -236,6 +236,12 @@ __device__ __forceinline__ void buffer_to_lds16(const void* src, int voff, int s
                                              (lds_void*)dst, 16, voff, soff, 0, 0);
 }
 
+// The same with 4 bytes per lane (to dst + 4 * lane).
+__device__ __forceinline__ void buffer_to_lds4(const void* src, int voff, int soff, char* dst) {
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(__builtin_amdgcn_make_buffer_rsrc((void*)src, 0, -1, 0x00027000),
+                                             (lds_void*)dst, 4, voff, soff, 0, 0);
+}
+
 __device__ __forceinline__ u32x4_t ldg16(const void* p) { return *(const u32x4_t*)p; }
 __device__ __forceinline__ u32x4_t ldg16_nt(const void* p) {
     return __builtin_nontemporal_load((const u32x4_t*)p);

@@ -1256,7 +1256,7 @@ static int batch_step(dllm_model* m, void* d_pages, size_t bytes, const dllm_bat
     }
     dllm_attn_args ga = batch_attn_args(m, b);
     size_t aws = 0;
-    if ((rc = dllm_attention_paged_ws(&ga, &aws))) return rc;
+    if ((rc = attention_ws(&ga, d_tree != nullptr, &aws))) return rc;
     m->rows_qkv = true;
     if ((rc = ensure_ws(m, b->n_rows))) return rc;
     if (aws > m->attn_ws_bytes) {
@@ -1289,6 +1289,7 @@ int dllm_batch_step_tree(dllm_model* m, void* d_pages, size_t bytes, const dllm_
                          int32_t* d_out_id, float* d_out_conf, dllm_stream stream) {
     if (!d_tree || ((uintptr_t)d_tree & 3) != 0) return fail(DLLM_E_INVAL, "tree: NULL or not 4-byte aligned");
     if (tree_ld < 1 || tree_ld > (1 << 24)) return fail(DLLM_E_INVAL, "tree_ld must be in [1, 2^24]");
+    if (rows && (int64_t)rows->n_rows * tree_ld >= (1ll << 29)) return fail(DLLM_E_INVAL, "n_rows * tree_ld must be < 2^29");
     return batch_step(m, d_pages, bytes, rows, d_tree, tree_ld, d_tok, d_mask, sel, d_out_id, d_out_conf, stream);
 }
 

@@ -17,6 +17,7 @@ int fail(int code, const std::string& msg);
 int select_check(const dllm_select_args* args);
 
 // dllm_attention_paged, with d_mask dllm_attention_tree; out_f32: d_out holds floats whatever the type (batch.hip).
+int attention_ws(const dllm_attn_args* args, bool tree, size_t* bytes);
 int attention_paged(const dllm_attn_args* args, const uint32_t* d_mask, int mask_ld, bool out_f32, hipStream_t s);
 
 // An error that a call reports is taken from the runtime, so that the next call (or another library) does not

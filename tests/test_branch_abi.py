@@ -23,6 +23,9 @@ def test_attention_tree_refusals(dl, change, mask, ld, code):  # noqa: F811
     a = fill(dl.dllm_attn_args, **dict(ATTN, **change))
     assert dl.lib().dllm_attention_tree(ctypes.byref(a), mask, ld, None) == code and dl.lib().dllm_last_error()
     assert dl.lib().dllm_attention_tree(None, P, 1, None) == dl.DLLM_E_INVAL
+    n = ctypes.c_size_t()
+    assert dl.lib().dllm_attention_tree_ws(None, ctypes.byref(n)) == dl.DLLM_E_INVAL
+    assert dl.lib().dllm_attention_tree_ws(ctypes.byref(a), None) == dl.DLLM_E_INVAL
 
 
 def test_batch_step_tree_refusals(dl):  # noqa: F811
