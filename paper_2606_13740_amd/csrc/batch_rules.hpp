@@ -145,11 +145,17 @@ inline size_t lp_ws_bytes(int T, int vocab, int top) {
     return parts == 1 ? 0 : (size_t)T * parts * (16 + 8 * (size_t)top);
 }
 
-// Threads of a fork's workgroup, and pages whose marks its LDS holds (beside 32 KB of the sequences').
-constexpr int FORK_NT = 1024, FORK_LDS_PAGES = 31 * 1024;
-// The copies' count (16 bytes), their list, and the marks where they do not fit.
+// Heads of a compaction's workgroup for V^T: as many as leave 1536 workgroups (six for every CU, which its registers
+// hold), at most eight; and workgroups, one more for K.  32 trees of 64 rows, 28 layers of 4 heads, fp16: one head a
+// workgroup 44.5 us, two 39.4, four 42.6.
+inline int compact_heads_per(long B, int L, int Hk) { return (int)std::min<long>(8, std::max<long>(1, B * L * Hk / (6 * N_CU))); }
+inline long compact_wgs(long B, int L, int Hk) { return B * L * (1 + ceil_div(Hk, compact_heads_per(B, L, Hk))); }
+
+// Threads of a fork's workgroup, and pages whose marks its LDS holds (beside 48 KB of the sequences').
+constexpr int FORK_NT = 1024, FORK_LDS_PAGES = 27 * 1024;
+// The copies' count (16 bytes), their list, the new tables' sources, and the marks where they do not fit.
 inline size_t fork_ws_bytes(int n_seqs, int n_pages) {
-    return 16 + (size_t)n_seqs * 16 + (n_pages > FORK_LDS_PAGES ? (size_t)n_pages * 4 : 0);
+    return 16 + (size_t)n_seqs * 24 + (n_pages > FORK_LDS_PAGES ? (size_t)n_pages * 4 : 0);
 }
 
 }  // namespace dllm

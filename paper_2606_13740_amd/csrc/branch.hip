@@ -61,18 +61,24 @@ void launch_logprobs(const LogprobArgs& a, hipStream_t s) {
 
 template <typename E>
 void launch_compact(const CompactArgs& a, hipStream_t s) {
-    const dim3 grid((unsigned)((long)a.B * a.c.L * 2 * a.c.Hk));
-    if (a.c.Dh == 128) hipLaunchKernelGGL((cache_compact_kernel<E, 128>), grid, dim3(COMPACT_NT), 0, s, a);
-    else if (a.c.Dh == 64) hipLaunchKernelGGL((cache_compact_kernel<E, 64>), grid, dim3(COMPACT_NT), 0, s, a);
-    else hipLaunchKernelGGL((cache_compact_kernel<E, 32>), grid, dim3(COMPACT_NT), 0, s, a);
+    const int hp = compact_heads_per(a.B, a.c.L, a.c.Hk);
+    const dim3 grid((unsigned)compact_wgs(a.B, a.c.L, a.c.Hk));
+    if (a.c.Dh == 128) hipLaunchKernelGGL((cache_compact_kernel<E, 128>), grid, dim3(COMPACT_NT), 0, s, a, hp);
+    else if (a.c.Dh == 64) hipLaunchKernelGGL((cache_compact_kernel<E, 64>), grid, dim3(COMPACT_NT), 0, s, a, hp);
+    else hipLaunchKernelGGL((cache_compact_kernel<E, 32>), grid, dim3(COMPACT_NT), 0, s, a, hp);
 }
 
 template <typename E>
-void launch_copies(const CacheArgs& c, const ForkArgs& a, hipStream_t s) {
+void launch_copies(const CacheArgs& c, const ForkArgs& a, int* table_out, hipStream_t s) {
+    // (tables are vectors where the rows of both are)
+    const bool vec = a.vec && aligned(table_out, 16);
     const dim3 grid((unsigned)std::min<long>((long)a.B * c.L * 2 * c.Hk, 8 * N_CU));
-    if (c.Dh == 128) hipLaunchKernelGGL((cache_copy_kernel<E, 128>), grid, dim3(256), 0, s, c, a.n_copies, a.copies, a.B);
-    else if (c.Dh == 64) hipLaunchKernelGGL((cache_copy_kernel<E, 64>), grid, dim3(256), 0, s, c, a.n_copies, a.copies, a.B);
-    else hipLaunchKernelGGL((cache_copy_kernel<E, 32>), grid, dim3(256), 0, s, c, a.n_copies, a.copies, a.B);
+#define COPY(DH_) \
+    hipLaunchKernelGGL((fork_copy_kernel<E, DH_>), grid, dim3(256), 0, s, c, a.n_copies, a.copies, a.rows, a.B, a.table, table_out, a.ld, vec)
+    if (c.Dh == 128) COPY(128);
+    else if (c.Dh == 64) COPY(64);
+    else COPY(32);
+#undef COPY
 }
 
 }  // namespace
@@ -155,7 +161,7 @@ int dllm_cache_compact(const dllm_cache* cache, const int32_t* d_table, int32_t 
     if (int rc = check_table(table_ld, cache->page)) return rc;
     if (path_ld < 1 || path_ld > 32 * TREE_MAX_LD) return fail(DLLM_E_INVAL, "path_ld must be in [1, 1024]");
     CompactArgs a{cache_args(cache, shift), d_table, table_ld, d_base, d_path, path_ld, d_n, n_seqs};
-    if (!grid_ok((long)n_seqs * a.c.L * 2 * a.c.Hk, COMPACT_NT)) return fail(DLLM_E_INVAL, "the cache and n_seqs need too many workgroups");
+    if (!grid_ok(compact_wgs(n_seqs, a.c.L, a.c.Hk), COMPACT_NT)) return fail(DLLM_E_INVAL, "the cache and n_seqs need too many workgroups");
     if (cache->dtype == DLLM_F32) launch_compact<uint32_t>(a, (hipStream_t)stream);
     else launch_compact<uint16_t>(a, (hipStream_t)stream);
     HIP_TRY(hipGetLastError());
@@ -190,17 +196,18 @@ int dllm_batch_fork(const dllm_cache* cache, const dllm_fork_args* g, dllm_strea
     if (need > g->ws_bytes)
         return fail(DLLM_E_CAPACITY, "the call needs " + std::to_string(need) + " bytes of workspace");
     int4* copies = (int4*)((char*)g->d_ws + 16);
-    ForkArgs a{g->d_src, g->d_keep, g->d_owned, g->d_owned_out, g->d_table, g->d_table_out, g->table_ld, g->d_free, g->d_n_free,
-               g->d_n_free_out, g->d_status, g->n_seqs, cache->n_pages, shift, g->shared_pages, (int*)g->d_ws, copies,
-               (uint32_t*)(copies + g->n_seqs)};
+    uint2* rows = (uint2*)(copies + g->n_seqs);
+    ForkArgs a{g->d_src, g->d_keep, g->d_owned, g->d_owned_out, g->d_table, g->table_ld,
+               g->table_ld % 4 == 0 && aligned(g->d_table, 16), g->d_free, g->d_n_free, g->d_n_free_out, g->d_status, g->n_seqs,
+               cache->n_pages, shift, g->shared_pages, (int*)g->d_ws, copies, rows, (uint32_t*)(rows + g->n_seqs)};
     const CacheArgs c = cache_args(cache, shift);
     hipStream_t s = (hipStream_t)stream;
     if (cache->n_pages <= FORK_LDS_PAGES)
         hipLaunchKernelGGL((batch_fork_kernel<true>), dim3(1), dim3(FORK_NT), (size_t)cache->n_pages * 4, s, a);
     else hipLaunchKernelGGL((batch_fork_kernel<false>), dim3(1), dim3(FORK_NT), 0, s, a);
     HIP_TRY(hipGetLastError());
-    if (cache->dtype == DLLM_F32) launch_copies<uint32_t>(c, a, s);
-    else launch_copies<uint16_t>(c, a, s);
+    if (cache->dtype == DLLM_F32) launch_copies<uint32_t>(c, a, g->d_table_out, s);
+    else launch_copies<uint16_t>(c, a, g->d_table_out, s);
     HIP_TRY(hipGetLastError());
     return DLLM_OK;
 }
