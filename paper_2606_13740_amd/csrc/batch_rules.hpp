@@ -142,7 +142,7 @@ inline int lp_per(int T, int vocab) {
 inline int lp_parts(int T, int vocab) { return ceil_div(ceil_div(vocab, LP_BLOCK), lp_per(T, vocab)); }
 inline size_t lp_ws_bytes(int T, int vocab, int top) {
     const int parts = lp_parts(T, vocab);
-    return parts == 1 ? 0 : (size_t)T * parts * (16 + 8 * (size_t)top);
+    return parts == 1 ? 0 : (size_t)T * parts * (LP_NT / 64) * (16 + 8 * (size_t)top);
 }
 
 // Heads of a compaction's workgroup for V^T: as many as leave 1536 workgroups (six for every CU, which its registers

@@ -139,7 +139,7 @@ int dllm_logprobs(const dllm_logprobs_args* g, dllm_stream stream) {
         return fail(DLLM_E_CAPACITY, "the call needs " + std::to_string(need) + " bytes of workspace");
     LogprobArgs a{g->d_logits, g->ld, g->n_rows, g->vocab, g->mask_id, g->n_tok, g->top, g->d_tok, g->d_tok_row, g->d_logp,
                   g->d_entropy, g->d_top_id, g->d_top_logp, parts, lp_per(g->n_rows, g->vocab), (LogStat*)g->d_ws, nullptr};
-    a.keys = (uint64_t*)((char*)g->d_ws + (size_t)a.T * parts * sizeof(LogStat));
+    a.keys = (uint64_t*)((char*)g->d_ws + (size_t)a.T * parts * (LP_NT / 64) * sizeof(LogStat));
     hipStream_t s = (hipStream_t)stream;
     if (g->dtype == DLLM_F32) launch_logprobs<float>(a, s);
     else if (g->dtype == DLLM_F16) launch_logprobs<_Float16>(a, s);

@@ -3,6 +3,8 @@
 
 #include <float.h>
 
+#include <type_traits>
+
 #include "batch_rules.hpp"
 #include "common.hpp"
 #include "qk_rope.hpp"
@@ -18,8 +20,8 @@ struct LogprobArgs {
     int* top_id;
     float* top_logp;
     int parts, per;               // parts of a row, blocks of LP_BLOCK ids each
-    struct LogStat* stat;         // [T][parts]
-    uint64_t* keys;               // [T][parts][top]
+    struct LogStat* stat;         // [T][parts][waves]
+    uint64_t* keys;               // [T][parts][waves][top]
 };
 
 // Sums over a set of logits: s = sum e^(x - m), t = sum (x - m) e^(x - m), m the largest.  Then the log of the
@@ -122,8 +124,21 @@ template <int NW> __device__ __forceinline__ uint64_t keys_top(const uint64_t* s
     return best;
 }
 
-// What a row's workgroup writes once its sums (in every thread) and best keys (in wave 0) are known.
-template <typename T, int NT> __device__ __forceinline__ void lp_write(const LogprobArgs& a, int row, const LogStat& st, uint64_t best) {
+// Given token i of row `row`: -> whether it is that workgroup's (row 0's also has those of rows that there are not), and
+// its logit.
+template <typename T> __device__ __forceinline__ bool lp_token(const LogprobArgs& a, int row, int i, float& x) {
+    const int r = a.tok_row ? a.tok_row[i] : i, v = a.tok[i];
+    const bool there = r >= 0 && r < a.T;
+    x = -INFINITY;
+    if (there ? r != row : row != 0) return false;
+    if (there && v >= 0 && v < a.V && v != a.mask_id) x = elem_to_f32<T>(((const T*)a.logits)[(long)row * a.ld + v]);
+    x = x < FLT_MAX ? x : (x >= FLT_MAX ? FLT_MAX : -INFINITY);             // (a NaN is neither)
+    return true;
+}
+// What a row's workgroup writes once its sums (in every thread) and best keys (in wave 0) are known.  mine, x0: lp_token of
+// token tid, asked for before.
+template <typename T, int NT>
+__device__ __forceinline__ void lp_write(const LogprobArgs& a, int row, const LogStat& st, uint64_t best, bool mine, float x0) {
     const int tid = threadIdx.x;
     const bool any = st.m > -INFINITY;
     const float lse = any ? logf(st.s) : 0.f;
@@ -133,49 +148,62 @@ template <typename T, int NT> __device__ __forceinline__ void lp_write(const Log
         a.top_logp[(size_t)row * a.top + tid] = best ? (value_of_key(best) - st.m) - lse : -INFINITY;
     }
     for (int i = tid; i < a.n_tok; i += NT) {
-        const int r = a.tok_row ? a.tok_row[i] : i;
-        const bool there = r >= 0 && r < a.T;
-        if (there ? r != row : row != 0) continue;        // (rows that there are not: row 0's workgroup)
-        const int v = a.tok[i];
-        float x = -INFINITY;
-        if (there && v >= 0 && v < a.V && v != a.mask_id) x = elem_to_f32<T>(((const T*)a.logits)[(long)row * a.ld + v]);
-        x = x < FLT_MAX ? x : (x >= FLT_MAX ? FLT_MAX : -INFINITY);         // (a NaN is neither)
-        a.logp[i] = any ? (x - st.m) - lse : -INFINITY;
+        if (i != tid) mine = lp_token<T>(a, row, i, x0);
+        if (mine) a.logp[i] = any ? (x0 - st.m) - lse : -INFINITY;
     }
 }
 
+// The largest of 32 logits, two an instruction.  (In assembly: the compiler would quiet every operand first.  A signalling
+// NaN may hide a larger logit here; whoever uses this looks for NaNs afterwards.)
+__device__ __forceinline__ float max_of_block(const float (&x)[LP_PT]) {
+    float m[2] = {x[0], x[1]};
+#pragma unroll
+    for (int i = 2; i < LP_PT; i += 4) {
+        asm("v_max3_f32 %0, %0, %1, %2" : "+v"(m[0]) : "v"(x[i]), "v"(x[i + 1]));
+        if (i + 3 < LP_PT) asm("v_max3_f32 %0, %0, %1, %2" : "+v"(m[1]) : "v"(x[i + 2]), "v"(x[i + 3]));
+    }
+    return fmaxf(m[0], m[1]);
+}
+
 // A workgroup takes a part of a row, its waves blocks of 64 x 32 ids.  A lane holds 32 logits: their largest moves its
-// reference, then every logit costs a subtraction, a clamp (which also takes NaN and the infinities), an exponential and
-// two sums.
+// reference m, then every logit costs one multiply-add, an exponential and two sums: with c = m log2 e rounded, y = x log2 e -
+// c is off by the rounding of c alone, the same for all, which the exact remainder r = m log2 e - c takes back from the
+// block's sums.  A block with a NaN, an infinity or logits past 2^16 (where r is no longer small) is done again with a
+// subtraction and a clamp a logit.
 //
 // The most probable ids: a wave keeps the 64 largest keys (logit, id) it has seen, a sorted list over its lanes, and the
-// bound that a logit has to pass, the `top`-th of them.  Before the first block that is the top-th largest of the lanes'
-// maxima, which as many logits reach.  What passes goes to a buffer in LDS, by ballots, and 64 at a time are sorted and
-// merged into the list.  Ids ascend from block to block, so an equal logit in a later block has lost: the bound is strict,
-// but inside a block, whose ids are not taken in order.
+// bound that a logit has to pass, the `top`-th of them.  In the first block that is the least of what the waves' top / NW-th
+// largest lane maxima are, which `top` logits of the workgroup reach.  What passes goes to a buffer in LDS, by ballots, and
+// 64 at a time are sorted and merged into the list.  Ids ascend from block to block, so an equal logit in a later block has
+// lost: the bound is strict, but inside a block, whose ids are not taken in order.
 template <typename T, bool TOP>
 __global__ void __launch_bounds__(LP_NT) logprobs_kernel(LogprobArgs a) {
     constexpr int NL = 16 / (int)sizeof(T), U = LP_PT / NL, NW = LP_NT / 64;
     __shared__ uint64_t pend_all[TOP ? NW * 128 : 1], list_s[TOP ? NW * 64 : 1];
     __shared__ LogStat stat_s[NW];
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    __shared__ uint32_t first_s[NW];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int part = (int)(blockIdx.x % a.parts), row = (int)(blockIdx.x / a.parts);
-    const int b1 = min((part + 1) * a.per, (a.V + LP_BLOCK - 1) / LP_BLOCK);
+    const int b0 = part * a.per, b1 = min(b0 + a.per, (a.V + LP_BLOCK - 1) / LP_BLOCK);
     const T* src = (const T*)a.logits + (long)row * a.ld;
     uint64_t* pend = pend_all + (TOP ? 128 * wave : 0);
 
     u32x4_t raw[U];
+    // (32-bit byte offsets from the row: no address registers; rows start at any element; read once: not kept in the
+    // caches, which is 6% faster)
+    typedef u32x4_t __attribute__((aligned(sizeof(T)))) any_u32x4;
     auto load = [&](int blk) {
-        const int v0 = blk * LP_BLOCK + lane * NL;
+        const uint32_t at = ((uint32_t)blk * LP_BLOCK + lane * NL) * sizeof(T);
         if ((blk + 1) * LP_BLOCK <= a.V) {
 #pragma unroll
-            for (int u = 0; u < U; ++u) __builtin_memcpy(&raw[u], src + v0 + u * 64 * NL, 16);
+            for (int u = 0; u < U; ++u) raw[u] = __builtin_nontemporal_load((const any_u32x4*)((const char*)src + (at + u * 1024u)));
         } else {
+            const uint32_t last = (uint32_t)(a.V - 1) * sizeof(T);
 #pragma unroll
             for (int u = 0; u < U; ++u) {
                 T x[NL];
 #pragma unroll
-                for (int j = 0; j < NL; ++j) x[j] = src[min(v0 + u * 64 * NL + j, a.V - 1)];
+                for (int j = 0; j < NL; ++j) __builtin_memcpy(&x[j], (const char*)src + min(at + u * 1024u + j * (uint32_t)sizeof(T), last), sizeof(T));
                 __builtin_memcpy(&raw[u], x, 16);
             }
         }
@@ -198,8 +226,10 @@ __global__ void __launch_bounds__(LP_NT) logprobs_kernel(LogprobArgs a) {
         return o ? of_order(o) : -INFINITY;
     };
 
-    int blk = part * a.per + wave;
+    int blk = b0 + wave;
     if (blk < b1) load(blk);
+    // (every wave has a block, or its workgroup's first bound is each wave's own)
+    const bool together = TOP && b1 - b0 >= NW;
     for (bool first = true; blk < b1; blk += NW, first = false) {
         float x[LP_PT];
 #pragma unroll
@@ -217,29 +247,62 @@ __global__ void __launch_bounds__(LP_NT) logprobs_kernel(LogprobArgs a) {
                 if (id_of(i) >= a.V || id_of(i) == a.mask_id) x[i] = -INFINITY;
         }
         if (blk + NW < b1) load(blk + NW);
-        float mx = -INFINITY;
+        float mx = max_of_block(x);
+        const float m = fmaxf(st.m, mx);
+        bool plain = __builtin_amdgcn_ballot_w64(!(fabsf(m) < 65536.f)) == 0;
+        if (plain) {
+            constexpr float L = 1.4426950408889634f;
+            const float c = m * L, r = fmaf(m, L, -c);
+            float s[2] = {0.f, 0.f}, t[2] = {0.f, 0.f};
 #pragma unroll
-        for (int i = 0; i < LP_PT; ++i) mx = fmaxf(mx, x[i]);
-        mx = fminf(mx, FLT_MAX);
-        stat_move(st, fmaxf(st.m, mx));
+            for (int i = 0; i < LP_PT; ++i) {
+                const float y = fmaf(x[i], L, -c), e = __builtin_amdgcn_exp2f(y);
+                s[i & 1] += e;
+                t[i & 1] = fmaf(e, y, t[i & 1]);
+            }
+            s[0] += s[1];
+            t[0] += t[1];
+            plain = __builtin_amdgcn_ballot_w64(!(t[0] <= 1.f)) == 0;      // (y <= 0 but for c's rounding; a NaN is not)
+            if (plain) {
+                const float w = __builtin_amdgcn_exp2f(-r);
+                stat_move(st, m);
+                st.s = fmaf(w, s[0], st.s);
+                st.t = fmaf(w * 0.6931471805599453f, fmaf(-r, s[0], t[0]), st.t);
+            }
+        }
+        if (!plain) {
+            mx = -INFINITY;
 #pragma unroll
-        for (int i = 0; i < LP_PT; ++i) {
-            const float d = __builtin_amdgcn_fmed3f(x[i] - st.m, LP_LEAST, 0.f);
-            const float e = lp_exp(d);
-            st.s += e;
-            st.t = fmaf(e, d, st.t);
+            for (int i = 0; i < LP_PT; ++i) mx = fmaxf(mx, x[i]);
+            mx = fminf(mx, FLT_MAX);
+            stat_move(st, fmaxf(st.m, mx));
+#pragma unroll
+            for (int i = 0; i < LP_PT; ++i) {
+                const float d = __builtin_amdgcn_fmed3f(x[i] - st.m, LP_LEAST, 0.f);
+                const float e = lp_exp(d);
+                st.s += e;
+                st.t = fmaf(e, d, st.t);
+            }
         }
         if constexpr (TOP) {
             if (first) {
-                // the top-th largest of the lanes' maxima, bit by bit
+                // the k-th largest of the lanes' maxima, bit by bit (16-bit logits differ in the upper bits, of fp32 15 of 23 will do)
+                const int k = together ? (a.top + NW - 1) / NW : a.top;
                 const uint32_t o = order_of(mx);
                 uint32_t t = 0;
-                for (int bit = 31; bit >= 0; --bit) {
+                constexpr int LOW = sizeof(T) == 4 ? 8 : (std::is_same<T, __bf16>::value ? 16 : 13);
+                for (int bit = 31; bit >= LOW; --bit) {
                     const uint32_t c = t | 1u << bit;
-                    if (__builtin_popcountll(__builtin_amdgcn_ballot_w64(o >= c)) >= a.top) t = c;
+                    if (__builtin_popcountll(__builtin_amdgcn_ballot_w64(o >= c)) >= k) t = c;
                 }
-                bound = below(of_order(t));
-                if (!(bound > -INFINITY)) bound = -INFINITY;
+                if (together) {
+                    if (lane == 0) first_s[wave] = t;
+                    __syncthreads();
+#pragma unroll
+                    for (int w = 0; w < NW; ++w) t = min(t, first_s[w]);
+                }
+                // (a bound of no float's order, of the lowest bits cut off, is lower still)
+                bound = t > order_of(-INFINITY) ? below(of_order(t)) : -INFINITY;
             }
             if (__builtin_amdgcn_ballot_w64(mx > bound) != 0) {
                 float pass = bound;
@@ -263,38 +326,40 @@ __global__ void __launch_bounds__(LP_NT) logprobs_kernel(LogprobArgs a) {
             }
         }
     }
-    if constexpr (TOP) {
-        if (n_pend > 0) flush(n_pend);
-        if (lane < a.top) list_s[wave * a.top + lane] = best;       // (as one list of NW * top keys)
-    }
+    if (TOP && n_pend > 0) flush(n_pend);
     st = wave_stat(st);
+    if (a.parts > 1) {                                     // every wave's own, for the merge
+        const size_t rec = ((size_t)row * a.parts + part) * NW + wave;
+        if (lane == 0) a.stat[rec] = st;
+        if (TOP && lane < a.top) a.keys[rec * a.top + lane] = best;
+        return;
+    }
+    if (TOP && lane < a.top) list_s[wave * a.top + lane] = best;           // (as one list of NW * top keys)
     if (lane == 0) stat_s[wave] = st;
     __syncthreads();
     st = stat_s[0];
 #pragma unroll
     for (int w = 1; w < NW; ++w) st = stat_merge(st, stat_s[w]);
     if constexpr (TOP) best = keys_top<NW>(list_s, NW * a.top, pend_all);
-    if (a.parts == 1) {
-        lp_write<T, LP_NT>(a, row, st, best);
-    } else {
-        const size_t rec = (size_t)row * a.parts + part;
-        if (tid == 0) a.stat[rec] = st;
-        if (TOP && tid < a.top) a.keys[rec * a.top + tid] = best;
-    }
+    float x0 = 0.f;
+    const bool mine = tid < a.n_tok && lp_token<T>(a, row, tid, x0);
+    lp_write<T, LP_NT>(a, row, st, best, mine, x0);
 }
 
-// Merge of a row's parts.
+// Merge of a row's waves.
 template <typename T>
 __global__ void __launch_bounds__(LP_NT) logprobs_merge_kernel(LogprobArgs a) {
     constexpr int NW = LP_NT / 64;
     __shared__ uint64_t tmp[NW * 64];
-    const int row = blockIdx.x, lane = threadIdx.x & 63;
+    const int row = blockIdx.x, lane = threadIdx.x & 63, n = a.parts * NW;
+    float x0 = 0.f;
+    const bool mine = (int)threadIdx.x < a.n_tok && lp_token<T>(a, row, threadIdx.x, x0);
     LogStat st{-INFINITY, 0.f, 0.f, 0.f};
-    for (int i = lane; i < a.parts; i += 64) st = stat_merge(st, a.stat[(size_t)row * a.parts + i]);
+    for (int i = lane; i < n; i += 64) st = stat_merge(st, a.stat[(size_t)row * n + i]);
     st = wave_stat(st);                                   // (every wave for itself)
     uint64_t best = 0;
-    if (a.top > 0) best = keys_top<NW>(a.keys + (size_t)row * a.parts * a.top, a.parts * a.top, tmp);
-    lp_write<T, LP_NT>(a, row, st, best);
+    if (a.top > 0) best = keys_top<NW>(a.keys + (size_t)row * n * a.top, n * a.top, tmp);
+    lp_write<T, LP_NT>(a, row, st, best, mine, x0);
 }
 
 }  // namespace dllm

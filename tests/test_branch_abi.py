@@ -114,7 +114,7 @@ int main() {
             const int blocks = (V + LP_BLOCK - 1) / LP_BLOCK, per = lp_per(T, V), parts = lp_parts(T, V);
             if (per < 1 || per % (LP_NT / 64) || (long)parts * per < blocks || (long)(parts - 1) * per >= blocks) return 1;
             if (T >= 4 * N_CU && parts != 1) return 2;
-            if (lp_ws_bytes(T, V, 64) != (parts == 1 ? 0 : (size_t)T * parts * 528)) return 3;
+            if (lp_ws_bytes(T, V, 64) != (parts == 1 ? 0 : (size_t)T * parts * 4 * 528)) return 3;
             ++n;
         }
     for (int ld = 1; ld <= TREE_MAX_LD; ++ld)
