@@ -392,7 +392,8 @@ class _Types:
         import torch
         cls.i32, cls.f32 = torch.int32, torch.float32
         cls.elem = {torch.float32: DLLM_F32, torch.bfloat16: DLLM_BF16, torch.float16: DLLM_F16}
-        cls.device = torch.cuda.current_device
+        # (the index without torch's check for its first use, which a tensor on a GPU has made: 0.2 us a call)
+        cls.device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
         cls.torch = torch
 
 

@@ -126,9 +126,8 @@ inline int select_rows_per(int T, int n_ranges) {
 inline long select_wgs(int T, int n_ranges) { return (long)n_ranges * ceil_div(T, select_rows_per(T, n_ranges)); }
 inline bool select_four_waves(long wgs) { return wgs <= 4 * N_CU; }
 
-// Rows of a sequence's tree: bits of a mask row that the plan of trees keeps in LDS.
-constexpr int TREE_MAX_LD = 32;
-inline size_t tree_lds_bytes(int ld) { return (size_t)32 * ld * (ld + 3) * 4; }
+// Words of a mask row in the plan of trees, whose LDS holds 32 rows a word.
+constexpr int TREE_MAX_LD = DLLM_MAX_TREE / 32;
 
 // Threads of a log probability workgroup, logits of a lane, ids of a wave's block.
 constexpr int LP_NT = 256, LP_PT = 32, LP_BLOCK = 64 * LP_PT, LP_MAX_TOP = 64;

@@ -98,7 +98,7 @@ int dllm_tree_plan(const int32_t* d_parent, const int32_t* d_row0, const int32_t
     if (mask_ld < 1 || mask_ld > TREE_MAX_LD) return fail(DLLM_E_INVAL, "mask_ld must be in [1, 32]");
     if (n_rows == 0) return DLLM_OK;
     TreeArgs a{d_parent, d_row0, d_len, n_rows, n_seqs, d_pos, d_mask, mask_ld};
-    hipLaunchKernelGGL(tree_plan_kernel, dim3(n_seqs), dim3(TREE_NT), tree_lds_bytes(mask_ld), (hipStream_t)stream, a);
+    hipLaunchKernelGGL(tree_plan_kernel, dim3(n_seqs), dim3(TREE_NT), 0, (hipStream_t)stream, a);
     HIP_TRY(hipGetLastError());
     return DLLM_OK;
 }

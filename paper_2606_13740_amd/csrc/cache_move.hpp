@@ -160,7 +160,7 @@ struct ForkArgs {
 // One workgroup does it, with the marks in LDS (or, for large pools, in the workspace): no launch waits for
 // another's.  What bounds it: dependent loads.  A wave takes as many sequences at once as have room in its lanes, four
 // entries a lane, four times over, so that one round trip brings up to 1024 entries (one sequence at a time: 512
-// sequences of up to 47 pages 40 us, SO).  The new tables are written by the launch that copies the pages, on the whole chip.
+// sequences of up to 47 pages 40 us, 14 so).  The new tables are written by the launch that copies the pages, on the whole chip.
 constexpr uint32_t FORK_HELD = 0xFFFFFFFEu, FORK_FREE = 0xFFFFFFFFu;
 template <bool LDS>
 __global__ void __launch_bounds__(FORK_NT) batch_fork_kernel(ForkArgs a) {
@@ -168,7 +168,7 @@ __global__ void __launch_bounds__(FORK_NT) batch_fork_kernel(ForkArgs a) {
     __shared__ int fresh_s[DLLM_MAX_SEQS];                // page of copy c
     __shared__ uint32_t to_s[DLLM_MAX_SEQS];              // source | pages needed << 12 | (whole pages only) << 31
     __shared__ int own_s[DLLM_MAX_SEQS];                  // pages owned; in a granted fork then copy of sequence b, or -1
-    __shared__ int wsum[NW], gsum[NW], most_s;
+    __shared__ int wsum[NW], gsum[NW], most_s[NW];
     extern __shared__ uint32_t marks_lds[];
     uint32_t* marks = LDS ? marks_lds : a.marks;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
@@ -185,33 +185,36 @@ __global__ void __launch_bounds__(FORK_NT) batch_fork_kernel(ForkArgs a) {
         keep[k] = a.keep[b];
         own[k] = a.owned[b];
     }
-    if (tid == 0) most_s = 0;
     for (int i = tid; i < a.n_pages; i += FORK_NT) {
         if (LDS) marks[i] = FORK_FREE;
         else __hip_atomic_store(&marks[i], FORK_FREE, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     }
+    // (what is out of range is cut here, so that the tables may be read before all sequences' checks are in)
     bool bad = n_free < 0 || n_free > a.n_pages;
-    int longest = 0;
+    int longest = 0, part[PER];
 #pragma unroll
     for (int k = 0; k < PER; ++k) {
         const int b = tid * per + k;
-        if (k >= per || b >= a.B) break;
-        const int s = src[k], held = a.owned[min(max(s, 0), a.B - 1)];
+        part[k] = -1;
+        if (k >= per || b >= a.B) continue;
         const long need = ((long)max(keep[k], 0) + in_page) >> a.page_shift;
-        bad |= s < 0 || s >= a.B || keep[k] < 0 || own[k] < 0 || own[k] > a.ld || need > held || need > a.ld;
-        to_s[b] = (uint32_t)s | (uint32_t)need << 12 | ((keep[k] & in_page) == 0 ? 0x80000000u : 0u);      // (read if all are good)
-        own_s[b] = own[k];
-        longest = max(longest, max((int)min(need, (long)a.ld), min(own[k], a.ld)));
+        bad |= src[k] < 0 || src[k] >= a.B || keep[k] < 0 || own[k] < 0 || own[k] > a.ld || need > a.ld;
+        const int s = min(max(src[k], 0), a.B - 1), n = (int)min(need, (long)a.ld), o = min(max(own[k], 0), a.ld);
+        const bool whole = (keep[k] & in_page) == 0;
+        to_s[b] = (uint32_t)s | (uint32_t)n << 12 | (whole ? 0x80000000u : 0u);
+        own_s[b] = o;
+        longest = max(longest, max(n, o));
+        if (!whole && n > a.shared) part[k] = a.table[(size_t)s * a.ld + n - 1];        // the page kept in part
     }
-    if (!LDS) __threadfence();                            // (a barrier alone does not wait for memory)
-    const bool any_bad = __syncthreads_or(bad);
-    longest = max(longest, __shfl_xor(longest, 32));
 #pragma unroll
-    for (int o = 16; o > 0; o >>= 1) longest = max(longest, __shfl_xor(longest, o));
-    if (lane == 0) atomicMax(&most_s, longest);
+    for (int o = 32; o > 0; o >>= 1) longest = max(longest, __shfl_xor(longest, o));
+    if (lane == 0) most_s[wave] = longest;
+    if (!LDS) __threadfence();                            // (a barrier alone does not wait for memory)
     __syncthreads();
+#pragma unroll
+    for (int w = 0; w < NW; ++w) longest = max(longest, most_s[w]);
     // lanes of a sequence: a power of two, as many as the longest table has groups of four pages
-    const int most = most_s, quads = (most + 3) >> 2, lp = quads > 1 ? min(6, 32 - __builtin_clz(quads - 1)) : 0;
+    const int most = longest, quads = (most + 3) >> 2, lp = quads > 1 ? min(6, 32 - __builtin_clz(quads - 1)) : 0;
     const int per_wave = 64 >> lp, sub = lane >> lp, col = 4 * (lane & ((1 << lp) - 1));
     auto source = [&](uint32_t to) { return (int)(to & 0xFFF); };
     auto need_of = [&](uint32_t to) { return (int)(to >> 12 & 0x7FFFF); };
@@ -221,51 +224,47 @@ __global__ void __launch_bounds__(FORK_NT) batch_fork_kernel(ForkArgs a) {
         else __hip_atomic_fetch_min(&marks[pg], m, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     };
     auto mark_at = [&](int pg) { return LDS ? marks[pg] : __hip_atomic_load(&marks[pg], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); };
-    if (!any_bad) {
-        for (int b0 = wave * per_wave * BATCH; b0 < a.B; b0 += NW * per_wave * BATCH) {
-            for (int j0 = a.shared & ~3; j0 < most; j0 += 4 << lp) {
-                const int j = j0 + col;
-                int4 was[BATCH], now[BATCH];
+    for (int b0 = wave * per_wave * BATCH; b0 < a.B; b0 += NW * per_wave * BATCH) {
+        for (int j0 = a.shared & ~3; j0 < most; j0 += 4 << lp) {
+            const int j = j0 + col;
+            int4 was[BATCH], now[BATCH];
 #pragma unroll
-                for (int k = 0; k < BATCH; ++k) {
-                    const int b = min(b0 + k * per_wave + sub, a.B - 1);
-                    const uint32_t to = to_s[b];
-                    was[k] = table4(a.table + (size_t)b * a.ld, j, own_s[b], a.vec);
-                    now[k] = table4(a.table + (size_t)source(to) * a.ld, j, need_of(to), a.vec);
-                }
+            for (int k = 0; k < BATCH; ++k) {
+                const int b = min(b0 + k * per_wave + sub, a.B - 1);
+                const uint32_t to = to_s[b];
+                was[k] = table4(a.table + (size_t)b * a.ld, j, own_s[b], a.vec);
+                now[k] = table4(a.table + (size_t)source(to) * a.ld, j, need_of(to), a.vec);
+            }
 #pragma unroll
-                for (int k = 0; k < BATCH; ++k) {
-                    const int b = min(b0 + k * per_wave + sub, a.B - 1);           // (the last one again: the same marks)
-                    const uint32_t to = to_s[b];
-                    const int n_own = own_s[b], need = need_of(to);
-                    const int w[4] = {was[k].x, was[k].y, was[k].z, was[k].w}, n[4] = {now[k].x, now[k].y, now[k].z, now[k].w};
+            for (int k = 0; k < BATCH; ++k) {
+                const int b = min(b0 + k * per_wave + sub, a.B - 1);           // (the last one again: the same marks)
+                const uint32_t to = to_s[b];
+                const int n_own = own_s[b], need = need_of(to);
+                const int w[4] = {was[k].x, was[k].y, was[k].z, was[k].w}, n[4] = {now[k].x, now[k].y, now[k].z, now[k].w};
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        if (j + e < a.shared) continue;
-                        if (j + e < n_own) mark(w[e], FORK_HELD);
-                        if (j + e < need) mark(n[e], j + e < need - 1 || to >> 31 ? 0u : 1u + b);
-                    }
+                for (int e = 0; e < 4; ++e) {
+                    if (j + e < a.shared) continue;
+                    if (j + e < n_own) mark(w[e], FORK_HELD);
+                    if (j + e < need) mark(n[e], j + e < need - 1 || to >> 31 ? 0u : 1u + b);
                 }
             }
         }
     }
-    if (!LDS) __threadfence();
-    __syncthreads();
-
-    // copies, numbered by sequence
-    int mine = 0, part[PER];
-    uint32_t is_copy = 0;
+    // no sequence keeps more than its source has
 #pragma unroll
     for (int k = 0; k < PER; ++k) {
         const int b = tid * per + k;
-        part[k] = -1;
-        if (any_bad || k >= per || b >= a.B) continue;
-        const uint32_t to = to_s[b];
-        if (!(to >> 31) && need_of(to) > a.shared) part[k] = a.table[(size_t)source(to) * a.ld + need_of(to) - 1];
+        if (k < per && b < a.B) bad |= need_of(to_s[b]) > own_s[source(to_s[b])];
     }
+    if (!LDS) __threadfence();
+    const bool any_bad = __syncthreads_or(bad);
+
+    // copies, numbered by sequence
+    int mine = 0;
+    uint32_t is_copy = 0;
 #pragma unroll
     for (int k = 0; k < PER; ++k) {
-        if (part[k] >= 0 && part[k] < a.n_pages && mark_at(part[k]) < 1u + tid * per + k) {
+        if (!any_bad && part[k] >= 0 && part[k] < a.n_pages && mark_at(part[k]) < 1u + tid * per + k) {
             is_copy |= 1u << k;
             ++mine;
         }
@@ -367,7 +366,8 @@ __global__ void __launch_bounds__(256) fork_copy_kernel(CacheArgs c, const int* 
     // (the first job is asked for beside their number)
     int4 job = copies[min((int)(blockIdx.x / units), B - 1)];
     const long n = (long)min(*n_copies, B) * units;
-    for (int b = blockIdx.x * 4 + (tid >> 6); b < B; b += gridDim.x * 4) {
+    // (from the grid's end: a fork rarely copies for all sequences)
+    for (int b = (gridDim.x - 1 - blockIdx.x) * 4 + (tid >> 6); b < B; b += gridDim.x * 4) {
         const uint2 to = rows[b];
         const int len = to.x >> 12 & 0x7FFFF;
         const int *src = table + (size_t)(to.x & 0xFFF) * ld;

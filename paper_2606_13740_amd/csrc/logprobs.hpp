@@ -95,20 +95,20 @@ template <int M> __device__ __forceinline__ uint64_t key_clean(uint64_t v, int l
     if constexpr (M > 1) v = key_clean<M / 2>(v, lane, down);
     return v;
 }
-// A wave's 64 keys sorted, ascending by lane.
-__device__ __forceinline__ uint64_t key_sort_up(uint64_t v, int lane) {
+// A wave's 64 keys sorted by lane.
+__device__ __forceinline__ uint64_t key_sort(uint64_t v, int lane, bool down) {
     v = key_clean<1>(v, lane, (lane & 2) == 0);
     v = key_clean<2>(v, lane, (lane & 4) == 0);
     v = key_clean<4>(v, lane, (lane & 8) == 0);
     v = key_clean<8>(v, lane, (lane & 16) == 0);
     v = key_clean<16>(v, lane, (lane & 32) == 0);
-    return key_clean<32>(v, lane, false);
+    return key_clean<32>(v, lane, down);
 }
 // The 64 largest of a descending list and of 64 more keys, descending: the lane-wise maximum of one list and the other
-// reversed holds them and is bitonic.
-__device__ __forceinline__ uint64_t key_merge(uint64_t best, uint64_t more, int lane) {
-    const uint64_t up = key_sort_up(more, lane);
-    return key_clean<32>(best > up ? best : up, lane, true);
+// reversed holds them and is bitonic.  empty: nothing is in the list yet.
+__device__ __forceinline__ uint64_t key_merge(uint64_t best, uint64_t more, int lane, bool empty) {
+    const uint64_t sorted = key_sort(more, lane, empty);
+    return empty ? sorted : key_clean<32>(best > sorted ? best : sorted, lane, true);
 }
 
 // Where the 64 largest of the keys src[0 .. n) end: every wave of the workgroup takes chunks of 64, wave 0 joins them
@@ -116,7 +116,7 @@ __device__ __forceinline__ uint64_t key_merge(uint64_t best, uint64_t more, int 
 template <int NW> __device__ __forceinline__ uint64_t keys_top(const uint64_t* src, int n, uint64_t* tmp) {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     uint64_t best = 0;
-    for (int i = 64 * wave; i < n; i += 64 * NW) best = key_merge(best, i + lane < n ? src[i + lane] : 0, lane);
+    for (int i = 64 * wave; i < n; i += 64 * NW) best = key_merge(best, i + lane < n ? src[i + lane] : 0, lane, i == 64 * wave);
     if (n <= 64) return best;                             // (wave 0 has had them all)
     __syncthreads();
     tmp[64 * wave + lane] = best;
@@ -213,9 +213,11 @@ __global__ void __launch_bounds__(LP_NT) logprobs_kernel(LogprobArgs a) {
     uint64_t best = 0;                                     // TOP: the list
     float bound = -INFINITY;                               // a logit has to exceed it
     int n_pend = 0;
+    bool empty = true;
     auto flush = [&](int n) {                              // the first n <= 64 of the buffer into the list
         __builtin_amdgcn_wave_barrier();                   // (a wave's LDS operations keep their order)
-        best = key_merge(best, lane < n ? pend[lane] : 0, lane);
+        best = key_merge(best, lane < n ? pend[lane] : 0, lane, empty);
+        empty = false;
         const uint64_t more = pend[64 + lane];
         pend[lane] = more;
         n_pend -= n;
@@ -228,6 +230,9 @@ __global__ void __launch_bounds__(LP_NT) logprobs_kernel(LogprobArgs a) {
 
     int blk = b0 + wave;
     if (blk < b1) load(blk);
+    // (where this workgroup writes the row: a token's three loads, one after the other, beside the logits)
+    float x0 = 0.f;
+    const bool mine = a.parts == 1 && tid < a.n_tok && lp_token<T>(a, row, tid, x0);
     // (every wave has a block, or its workgroup's first bound is each wave's own)
     const bool together = TOP && b1 - b0 >= NW;
     for (bool first = true; blk < b1; blk += NW, first = false) {
@@ -336,9 +341,7 @@ __global__ void __launch_bounds__(LP_NT) logprobs_kernel(LogprobArgs a) {
     st = stat_s[0];
 #pragma unroll
     for (int w = 1; w < NW; ++w) st = stat_merge(st, stat_s[w]);
-    if constexpr (TOP) best = keys_top<NW>(list_s, NW * a.top, pend_all);
-    float x0 = 0.f;
-    const bool mine = tid < a.n_tok && lp_token<T>(a, row, tid, x0);
+    if (TOP && b1 - b0 > 1) best = keys_top<NW>(list_s, NW * a.top, pend_all);      // (else wave 0 has them)
     lp_write<T, LP_NT>(a, row, st, best, mine, x0);
 }
 

@@ -117,8 +117,6 @@ int main() {
             if (lp_ws_bytes(T, V, 64) != (parts == 1 ? 0 : (size_t)T * parts * 4 * 528)) return 3;
             ++n;
         }
-    for (int ld = 1; ld <= TREE_MAX_LD; ++ld)
-        if (tree_lds_bytes(ld) > 160 * 1024 || tree_lds_bytes(ld) != (size_t)(32 * ld) * ld * 4 + 3 * 128 * ld) return 4;
     if ((size_t)FORK_LDS_PAGES * 4 + 3 * 4 * DLLM_MAX_SEQS + 1024 > 160 * 1024) return 5;
     if (fork_ws_bytes(3, FORK_LDS_PAGES) != 88 || fork_ws_bytes(3, FORK_LDS_PAGES + 1) != 88 + 4 * (FORK_LDS_PAGES + 1)) return 6;
     std::printf("%ld", n);
