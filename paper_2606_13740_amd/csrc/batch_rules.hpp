@@ -144,11 +144,14 @@ inline size_t lp_ws_bytes(int T, int vocab, int top) {
     return parts == 1 ? 0 : (size_t)T * parts * (LP_NT / 64) * (16 + 8 * (size_t)top);
 }
 
-// Heads of a compaction's workgroup for V^T: as many as leave 1536 workgroups (six for every CU, which its registers
-// hold), at most eight; and workgroups, one more for K.  32 trees of 64 rows, 28 layers of 4 heads, fp16: one head a
-// workgroup 44.5 us, two 39.4, four 42.6.
+// Heads (of all layers) of a compaction's workgroup for V^T: as many as leave 1536 workgroups (six for every CU, which its
+// registers hold), at most eight; and workgroups, with K's of COMPACT_NT lanes of 16 bytes.  32 trees of 64 rows, 28 layers of
+// 4 heads, fp16: one head a workgroup 37.8 us, two to four 36, six 37.4.
+constexpr int COMPACT_NT = 256;
 inline int compact_heads_per(long B, int L, int Hk) { return (int)std::min<long>(8, std::max<long>(1, B * L * Hk / (6 * N_CU))); }
-inline long compact_wgs(long B, int L, int Hk) { return B * L * (1 + ceil_div(Hk, compact_heads_per(B, L, Hk))); }
+inline long compact_wgs(long B, int L, int Hk, int Dh, int es) {
+    return B * (ceil_div((long)L * Hk * (Dh * es / 16), COMPACT_NT) + ceil_div((long)L * Hk, compact_heads_per(B, L, Hk)));
+}
 
 // Threads of a fork's workgroup, and pages whose marks its LDS holds (beside 48 KB of the sequences').
 constexpr int FORK_NT = 1024, FORK_LDS_PAGES = 27 * 1024;

@@ -62,7 +62,7 @@ void launch_logprobs(const LogprobArgs& a, hipStream_t s) {
 template <typename E>
 void launch_compact(const CompactArgs& a, hipStream_t s) {
     const int hp = compact_heads_per(a.B, a.c.L, a.c.Hk);
-    const dim3 grid((unsigned)compact_wgs(a.B, a.c.L, a.c.Hk));
+    const dim3 grid((unsigned)compact_wgs(a.B, a.c.L, a.c.Hk, a.c.Dh, sizeof(E)));
     if (a.c.Dh == 128) hipLaunchKernelGGL((cache_compact_kernel<E, 128>), grid, dim3(COMPACT_NT), 0, s, a, hp);
     else if (a.c.Dh == 64) hipLaunchKernelGGL((cache_compact_kernel<E, 64>), grid, dim3(COMPACT_NT), 0, s, a, hp);
     else hipLaunchKernelGGL((cache_compact_kernel<E, 32>), grid, dim3(COMPACT_NT), 0, s, a, hp);
@@ -161,7 +161,7 @@ int dllm_cache_compact(const dllm_cache* cache, const int32_t* d_table, int32_t 
     if (int rc = check_table(table_ld, cache->page)) return rc;
     if (path_ld < 1 || path_ld > 32 * TREE_MAX_LD) return fail(DLLM_E_INVAL, "path_ld must be in [1, 1024]");
     CompactArgs a{cache_args(cache, shift), d_table, table_ld, d_base, d_path, path_ld, d_n, n_seqs};
-    if (!grid_ok(compact_wgs(n_seqs, a.c.L, a.c.Hk), COMPACT_NT)) return fail(DLLM_E_INVAL, "the cache and n_seqs need too many workgroups");
+    if (!grid_ok(compact_wgs(n_seqs, a.c.L, a.c.Hk, a.c.Dh, esize(cache->dtype)), COMPACT_NT)) return fail(DLLM_E_INVAL, "the cache and n_seqs need too many workgroups");
     if (cache->dtype == DLLM_F32) launch_compact<uint32_t>(a, (hipStream_t)stream);
     else launch_compact<uint16_t>(a, (hipStream_t)stream);
     HIP_TRY(hipGetLastError());

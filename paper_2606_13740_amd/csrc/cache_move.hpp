@@ -32,17 +32,22 @@ struct CompactArgs {
 // Position base + path[i] to base + i, for i < n: path ascends, so path[i] >= i and a chunk's destinations lie before the
 // sources of the chunks behind it: load a chunk, wait, store it, in place.
 //
-// A workgroup takes one sequence's K of one layer, or its V^T of one layer and hp heads.  K: a position is Dh consecutive
-// elements of each head; a lane has 16 bytes of a head and takes the positions in chunks of eight.  V^T: a position is a
+// A workgroup takes one sequence's K of as many heads (of all layers) as have 16 bytes for each of its lanes, or its V^T of hp
+// heads.  K: a position is Dh consecutive elements of each head; a lane takes the positions in chunks of eight.  V^T: a position is a
 // column; 16 lanes have 16 positions of a dim, which lie in one or two lines of its page, and are read and written
 // together.  Either way a chunk's source and destinations are one wave's, which needs no barrier.
-constexpr int COMPACT_NT = 256, COMPACT_POS = 16, COMPACT_K = 8;
+constexpr int COMPACT_POS = 16, COMPACT_K = 8;
 template <typename E, int DH>
 __global__ void __launch_bounds__(COMPACT_NT) cache_compact_kernel(CompactArgs a, int hp) {
     constexpr int ES = sizeof(E);
     __shared__ int src_s[DLLM_MAX_TREE], dst_s[DLLM_MAX_TREE], end_s;       // slots (page id * page + offset), -1: not moved
-    const int tid = threadIdx.x, parts = 1 + (a.c.Hk + hp - 1) / hp;
-    const int part = blockIdx.x % parts, i1 = blockIdx.x / parts, l = i1 % a.c.L, b = i1 / a.c.L;
+    constexpr int LP = DH * ES / 16;                      // lanes of a head's position
+    const int tid = threadIdx.x, heads = a.c.L * a.c.Hk;  // (head u is head u % Hk of layer u / Hk)
+    // K's workgroups first: they are few and short, and next to V^T's those wait for less
+    const int k_parts = (heads * LP + COMPACT_NT - 1) / COMPACT_NT, v_parts = (heads + hp - 1) / hp;
+    const bool is_k = (int)blockIdx.x < k_parts * a.B;
+    const int at0 = is_k ? blockIdx.x : blockIdx.x - k_parts * a.B, parts = is_k ? k_parts : v_parts;
+    const int part = at0 % parts, b = at0 / parts;
     const int n = min(max(a.n[b], 0), a.path_ld), base = a.base[b];
     if (n == 0 || base < 0) return;
     if (tid == 0) end_s = n;
@@ -69,39 +74,39 @@ __global__ void __launch_bounds__(COMPACT_NT) cache_compact_kernel(CompactArgs a
     }
     if (!__syncthreads_or(moved)) return;
     const int m = end_s;
-    if (part == 0) {
-        constexpr int LP = DH * ES / 16;                  // lanes of a head's position
-        for (int c = tid; c < a.c.Hk * LP; c += COMPACT_NT) {
-            const int hk = c / LP;
-            auto at = [&](int s) {
-                return (u32x4_t*)(head_of<ES>(a.c, l, 0, s >> a.c.page_shift, hk) + (size_t)(s & (page - 1)) * (DH * ES)) + c % LP;
-            };
-            for (int i0 = 0; i0 < m; i0 += COMPACT_K) {
-                u32x4_t v[COMPACT_K];
-                int from[COMPACT_K];
+    if (is_k) {
+        const int c = part * COMPACT_NT + tid, u = c / LP;
+        if (u >= heads) return;
+        auto at = [&](int s) {
+            return (u32x4_t*)(head_of<ES>(a.c, u / a.c.Hk, 0, s >> a.c.page_shift, u % a.c.Hk) + (size_t)(s & (page - 1)) * (DH * ES)) + c % LP;
+        };
+        for (int i0 = 0; i0 < m; i0 += COMPACT_K) {
+            u32x4_t v[COMPACT_K];
+            int from[COMPACT_K];
 #pragma unroll
-                for (int k = 0; k < COMPACT_K; ++k) {
-                    from[k] = i0 + k < m ? src_s[i0 + k] : -1;
-                    if (from[k] >= 0) v[k] = *at(from[k]);
-                }
-                asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-#pragma unroll
-                for (int k = 0; k < COMPACT_K; ++k)
-                    if (from[k] >= 0) *at(dst_s[i0 + k]) = v[k];
+            for (int k = 0; k < COMPACT_K; ++k) {
+                from[k] = i0 + k < m ? src_s[i0 + k] : -1;
+                if (from[k] >= 0) v[k] = *at(from[k]);
             }
+            asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+#pragma unroll
+            for (int k = 0; k < COMPACT_K; ++k)
+                if (from[k] >= 0) *at(dst_s[i0 + k]) = v[k];
         }
         return;
     }
     constexpr int ND = COMPACT_NT / COMPACT_POS, PASS = DH / ND;
-    const int h1 = min(a.c.Hk, part * hp), dim = tid / COMPACT_POS;
+    const int u1 = min(heads, (part + 1) * hp), dim = tid / COMPACT_POS;
     for (int i0 = 0; i0 < m; i0 += COMPACT_POS) {
         const int i = i0 + tid % COMPACT_POS, from = i < m ? src_s[i] : -1;
         if (from < 0) continue;
         const int to = dst_s[i];
-        auto at = [&](int s, int hk) { return (E*)head_of<ES>(a.c, l, 1, s >> a.c.page_shift, hk) + (s & (page - 1)) + ((size_t)dim << a.c.page_shift); };
-        for (int hk = (part - 1) * hp; hk < h1; hk += 2) {
-            const int other = min(hk + 1, h1 - 1);        // (two heads' loads at once; the last one alone twice)
-            const E *p0 = at(from, hk), *p1 = at(from, other);
+        auto at = [&](int s, int u) {
+            return (E*)head_of<ES>(a.c, u / a.c.Hk, 1, s >> a.c.page_shift, u % a.c.Hk) + (s & (page - 1)) + ((size_t)dim << a.c.page_shift);
+        };
+        for (int u = part * hp; u < u1; u += 2) {
+            const int other = min(u + 1, u1 - 1);         // (two heads' loads at once; the last one alone twice)
+            const E *p0 = at(from, u), *p1 = at(from, other);
             E v[2][PASS];
 #pragma unroll
             for (int k = 0; k < PASS; ++k) {
@@ -109,7 +114,7 @@ __global__ void __launch_bounds__(COMPACT_NT) cache_compact_kernel(CompactArgs a
                 v[1][k] = p1[(size_t)(k * ND) << a.c.page_shift];
             }
             asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-            E *q0 = at(to, hk), *q1 = at(to, other);
+            E *q0 = at(to, u), *q1 = at(to, other);
 #pragma unroll
             for (int k = 0; k < PASS; ++k) {
                 q0[(size_t)(k * ND) << a.c.page_shift] = v[0][k];

@@ -123,3 +123,32 @@ int main() {
 }
 """)
     assert out == "100"
+
+
+def test_rules_of_the_attention_with_masks(tmp_path):
+    """Groups of tiles for every sequence, head and split, the same number for each XCD; splits that cover the keys, none
+    empty; the paged attention's launches as they were."""
+    out = run_cpp(tmp_path, r"""
+int main() {
+    long n = 0;
+    for (int dtype : {DLLM_F32, DLLM_F16})
+        for (int B : {1, 3, 16, 256, 300, 4096})
+            for (int rows : {1, 5, 64, 1000})
+                for (int share : {0, 1024, 8192})
+                    for (int own : {0, 1, 900, 30000}) {
+                        dllm_attn_args g{};
+                        g.dtype = dtype; g.n_seqs = B; g.max_rows = rows; g.n_rows = (int)((long)B * rows * 2 / 3 + 1);
+                        g.n_heads = 28; g.n_kv_heads = 4; g.head_dim = 128; g.page = 64; g.shared_len = share; g.max_len = share + own;
+                        const AttnPlan p = attn_plan(&g, true), q = attn_plan(&g);
+                        const int step = dtype == DLLM_F32 ? 32 : 64, steps = own + (share - p.shared);
+                        if (p.wgs_o % (8 * p.nt_o) || p.wgs_o < (long)B * 4 * p.ns_o * p.nt_o || p.wgs_o >= (long)(B * 4 * p.ns_o + 8) * p.nt_o) return 1;
+                        if (p.nt_o * 16l * p.qg * p.qt < (long)(rows < g.n_rows ? rows : g.n_rows) * 7) return 2;
+                        if (p.ns_o < 1 || p.ns_o > MAX_ATTN_SPLITS || p.ns_s > MAX_ATTN_SPLITS || (p.shared > 0) != (p.ns_s > 0)) return 3;
+                        if (steps > 0 && (p.ns_o - 1) * (long)ceil_div(ceil_div(steps, step), p.ns_o) >= ceil_div(steps, step)) return 4;
+                        if (p.shared != q.shared || q.wgs_o != (long)B * 4 * q.nt_o * q.ns_o || p.wgs_s != (p.shared ? 4l * p.nt_s * p.ns_s : 0)) return 5;
+                        ++n;
+                    }
+    std::printf("%ld", n);
+}
+""")
+    assert out == "576"

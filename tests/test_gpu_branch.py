@@ -253,6 +253,35 @@ def test_attention_tree_large_tiles(dl, dtype):
         check_out(c, run_tree(dl, c, sets_to_mask(c, seen, 2)), seen)
 
 
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+def test_attention_tree_pages_that_are_none(dl, dtype):
+    """Table entries that are no page, before and among the rows: their positions are seen by nobody."""
+    rng = np.random.default_rng(14)
+    for rows, cached, H, Hk, D, shared in (([40, 5, 33], [400, 31, 64], 4, 2, 64, 0), ([33, 64, 7], [900, 650, 700], 8, 8, 128, 640)):
+        c = attn_case(rng, dtype, rows, cached, H, Hk, D, 32, shared)
+        for b in range(3):
+            last = -(-int(c["lens"][b]) // 32)
+            for j in rng.choice(np.arange(shared // 32, last), max(1, (last - shared // 32) // 4), replace=False):
+                c["table"][b, j] = [-1, c["k"].shape[0], 2 ** 31 - 1, -2 ** 31][j % 4]
+        c["table"][:, shared // 64] = -1 if shared else c["table"][:, 0]
+        seen = random_sets(rng, rows, c["row0"])
+        check_out(c, run_tree(dl, c, sets_to_mask(c, seen, 2)), seen)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "f16"])
+def test_attention_tree_many_sequences(dl, dtype):
+    """More sequences than a workgroup's scan holds, and ragged ones, several tiles each; one more row than the scan's lanes."""
+    rng = np.random.default_rng(15)
+    for B in (300, 256, 65):
+        rows = rng.integers(0, 41, B)
+        rows[0] = 40
+        rows[rng.random(B) < 0.3] = 0
+        rows[0] = 40
+        c = attn_case(rng, dtype, rows.tolist(), rng.integers(0, 60, B).tolist(), 4, 1, 64, 32, 0, first=3)
+        seen = random_sets(rng, rows.tolist(), c["row0"])
+        check_out(c, run_tree(dl, c, sets_to_mask(c, seen, 2)), seen)
+
+
 def test_attention_tree_strided_rows_scales_and_bounds(dl):
     import torch
     rng = np.random.default_rng(9)
@@ -319,7 +348,7 @@ def logits_of(rng, T, V, dtype, std=3.0):
 
 @pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
 @pytest.mark.parametrize("T,V,n,top", [(1, 1, 1, 1), (3, 5, 9, 8), (2, 64, 2, 64), (16, 1024, 15, 4), (5, 2047, 3, 1), (4, 2049, 40, 33),
-                                       (7, 8193, 0, 64), (300, 5000, 7, 20), (1, 126464, 1, 8), (33, 40001, 64, 20), (2, 152064, 5, 0)])
+                                       (7, 8193, 0, 64), (3, 700, 1000, 2), (300, 5000, 7, 20), (1, 126464, 1, 8), (33, 40001, 64, 20), (2, 152064, 5, 0)])
 def test_logprobs(dl, dtype, T, V, n, top):
     rng = np.random.default_rng(T + V)
     x = logits_of(rng, T, V, dtype)
@@ -379,6 +408,23 @@ def test_logprobs_far_logits_and_large_offsets(dl):
     x = torch.from_numpy(np.concatenate([rng.normal(0, 1, (1, 9000)) + 1e4, rng.normal(0, 1e30, (1, 9000)), rng.normal(0, 1, (1, 9000)) * 1e-30,
                                          rng.normal(-3e38, 1e36, (1, 9000))]).astype(np.float32))
     check_logprobs(dl, x, "f32", tok=[0, 1, 2, 3], top=10)
+
+
+def test_logprobs_past_2_31_logits(dl):
+    """Rows that begin past element 2^31."""
+    import torch
+    T, V = 16500, 131101
+    g = torch.Generator(device="cuda").manual_seed(3)
+    x = torch.empty(T, V, dtype=torch.bfloat16, device="cuda").normal_(0, 3, generator=g)
+    tok = torch.randint(0, V, (T,), dtype=torch.int32, device="cuda", generator=g)
+    lp, ent = torch.zeros(T, device="cuda"), torch.zeros(T, device="cuda")
+    ids, tl = torch.zeros(T, 3, dtype=torch.int32, device="cuda"), torch.zeros(T, 3, device="cuda")
+    dl.dllm_logprobs(x, tok, None, lp, ent, ids, tl)
+    for r in (0, 9000, T - 1):
+        want = logprobs(x[r:r + 1].double().cpu().numpy(), -1, [tok[r].item()], None, 3)
+        assert np.array_equal(ids[r].cpu().numpy(), want[2][0])
+        assert abs(lp[r].item() - want[0][0]) <= want[4][0] and abs(ent[r].item() - want[1][0]) <= want[5][0]
+        assert (abs(tl[r].double().cpu().numpy() - want[3][0]) <= want[6][0]).all()
 
 
 # ---------------------------------------------------------------------------- moves in the cache
@@ -510,6 +556,30 @@ def test_batch_fork_many_sequences_and_pages_past_the_lds(dl):
     a, t = cache_of(rng, "f16", 1, n_pages, 1, 32, 32)
     assert n_pages > 31 * 1024
     assert check_fork(dl, src, keep, owned, table, free, n_free, 1, 32, a, t, 32)["status"][0] > 0
+
+
+def test_moves_past_2_31_elements(dl):
+    """Planes of more than 2^31 elements: positions and copies at their end, marks of 70000 pages in the workspace."""
+    import torch
+    n_pages, page, D, last = 70000, 256, 128, 69999
+    t = torch.zeros(1, 2, n_pages, 1, page * D, dtype=torch.float16, device="cuda")
+    k, v = t[0, 0].view(n_pages, page, D), t[0, 1].view(n_pages, D, page)
+    g = torch.Generator(device="cuda").manual_seed(1)
+    k[last - 1:].normal_(generator=g), v[last - 1:].normal_(generator=g)
+    k0, v0 = k[last - 1:].clone(), v[last - 1:].clone()
+    table = i32([[last, last - 1]])
+    dl.dllm_cache_compact(t, page, table, i32([250]), i32([[3, 9]]), i32([2]))         # 253 and 259 to 250 and 251
+    k0[1, 250], k0[1, 251] = k0[1, 253].clone(), k0[0, 3].clone()
+    v0[1, :, 250], v0[1, :, 251] = v0[1, :, 253].clone(), v0[0, :, 3].clone()
+    assert torch.equal(k[last - 1:], k0) and torch.equal(v[last - 1:], v0)
+    free = torch.full((n_pages,), -1, dtype=torch.int32, device="cuda")
+    free[0] = 65000
+    z = lambda *n: torch.zeros(n, dtype=torch.int32, device="cuda")  # noqa: E731
+    table, table_out, owned, n_free, status = i32([[last, last - 1], [-1, -1]]), z(2, 2) - 5, z(2), z(1), z(3)
+    dl.dllm_batch_fork(i32([0, 0]), i32([300, 300]), i32([2, 0]), owned, table, table_out, free, i32([1]), n_free, 0, t, page, status)
+    assert table_out.tolist() == [[last, last - 1], [last, 65000]] and status.tolist() == [1, 0, 0] and n_free.item() == 0
+    assert torch.equal(k[65000, :44], k0[0, :44]) and torch.equal(v[65000, :, :44], v0[0, :, :44])
+    assert k[65000, 44:].eq(0).all() and v[65000, :, 44:].eq(0).all() and owned.tolist() == [2, 2]
 
 
 def test_batch_fork_takes_pages_that_the_same_call_gives_back(dl):
