@@ -235,14 +235,15 @@ template <typename T> __device__ __forceinline__ void store_out4(const PagedArgs
 // What bounds it: many rows, the chain of products and exponentials of the two waves that a SIMD holds
 // (16 sequences of 64 rows, 28 heads over 4, behind 16384 bf16 keys: 145-153 us with the merge, 850 to 900
 // TFLOP/s where a large library product reaches 1100; waiting 22% of the wave cycles); rows enough for the prefix only, LDS reads and the K/V
-// themselves (8 x 32 rows of 32 fp16 heads behind 4096: 37 us and 6, 115 MB); few rows, latency (8 x 1 rows
+// themselves (8 x 32 rows of 32 fp16 heads behind 4096: 46 us with the merge, 115 MB); few rows, latency (8 x 1 rows
 // behind 1564: 9.8 us and 4.8, 288 workgroups of three steps, each asked for when the one before has landed).
 //
 // TREE: a row sees the cached positions and, of its sequence's rows, those that its mask has.  Steps whose keys are all
 // cached run as without; in the others a lane takes the 32 bits of its row for a block from two words, which come to LDS
 // beside the step's K/V (a load waited for inside a step would wait for the staging behind it).  What a lane needs for
 // that waits in LDS too: kept in registers, the 32 x 32 tiles spilled three, and a spill's reload waits for the staging
-// in every step.
+// in every step.  16 trees of up to 64 rows, 28 heads over 4, behind 8192 + 3000 bf16 keys: 105 us with the merge, 690
+// TFLOP/s; 4 x 4 candidates of 32 rows, 32 fp16 heads, behind 4000: 74 us, K/V at 4.6 TB/s before the merge.
 template <typename T, int DH, int QG, int RT, int KG, int SUB, bool TREE>
 __global__ void __launch_bounds__(QG * KG * 64)
 __attribute__((amdgpu_waves_per_eu(QG * KG * (160 * 1024 / (2 * SUB * 64 * DH * (int)sizeof(T))) >= 8 ? 2 : 1)))

@@ -177,6 +177,10 @@ __device__ __forceinline__ float max_of_block(const float (&x)[LP_PT]) {
 // largest lane maxima are, which `top` logits of the workgroup reach.  What passes goes to a buffer in LDS, by ballots, and
 // 64 at a time are sorted and merged into the list.  Ids ascend from block to block, so an equal logit in a later block has
 // lost: the bound is strict, but inside a block, whose ids are not taken in order.
+//
+// What bounds it: 256 rows of 152064 bf16 logits, 24 us and 5 for the merge, where reading takes 16 and VALU issue 14: the
+// start, the first bound and the last sorts of all waves, which run at once; few or short rows, latency: load, bound, sort,
+// logarithm (16 rows of 1024 7 us, 32 of 126464 fp32 8 and 5).
 template <typename T, bool TOP>
 __global__ void __launch_bounds__(LP_NT) logprobs_kernel(LogprobArgs a) {
     constexpr int NL = 16 / (int)sizeof(T), U = LP_PT / NL, NW = LP_NT / 64;
