@@ -242,8 +242,9 @@ template <typename T> __device__ __forceinline__ void store_out4(const PagedArgs
 // cached run as without; in the others a lane takes the 32 bits of its row for a block from two words, which come to LDS
 // beside the step's K/V (a load waited for inside a step would wait for the staging behind it).  What a lane needs for
 // that waits in LDS too: kept in registers, the 32 x 32 tiles spilled three, and a spill's reload waits for the staging
-// in every step.  16 trees of up to 64 rows, 28 heads over 4, behind 8192 + 3000 bf16 keys: 105 us with the merge, 690
-// TFLOP/s; 4 x 4 candidates of 32 rows, 32 fp16 heads, behind 4000: 74 us, K/V at 4.6 TB/s before the merge.
+// in every step.  Of a SIMD's two waves the one that reads and multiplies goes before the one in its exponentials: 98 us
+// for 105 below, 260 for 281 with full trees behind 16384, at worst 1% (the paged calls' long case loses 3%, so not there).
+// 16 trees of up to 64 rows, 28 heads over 4, behind 8192 + 3000 bf16 keys: 98 us with the merge, 740 TFLOP/s; 4 x 4 candidates of 32 rows, 32 fp16 heads, behind 4000: 74 us, K/V at 4.6 TB/s before the merge.
 template <typename T, int DH, int QG, int RT, int KG, int SUB, bool TREE>
 __global__ void __launch_bounds__(QG * KG * 64)
 __attribute__((amdgpu_waves_per_eu(QG * KG * (160 * 1024 / (2 * SUB * 64 * DH * (int)sizeof(T))) >= 8 ? 2 : 1)))
@@ -545,6 +546,7 @@ attn_paged_kernel(PagedArgs a) {
 
         // all of the step's K fragments are read before the first product, its V^T fragments between
         // the scores and the softmax, which covers their latency
+        if constexpr (TREE) __builtin_amdgcn_s_setprio(2);
         const char* buf = cur + kw * SW * SBUF;
         u32x4_t kf[SW][NC][NU], vf[SW][ND][NV];
 #pragma unroll
@@ -583,6 +585,7 @@ attn_paged_kernel(PagedArgs a) {
                 }
         __builtin_amdgcn_sched_barrier(0);
 
+        if constexpr (TREE) __builtin_amdgcn_s_setprio(0);
         float sv[SW][NS];
 #pragma unroll
         for (int w = 0; w < SW; ++w)
