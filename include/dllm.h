@@ -769,7 +769,8 @@ int dllm_cache_compact(const dllm_cache* cache, const int32_t* d_table, int32_t 
  * written to, so only one sequence may go on with it: the first in order, if no sequence
  * keeps it whole; the others get a page of their own with the kept positions copied, in every layer.
  * Pages in the old tables that no sequence keeps any more are given back.  The first
- * shared_pages of a table belong to all and are never counted, copied or given back.  In order:
+ * shared_pages of a table belong to all and are never counted, copied or given back (a sequence
+ * cut inside them would go on in pages that all have: keep them, or end it).  In order:
  * pages given back are pushed onto the stack d_free[0 .. *d_n_free), the lowest id first, then
  * the copies' pages are popped off its top, for the lowest sequence first.
  * d_table_out, d_owned_out and d_n_free_out receive the new tables and counts and must be other

@@ -558,6 +558,18 @@ def test_batch_fork_many_sequences_and_pages_past_the_lds(dl):
     assert check_fork(dl, src, keep, owned, table, free, n_free, 1, 32, a, t, 32)["status"][0] > 0
 
 
+@pytest.mark.parametrize("n_pages", [27 * 1024, 27 * 1024 + 1])
+def test_batch_fork_at_the_lds_limit(dl, n_pages):
+    """As many pages as have their marks in LDS, and one more."""
+    rng = np.random.default_rng(n_pages)
+    src, keep, owned, table, free, n_free, n = fork_case(rng, 20, 9, 32, 1, 400)
+    assert n < n_pages
+    more = np.full(n_pages, -9)
+    more[:n_free + n_pages - n] = np.concatenate([np.arange(n, n_pages), free[:n_free]])
+    a, t = cache_of(rng, "f16", 1, n_pages, 1, 32, 32)
+    assert check_fork(dl, src, keep, owned, table, more, n_free + n_pages - n, 1, 32, a, t, 32)["status"][2] == 0
+
+
 def test_moves_past_2_31_elements(dl):
     """Planes of more than 2^31 elements: positions and copies at their end, marks of 70000 pages in the workspace."""
     import torch
