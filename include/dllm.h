@@ -716,8 +716,8 @@ int dllm_batch_step_tree(dllm_model* m, void* d_pages, size_t bytes, const dllm_
  * An id of -inf, a token outside the vocabulary and one of a row that there is not have log
  * probability -inf; where fewer than `top` ids are left the others are -1 and -inf; a row
  * with none left has entropy 0.  The same token may be given any number of times, in
- * any order.  The workspace of dllm_logprobs_ws() bytes is the caller's; calls that may overlap, and
- * captured graphs that may, need one each.  E_INVAL for NULL pointers, pointers not aligned to
+ * any order.  The workspace of dllm_logprobs_ws() bytes is the caller's (how many depends on the sizes and on
+ * whether there is a d_tok_row); calls that may overlap, and captured graphs that may, need one each.  E_INVAL for NULL pointers, pointers not aligned to
  * their elements and sizes out of range (top in [0, DLLM_MAX_TOP]); E_DTYPE for another type;
  * E_CAPACITY for a workspace too small. */
 typedef struct dllm_logprobs_args {

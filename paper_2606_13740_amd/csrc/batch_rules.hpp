@@ -143,6 +143,16 @@ inline size_t lp_ws_bytes(int T, int vocab, int top) {
     const int parts = lp_parts(T, vocab);
     return parts == 1 ? 0 : (size_t)T * parts * (LP_NT / 64) * (16 + 8 * (size_t)top);
 }
+// Given tokens whose rows are named: every row's workgroup looks through a short list, and a long one gets a launch of its
+// own once the rows' sums are in the workspace (8 bytes a row).  That launch takes 1.2 us; a list costs a row 0.4 us for each
+// 256 tokens and the chip 1 us for each 2^20 (row, token): 32 rows of 126464 and 1024 tokens 13.5 us searched, 13.8 apart, 2048 tokens
+// 15.2 and 13.7; 2048 rows of 1024 and 512 tokens 15.7 and 16.2, 1024 tokens 16.9 and 16.2; 16384 rows of 1024 and 64 tokens 92.4
+// and 91.3, 16384 tokens 339 and 93.
+constexpr int LP_SEARCHED = 1024;
+constexpr long LP_SEARCHED_ALL = 1l << 20;
+inline bool lp_tokens_apart(int T, int n_tok, bool named) {
+    return named && (n_tok > LP_SEARCHED || (long)T * n_tok > LP_SEARCHED_ALL);
+}
 
 // Heads (of all layers) of a compaction's workgroup for V^T: as many as leave 1536 workgroups (six for every CU, which its
 // registers hold), at most eight; and workgroups, with K's of COMPACT_NT lanes of 16 bytes.  32 trees of 64 rows, 28 layers of

@@ -51,12 +51,23 @@ int check_logprobs(const dllm_logprobs_args* g) {
     return DLLM_OK;
 }
 
+// apart: given tokens that get a launch of their own.
 template <typename T>
-void launch_logprobs(const LogprobArgs& a, hipStream_t s) {
+void launch_logprobs(const LogprobArgs& a, int apart, hipStream_t s) {
     const dim3 grid((unsigned)((long)a.T * a.parts));
     if (a.top > 0) hipLaunchKernelGGL((logprobs_kernel<T, true>), grid, dim3(LP_NT), 0, s, a);
     else hipLaunchKernelGGL((logprobs_kernel<T, false>), grid, dim3(LP_NT), 0, s, a);
     if (a.parts > 1) hipLaunchKernelGGL((logprobs_merge_kernel<T>), dim3(a.T), dim3(LP_NT), 0, s, a);
+    if (apart > 0) hipLaunchKernelGGL((logprobs_tokens_kernel<T>), dim3(ceil_div(apart, LP_NT)), dim3(LP_NT), 0, s, a, apart);
+}
+
+// Tokens of a call that get a launch of their own: all or none.
+int tokens_apart(const dllm_logprobs_args* g) {
+    return lp_tokens_apart(g->n_rows, g->n_tok, g->d_tok_row != nullptr) ? g->n_tok : 0;
+}
+
+size_t logprobs_ws(const dllm_logprobs_args* g) {
+    return lp_ws_bytes(g->n_rows, g->vocab, g->top) + (tokens_apart(g) > 0 ? (size_t)g->n_rows * sizeof(float2) : 0);
 }
 
 template <typename E>
@@ -115,7 +126,7 @@ int dllm_attention_tree_ws(const dllm_attn_args* g, size_t* bytes) { return atte
 int dllm_logprobs_ws(const dllm_logprobs_args* g, size_t* bytes) {
     if (!bytes) return fail(DLLM_E_INVAL, "bytes is NULL");
     if (int rc = check_logprobs(g)) return rc;
-    *bytes = lp_ws_bytes(g->n_rows, g->vocab, g->top);
+    *bytes = logprobs_ws(g);
     return DLLM_OK;
 }
 
@@ -133,17 +144,19 @@ int dllm_logprobs(const dllm_logprobs_args* g, dllm_stream stream) {
     if (g->n_rows == 0) return g->n_tok == 0 ? DLLM_OK : fail(DLLM_E_INVAL, "tokens need rows");
     const int parts = lp_parts(g->n_rows, g->vocab);
     if (!grid_ok((long)g->n_rows * parts, LP_NT)) return fail(DLLM_E_INVAL, "n_rows and vocab need too many workgroups");
-    const size_t need = lp_ws_bytes(g->n_rows, g->vocab, g->top);
+    const size_t need = logprobs_ws(g);
     if (need > 0 && (!g->d_ws || !aligned(g->d_ws, 16))) return fail(DLLM_E_INVAL, "workspace: NULL or not 16-byte aligned");
     if (need > g->ws_bytes)
         return fail(DLLM_E_CAPACITY, "the call needs " + std::to_string(need) + " bytes of workspace");
-    LogprobArgs a{g->d_logits, g->ld, g->n_rows, g->vocab, g->mask_id, g->n_tok, g->top, g->d_tok, g->d_tok_row, g->d_logp,
-                  g->d_entropy, g->d_top_id, g->d_top_logp, parts, lp_per(g->n_rows, g->vocab), (LogStat*)g->d_ws, nullptr};
+    const int apart = tokens_apart(g);
+    LogprobArgs a{g->d_logits, g->ld, g->n_rows, g->vocab, g->mask_id, g->n_tok - apart, g->top, g->d_tok, g->d_tok_row, g->d_logp,
+                  g->d_entropy, g->d_top_id, g->d_top_logp, parts, lp_per(g->n_rows, g->vocab), (LogStat*)g->d_ws, nullptr, nullptr};
     a.keys = (uint64_t*)((char*)g->d_ws + (size_t)a.T * parts * (LP_NT / 64) * sizeof(LogStat));
+    if (apart > 0) a.row_stat = (float2*)((char*)g->d_ws + lp_ws_bytes(a.T, a.V, a.top));
     hipStream_t s = (hipStream_t)stream;
-    if (g->dtype == DLLM_F32) launch_logprobs<float>(a, s);
-    else if (g->dtype == DLLM_F16) launch_logprobs<_Float16>(a, s);
-    else launch_logprobs<__bf16>(a, s);
+    if (g->dtype == DLLM_F32) launch_logprobs<float>(a, apart, s);
+    else if (g->dtype == DLLM_F16) launch_logprobs<_Float16>(a, apart, s);
+    else launch_logprobs<__bf16>(a, apart, s);
     HIP_TRY(hipGetLastError());
     return DLLM_OK;
 }

@@ -16,7 +16,9 @@ typedef u32x4_t __attribute__((aligned(2))) any_u32x4;     // 16 bytes from any 
 struct LogprobArgs {
     const void* logits;
     long ld;
-    int T, V, mask_id, n_tok, top;
+    int T, V, mask_id;
+    int n_tok;                    // given tokens that the rows' workgroups write (0: a launch of their own does)
+    int top;
     const int *tok, *tok_row;
     float *logp, *entropy;
     int* top_id;
@@ -24,6 +26,7 @@ struct LogprobArgs {
     int parts, per;               // parts of a row, blocks of LP_BLOCK ids each
     struct LogStat* stat;         // [T][parts][waves]
     uint64_t* keys;               // [T][parts][waves][top]
+    float2* row_stat;             // [T] largest logit and log of the sum, for the tokens' own launch, or NULL
 };
 
 // Sums over a set of logits: s = sum e^(x - m), t = sum (x - m) e^(x - m), m the largest.  Then the log of the
@@ -126,6 +129,12 @@ template <int NW> __device__ __forceinline__ uint64_t keys_top(const uint64_t* s
     return best;
 }
 
+// Logit of id v in row r as the sums count it; a NaN, the MASK id and what is no id are -inf.
+template <typename T> __device__ __forceinline__ float lp_logit(const LogprobArgs& a, int r, int v) {
+    float x = -INFINITY;
+    if (v >= 0 && v < a.V && v != a.mask_id) x = elem_to_f32<T>(((const T*)a.logits)[(long)r * a.ld + v]);
+    return x < FLT_MAX ? x : (x >= FLT_MAX ? FLT_MAX : -INFINITY);          // (a NaN is neither)
+}
 // Given token i of row `row`: -> whether it is that workgroup's (row 0's also has those of rows that there are not), and
 // its logit.
 template <typename T> __device__ __forceinline__ bool lp_token(const LogprobArgs& a, int row, int i, float& x) {
@@ -133,14 +142,18 @@ template <typename T> __device__ __forceinline__ bool lp_token(const LogprobArgs
     const bool there = r >= 0 && r < a.T;
     x = -INFINITY;
     if (there ? r != row : row != 0) return false;
-    if (there && v >= 0 && v < a.V && v != a.mask_id) x = elem_to_f32<T>(((const T*)a.logits)[(long)row * a.ld + v]);
-    x = x < FLT_MAX ? x : (x >= FLT_MAX ? FLT_MAX : -INFINITY);             // (a NaN is neither)
+    if (there) x = lp_logit<T>(a, row, v);
     return true;
 }
+// First token that a thread of row `row`'s workgroup looks at.  Without tok_row the row's own is the only one, else the
+// workgroup looks at all of them (the launch rules bound how many).
+__device__ __forceinline__ int lp_first(const LogprobArgs& a, int row) {
+    return a.tok_row ? (int)threadIdx.x : (threadIdx.x == 0 ? row : a.n_tok);
+}
 // What a row's workgroup writes once its sums (in every thread) and best keys (in wave 0) are known.  mine, x0: lp_token of
-// token tid, asked for before.
+// the thread's first token `first`, asked for before.
 template <typename T, int NT>
-__device__ __forceinline__ void lp_write(const LogprobArgs& a, int row, const LogStat& st, uint64_t best, bool mine, float x0) {
+__device__ __forceinline__ void lp_write(const LogprobArgs& a, int row, const LogStat& st, uint64_t best, int first, bool mine, float x0) {
     const int tid = threadIdx.x;
     const bool any = st.m > -INFINITY;
     const float lse = any ? logf(st.s) : 0.f;
@@ -149,8 +162,15 @@ __device__ __forceinline__ void lp_write(const LogprobArgs& a, int row, const Lo
         a.top_id[(size_t)row * a.top + tid] = best ? id_of_key(best) : -1;
         a.top_logp[(size_t)row * a.top + tid] = best ? (value_of_key(best) - st.m) - lse : -INFINITY;
     }
-    for (int i = tid; i < a.n_tok; i += NT) {
-        if (i != tid) mine = lp_token<T>(a, row, i, x0);
+    if (a.n_tok == 0) {
+        if (tid == 0 && a.row_stat) a.row_stat[row] = make_float2(st.m, lse);
+        return;
+    }
+    for (int i = first; i < a.n_tok; i += NT) {
+        if (i != first) {
+            if (!a.tok_row) break;
+            mine = lp_token<T>(a, row, i, x0);
+        }
         if (mine) a.logp[i] = any ? (x0 - st.m) - lse : -INFINITY;
     }
 }
@@ -236,7 +256,8 @@ __global__ void __launch_bounds__(LP_NT) logprobs_kernel(LogprobArgs a) {
     if (blk < b1) load(blk);
     // (where this workgroup writes the row: a token's three loads, one after the other, beside the logits)
     float x0 = 0.f;
-    const bool mine = a.parts == 1 && tid < a.n_tok && lp_token<T>(a, row, tid, x0);
+    const int tok0 = lp_first(a, row);
+    const bool mine = a.parts == 1 && tok0 < a.n_tok && lp_token<T>(a, row, tok0, x0);
     // (every wave has a block, or its workgroup's first bound is each wave's own)
     const bool together = TOP && b1 - b0 >= NW;
     for (bool first = true; blk < b1; blk += NW, first = false) {
@@ -346,7 +367,7 @@ __global__ void __launch_bounds__(LP_NT) logprobs_kernel(LogprobArgs a) {
 #pragma unroll
     for (int w = 1; w < NW; ++w) st = stat_merge(st, stat_s[w]);
     if (TOP && b1 - b0 > 1) best = keys_top<NW>(list_s, NW * a.top, pend_all);      // (else wave 0 has them)
-    lp_write<T, LP_NT>(a, row, st, best, mine, x0);
+    lp_write<T, LP_NT>(a, row, st, best, tok0, mine, x0);
 }
 
 // Merge of a row's waves.
@@ -356,13 +377,29 @@ __global__ void __launch_bounds__(LP_NT) logprobs_merge_kernel(LogprobArgs a) {
     __shared__ uint64_t tmp[NW * 64];
     const int row = blockIdx.x, lane = threadIdx.x & 63, n = a.parts * NW;
     float x0 = 0.f;
-    const bool mine = (int)threadIdx.x < a.n_tok && lp_token<T>(a, row, threadIdx.x, x0);
+    const int tok0 = lp_first(a, row);
+    const bool mine = tok0 < a.n_tok && lp_token<T>(a, row, tok0, x0);
     LogStat st{-INFINITY, 0.f, 0.f, 0.f};
     for (int i = lane; i < n; i += 64) st = stat_merge(st, a.stat[(size_t)row * n + i]);
     st = wave_stat(st);                                   // (every wave for itself)
     uint64_t best = 0;
     if (a.top > 0) best = keys_top<NW>(a.keys + (size_t)row * n * a.top, n * a.top, tmp);
-    lp_write<T, LP_NT>(a, row, st, best, mine, x0);
+    lp_write<T, LP_NT>(a, row, st, best, tok0, mine, x0);
+}
+
+// Given tokens once the rows' sums are known, a thread each.
+template <typename T>
+__global__ void __launch_bounds__(LP_NT) logprobs_tokens_kernel(LogprobArgs a, int n_tok) {
+    const int i = blockIdx.x * LP_NT + threadIdx.x;
+    if (i >= n_tok) return;
+    const int r = a.tok_row[i], v = a.tok[i];
+    float lp = -INFINITY;
+    if (r >= 0 && r < a.T) {
+        const float2 st = a.row_stat[r];
+        const float x = lp_logit<T>(a, r, v);
+        if (st.x > -INFINITY) lp = (x - st.x) - st.y;
+    }
+    a.logp[i] = lp;
 }
 
 }  // namespace dllm

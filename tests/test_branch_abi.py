@@ -152,3 +152,31 @@ int main() {
 }
 """)
     assert out == "576"
+
+
+def test_work_of_the_given_tokens_is_bounded(dl, tmp_path):  # noqa: F811
+    """No launch in which every row looks through a long list: at most 1024 tokens a row and 2^20 in all; longer lists get a
+    launch of their own and the rows' sums 8 bytes each in the workspace.  Without a list of rows a token is its row's."""
+    out = run_cpp(tmp_path, r"""
+int main() {
+    long n = 0;
+    for (int T : {0, 1, 5, 256, 1024, 1025, 2048, 16384, 1 << 20, 1 << 24})
+        for (int k : {0, 1, 64, 512, 1024, 1025, 4096, 1 << 20, 1 << 24}) {
+            if (lp_tokens_apart(T, k, false)) return 1;
+            if (!lp_tokens_apart(T, k, true) && (k > 1024 || (long)T * k > 1l << 20)) return 2;
+            n += lp_tokens_apart(T, k, true);
+        }
+    if (lp_tokens_apart(256, 512, true) || !lp_tokens_apart(16384, 256, true)) return 3;
+    std::printf("%ld", n);
+}
+""")
+    assert int(out) > 0
+    L, n = dl.lib(), ctypes.c_size_t()
+    size = lambda **kw: L.dllm_logprobs_ws(ctypes.byref(fill(dl.dllm_logprobs_args, **dict(LOGP, **kw))), ctypes.byref(n)) or n.value  # noqa: E731
+    few, many = dict(n_rows=3000, n_tok=300), dict(n_rows=3000, n_tok=3000)
+    assert size(**few) == 0 and size(**many, d_tok_row=None) == 0 and size(**many) == 3000 * 8
+    assert size(vocab=50000, ld=50000, n_tok=2000) == size(vocab=50000, ld=50000) + 4 * 8
+    a = fill(dl.dllm_logprobs_args, **dict(LOGP, **many, ws_bytes=3000 * 8 - 1))
+    assert L.dllm_logprobs(ctypes.byref(a), None) == dl.DLLM_E_CAPACITY
+    a.d_ws = None
+    assert L.dllm_logprobs(ctypes.byref(a), None) == dl.DLLM_E_INVAL
