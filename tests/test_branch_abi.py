@@ -180,3 +180,15 @@ int main() {
     assert L.dllm_logprobs(ctypes.byref(a), None) == dl.DLLM_E_CAPACITY
     a.d_ws = None
     assert L.dllm_logprobs(ctypes.byref(a), None) == dl.DLLM_E_INVAL
+
+
+def test_sizes_of_the_gpu_tests_reach_their_launches(tmp_path):
+    """test_gpu_branch_sizes.py: several blocks a wave, with several parts a row and with one."""
+    out = run_cpp(tmp_path, r"""
+int main() {
+    if (lp_per(256, 70001) <= 4 || lp_parts(256, 70001) <= 1 || lp_per(300, 152064) <= 4 || lp_parts(300, 152064) <= 1) return 1;
+    if (lp_parts(1100, 70001) != 1 || lp_per(1100, 70001) < 35) return 2;
+    std::printf("ok");
+}
+""")
+    assert out == "ok"

@@ -3,6 +3,8 @@ wave, several heads a workgroup."""
 import numpy as np
 import pytest
 
+from batch_util import tdtype
+from branch_util import logprobs
 from test_gpu_branch import check_logprobs, i32, logits_of
 
 pytestmark = pytest.mark.gpu
@@ -92,3 +94,71 @@ def test_long_lists_captured_and_replayed(dl):
         dl.dllm_logprobs(*cases[k], *ref)
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(out, ref))
+
+
+# ---------------------------------------------------------------------------- several blocks a wave
+
+
+def special_rows(rng, V, dtype, mask_id):
+    """Rows whose best ids, largest logits, ties, NaN and infinities lie in one of a wave's later blocks, or in several."""
+    import torch
+    t = tdtype(dtype)
+    i, top, inf = torch.arange(V), float(torch.finfo(t).max), float("inf")
+    blk = i.div(2048, rounding_mode="floor")
+    noise = torch.from_numpy(rng.normal(0, 3, V).astype(np.float32))
+    rows = [torch.zeros(V), torch.from_numpy(rng.integers(0, 3, V).astype(np.float32)), blk.float(), -blk.float(),      # ties
+            torch.where(i % 7 == 0, 0.0, -0.0), (blk == blk.max() - 1).float() * 5,
+            torch.where(i % 2048 == 5, 4.0, noise.clamp(max=3.9)), torch.where((i % 2048 < 3) & (blk % 4 == 2), 9.0, noise.clamp(max=8)),
+            torch.linspace(-20, 30, V), torch.linspace(30, -20, V), torch.linspace(-1000, 1000, V),                     # sorted
+            noise + 5.0 * blk, noise - 5.0 * blk, noise + 60.0 * (blk % 3 == 1)]                                       # the largest moves
+    odd = noise.clone()
+    odd[blk >= 5], odd[V - 100:] = float("nan"), 2.5
+    rows.append(odd)
+    odd = torch.where(i % 2 == 0, float("nan"), noise)
+    odd[: 6 * 2048] = -inf
+    rows.append(odd)
+    odd = noise.clone()
+    odd[7 * 2048 + 3], odd[V - 2], odd[9 * 2048] = inf, inf, top
+    rows.append(odd)
+    odd = torch.full((V,), -inf)
+    odd[V - 5] = 1.5                                   # one id left, in the last block
+    rows.append(odd)
+    odd = torch.full((V,), -top)
+    odd[5 * 2048: 5 * 2048 + 70], odd[V - 1] = 3.0, 3.0
+    rows.append(odd)
+    odd = torch.full((V,), -inf)
+    odd[mask_id] = 4.0
+    rows += [odd, torch.full((V,), float("nan")), torch.full((V,), -top)]
+    odd = noise.clone()
+    odd[3000::2048] = -inf
+    rows.append(odd)
+    return torch.stack(rows).to(t)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("T,V", [(256, 70001), (1100, 70001), (300, 152064)])
+@pytest.mark.parametrize("top", [1, 20, 64])
+def test_logprobs_several_blocks_a_wave(dl, dtype, T, V, top):
+    """A wave's list, its bound, what waits and its reference carried from block to block, with several parts a row and one:
+    special rows at several places among T, all copies alike to the bit, one of each against 64 bits."""
+    import torch
+    mask_id = 11 * 2048 + 7
+    rng = np.random.default_rng(top)
+    x = special_rows(rng, V, dtype, mask_id)
+    n = len(x)
+    rows = torch.arange(T) % n
+    g = x.cuda()[rows.cuda()]
+    tok = np.concatenate([rng.integers(0, V, 300), [mask_id, 0, V - 1, V - 2, V - 5, 5 * 2048] * 20])
+    of = rng.integers(0, T, len(tok))
+    z = lambda *s: torch.full(s, 77.0, device="cuda")  # noqa: E731
+    lp, ent, tl, ids = z(len(tok)), z(T), z(T, top), torch.full((T, top), -77, dtype=torch.int32, device="cuda")
+    dl.dllm_logprobs(g, i32(tok), i32(of), lp, ent, ids, tl, mask_id)
+    for out in (ent, ids, tl):
+        assert torch.equal(out, out[:n][rows.cuda()])
+    want = logprobs(x.double().numpy(), mask_id, tok, of % n, top)
+    far = lambda got, ref: np.where(np.isneginf(ref) & np.isneginf(got), 0, abs(got - ref))  # noqa: E731
+    with np.errstate(invalid="ignore"):
+        assert np.array_equal(ids[:n].cpu().numpy(), want[2])
+        assert (far(tl[:n].double().cpu().numpy(), want[3]) <= want[6]).all()
+        assert (far(lp.double().cpu().numpy(), want[0]) <= want[4]).all()
+        assert (abs(ent[:n].double().cpu().numpy() - want[1]) <= want[5]).all()
