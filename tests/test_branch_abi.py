@@ -183,11 +183,15 @@ int main() {
 
 
 def test_sizes_of_the_gpu_tests_reach_their_launches(tmp_path):
-    """test_gpu_branch_sizes.py: several blocks a wave, with several parts a row and with one."""
+    """test_gpu_branch_sizes.py: several blocks a wave with several parts a row and with one; two, three and eight heads of V^T a
+    workgroup, the last one with fewer; the measured compaction's two."""
     out = run_cpp(tmp_path, r"""
 int main() {
     if (lp_per(256, 70001) <= 4 || lp_parts(256, 70001) <= 1 || lp_per(300, 152064) <= 4 || lp_parts(300, 152064) <= 1) return 1;
     if (lp_parts(1100, 70001) != 1 || lp_per(1100, 70001) < 35) return 2;
+    if (compact_heads_per(64, 7, 7) != 2 || compact_heads_per(60, 4, 13) != 2 || compact_heads_per(34, 13, 7) != 2) return 3;
+    if (compact_heads_per(96, 7, 7) != 3 || compact_heads_per(96, 11, 12) != 8 || compact_heads_per(100, 11, 13) != 8) return 4;
+    if (49 % 2 != 1 || 49 % 3 != 1 || 132 % 8 != 4 || 143 % 8 != 7 || compact_heads_per(32, 28, 4) != 2) return 5;
     std::printf("ok");
 }
 """)

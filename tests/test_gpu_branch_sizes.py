@@ -3,6 +3,7 @@ wave, several heads a workgroup."""
 import numpy as np
 import pytest
 
+import test_gpu_branch
 from batch_util import tdtype
 from branch_util import logprobs
 from test_gpu_branch import check_logprobs, i32, logits_of
@@ -162,3 +163,15 @@ def test_logprobs_several_blocks_a_wave(dl, dtype, T, V, top):
         assert (far(tl[:n].double().cpu().numpy(), want[3]) <= want[6]).all()
         assert (far(lp.double().cpu().numpy(), want[0]) <= want[4]).all()
         assert (abs(ent[:n].double().cpu().numpy() - want[1]) <= want[5]).all()
+
+
+# ---------------------------------------------------------------------------- several heads a workgroup
+
+
+@pytest.mark.parametrize("dtype,B,W,P,L,Hk,D,page", [
+    ("f16", 64, 20, 9, 7, 7, 32, 32), ("f32", 64, 20, 9, 7, 7, 32, 32), ("bf16", 60, 33, 16, 4, 13, 64, 32), ("f16", 34, 64, 20, 13, 7, 128, 32),
+    ("f16", 96, 20, 9, 7, 7, 32, 32), ("f32", 96, 20, 9, 7, 7, 32, 32), ("f16", 96, 20, 9, 11, 12, 32, 32), ("f16", 100, 20, 17, 11, 13, 32, 32),
+    ("f32", 100, 20, 9, 11, 13, 32, 32)])
+def test_cache_compact_several_heads_a_workgroup(dl, dtype, B, W, P, L, Hk, D, page):
+    """Two, three and eight heads of V^T a workgroup, the last one with fewer, even and odd."""
+    test_gpu_branch.test_cache_compact(dl, dtype, B, W, P, L, Hk, D, page)
