@@ -5,8 +5,8 @@ import pytest
 
 import test_gpu_branch
 from batch_util import tdtype
-from branch_util import logprobs
-from test_gpu_branch import check_logprobs, i32, logits_of
+from branch_util import logprobs, tree_attention
+from test_gpu_branch import attn_case, check_logprobs, check_out, i32, logits_of, random_sets, run_tree, sets_to_mask
 
 pytestmark = pytest.mark.gpu
 
@@ -175,3 +175,57 @@ def test_logprobs_several_blocks_a_wave(dl, dtype, T, V, top):
 def test_cache_compact_several_heads_a_workgroup(dl, dtype, B, W, P, L, Hk, D, page):
     """Two, three and eight heads of V^T a workgroup, the last one with fewer, even and odd."""
     test_gpu_branch.test_cache_compact(dl, dtype, B, W, P, L, Hk, D, page)
+
+
+# ---------------------------------------------------------------------------- row bounds that are none
+
+
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("shared", [0, 64])
+def test_attention_tree_writes_rows_of_its_sequences_only(dl, dtype, shared):
+    """Row bounds past the call's rows, negative and falling: guard rows around the output and rows that are neither a
+    sequence's nor in [row0[0], row0[B]) stay, and where bounds cut to the call are those of whole sequences, so are the results."""
+    import torch
+    rng = np.random.default_rng(21)
+    c = attn_case(rng, dtype, [20, 33], [100, 70], 4, 2, 64, 32, shared)
+    T, G = c["T"], 64
+    c["table"] = np.where(c["table"] < 0, 0, c["table"])          # (whatever is read is a page)
+    ld = 2
+    mask = sets_to_mask(c, random_sets(rng, c["rows"], c["row0"]), ld)
+    bits = mask.cpu().numpy().view(np.uint32)
+    seen_of = lambda r: {j for j in range(32 * ld) if bits[r, j // 32] >> np.uint32(j % 32) & 1}  # noqa: E731
+    lo, hi = -2 ** 31, 2 ** 31 - 1
+    for row0 in ([-5, 20, hi], [0, 20, 40], [lo, lo, lo], [hi, hi, hi], [0, lo, 40], [hi, 3, 9], [30, 10, 50], [7, 7, 7], [0, 0, hi], [lo, 20, 53]):
+        for ln in ([120, 103], [120, 40], [lo, hi], [0, -1]):
+            big = torch.full((T + 2 * G, 4, 64), 77.0, dtype=c["q"].dtype, device="cuda")
+            out = big[G:G + T]
+            dl.dllm_attention_tree(c["q"], c["k"], c["v"], i32(c["table"]), i32(row0), i32(ln), mask, out, T, 120, shared_len=shared)
+            cut = [min(max(r, 0), T) for r in row0]
+            inside = torch.zeros(T + 2 * G, dtype=torch.bool, device="cuda")
+            for a, e in ((cut[0], cut[2]), (cut[0], cut[1]), (cut[1], cut[2])):       # all rows (the parts' merge), each sequence's
+                inside[G + a:G + max(a, e)] = True
+            assert big[~inside].eq(77).all(), (row0, ln)
+            if cut == sorted(cut) and all(0 <= n <= 120 and n >= max(shared, e - a) for n, a, e in zip(ln, cut, cut[1:])):
+                seen = {cut[b] + i: {j for j in seen_of(cut[b] + i) if j < cut[b + 1] - cut[b]} for b in range(2) for i in range(cut[b + 1] - cut[b])}
+                for rows, want, bound in tree_attention(c["q"].double(), c["k"].double(), c["v"].double(), c["table"], cut, ln, None, seen, shared,
+                                                        32, 64 ** -0.5, dtype):
+                    assert ((out[rows].double() - want).abs() <= bound).all(), (row0, ln, rows)
+
+
+# ---------------------------------------------------------------------------- the same bits
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("rows,cached,H,Hk,shared", [([128] * 4, [2000] * 4, 32, 32, 0), ([64, 0, 33, 64, 5, 64], [8192 + 900] * 6, 28, 4, 8192)])
+def test_attention_tree_repeats_itself(dl, dtype, rows, cached, H, Hk, shared):
+    """Candidates of 32 rows and trees behind a shared prefix: equal bits on repeated calls, and, as the formula's bound has it, off by
+    no more than the roundings of probabilities and output."""
+    import torch
+    rng = np.random.default_rng(4)
+    c = attn_case(rng, dtype, rows, cached, H, Hk, 128, 64, shared)
+    seen = {int(c["row0"][b]) + i: set(range(i // 32 * 32, i // 32 * 32 + 32)) & set(range(n)) for b, n in enumerate(rows) for i in range(n)}
+    mask = sets_to_mask(c, seen, 4)
+    out = run_tree(dl, c, mask)
+    check_out(c, out, seen)
+    for _ in range(10):
+        assert torch.equal(run_tree(dl, c, mask), out)
