@@ -130,7 +130,8 @@ inline bool select_four_waves(long wgs) { return wgs <= 4 * N_CU; }
 constexpr int TREE_MAX_LD = DLLM_MAX_TREE / 32;
 
 // Threads of a log probability workgroup, logits of a lane, ids of a wave's block.
-constexpr int LP_NT = 256, LP_PT = 32, LP_BLOCK = 64 * LP_PT, LP_MAX_TOP = 64;
+constexpr int LP_NT = 256, LP_PT = 32, LP_BLOCK = 64 * LP_PT;
+static_assert(DLLM_MAX_TOP <= 64, "a row's best ids are a lane's each");
 
 // Blocks of a part of a row: whole rounds of the four waves, as many as leave 1024 workgroups (four for every CU).
 inline int lp_per(int T, int vocab) {

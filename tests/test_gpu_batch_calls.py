@@ -289,3 +289,13 @@ def test_heads_norm_in_the_merged_and_the_windowed_step(dl, shape, dtype, rtol):
     for a, b, c in zip(one, all_, plain):
         np.testing.assert_allclose(b, a, rtol=rtol)
         assert not np.allclose(a, c, rtol=1e-6)
+
+
+def test_the_bindings_current_gpu_is_torchs(dl):
+    """The binding asks for the current GPU and stream below torch's public functions; they agree, on another stream too."""
+    import torch
+    t = torch.zeros(1, dtype=torch.int32, device="cuda")
+    assert dl._gpu("f", t) == torch.cuda.current_device() == dl._Types.device()
+    for s in (torch.cuda.default_stream(), torch.cuda.Stream()):
+        with torch.cuda.stream(s):
+            assert dl._stream(None) == dl._stream(None, t.get_device()) == torch.cuda.current_stream().cuda_stream == dl._stream(s)
