@@ -701,7 +701,9 @@ int dllm_attention_tree_ws(const dllm_attn_args* args, size_t* bytes);
 int dllm_attention_tree(const dllm_attn_args* args, const uint32_t* d_mask, int32_t mask_ld, dllm_stream stream);
 
 /* dllm_batch_step with a mask for every row (dllm_tree_plan's d_mask; rows->d_pos its
- * d_pos): the rows attend as in dllm_attention_tree. */
+ * d_pos, or the caller's own: of candidate windows side by side a row has its candidate's rows
+ * and the position it would have if that were the only one): the rows attend as in
+ * dllm_attention_tree. */
 int dllm_batch_step_tree(dllm_model* m, void* d_pages, size_t bytes, const dllm_batch_rows* rows, const uint32_t* d_tree,
                          int32_t tree_ld, const int32_t* d_tok, const uint8_t* d_mask, const dllm_select_args* sel,
                          int32_t* d_out_id, float* d_out_conf, dllm_stream stream);

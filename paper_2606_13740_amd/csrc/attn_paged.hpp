@@ -244,7 +244,9 @@ template <typename T> __device__ __forceinline__ void store_out4(const PagedArgs
 // that waits in LDS too: kept in registers, the 32 x 32 tiles spilled three, and a spill's reload waits for the staging
 // in every step.  Of a SIMD's two waves the one that reads and multiplies goes before the one in its exponentials: 98 us
 // for 105 below, 260 for 281 with full trees behind 16384, at worst 1% (the paged calls' long case loses 3%, so not there).
-// 16 trees of up to 64 rows, 28 heads over 4, behind 8192 + 3000 bf16 keys: 98 us with the merge, 740 TFLOP/s; 4 x 4 candidates of 32 rows, 32 fp16 heads, behind 4000: 74 us, K/V at 4.6 TB/s before the merge.
+// 16 trees of up to 64 rows, 28 heads over 4, behind 8192 + 3000 bf16 keys: 98 us with the merge, 740 TFLOP/s;
+// 4 x 4 candidates of 32 rows, 32 fp16 heads, behind 4000: 73 us, of which the parts take 64, 270 MB of K/V at 4.2 TB/s where a
+// plain read has 6.5: the waves are ready and wait to issue for 44% of their cycles, and wait for data for 29%.
 template <typename T, int DH, int QG, int RT, int KG, int SUB, bool TREE>
 __global__ void __launch_bounds__(QG * KG * 64)
 __attribute__((amdgpu_waves_per_eu(QG * KG * (160 * 1024 / (2 * SUB * 64 * DH * (int)sizeof(T))) >= 8 ? 2 : 1)))
@@ -655,8 +657,9 @@ attn_paged_kernel(PagedArgs a) {
 #pragma unroll
                 for (int e = 0; e < NS; ++e) pf[w][e >> 2][e & 3] = __float_as_uint(p[e]);
             } else {
-                // rounded to nearest for the product with V (half a step of T a probability: as much as the
-                // output's own rounding); the sum keeps fp32
+                // rounded to nearest for the product with V, which takes operands of T (half a step of T a
+                // probability: as much as the output's own rounding, together 1.4 times the error of a form in fp32
+                // rounded once); the sum keeps fp32
 #pragma unroll
                 for (int e = 0; e < NS / 2; ++e)
                     pf[w][e >> 2][e & 3] = __builtin_bit_cast(uint32_t, (typename E::x2){(T)p[2 * e], (T)p[2 * e + 1]});

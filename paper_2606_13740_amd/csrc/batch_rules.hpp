@@ -133,7 +133,11 @@ constexpr int TREE_MAX_LD = DLLM_MAX_TREE / 32;
 constexpr int LP_NT = 256, LP_PT = 32, LP_BLOCK = 64 * LP_PT;
 static_assert(DLLM_MAX_TOP <= 64, "a row's best ids are a lane's each");
 
-// Blocks of a part of a row: whole rounds of the four waves, as many as leave 1024 workgroups (four for every CU).
+// Blocks of a part of a row: whole rounds of the four waves, as many as leave 1024 workgroups (four for every CU).  A call in
+// us with parts for 256, 512, 768, 1024 and 2048 workgroups: 256 rows of 152064 bf16 logits 39.6, 30.1, 28.0, 28.3, 31.3, 300 rows 42.2,
+// 42.7, 34.3, 32.2, 32.3, 128 rows 26.7, 22.1, 21.6, 22.0, 24.4; 256 of 126464 fp32 36.1, 30.4, 33.0, 32.6, 33.4, 64 rows 16.7, 15.6,
+// 15.5, 16.2, 16.1; 1000 of 50000 bf16 30 with one part each, 37.4 with two; 32 of 126464, 8 and 64 of 32000 and 600 of
+// 152064 within 3%.
 inline int lp_per(int T, int vocab) {
     const int blocks = ceil_div(vocab, LP_BLOCK), waves = LP_NT / 64;
     const long parts = std::max<long>(1, 4 * N_CU / std::max(T, 1));
@@ -156,8 +160,10 @@ inline bool lp_tokens_apart(int T, int n_tok, bool named) {
 }
 
 // Heads (of all layers) of a compaction's workgroup for V^T: as many as leave 1536 workgroups (six for every CU, which its
-// registers hold), at most eight; and workgroups, with K's of COMPACT_NT lanes of 16 bytes.  32 trees of 64 rows, 28 layers of
-// 4 heads, fp16: one head a workgroup 37.8 us, two to four 36, six 37.4.
+// registers hold), at most eight; and workgroups, with K's of COMPACT_NT lanes of 16 bytes.  With 1, 2, 3, 4, 6 and 8 heads, fp16:
+// 32 trees of 64 rows, 28 layers of 4 heads 34.6, 32.6, 33.2, 33.1, 33.9, 33.9 us (the rule's 2), 16 trees 18.0, 17.3, 16.4, 17.3, 17.1, 16.7
+// (1), 64 trees 81.5, 81.7, 84.6, 84.5, 84.0, 86.3 (4); 32 trees, 24 layers of 8 heads of 64 23.1, 21.7, 22.8, 21.9, 23.4, 23.1 (4); 32
+// layers of 32 heads 354 with one, 361 to 365 with more (8).
 constexpr int COMPACT_NT = 256;
 inline int compact_heads_per(long B, int L, int Hk) { return (int)std::min<long>(8, std::max<long>(1, B * L * Hk / (6 * N_CU))); }
 inline long compact_wgs(long B, int L, int Hk, int Dh, int es) {

@@ -37,8 +37,10 @@ struct CompactArgs {
 // column; 16 lanes have 16 positions of a dim, which lie in one or two lines of its page, and are read and written
 // together.  Either way a chunk's source and destinations are one wave's, which needs no barrier.
 //
-// What bounds it: V^T's lines, 2 or 4 bytes of each (32 trees of 64 rows, 28 layers of 4 heads, fp16, 7 MB moved: 49 MB
-// fetched, 28 written, 36 us, of which K takes 5), and in small calls four dependent loads (3.7 us).
+// What bounds it: V^T, of which a position is 2 or 4 bytes of a line for every dim.  32 trees of 64 rows, 28 layers of 4 heads,
+// fp16, 7 MB moved: 36 us, of which K takes 5.  49 MB are fetched and 28 written, 16 us at a copy's rate; the rest is instructions, a
+// load and a store for every element of V^T, many to a part of a line that others write too (the waves are ready and wait to
+// issue for 63% of their cycles).  fp32: 62 us.  Small calls: four dependent loads (4.9 us).
 constexpr int COMPACT_POS = 16, COMPACT_K = 8;
 template <typename E, int DH>
 __global__ void __launch_bounds__(COMPACT_NT) cache_compact_kernel(CompactArgs a, int hp) {
@@ -365,7 +367,7 @@ __global__ void __launch_bounds__(FORK_NT) batch_fork_kernel(ForkArgs a) {
 }
 
 // A fork's new tables, a wave a sequence, and its copies: positions [0, n) of a page, of every layer, plane and head, a
-// workgroup each; what lies past the positions stays.  8 sequences, 28 layers: 6 MB in 4.6 to 6.3 us, four dependent loads.
+// workgroup each; what lies past the positions stays.  8 sequences, 28 layers: 6 MB in 6.5 us, four dependent loads.
 template <typename E, int DH>
 __global__ void __launch_bounds__(256) fork_copy_kernel(CacheArgs c, const int* n_copies, const int4* copies, const uint2* rows, int B,
                                                         const int* table, int* table_out, int ld, bool vec) {

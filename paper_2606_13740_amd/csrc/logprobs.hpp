@@ -198,9 +198,10 @@ __device__ __forceinline__ float max_of_block(const float (&x)[LP_PT]) {
 // 64 at a time are sorted and merged into the list.  Ids ascend from block to block, so an equal logit in a later block has
 // lost: the bound is strict, but inside a block, whose ids are not taken in order.
 //
-// What bounds it: 256 rows of 152064 bf16 logits, 24 us and 5 for the merge, where reading takes 16 and VALU issue 14: the
-// start, the first bound and the last sorts of all waves, which run at once; few or short rows, latency: load, bound, sort,
-// logarithm (16 rows of 1024 7 us, 32 of 126464 fp32 8 and 5).
+// What bounds it: 256 rows of 152064 bf16 logits, 24 us and 5 for the merge, where reading takes 12 (at a plain read's 6.5 TB/s)
+// and VALU issue 14: the start, the first bound and the last sorts of all waves, which run at once (256 of 126464 fp32 33 us in
+// all, reading 20; 1024 rows, one part each, 87 and 79); few or short rows, latency: load, bound, sort, logarithm (16 rows of 1024
+// 7 us, 32 of 126464 fp32 8 and 6).
 template <typename T, bool TOP>
 __global__ void __launch_bounds__(LP_NT) logprobs_kernel(LogprobArgs a) {
     constexpr int NL = 16 / (int)sizeof(T), U = LP_PT / NL, NW = LP_NT / 64;

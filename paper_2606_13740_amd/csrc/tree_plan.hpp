@@ -19,8 +19,8 @@ struct TreeArgs {
 // A workgroup takes a sequence.  Inside blocks of 32 rows the ancestors are found by doubling (after step s a row knows
 // its next 2^s nodes and the one behind them: five steps), for all blocks at once.  What lies before a row's block are the
 // bits that its first ancestor outside of it has in its own block, and so on: a thread takes a row and one LDS read a
-// block, whatever the trees' depth.  What bounds it is launch and latency: 2.4 us for 8 trees of 16 rows, 3.3 for 64 of up to
-// 256 (block after block in order, with the rows' masks in LDS and a barrier each, 5.1).
+// block, whatever the trees' depth.  What bounds it is launch and latency: 1.9 us a call in a row of them for 8 trees of 16 rows,
+// 2.9 for 64 of up to 256 (block after block in order, with the rows' masks in LDS and a barrier each, 2.1 and 4.7); alone 3.4 and 4.7.
 constexpr int TREE_NT = 256;
 __global__ void __launch_bounds__(TREE_NT) tree_plan_kernel(TreeArgs a) {
     __shared__ uint2 node_s[32 * TREE_MAX_LD];           // a row's bits in its block, and its first ancestor outside, or -1
